@@ -151,7 +151,8 @@ freqattn_status freqattn_forward_static(freqattn_ctx* ctx, const void* q, const 
 /* Releases everything the context owns.  freqattn_destroy(NULL) is a no-op.  The caller must have synchronised. */
 void freqattn_destroy(freqattn_ctx* ctx);
 
-/* Text of the last error on this context (or of the last failed freqattn_create when ctx is NULL). Never NULL. */
+/* Text of the last error on this context (ctx NULL: of the calling thread's last failed freqattn_create or call without a
+ * context). Never NULL. */
 const char* freqattn_last_error(const freqattn_ctx* ctx);
 
 /* FREQATTN_LAUNCH_FUSED (default): low, mid and high work items run in one persistent launch (section 6.2).
@@ -289,6 +290,131 @@ freqattn_status freqattn_check_range(freqattn_ctx* ctx, int32_t* out_of_range, v
 
 /* Device bytes owned by the context (tables + scratch). */
 int64_t freqattn_workspace_bytes(const freqattn_ctx* ctx);
+
+/* ==== operators next to the layer ===============================================================================
+ * What a video transformer puts around the attention of this library: rotary positions and per-head norms of Q and K, and
+ * dense attention over sequences of different lengths with its gradients.  They need no context.  Every call enqueues its
+ * kernels on `stream` of the current device and returns; it allocates nothing, copies nothing between host and device and may
+ * be captured into a HIP graph.  All device pointers and the stream belong to the current device.  Failures are returned as codes;
+ * freqattn_last_error(NULL) gives the text of the calling thread's last one (also of freqattn_create).  Calls may run at the same time
+ * from any threads and on any streams as long as their outputs and workspaces are disjoint. */
+
+/* A device tensor [batch or sequences][rows][heads][channels]: element (b, n, h, c) at b*batch_stride + n*row_stride +
+ * h*head_stride + c, strides in elements.  Any order of the axes, also views of larger tensors; strides of outputs must
+ * keep elements apart.  No alignment beyond the element's own is required, 16-byte aligned bases and strides are faster. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, row_stride, head_stride;
+} freqattn_heads;
+
+/* Rotary positions.  Pairs of channels turn by position times frequency: axis a of a token's position (1 to 4 axes: a
+ * sequence, or T, H, W of a grid) owns the next axis_dim[a] / 2 pairs, pair j of them with frequency base^(-2j/axis_dim[a]).
+ * HALF: pair i is channels i and i + R/2, R = the sum of axis_dim; INTERLEAVED: channels 2i and 2i + 1.  Channels from R on stay.
+ * Scaling to positions beyond the trained length: LINEAR divides the frequencies by factor; NTK takes the base
+ * base * factor^(D/(D-2)) per axis of D > 2 channels; BY_PARTS (context = trained length L) keeps frequencies of more than
+ * beta_fast turns over L, divides those of fewer than beta_slow by factor, blends in between linearly in the turns, and scales the rotated
+ * channels by 0.1 ln(factor) + 1.  amplitude > 0 overrides that scale (any scaling). */
+typedef enum { FREQATTN_ROTARY_HALF = 0, FREQATTN_ROTARY_INTERLEAVED = 1 } freqattn_rotary_layout;
+typedef enum { FREQATTN_ROTARY_PLAIN = 0, FREQATTN_ROTARY_LINEAR = 1, FREQATTN_ROTARY_NTK = 2, FREQATTN_ROTARY_BY_PARTS = 3 } freqattn_rotary_scaling;
+typedef struct {
+  int32_t head_dim;    /* even, at most 512 */
+  int32_t axes;        /* 1..4 */
+  int32_t axis_dim[4]; /* even, >= 0, their sum even and in 2..head_dim */
+  int32_t layout;      /* freqattn_rotary_layout */
+  int32_t scaling;     /* freqattn_rotary_scaling */
+  int32_t context;     /* BY_PARTS: trained length, > 0 */
+  int32_t grid[4];     /* extents of the token grid (all > 0) or all 0: where a call gives no positions, token n is at the grid's row-major
+                          coordinates of n (one entry per axis), or, without a grid and with one axis, at n */
+  double base, factor; /* base > 1; factor > 0, >= 1 for BY_PARTS */
+  double beta_fast, beta_slow; /* BY_PARTS: beta_fast > beta_slow >= 0 */
+  double amplitude;    /* 0: what the scaling says */
+} freqattn_rotary_cfg;
+typedef struct freqattn_rotary freqattn_rotary; /* opaque, host memory only, constant: usable from any thread, device and stream */
+
+/* EINVAL: NULL, values outside the ranges above. */
+freqattn_status freqattn_rotary_create(const freqattn_rotary_cfg* cfg /*HOST*/, freqattn_rotary** out /*HOST*/);
+/* Calls that were enqueued with it may still be running or wait in a captured graph.  NULL is a no-op. */
+void freqattn_rotary_destroy(freqattn_rotary* rotary);
+/* Radians per position of every pair and the amplitude, as the kernels use them: HOST out [sum of axis_dim / 2], HOST out. */
+freqattn_status freqattn_rotary_frequencies(const freqattn_rotary* rotary, double* radians, double* amplitude);
+
+/* out = x rotated, or (inverse != 0) rotated by the negative angles: the gradient with respect to x of the forward call.
+ *   dtype     freqattn_dtype of x and out; computed in fp32 from angles that are exact to 2^-31 turns at any position
+ *   x, out    [batch][tokens][heads][head_dim]; out may be x itself (same pointer and strides), else must not overlap it
+ *   positions DEVICE int32 [batch][tokens][axes], entry (b, n, a) at b*positions_stride + n*axes + a (stride 0: one list for all);
+ *             any int32 value.  NULL: from the token index, see grid (EINVAL without a grid on several axes, or if tokens is not the grid's size)
+ * EINVAL: NULL, sizes < 0, unknown dtype, head_dim other than the rotary's; EUNSUPPORTED: rows for more than 2^25 waves.  Nothing is launched where batch, tokens or heads is 0. */
+freqattn_status freqattn_rotary_apply(const freqattn_rotary* rotary, int32_t dtype, int32_t batch, int32_t tokens, int32_t heads,
+                                      const freqattn_heads* x, const int32_t* positions, int64_t positions_stride, int32_t inverse,
+                                      const freqattn_heads* out, void* stream);
+
+/* Norms of queries and keys per head, x * (mean_c x_c^2 + eps)^-1/2 * w, and the rotation in the same pass.  q has q_heads heads, k has
+ * k_heads (0: q alone, the k pointers are ignored); w_q, w_k DEVICE [head_dim] of `dtype`, NULL: ones.  rotary NULL: no rotation.
+ * Typical use: q and k are views of a fused projection [batch][tokens][heads...][head_dim], the outputs head-major
+ * [batch, heads, N, head_dim] as freqattn_forward takes them.  Sums are fp32.  q_out may be q itself and k_out k. */
+typedef struct {
+  int32_t batch, tokens, q_heads, k_heads;
+  int32_t head_dim; /* even, at most 512 */
+  int32_t dtype;    /* freqattn_dtype */
+  float eps;        /* >= 0 */
+} freqattn_qk_shape;
+freqattn_status freqattn_qk_norm(const freqattn_qk_shape* shape, const freqattn_rotary* rotary, const int32_t* positions, int64_t positions_stride,
+                                 const freqattn_heads* q, const freqattn_heads* k, const void* w_q, const void* w_k,
+                                 const freqattn_heads* q_out, const freqattn_heads* k_out, void* stream);
+/* Gradients of freqattn_qk_norm: q, k, w_q, w_k, positions as in that call (q and k before the norm), dq_out, dk_out the gradients of its
+ * outputs; dq, dk of dtype (may be dq_out and dk_out themselves); dw_q, dw_k DEVICE fp32 [head_dim], summed over batch, tokens and heads in a fixed
+ * order (equal calls give equal bits), NULL: not wanted.  workspace DEVICE, freqattn_qk_norm_workspace(head_dim) bytes, 16-byte aligned, its
+ * content does not matter; NULL is fine where both dw are NULL.  EINVAL as above, also a workspace that is too small. */
+int64_t freqattn_qk_norm_workspace(int32_t head_dim);
+freqattn_status freqattn_qk_norm_backward(const freqattn_qk_shape* shape, const freqattn_rotary* rotary, const int32_t* positions, int64_t positions_stride,
+                                          const freqattn_heads* q, const freqattn_heads* k, const void* w_q, const void* w_k,
+                                          const freqattn_heads* dq_out, const freqattn_heads* dk_out, const freqattn_heads* dq,
+                                          const freqattn_heads* dk, float* dw_q, float* dw_k, void* workspace, int64_t workspace_bytes,
+                                          void* stream);
+
+/* Dense attention over sequences: softmax(scale * q k^T) v within each sequence and head.
+ * Two forms, each for the queries (q, out) and for the keys (k, v) on its own:
+ *   packed   *_offsets given, DEVICE int32 [sequences + 1], ascending: sequence i owns rows offsets[i] .. offsets[i+1] - 1 of a tensor of
+ *            *_rows rows (batch_stride is ignored)
+ *   batched  *_offsets NULL: sequence i is entry i of the batch axis, *_rows rows
+ * and in both, *_lengths (DEVICE int32 [sequences] or NULL) cuts sequence i to its first lengths[i] rows (a cache filled so far, padding).
+ * Rows that belong to no sequence are neither read nor written.  Offsets and lengths are held to the tensors' rows on the device: wrong ones
+ * give wrong results, never an access outside.
+ * Heads: q_heads a multiple of kv_heads; query head h reads key head h / (q_heads / kv_heads).
+ * causal: the last query sees all keys, query i of a sequence with nq queries and nk keys sees keys j <= i + nk - nq.
+ * A query that sees no key gets zeros, lse -inf, and gives no gradient.  Keys behind what a query sees reach it in no way, whatever they hold
+ * (NaN and infinities too).
+ * dtype of q, k, v, out: BF16 (products on the matrix cores from bf16 operands, sums and softmax fp32) or F32 (fp32 throughout).  head_dim 1..128.
+ * softmax_scale <= 0 selects 1/sqrt(head_dim). */
+typedef struct {
+  int32_t sequences, q_heads, kv_heads, head_dim;
+  int32_t q_rows, k_rows;
+  int32_t dtype;
+  int32_t causal;
+  float softmax_scale;
+} freqattn_sequence_shape;
+typedef struct {
+  const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;
+} freqattn_sequence_rows;
+/* lse: DEVICE fp32 [q_heads][rows of q] or NULL: log of each query's sum of exponentials, what the backward pass needs.  Row n of the packed
+ * form is column n, row n of sequence i of the batched form column i*q_rows + n.
+ * workspace DEVICE, at least freqattn_sequence_attention_workspace(shape, rows) bytes (may be 0: NULL), 16-byte aligned, content does not matter.
+ * Few queries over many keys are split along the keys and joined from there.  rows: only which of its pointers are NULL matters to the size.
+ * EINVAL: NULL, sizes out of range, a workspace that is too small; EUNSUPPORTED: head_dim above 128, 2^30 rows of a group or more, more workgroups
+ * than a launch holds. */
+int64_t freqattn_sequence_attention_workspace(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows);
+freqattn_status freqattn_sequence_attention(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows, const freqattn_heads* q,
+                                            const freqattn_heads* k, const freqattn_heads* v, const freqattn_heads* out, float* lse,
+                                            void* workspace, int64_t workspace_bytes, void* stream);
+/* Gradients dq, dk, dv (of dtype) from dout and what the forward call read and wrote (out, lse).  Keys' gradients are summed over the queries and the
+ * heads of their group in fp32 in a fixed order: equal calls give equal bits.  Key rows no query sees get zeros.  dq, dk, dv must not overlap inputs.
+ * workspace: freqattn_sequence_attention_backward_workspace(shape, rows) bytes. */
+int64_t freqattn_sequence_attention_backward_workspace(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows);
+freqattn_status freqattn_sequence_attention_backward(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows,
+                                                     const freqattn_heads* dout, const freqattn_heads* q, const freqattn_heads* k,
+                                                     const freqattn_heads* v, const freqattn_heads* out, const float* lse,
+                                                     const freqattn_heads* dq, const freqattn_heads* dk, const freqattn_heads* dv,
+                                                     void* workspace, int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -18,6 +18,8 @@ F32, BF16 = 0, 1
 LAUNCH_FUSED, LAUNCH_SEPARATE = 0, 1
 PATH_AUTO, PATH_GENERIC, PATH_MFMA, PATH_TABLES_ONLY = 0, 1, 2, 3
 TRANSFORM_DCT, TRANSFORM_HAAR = 0, 1
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_NTK, ROTARY_BY_PARTS = 0, 1, 2, 3
 
 
 class Shape(C.Structure):
@@ -29,6 +31,34 @@ class BandCfg(C.Structure):
                                          "mid_diag", "mid_stride", "mid_block0", "high_window", "n_summary")] + \
                [("softmax_scale", C.c_float), ("transform", C.c_int32), ("mid2_num", C.c_int32), ("mid2_den", C.c_int32)]
 
+
+class Heads(C.Structure):
+    """freqattn_heads: a device tensor [batch][rows][heads][channels] by its address and strides (elements)."""
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RotaryCfg(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("axes", C.c_int32), ("axis_dim", C.c_int32 * 4), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("context", C.c_int32), ("grid", C.c_int32 * 4), ("base", C.c_double), ("factor", C.c_double), ("beta_fast", C.c_double),
+                ("beta_slow", C.c_double), ("amplitude", C.c_double)]
+
+
+class QkShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "tokens", "q_heads", "k_heads", "head_dim", "dtype")] + [("eps", C.c_float)]
+
+
+class SequenceShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("sequences", "q_heads", "kv_heads", "head_dim", "q_rows", "k_rows", "dtype", "causal")] + \
+               [("softmax_scale", C.c_float)]
+
+
+class SequenceRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_offsets", "k_offsets", "q_lengths", "k_lengths")]
+
+
+_H, _P = C.POINTER(Heads), C.c_void_p
+_SEQ = [C.POINTER(SequenceShape), C.POINTER(SequenceRows)]
+_ROT = [_P, _P, C.c_int64]     # rotary, positions, positions_stride
 
 EXPORTS = {
     "freqattn_create": (C.c_int, [C.POINTER(Shape), C.POINTER(BandCfg), C.c_int32, C.POINTER(C.c_void_p)]),
@@ -69,6 +99,17 @@ EXPORTS = {
     "freqattn_workspace_bytes": (C.c_int64, [C.c_void_p]),
     "freqattn_check_range": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.c_void_p]),
     "freqattn_measure_peaks": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_void_p]),
+    "freqattn_rotary_create": (C.c_int, [C.POINTER(RotaryCfg), C.POINTER(_P)]),
+    "freqattn_rotary_destroy": (None, [_P]),
+    "freqattn_rotary_frequencies": (C.c_int, [_P, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
+    "freqattn_rotary_apply": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _H, _P, C.c_int64, C.c_int32, _H, _P]),
+    "freqattn_qk_norm": (C.c_int, [C.POINTER(QkShape)] + _ROT + [_H, _H, _P, _P, _H, _H, _P]),
+    "freqattn_qk_norm_workspace": (C.c_int64, [C.c_int32]),
+    "freqattn_qk_norm_backward": (C.c_int, [C.POINTER(QkShape)] + _ROT + [_H, _H, _P, _P, _H, _H, _H, _H, _P, _P, _P, C.c_int64, _P]),
+    "freqattn_sequence_attention_workspace": (C.c_int64, _SEQ),
+    "freqattn_sequence_attention": (C.c_int, _SEQ + [_H, _H, _H, _H, _P, _P, C.c_int64, _P]),
+    "freqattn_sequence_attention_backward_workspace": (C.c_int64, _SEQ),
+    "freqattn_sequence_attention_backward": (C.c_int, _SEQ + [_H] * 5 + [_P] + [_H] * 3 + [_P, C.c_int64, _P]),
 }
 
 _lib = None
@@ -351,3 +392,248 @@ def route_fixed(heads, n_low, n_mid, n_high):
     if st != OK:
         raise FreqAttnError(st, "freqattn_route_fixed: bad arguments")
     return out
+
+
+# ---- operators next to the layer: rotary positions, norms of Q and K, attention over sequences ---------------------------
+# They need no context.  A tensor of heads is [batch, rows, heads, head_dim] (packed sequences: [rows, heads, head_dim]) with adjacent
+# channels and any other strides: a head-major tensor is passed as x.transpose(1, 2), a part of a fused projection as the slice that it is.
+
+def _heads(who, name, t, like=None, shape=None, written=False):
+    """The freqattn_heads of a tensor, after the checks that the library cannot make on an address."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{who}: {name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{who}: {name} must be a device tensor")
+    dim, sh, st = t.dim(), t.shape, t.stride()
+    if dim != 3 and dim != 4:
+        raise ValueError(f"{who}: {name} must be [batch, rows, heads, head_dim] or [rows, heads, head_dim], got {tuple(sh)}")
+    if like is None:
+        if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
+            raise ValueError(f"{who}: {name} has dtype {t.dtype}, expected bfloat16 or float32")
+    else:
+        if t.dtype is not like.dtype:
+            raise ValueError(f"{who}: {name} has dtype {t.dtype}, expected {like.dtype}")
+        if t.device != like.device:
+            raise ValueError(f"{who}: {name} is on {t.device}, expected {like.device}")
+    if shape is not None and sh != shape:
+        raise ValueError(f"{who}: {name} has shape {tuple(sh)}, expected {tuple(shape)}")
+    if st[-1] != 1 and sh[-1] > 1:
+        raise ValueError(f"{who}: the channels of {name} must be adjacent")
+    if written and any(s == 0 and n > 1 for s, n in zip(st, sh)):
+        raise ValueError(f"{who}: {name} is written and must not be expanded")
+    return Heads(t.data_ptr(), st[0] if dim == 4 else 0, st[-3], st[-2])
+
+
+def _int32(who, name, t, like, *shapes):
+    """Address of a contiguous int32 device tensor of one of the shapes; None passes."""
+    import torch
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.device != like.device or not t.is_contiguous() or tuple(t.shape) not in shapes:
+        raise ValueError(f"{who}: {name} must be a contiguous int32 tensor on {like.device} of shape {' or '.join(map(str, shapes))}")
+    return t.data_ptr()
+
+
+def _vector(who, name, t, like, n, dtype):
+    import torch
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != like.device or not t.is_contiguous() or tuple(t.shape) != (n,):
+        raise ValueError(f"{who}: {name} must be a contiguous {dtype} tensor of shape {(n,)} on {like.device}")
+    return t.data_ptr()
+
+
+def _call(fn, t, *args):
+    """fn(*args, stream) on the device of t, with its current stream; raises on failure."""
+    import torch
+    if t.device.index == torch.cuda.current_device():
+        st = fn(*args, _stream())
+    else:
+        with torch.cuda.device(t.device):
+            st = fn(*args, _stream())
+    if st != OK:
+        raise FreqAttnError(st, lib().freqattn_last_error(None).decode())
+
+
+def _workspace(who, t, need, like):
+    """Address and size of the caller's workspace, or of one from torch's allocator (on the stream that the call uses)."""
+    import torch
+    if need == 0:
+        return None, 0, None
+    if t is None:
+        t = torch.empty(need, dtype=torch.uint8, device=like.device)
+    elif not isinstance(t, torch.Tensor) or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{who}: workspace must be a contiguous tensor on {like.device}")
+    return t.data_ptr(), t.numel() * t.element_size(), t
+
+
+def _io(t):
+    import torch
+    return BF16 if t.dtype is torch.bfloat16 else F32
+
+
+class Rotary:
+    """Rotary positions (freqattn_rotary): `axis_dims` channels rotate per position axis, the rest of head_dim stays."""
+
+    def __init__(self, head_dim, axis_dims, layout=ROTARY_HALF, base=10000.0, scaling=ROTARY_PLAIN, factor=1.0, context=0, grid=None,
+                 beta_fast=32.0, beta_slow=1.0, amplitude=0.0):
+        axis_dims = [int(x) for x in (axis_dims if hasattr(axis_dims, "__len__") else [axis_dims])]
+        self._h = C.c_void_p()
+        if not 1 <= len(axis_dims) <= 4 or (grid is not None and len(grid) != len(axis_dims)):
+            raise ValueError("Rotary: 1 to 4 axes, and one grid extent for each")
+        self.head_dim, self.axes, self.pairs = int(head_dim), len(axis_dims), sum(axis_dims) // 2
+        cfg = RotaryCfg(head_dim, self.axes, (C.c_int32 * 4)(*axis_dims), layout, scaling, context, (C.c_int32 * 4)(*(grid or ())), base, factor,
+                        beta_fast, beta_slow, amplitude)
+        st = lib().freqattn_rotary_create(C.byref(cfg), C.byref(self._h))
+        if st != OK:
+            raise FreqAttnError(st, lib().freqattn_last_error(None).decode())
+
+    def frequencies(self):
+        """(radians per position of every pair, amplitude)."""
+        out, amp = np.zeros(self.pairs, np.float64), C.c_double(0.0)
+        st = lib().freqattn_rotary_frequencies(self._h, out.ctypes.data_as(C.POINTER(C.c_double)), C.byref(amp))
+        if st != OK:
+            raise FreqAttnError(st, lib().freqattn_last_error(None).decode())
+        return out, amp.value
+
+    def __del__(self):
+        try:
+            if self._h:
+                lib().freqattn_rotary_destroy(self._h)
+                self._h = C.c_void_p()
+        except Exception:
+            pass
+
+
+def _positions(who, rotary, positions, batch, tokens, like):
+    """(rotary handle, positions address, batch stride): positions int32 [batch, tokens, axes] or, one list for all, [tokens, axes]; the last axis may
+    be left out where there is one."""
+    if rotary is None:
+        if positions is not None:
+            raise ValueError(f"{who}: positions without a rotary")
+        return None, None, 0
+    if not isinstance(rotary, Rotary):
+        raise TypeError(f"{who}: rotary must be a Rotary")
+    n = rotary.axes
+    each, one = [(batch, tokens, n)], [(tokens, n)]
+    if n == 1:
+        each.append((batch, tokens))
+        one.append((tokens,))
+    at = _int32(who, "positions", positions, like, *each, *one)
+    return rotary._h, at, tokens * n if at is not None and tuple(positions.shape) in each else 0
+
+
+def rotary_apply(rotary, x, out, positions=None, inverse=False):
+    """freqattn_rotary_apply: x, out [batch, tokens, heads, head_dim]; out may be x."""
+    who = "rotary_apply"
+    if not isinstance(rotary, Rotary):
+        raise TypeError(f"{who}: rotary must be a Rotary")
+    hx = _heads(who, "x", x)
+    if x.dim() != 4:
+        raise ValueError(f"{who}: x must be [batch, tokens, heads, head_dim]")
+    ho = _heads(who, "out", out, x, x.shape, True)
+    b, n, h, d = x.shape
+    if d != rotary.head_dim:
+        raise ValueError(f"{who}: head_dim {d}, the rotary was made for {rotary.head_dim}")
+    hr, at, stride = _positions(who, rotary, positions, b, n, x)
+    _call(lib().freqattn_rotary_apply, x, hr, _io(x), b, n, h, hx, at, stride, 1 if inverse else 0, ho)
+    return out
+
+
+def _qk_args(who, q, k, wq, wk, eps, rotary, positions):
+    hq = _heads(who, "q", q)
+    if q.dim() != 4:
+        raise ValueError(f"{who}: q must be [batch, tokens, heads, head_dim]")
+    b, n, h, d = q.shape
+    hk, kh = None, 0
+    if k is not None:
+        if getattr(k, "dim", lambda: 0)() != 4:
+            raise ValueError(f"{who}: k must be [batch, tokens, heads, head_dim]")
+        kh = k.shape[2]
+        hk = _heads(who, "k", k, q, q.shape[:2] + (kh, d))
+    w = [_vector(who, name, x, q, d, q.dtype) for name, x in (("wq", wq), ("wk", wk))]
+    rot = _positions(who, rotary, positions, b, n, q)
+    if rotary is not None and d != rotary.head_dim:
+        raise ValueError(f"{who}: head_dim {d}, the rotary was made for {rotary.head_dim}")
+    return QkShape(b, n, h, kh, d, _io(q), eps), rot, hq, hk, w
+
+
+def qk_norm(q, k, wq, wk, q_out, k_out, eps=1e-6, rotary=None, positions=None):
+    """freqattn_qk_norm: q [batch, tokens, heads, head_dim], k likewise with its own number of heads (or None); weights [head_dim] or None."""
+    who = "qk_norm"
+    shape, rot, hq, hk, w = _qk_args(who, q, k, wq, wk, eps, rotary, positions)
+    oq = _heads(who, "q_out", q_out, q, q.shape, True)
+    ok = None if k is None else _heads(who, "k_out", k_out, q, k.shape, True)
+    _call(lib().freqattn_qk_norm, q, shape, *rot, hq, hk, *w, oq, ok)
+    return q_out, k_out
+
+
+def qk_norm_backward(q, k, wq, wk, dq_out, dk_out, dq, dk, dwq=None, dwk=None, eps=1e-6, rotary=None, positions=None, workspace=None):
+    """freqattn_qk_norm_backward: q, k, wq, wk, rotary, positions as in qk_norm; dwq, dwk fp32 [head_dim] or None."""
+    import torch
+    who = "qk_norm_backward"
+    shape, rot, hq, hk, w = _qk_args(who, q, k, wq, wk, eps, rotary, positions)
+    yq, xq = _heads(who, "dq_out", dq_out, q, q.shape), _heads(who, "dq", dq, q, q.shape, True)
+    yk = xk = None
+    if k is not None:
+        yk, xk = _heads(who, "dk_out", dk_out, q, k.shape), _heads(who, "dk", dk, q, k.shape, True)
+    dw = [_vector(who, name, x, q, q.shape[3], torch.float32) for name, x in (("dwq", dwq), ("dwk", dwk))]
+    need = 0 if dwq is None and dwk is None else lib().freqattn_qk_norm_workspace(q.shape[3])
+    ws, size, keep = _workspace(who, workspace, need, q)
+    _call(lib().freqattn_qk_norm_backward, q, shape, *rot, hq, hk, *w, yq, yk, xq, xk, *dw, ws, size)
+    return dq, dk, dwq, dwk
+
+
+def _sequence_args(who, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths):
+    hq, hk = _heads(who, "q", q), _heads(who, "k", k, q)
+    hv = _heads(who, "v", v, k, k.shape)
+    for name, t, off in (("q", q, q_offsets), ("k", k, k_offsets)):
+        if off is not None and not hasattr(off, "numel"):
+            raise ValueError(f"{who}: {name}_offsets must be a tensor")
+        if t.dim() != (4 if off is None else 3):
+            raise ValueError(f"{who}: {name} must be [rows, heads, head_dim] with {name}_offsets, [sequences, rows, heads, head_dim] without")
+    n = q.shape[0] if q_offsets is None else q_offsets.numel() - 1
+    if (k.shape[0] if k_offsets is None else k_offsets.numel() - 1) != n or n < 0:
+        raise ValueError(f"{who}: q and k must have the same number of sequences")
+    if q.shape[-1] != k.shape[-1]:
+        raise ValueError(f"{who}: q and k must have the same head_dim")
+    rows = SequenceRows(_int32(who, "q_offsets", q_offsets, q, (n + 1,)), _int32(who, "k_offsets", k_offsets, q, (n + 1,)),
+                        _int32(who, "q_lengths", q_lengths, q, (n,)), _int32(who, "k_lengths", k_lengths, q, (n,)))
+    shape = SequenceShape(n, q.shape[-2], k.shape[-2], q.shape[-1], q.shape[-3], k.shape[-3], _io(q), 1 if causal else 0, scale)
+    return shape, rows, hq, hk, hv
+
+
+def _lse(who, lse, q, q_offsets, heads):
+    import torch
+    cols = q.shape[0] if q_offsets is not None else q.shape[0] * q.shape[1]
+    if not isinstance(lse, torch.Tensor) or lse.dtype is not torch.float32 or lse.device != q.device or not lse.is_contiguous() \
+            or tuple(lse.shape) != (heads, cols):
+        raise ValueError(f"{who}: lse must be a contiguous float32 tensor of shape {(heads, cols)} on {q.device}")
+    return lse.data_ptr()
+
+
+def sequence_attention(q, k, v, out, lse=None, causal=False, scale=0.0, q_offsets=None, k_offsets=None, q_lengths=None, k_lengths=None,
+                       workspace=None):
+    """freqattn_sequence_attention: q, out [rows, heads, head_dim] with q_offsets (packed sequences) or [sequences, rows, heads, head_dim]; k, v
+    likewise with k_offsets and their own number of heads; lse [heads, rows] or [heads, sequences * rows] fp32."""
+    who = "sequence_attention"
+    shape, rows, hq, hk, hv = _sequence_args(who, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
+    ho = _heads(who, "out", out, q, q.shape, True)
+    at = None if lse is None else _lse(who, lse, q, q_offsets, shape.q_heads)
+    ws, size, keep = _workspace(who, workspace, lib().freqattn_sequence_attention_workspace(shape, rows), q)
+    _call(lib().freqattn_sequence_attention, q, shape, rows, hq, hk, hv, ho, at, ws, size)
+    return out
+
+
+def sequence_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, causal=False, scale=0.0, q_offsets=None, k_offsets=None, q_lengths=None,
+                                k_lengths=None, workspace=None):
+    """freqattn_sequence_attention_backward: arguments as in sequence_attention, out and lse as that call left them."""
+    who = "sequence_attention_backward"
+    shape, rows, hq, hk, hv = _sequence_args(who, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
+    hg, ho, xq = _heads(who, "dout", dout, q, q.shape), _heads(who, "out", out, q, q.shape), _heads(who, "dq", dq, q, q.shape, True)
+    xk, xv = _heads(who, "dk", dk, q, k.shape, True), _heads(who, "dv", dv, q, k.shape, True)
+    at = _lse(who, lse, q, q_offsets, shape.q_heads)
+    ws, size, keep = _workspace(who, workspace, lib().freqattn_sequence_attention_backward_workspace(shape, rows), q)
+    _call(lib().freqattn_sequence_attention_backward, q, shape, rows, hg, hq, hk, hv, ho, at, xq, xk, xv, ws, size)
+    return dq, dk, dv

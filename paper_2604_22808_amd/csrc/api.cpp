@@ -9,12 +9,15 @@
 #include <new>
 
 #include "ctx.h"
+#include "heads.h"
 
 using namespace fa;
 
 struct freqattn_ctx : public fa::Ctx {};
 
-static thread_local std::string g_create_error;
+static thread_local std::string g_create_error;   // also the last failure of a call without a context
+
+std::string& fa::context_free_error() { return g_create_error; }
 
 static freqattn_status fail(freqattn_ctx* c, freqattn_status s, const std::string& msg) {
   if (c) c->err = msg; else g_create_error = msg;

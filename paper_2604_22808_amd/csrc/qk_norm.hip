@@ -1,0 +1,471 @@
+// Rotary positions and per-head norms of queries and keys, forward and backward.
+//
+//   r = (mean_c x_c^2 + eps)^-1/2,  y = R(p) (x r w)                 R(p): turns pair i of the channels by p * theta_i, times the amplitude
+//   backward: g = R(p)^T dy,  dw = sum g x r,  dx = r (g w - x r^2 mean_c(g w x))
+//
+// Bound by memory: every element is read once (backward: x and dy) and written once.  A head's channels lie on LPR lanes, eight
+// per lane: four pairs, so that no channel has to change lanes for the rotation - in the HALF layout a lane loads four channels of the first half
+// and their four partners of the second.  The sums of the norm go through LPR lanes in registers.  A wave takes STEPS x 64 / LPR heads of
+// one token (all its loads go out before the first is used) and computes the token's sines and cosines once for all of them.
+// Angles: see RotTable; sine and cosine are Taylor sums on an eighth of a turn, |error| < 2^-24.
+#include <hip/hip_runtime.h>
+
+#include "heads.h"
+
+namespace fa {
+
+typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
+typedef unsigned int uint4v __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+struct Bf16 { uint16_t u; };
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(Bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
+template <typename T> __device__ __forceinline__ T narrow(float x);
+template <> __device__ __forceinline__ float narrow<float>(float x) { return x; }
+template <> __device__ __forceinline__ Bf16 narrow<Bf16>(float x) { return Bf16{__builtin_bit_cast(uint16_t, (__bf16)x)}; }   // to nearest, ties to even
+
+// Sine and cosine of u / 2^32 turns, times amp.
+__device__ __forceinline__ void sincos_turns(uint32_t u, float amp, float& s, float& c) {
+  const uint32_t quarter = (u + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(u - (quarter << 30)) * 1.46291807926715968e-9f;   // 2 pi / 2^32: within pi / 4
+  const float x2 = x * x;
+  const float ps = x * (1.f + x2 * (-1.f / 6 + x2 * (1.f / 120 + x2 * (-1.f / 5040 + x2 * (1.f / 362880)))));
+  const float pc = 1.f + x2 * (-0.5f + x2 * (1.f / 24 + x2 * (-1.f / 720 + x2 * (1.f / 40320 + x2 * (-1.f / 3628800)))));
+  s = (quarter & 1) ? pc : ps;
+  c = (quarter & 1) ? ps : pc;
+  s = (quarter & 2) ? -s : s;
+  c = ((quarter + 1) & 2) ? -c : c;
+  s *= amp;
+  c *= amp;
+}
+
+// The eight channels of a lane, as four pairs (a[j], b[j]).
+struct Pairs { float a[4], b[4]; };
+
+// Where a lane's channels lie.  SCALAR: pair by pair, for rows that are not made of aligned pieces; else two pieces of four (HALF) or one of eight.
+template <bool HALF, bool SCALAR>
+struct Place {
+  int ca[SCALAR ? 4 : 1], cb[SCALAR ? 4 : 1];
+  __device__ __forceinline__ void set(int unit, int half_r) {
+    if (SCALAR) {
+#pragma unroll
+      for (int j = 0; j < (SCALAR ? 4 : 1); ++j) {
+        const int i = unit * 4 + j;
+        ca[j] = HALF && i < half_r ? i : 2 * i;
+        cb[j] = HALF && i < half_r ? i + half_r : 2 * i + 1;
+      }
+    } else {
+      const int i = unit * 4;
+      ca[0] = HALF && i < half_r ? i : 2 * i;
+      cb[0] = HALF && i < half_r ? i + half_r : 2 * i + 4;
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
+  if constexpr (sizeof(T) == 4) {
+    const float4v v = *(const float4v*)p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = v[j];
+  } else {
+    const uint2v v = *(const uint2v*)p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = __uint_as_float((j & 1) ? (v[j >> 1] & 0xffff0000u) : (v[j >> 1] << 16));
+  }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return (uint32_t)narrow<Bf16>(a).u | ((uint32_t)narrow<Bf16>(b).u << 16);
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float (&x)[4]) {
+  if constexpr (sizeof(T) == 4) {
+    *(float4v*)p = float4v{x[0], x[1], x[2], x[3]};
+  } else {
+    *(uint2v*)p = uint2v{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  }
+}
+
+// valid: how many of the lane's pairs exist (4, except SCALAR at the end of a head)
+template <typename T, bool HALF, bool SCALAR>
+__device__ __forceinline__ Pairs load_pairs(const T* row, const Place<HALF, SCALAR>& pl, int valid) {
+  Pairs x;
+  if (SCALAR) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x.a[j] = j < valid ? widen(row[pl.ca[SCALAR ? j : 0]]) : 0.f;
+      x.b[j] = j < valid ? widen(row[pl.cb[SCALAR ? j : 0]]) : 0.f;
+    }
+  } else if (HALF) {
+    load4(row + pl.ca[0], x.a);
+    load4(row + pl.cb[0], x.b);
+    // (behind the rotated channels the two pieces are neighbours; which channel is whose partner does not matter there)
+  } else {
+    if constexpr (sizeof(T) == 2) {
+      const uint4v v = *(const uint4v*)(row + pl.ca[0]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { x.a[j] = __uint_as_float(v[j] << 16); x.b[j] = __uint_as_float(v[j] & 0xffff0000u); }
+    } else {
+      const float4v lo = *(const float4v*)(row + pl.ca[0]), hi = *(const float4v*)(row + pl.cb[0]);
+      x.a[0] = lo[0]; x.b[0] = lo[1]; x.a[1] = lo[2]; x.b[1] = lo[3];
+      x.a[2] = hi[0]; x.b[2] = hi[1]; x.a[3] = hi[2]; x.b[3] = hi[3];
+    }
+  }
+  return x;
+}
+template <typename T, bool HALF, bool SCALAR>
+__device__ __forceinline__ void store_pairs(T* row, const Place<HALF, SCALAR>& pl, int valid, const Pairs& x) {
+  if (SCALAR) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < valid) { row[pl.ca[SCALAR ? j : 0]] = narrow<T>(x.a[j]); row[pl.cb[SCALAR ? j : 0]] = narrow<T>(x.b[j]); }
+  } else if (HALF) {
+    store4(row + pl.ca[0], x.a);
+    store4(row + pl.cb[0], x.b);
+  } else if constexpr (sizeof(T) == 2) {
+    *(uint4v*)(row + pl.ca[0]) = uint4v{pack_bf16(x.a[0], x.b[0]), pack_bf16(x.a[1], x.b[1]), pack_bf16(x.a[2], x.b[2]), pack_bf16(x.a[3], x.b[3])};
+  } else {
+    *(float4v*)(row + pl.ca[0]) = float4v{x.a[0], x.b[0], x.a[1], x.b[1]};
+    *(float4v*)(row + pl.cb[0]) = float4v{x.a[2], x.b[2], x.a[3], x.b[3]};
+  }
+}
+
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+  for (int o = 1; o < LPR; o <<= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+// The rotation of a lane's pairs at one token.
+struct Turn { float s[4], c[4]; };
+
+// What a lane knows of its pairs' rotation, fixed for the launch.
+struct LaneRot { uint32_t lo[4], hi[4]; int axis[4]; bool on[4]; };
+
+__device__ __forceinline__ LaneRot lane_rot(const RotTable& t, int unit) {
+  LaneRot l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int i = unit * 4 + j;
+    l.on[j] = i < t.half;
+    const int at = l.on[j] ? i : 0;
+    l.lo[j] = (uint32_t)t.turn[at];
+    l.hi[j] = (uint32_t)(t.turn[at] >> 32);
+    l.axis[j] = t.axis[at];
+  }
+  return l;
+}
+
+__device__ __forceinline__ Turn turn_at(const QkParams& p, const RotTable& t, const LaneRot& l, int b, int n) {
+  int at[4] = {n, 0, 0, 0};
+  if (p.pos) {
+    const int32_t* q = p.pos + (int64_t)b * p.pos_bs + (int64_t)n * t.axes;
+    at[0] = q[0];
+#pragma unroll
+    for (int a = 1; a < 4; ++a)
+      if (a < t.axes) at[a] = q[a];
+  } else if (t.axes > 1 || t.grid[0]) {
+    uint32_t rest = (uint32_t)n;
+#pragma unroll
+    for (int a = 3; a > 0; --a)
+      if (a < t.axes) { at[a] = (int)(rest % t.grid[a]); rest /= t.grid[a]; }
+    at[0] = (int)rest;
+  }
+  Turn r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int pos = l.axis[j] == 0 ? at[0] : l.axis[j] == 1 ? at[1] : l.axis[j] == 2 ? at[2] : at[3];
+    const uint32_t u = __umulhi((uint32_t)pos, l.lo[j]) + (uint32_t)pos * l.hi[j] - (pos < 0 ? l.lo[j] : 0u);
+    sincos_turns(u, t.amplitude, r.s[j], r.c[j]);
+  }
+  return r;
+}
+
+__device__ __forceinline__ void rotate(Pairs& x, const Turn& t, const LaneRot& l, float sign) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (l.on[j]) {   // (channels that do not turn keep their bits, infinities too)
+      const float a = x.a[j], b = x.b[j], s = sign * t.s[j];
+      x.a[j] = a * t.c[j] - b * s;
+      x.b[j] = b * t.c[j] + a * s;
+    }
+}
+
+template <typename T, bool HALF, bool SCALAR>
+__device__ __forceinline__ Pairs load_weight(const void* w, const Place<HALF, SCALAR>& pl, int valid, bool live) {
+  Pairs x;
+  if (w && live) return load_pairs<T, HALF, SCALAR>((const T*)w, pl, valid);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x.a[j] = x.b[j] = 1.f;
+  return x;
+}
+
+// How a launch cuts the work: an item is `tpw` tokens x `64 / LPR * STEPS` heads (one wave).
+struct Items { int tpw, head_groups; uint32_t n; };
+enum : int64_t { MAX_ITEMS = (int64_t)1 << 25 };   // a launch has fewer than 2^32 threads
+
+template <typename T, int LPR, bool HALF, bool SCALAR, int STEPS>
+__global__ void __launch_bounds__(256) k_qk(QkParams p, const RotTable t, Items it) {
+  constexpr int RPW = 64 / LPR;
+  const int lane = threadIdx.x & 63, unit = lane % LPR, hr = lane / LPR;
+  const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
+  if (item >= it.n) return;
+  const uint32_t tg = item / (uint32_t)it.head_groups;
+  const int heads = p.heads[0] + p.heads[1];
+  // rows of the wave: several tokens' heads where a token has fewer heads than the wave has rows
+  const int sub = it.tpw > 1 ? hr / heads : 0, h_first = (it.tpw > 1 ? hr - sub * heads : (int)(item % (uint32_t)it.head_groups) * RPW * STEPS + hr);
+  const int64_t token = (int64_t)tg * it.tpw + sub;
+  const int valid_pairs = p.d / 2 - unit * 4;
+  const int valid = valid_pairs < 0 ? 0 : valid_pairs > 4 ? 4 : valid_pairs;
+  const bool live = valid > 0 && sub < it.tpw && token < (int64_t)p.batch * p.tokens;
+  const int b = live ? (int)(token / p.tokens) : 0, n = live ? (int)(token - (int64_t)b * p.tokens) : 0;
+  Place<HALF, SCALAR> pl;
+  pl.set(unit, t.half);
+  const LaneRot lr = lane_rot(t, unit);
+
+  Pairs x[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int h = h_first + s * RPW;
+    if (live && h < heads) {
+      const int w = h >= p.heads[0];
+      const HeadsPtr& v = p.in[w];
+      x[s] = load_pairs<T, HALF, SCALAR>((const T*)v.p + (int64_t)b * v.bs + (int64_t)n * v.ts + (int64_t)(h - (w ? p.heads[0] : 0)) * v.hs, pl, valid);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[s].a[j] = x[s].b[j] = 0.f;
+    }
+  }
+  Pairs wq, wk;
+  if (p.norm) {
+    wq = load_weight<T, HALF, SCALAR>(p.w[0], pl, valid, live);
+    wk = load_weight<T, HALF, SCALAR>(p.w[1], pl, valid, live);
+  }
+  Turn tn;
+  if (t.half > 0) tn = turn_at(p, t, lr, b, n);
+  const float sign = p.inverse ? -1.f : 1.f;
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int h = h_first + s * RPW;
+    const int w = h >= p.heads[0];
+    if (p.norm) {
+      float ss = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ss += x[s].a[j] * x[s].a[j] + x[s].b[j] * x[s].b[j];
+      const float r = 1.f / sqrtf(row_sum<LPR>(ss) / (float)p.d + p.eps);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[s].a[j] *= r * (w ? wk.a[j] : wq.a[j]);
+        x[s].b[j] *= r * (w ? wk.b[j] : wq.b[j]);
+      }
+    }
+    if (live && h < heads) {
+      if (t.half > 0) rotate(x[s], tn, lr, sign);
+      const HeadsPtr& v = p.out[w];
+      store_pairs<T, HALF, SCALAR>((T*)v.p + (int64_t)b * v.bs + (int64_t)n * v.ts + (int64_t)(h - (w ? p.heads[0] : 0)) * v.hs, pl, valid, x[s]);
+    }
+  }
+}
+
+// Backward: the blocks are dealt to the two tensors by `first_k`; a wave walks items of its tensor and keeps its lanes' sums of dw in
+// registers.  A block adds its waves' sums in a fixed order and stores one row of partial sums; k_qk_weights adds the rows.
+template <typename T, int LPR, bool HALF, bool SCALAR, int STEPS>
+__global__ void __launch_bounds__(256) k_qk_backward(QkParams p, const RotTable t, Items iq, Items ik, int first_k) {
+  constexpr int RPW = 64 / LPR;
+  const int lane = threadIdx.x & 63, unit = lane % LPR, hr = lane / LPR, wave = threadIdx.x >> 6;
+  const int which = (int)blockIdx.x >= first_k;
+  const Items it = which ? ik : iq;
+  const uint32_t waves = 4u * (which ? gridDim.x - first_k : first_k);
+  const int heads = p.heads[which];
+  const HeadsPtr vx = p.in[which], vy = p.dy[which], vo = p.out[which];
+  const int valid_pairs = p.d / 2 - unit * 4;
+  const int valid = valid_pairs < 0 ? 0 : valid_pairs > 4 ? 4 : valid_pairs;
+  Place<HALF, SCALAR> pl;
+  pl.set(unit, t.half);
+  const LaneRot lr = lane_rot(t, unit);
+  const Pairs w = load_weight<T, HALF, SCALAR>(p.w[which], pl, valid, valid > 0);
+  Pairs dw;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) dw.a[j] = dw.b[j] = 0.f;
+  const int sub = it.tpw > 1 ? hr / heads : 0;
+
+  for (uint32_t item = 4u * (blockIdx.x - (which ? first_k : 0)) + wave; item < it.n; item += waves) {
+    const uint32_t tg = item / (uint32_t)it.head_groups;
+    const int h_first = it.tpw > 1 ? hr - sub * heads : (int)(item - tg * (uint32_t)it.head_groups) * RPW * STEPS + hr;
+    const int64_t token = (int64_t)tg * it.tpw + sub;
+    const bool live = valid > 0 && sub < it.tpw && token < (int64_t)p.batch * p.tokens;
+    const int b = live ? (int)(token / p.tokens) : 0, n = live ? (int)(token - (int64_t)b * p.tokens) : 0;
+    Pairs x[STEPS], g[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int h = h_first + s * RPW;
+      if (live && h < heads) {
+        x[s] = load_pairs<T, HALF, SCALAR>((const T*)vx.p + (int64_t)b * vx.bs + (int64_t)n * vx.ts + (int64_t)h * vx.hs, pl, valid);
+        g[s] = load_pairs<T, HALF, SCALAR>((const T*)vy.p + (int64_t)b * vy.bs + (int64_t)n * vy.ts + (int64_t)h * vy.hs, pl, valid);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[s].a[j] = x[s].b[j] = g[s].a[j] = g[s].b[j] = 0.f;
+      }
+    }
+    Turn tn;
+    if (t.half > 0) tn = turn_at(p, t, lr, b, n);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int h = h_first + s * RPW;
+      if (t.half > 0) rotate(g[s], tn, lr, -1.f);
+      float ss = 0.f, gx = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ss += x[s].a[j] * x[s].a[j] + x[s].b[j] * x[s].b[j];
+        gx += g[s].a[j] * w.a[j] * x[s].a[j] + g[s].b[j] * w.b[j] * x[s].b[j];
+      }
+      ss = row_sum<LPR>(ss);
+      gx = row_sum<LPR>(gx);
+      const float r = 1.f / sqrtf(ss / (float)p.d + p.eps);
+      const float m = r * r * (gx / (float)p.d);
+      if (live && h < heads) {
+        Pairs o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          dw.a[j] += g[s].a[j] * (x[s].a[j] * r);
+          dw.b[j] += g[s].b[j] * (x[s].b[j] * r);
+          o.a[j] = r * (g[s].a[j] * w.a[j] - x[s].a[j] * m);
+          o.b[j] = r * (g[s].b[j] * w.b[j] - x[s].b[j] * m);
+        }
+        store_pairs<T, HALF, SCALAR>((T*)vo.p + (int64_t)b * vo.bs + (int64_t)n * vo.ts + (int64_t)h * vo.hs, pl, valid, o);
+      }
+    }
+  }
+  if (!p.part) return;
+  __shared__ float sums[4][8 * LPR];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1) { dw.a[j] += __shfl_xor(dw.a[j], o); dw.b[j] += __shfl_xor(dw.b[j], o); }
+    if (hr == 0) { sums[wave][unit * 8 + j] = dw.a[j]; sums[wave][unit * 8 + 4 + j] = dw.b[j]; }
+  }
+  __syncthreads();
+  // back to channel order: slot unit*8 + j is channel a[j], + 4 its partner b[j]
+  for (int i = threadIdx.x; i < p.d; i += 256) {
+    int pair, second;
+    if (HALF && i < 2 * t.half) { second = i >= t.half; pair = i - second * t.half; }
+    else if (!HALF || SCALAR) { pair = i >> 1; second = i & 1; }
+    else { pair = (i >> 3) * 4 + (i & 3); second = (i >> 2) & 1; }   // (aligned pieces behind the rotated channels of the HALF layout)
+    const int slot = (pair >> 2) * 8 + (pair & 3) + 4 * second;
+    p.part[(int64_t)blockIdx.x * p.d + i] = (sums[0][slot] + sums[1][slot]) + (sums[2][slot] + sums[3][slot]);
+  }
+}
+
+// dw[c] = sum over rows first..last - 1 of the partial sums; a block adds 32 channels, 32 threads a channel.
+__global__ void __launch_bounds__(1024) k_qk_weights(const float* __restrict__ part, int d, int first_k, int blocks, float* dwq, float* dwk) {
+  float* dst = blockIdx.y ? dwk : dwq;
+  if (!dst) return;   // (uniform over the block)
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
+  float s = 0.f;
+  if (c < d)
+    for (int i = (blockIdx.y ? first_k : 0) + row; i < (blockIdx.y ? blocks : first_k); i += 32) s += part[(int64_t)i * d + c];
+  __shared__ float acc[32][33];
+  acc[row][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (row == 0 && c < d) {
+    float r = 0.f;
+    for (int i = 0; i < 32; ++i) r += acc[i][threadIdx.x & 31];
+    dst[c] = r;
+  }
+}
+
+static bool pieces(const HeadsPtr& v, int bytes, int size) {
+  return (uintptr_t)v.p % bytes == 0 && (v.bs * size) % bytes == 0 && (v.ts * size) % bytes == 0 && (v.hs * size) % bytes == 0;
+}
+
+static Items make_items(int64_t tokens, int heads, int rpw, int steps) {
+  Items it;
+  it.tpw = heads < rpw ? rpw / heads : 1;
+  it.head_groups = it.tpw > 1 ? 1 : (heads + rpw * steps - 1) / (rpw * steps);
+  const int64_t n = (tokens + it.tpw - 1) / it.tpw * it.head_groups;
+  it.n = n <= MAX_ITEMS ? (uint32_t)n : ~0u;
+  return it;
+}
+
+template <typename T, int LPR, bool HALF, bool SCALAR, int STEPS>
+static hipError_t fwd_s(const QkParams& p, const RotTable& t, hipStream_t st) {
+  const Items it = make_items((int64_t)p.batch * p.tokens, p.heads[0] + p.heads[1], 64 / LPR, STEPS);
+  if (it.n == ~0u) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((k_qk<T, LPR, HALF, SCALAR, STEPS>), dim3((it.n + 3) / 4), dim3(256), 0, st, p, t, it);
+  return hipGetLastError();
+}
+template <typename T, int LPR, bool HALF, bool SCALAR>
+static hipError_t fwd(const QkParams& p, const RotTable& t, int num_cu, hipStream_t st) {
+  // Four steps share a token's sines and have four loads in flight; where that leaves fewer than 8 waves per compute unit, one step per wave.
+  const int64_t rows = (int64_t)p.batch * p.tokens * (p.heads[0] + p.heads[1]);
+  if (p.heads[0] + p.heads[1] <= 64 / LPR || rows < (int64_t)num_cu * 8 * 4 * (64 / LPR)) return fwd_s<T, LPR, HALF, SCALAR, 1>(p, t, st);
+  return fwd_s<T, LPR, HALF, SCALAR, 4>(p, t, st);
+}
+template <typename T, int LPR, bool HALF, bool SCALAR>
+static hipError_t bwd(const QkParams& p, const RotTable& t, float* const dw[2], int num_cu, hipStream_t st) {
+  constexpr int STEPS = 2;
+  const int64_t tokens = (int64_t)p.batch * p.tokens;
+  const Items iq = make_items(tokens, p.heads[0], 64 / LPR, STEPS);
+  Items ik = {1, 1, 0};
+  if (p.heads[1] > 0) ik = make_items(tokens, p.heads[1], 64 / LPR, STEPS);
+  if (iq.n == ~0u || ik.n == ~0u) return hipErrorInvalidConfiguration;
+  // resident blocks, dealt to q and k by their items
+  int64_t total = ((int64_t)iq.n + ik.n + 3) / 4;
+  if (total > 4 * num_cu) total = 4 * num_cu;
+  if (total > QK_BWD_BLOCKS) total = QK_BWD_BLOCKS;
+  if (total < 1) total = 1;
+  int first_k = (int)total, blocks = (int)total;
+  if (ik.n) {
+    if (total < 2) total = 2;
+    first_k = (int)(total * iq.n / ((int64_t)iq.n + ik.n));
+    if (first_k < 1) first_k = 1;
+    if (first_k > total - 1) first_k = (int)total - 1;
+    blocks = (int)total;
+  }
+  hipLaunchKernelGGL((k_qk_backward<T, LPR, HALF, SCALAR, STEPS>), dim3((unsigned)blocks), dim3(256), 0, st, p, t, iq, ik, first_k);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.part) return e;
+  hipLaunchKernelGGL(k_qk_weights, dim3((unsigned)((p.d + 31) / 32), p.heads[1] > 0 ? 2u : 1u), dim3(1024), 0, st, p.part, p.d, first_k, blocks,
+                     dw[0], dw[1]);
+  return hipGetLastError();
+}
+
+// The variant that fits a call: lanes per head, and whether rows are made of aligned pieces.
+template <typename T, bool HALF, typename F>
+static hipError_t dispatch(const QkParams& p, const RotTable& t, bool backward, F&& go) {
+  const int size = sizeof(T), piece = HALF ? 4 * size : 16;
+  bool al = p.d % 8 == 0 && (!HALF || t.half % 4 == 0);
+  for (int w = 0; w < 2; ++w)
+    if (p.heads[w] > 0) {
+      al = al && pieces(p.in[w], piece, size) && pieces(p.out[w], piece, size) && (!backward || pieces(p.dy[w], piece, size));
+      al = al && (!p.w[w] || (uintptr_t)p.w[w] % piece == 0);
+    }
+  const int lanes = (p.d / 2 + 3) / 4;
+#define FA_QK(L_, S_) if (lanes <= L_ && al == !S_) return go(std::integral_constant<int, L_>(), std::integral_constant<bool, S_>());
+  FA_QK(4, false) FA_QK(8, false) FA_QK(16, false) FA_QK(32, false) FA_QK(64, false) FA_QK(16, true) FA_QK(64, true)
+#undef FA_QK
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_qk(const QkParams& p, const RotTable& t, int dtype, int num_cu, hipStream_t st) {
+  auto with = [&](auto type, auto half) {
+    using T = decltype(type);
+    return dispatch<T, half.value>(p, t, false, [&](auto lanes, auto scalar) { return fwd<T, lanes.value, half.value, scalar.value>(p, t, num_cu, st); });
+  };
+  if (dtype == FREQATTN_BF16) return t.interleaved ? with(Bf16{}, std::false_type{}) : with(Bf16{}, std::true_type{});
+  return t.interleaved ? with(0.f, std::false_type{}) : with(0.f, std::true_type{});
+}
+
+hipError_t launch_qk_backward(const QkParams& p, const RotTable& t, int dtype, float* const dw[2], int num_cu, hipStream_t st) {
+  auto with = [&](auto type, auto half) {
+    using T = decltype(type);
+    return dispatch<T, half.value>(p, t, true, [&](auto lanes, auto scalar) { return bwd<T, lanes.value, half.value, scalar.value>(p, t, dw, num_cu, st); });
+  };
+  if (dtype == FREQATTN_BF16) return t.interleaved ? with(Bf16{}, std::false_type{}) : with(Bf16{}, std::true_type{});
+  return t.interleaved ? with(0.f, std::false_type{}) : with(0.f, std::true_type{});
+}
+
+}  // namespace fa

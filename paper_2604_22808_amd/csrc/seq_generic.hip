@@ -1,0 +1,363 @@
+// Attention over sequences with fp32 products (v_mfma_f32_32x32x2_f32), forward and backward: FREQATTN_F32 tensors, and bf16 ones that
+// the bf16 kernels do not take (rows that are not whole aligned 16-byte pieces).
+//
+//   S = scale Q K^T,  O = softmax(S) V,  lse = log sum exp S;  delta = rowsum(dO O),  P = exp(S - lse),  dS = P (dO V^T - delta),
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//
+// A wave owns 32 rows - query rows in the forward and dQ kernels, key rows in the dK / dV kernel - as columns of transposed products: S^T = K Q^T
+// leaves a column (a query) on two lanes, whose accumulator registers are then the B operand of O^T += V^T P^T as they stand: step
+// r of v_mfma_f32_32x32x2 takes k = 8 (r / 4) + r % 4 + 4 g from lane half g, which is where register r of the product before it lies.
+// The other side passes through LDS in tiles of 32 rows, widened to fp32.  The sums over keys (dQ) and over queries (dK, dV) are taken by
+// different kernels, each by one workgroup in a fixed order, instead of by atomics: 7 products instead of 5, equal bits every time.
+// Bound by the fp32 matrix rate (157 TFLOP/s peak) less the tile loads, which are not overlapped.
+#include <hip/hip_runtime.h>
+
+#include "seq_common.h"
+
+namespace fa {
+
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
+
+namespace {
+
+struct Bf16 { uint16_t u; };
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(Bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(Bf16* p, float x) { p->u = __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int TR = 32;    // rows of a tile
+
+__device__ __forceinline__ float16v zero16() {
+  float16v z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+
+template <typename T>
+__device__ __forceinline__ const T* row_of(const HeadsPtr& v, int seq, int64_t row, int head) {
+  return (const T*)v.p + (int64_t)seq * v.bs + row * v.ts + (int64_t)head * v.hs;
+}
+template <typename T>
+__device__ __forceinline__ T* row_of_out(const HeadsPtr& v, int seq, int64_t row, int head) {
+  return (T*)const_cast<char*>(v.p) + (int64_t)seq * v.bs + row * v.ts + (int64_t)head * v.hs;
+}
+
+// Four channels c .. c + 3 of a row, zero from d on.
+template <typename T>
+__device__ __forceinline__ float4v chunk(const T* row, int c, int d, bool live, int vec) {
+  float4v x = {0.f, 0.f, 0.f, 0.f};
+  if (!live || c >= d) return x;
+  if (vec) {
+    if constexpr (sizeof(T) == 4) return *(const float4v*)(row + c);
+    const uint2v u = *(const uint2v*)(row + c);
+    return float4v{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < d) x[j] = widen(row[c + j]);
+  return x;
+}
+
+// The lane's share of a row as an operand over the channels: chunk s holds channels 8 s + 4 g .. + 3.
+template <typename T, int D>
+struct RowOperand {
+  float4v x[D / 8];
+  __device__ __forceinline__ void load(const T* row, int g, int d, bool live, int vec) {
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) x[s] = chunk(row, 8 * s + 4 * g, d, live, vec);
+  }
+};
+
+// tile (32 rows, LDS, stride D + 4) x operand: rows of the tile on registers, the operand's row on the lane
+template <typename T, int D>
+__device__ __forceinline__ float16v product(const float* tile, const RowOperand<T, D>& b, int nn, int g) {
+  float16v acc = zero16();
+#pragma unroll
+  for (int s = 0; s < D / 8; ++s) {
+    const float4v a = *(const float4v*)(tile + nn * (D + 4) + 8 * s + 4 * g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b.x[s][j], acc, 0, 0, 0);
+  }
+  return acc;
+}
+
+// acc[dt] (channels on registers) += tile^T x w, w: one value per tile row on the registers, as product() leaves them
+template <int D>
+__device__ __forceinline__ void accumulate(float16v (&acc)[D / 32], const float* tile, const float16v& w, int nn, int g) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const float* row = tile + (8 * (r >> 2) + (r & 3) + 4 * g) * (D + 4);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(row[dt * 32 + nn], w[r], acc[dt], 0, 0, 0);
+  }
+}
+
+// A product of a probability that is exactly zero and a value that is not finite is NaN on the matrix core, but a masked pair contributes nothing.  So where a
+// tile has masked pairs and values that are not finite, those values are added to the rows that do see them and taken out of the tile.  Rare:
+// tiles without them pay one comparison per value.  `seen(i)`: does the lane's row see row i of the tile.
+template <int D, typename F>
+__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], float* tile, int nn, int g, F&& seen) {
+  bool odd = false;
+  for (int i = threadIdx.x; i < TR * D; i += blockDim.x) odd = odd || !(fabsf(tile[i / D * (D + 4) + i % D]) <= 3.4028235e38f);
+  if (!__syncthreads_or(odd)) return;
+  for (int i = 0; i < TR; ++i) {
+    const bool s = seen(i);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = tile[i * (D + 4) + dt * 32 + 8 * (r >> 2) + 4 * g + (r & 3)];
+        if (s && !(fabsf(x) <= 3.4028235e38f)) acc[dt][r] += x;
+      }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < TR * D; i += blockDim.x) {
+    float& x = tile[i / D * (D + 4) + i % D];
+    if (!(fabsf(x) <= 3.4028235e38f)) x = 0.f;
+  }
+  __syncthreads();
+}
+
+// What a query row is: token, head, and the last key it sees.
+struct Row { bool live; int token, head, last; };
+
+__device__ __forceinline__ Row query_row(const SeqParams& p, int kvh, int r, int nq, int nk) {
+  Row w;
+  w.live = r < nq * p.group;
+  w.token = w.live ? r / p.group : 0;
+  w.head = kvh * p.group + (w.live ? r - w.token * p.group : 0);
+  w.last = !w.live ? -1 : p.causal ? (w.token + nk - nq < nk - 1 ? w.token + nk - nq : nk - 1) : nk - 1;
+  return w;
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void load_tile(float* dst, const HeadsPtr& v, int seq, int base, int row0, int n, int head, int d, int vec) {
+  for (int i = threadIdx.x; i < TR * D / 4; i += blockDim.x) {
+    const int r = i / (D / 4), c = i % (D / 4) * 4;
+    const bool live = row0 + r < n;
+    *(float4v*)(dst + r * (D + 4) + c) = chunk(live ? row_of<T>(v, seq, base + row0 + r, head) : nullptr, c, d, live, vec);
+  }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void store_row(T* row, const float16v (&acc)[D / 32], float f, int g, int d) {
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int c = dt * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
+      if (c < d) put(row + c, acc[dt][r] * f);
+    }
+}
+
+// Which tile a workgroup takes: key heads fastest (they share nothing, and go to different XCDs), tiles from the last, so that under the causal
+// mask the longest come first.
+struct Work { int kvh, seq, tile; };
+__device__ __forceinline__ Work work_of(const SeqParams& p, const int32_t* off, int rows, int mult, int tile_rows) {
+  Work w;
+  w.kvh = (int)(blockIdx.x % (unsigned)p.hk);
+  seq_slot(off, rows, p.nseq, mult, tile_rows, p.slots - 1 - (int)(blockIdx.x / (unsigned)p.hk), w.seq, w.tile);
+  return w;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 1) k_seq_generic_fwd(SeqParams p) {
+  __shared__ float Ks[TR * (D + 4)], Vs[TR * (D + 4)];
+  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
+  const Work w = work_of(p, p.q_off, p.q_rows, p.group, 128);
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, w.seq), k = seq_range(p.k_off, p.k_len, p.k_rows, w.seq);
+  if ((int64_t)w.tile * 128 >= (int64_t)q.n * p.group) return;
+  const Row row = query_row(p, w.kvh, w.tile * 128 + wave * 32 + nn, q.n, k.n);
+  RowOperand<T, D> Q;
+  Q.load(row_of<T>(p.q, q.seq, q.base + row.token, row.head), g, p.d, row.live, p.vec);
+  const int last_row = min(w.tile * 128 + 127, q.n * p.group - 1);
+  const int last = query_row(p, w.kvh, last_row, q.n, k.n).last;    // of the whole tile: the last row sees the most
+  const float c2 = p.scale * LOG2E;
+  float16v O[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) O[dt] = zero16();
+  float m = -INFINITY, l = 0.f;
+  for (int key0 = 0; key0 <= last; key0 += TR) {
+    __syncthreads();
+    load_tile<T, D>(Ks, p.k, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
+    load_tile<T, D>(Vs, p.v, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
+    __syncthreads();
+    if (p.causal && key0 + TR - 1 > query_row(p, w.kvh, w.tile * 128, q.n, k.n).last)
+      set_aside<D>(O, Vs, nn, g, [&](int i) { return key0 + i <= row.last; });
+    float16v S = product<T, D>(Ks, Q, nn, g);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = key0 + 8 * (r >> 2) + 4 * g + (r & 3);
+      S[r] = key <= row.last ? S[r] * c2 : -INFINITY;
+      mx = fmaxf(mx, S[r]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
+    const float alpha = __builtin_amdgcn_exp2f(m - ref);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = key0 + 8 * (r >> 2) + 4 * g + (r & 3);
+      S[r] = key <= row.last ? __builtin_amdgcn_exp2f(S[r] - ref) : 0.f;
+      l += S[r];
+    }
+    accumulate<D>(O, Vs, S, nn, g);
+  }
+  l += __shfl_xor(l, 32);
+  if (!row.live) return;
+  store_row<T, D>(row_of_out<T>(p.o, q.seq, q.base + row.token, row.head), O, row.last < 0 ? 0.f : 1.f / l, g, p.d);
+  if (p.lse && g == 0)
+    p.lse[(int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)w.seq * p.q_rows) + row.token] = row.last < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+// dQ, and the row sums delta that the other kernel reads.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 1) k_seq_generic_dq(SeqParams p) {
+  __shared__ float Ks[TR * (D + 4)], Vs[TR * (D + 4)];
+  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
+  const Work w = work_of(p, p.q_off, p.q_rows, p.group, 128);
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, w.seq), k = seq_range(p.k_off, p.k_len, p.k_rows, w.seq);
+  if ((int64_t)w.tile * 128 >= (int64_t)q.n * p.group) return;
+  const Row row = query_row(p, w.kvh, w.tile * 128 + wave * 32 + nn, q.n, k.n);
+  RowOperand<T, D> Q, dO;
+  Q.load(row_of<T>(p.q, q.seq, q.base + row.token, row.head), g, p.d, row.live, p.vec);
+  dO.load(row_of<T>(p.dout, q.seq, q.base + row.token, row.head), g, p.d, row.live, p.vec);
+  float delta = 0.f;
+  {
+    const T* o = row_of<T>(p.o, q.seq, q.base + row.token, row.head);
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) {
+      const float4v x = chunk(o, 8 * s + 4 * g, p.d, row.live && row.last >= 0, p.vec);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) delta += row.last >= 0 ? x[j] * dO.x[s][j] : 0.f;
+    }
+    delta += __shfl_xor(delta, 32);
+  }
+  const int64_t at = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)w.seq * p.q_rows) + row.token;
+  if (row.live && g == 0) p.delta[at] = delta;
+  const float lse2 = row.live && row.last >= 0 ? p.lse[at] * LOG2E : 0.f;
+  const int last = query_row(p, w.kvh, min(w.tile * 128 + 127, q.n * p.group - 1), q.n, k.n).last;
+  const float c2 = p.scale * LOG2E;
+  float16v A[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) A[dt] = zero16();
+  for (int key0 = 0; key0 <= last; key0 += TR) {
+    __syncthreads();
+    load_tile<T, D>(Ks, p.k, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
+    load_tile<T, D>(Vs, p.v, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
+    __syncthreads();
+    float16v S = product<T, D>(Ks, Q, nn, g);
+    const float16v dP = product<T, D>(Vs, dO, nn, g);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = key0 + 8 * (r >> 2) + 4 * g + (r & 3);
+      S[r] = key <= row.last ? __builtin_amdgcn_exp2f(S[r] * c2 - lse2) * (dP[r] - delta) : 0.f;
+    }
+    if (p.causal && key0 + TR - 1 > query_row(p, w.kvh, w.tile * 128, q.n, k.n).last) {
+      set_aside<D>(A, Ks, nn, g, [&](int i) { return key0 + i <= row.last; });
+    }
+    accumulate<D>(A, Ks, S, nn, g);
+  }
+  if (row.live) store_row<T, D>(row_of_out<T>(p.dq, q.seq, q.base + row.token, row.head), A, p.scale, g, p.d);
+}
+
+// dK and dV of 128 keys, over all query rows of the sequence and group that see any of them.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 1) k_seq_generic_dkv(SeqParams p) {
+  __shared__ float Qs[TR * (D + 4)], Gs[TR * (D + 4)], Ls[TR], Ds[TR];
+  __shared__ int Last[TR];
+  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
+  const Work w = work_of(p, p.k_off, p.k_rows, 1, 128);
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, w.seq), k = seq_range(p.k_off, p.k_len, p.k_rows, w.seq);
+  if (w.tile * 128 >= k.n) return;
+  const int key = w.tile * 128 + wave * 32 + nn;
+  const bool live = key < k.n;
+  RowOperand<T, D> K, V;
+  K.load(row_of<T>(p.k, k.seq, k.base + (live ? key : 0), w.kvh), g, p.d, live, p.vec);
+  V.load(row_of<T>(p.v, k.seq, k.base + (live ? key : 0), w.kvh), g, p.d, live, p.vec);
+  float16v dK[D / 32], dV[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) { dK[dt] = zero16(); dV[dt] = zero16(); }
+  const float c2 = p.scale * LOG2E;
+  const int rows = q.n * p.group;
+  // the first token that sees the tile's first key
+  int first = p.causal ? w.tile * 128 - (k.n - q.n) : 0;
+  if (first < 0) first = 0;
+  const int last_key = min(w.tile * 128 + 127, k.n - 1);
+  for (int64_t r0 = (int64_t)first * p.group / TR * TR; r0 < rows; r0 += TR) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < TR * D / 4; i += blockDim.x) {
+      const int r = i / (D / 4), c = i % (D / 4) * 4;
+      const Row row = query_row(p, w.kvh, (int)r0 + r, q.n, k.n);
+      *(float4v*)(Qs + r * (D + 4) + c) = chunk(row_of<T>(p.q, q.seq, q.base + row.token, row.head), c, p.d, row.live, p.vec);
+      *(float4v*)(Gs + r * (D + 4) + c) = chunk(row_of<T>(p.dout, q.seq, q.base + row.token, row.head), c, p.d, row.live, p.vec);
+      if (c == 0) {
+        const int64_t at = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)w.seq * p.q_rows) + row.token;
+        Ls[r] = row.live && row.last >= 0 ? p.lse[at] * LOG2E : 0.f;
+        Ds[r] = row.live && row.last >= 0 ? p.delta[at] : 0.f;
+        Last[r] = row.last;
+      }
+    }
+    __syncthreads();
+    float16v S = product<T, D>(Qs, K, nn, g);
+    float16v dP = product<T, D>(Gs, V, nn, g);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int i = 8 * (r >> 2) + 4 * g + (r & 3);
+      const bool seen = live && key <= Last[i];
+      S[r] = seen ? __builtin_amdgcn_exp2f(S[r] * c2 - Ls[i]) : 0.f;
+      dP[r] = seen ? S[r] * (dP[r] - Ds[i]) : 0.f;
+    }
+    if (Last[0] < last_key || Last[TR - 1] < last_key) {   // (uniform) some pair is masked: queries before the diagonal, rows behind the last query
+      set_aside<D>(dV, Gs, nn, g, [&](int i) { return live && key <= Last[i]; });
+      set_aside<D>(dK, Qs, nn, g, [&](int i) { return live && key <= Last[i]; });
+    }
+    accumulate<D>(dV, Gs, S, nn, g);
+    accumulate<D>(dK, Qs, dP, nn, g);
+  }
+  if (!live) return;
+  store_row<T, D>(row_of_out<T>(p.dk, k.seq, k.base + key, w.kvh), dK, p.scale, g, p.d);
+  store_row<T, D>(row_of_out<T>(p.dv, k.seq, k.base + key, w.kvh), dV, 1.f, g, p.d);
+}
+
+template <typename T, int D>
+hipError_t fwd(SeqParams p, hipStream_t st) {
+  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 128);
+  if (p.slots == 0) return hipSuccess;
+  hipLaunchKernelGGL((k_seq_generic_fwd<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+template <typename T, int D>
+hipError_t bwd(SeqParams p, hipStream_t st) {
+  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 128);
+  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dq<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  p.slots = (int)seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 128);
+  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dkv<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_seq_generic_fwd(const SeqParams& p, int dtype, hipStream_t st) {
+  if (dtype == FREQATTN_BF16) return p.d <= 64 ? fwd<Bf16, 64>(p, st) : fwd<Bf16, 128>(p, st);
+  return p.d <= 64 ? fwd<float, 64>(p, st) : fwd<float, 128>(p, st);
+}
+hipError_t launch_seq_generic_bwd(const SeqParams& p, int dtype, hipStream_t st) {
+  if (dtype == FREQATTN_BF16) return p.d <= 64 ? bwd<Bf16, 64>(p, st) : bwd<Bf16, 128>(p, st);
+  return p.d <= 64 ? bwd<float, 64>(p, st) : bwd<float, 128>(p, st);
+}
+
+}  // namespace fa
