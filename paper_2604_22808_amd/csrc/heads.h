@@ -53,10 +53,18 @@ struct SeqParams {
   int64_t lse_rows;              // columns of lse
   float scale;
   int32_t slots;                 // tiles of the launch per key head (upper bound)
-  int32_t nsplit;
+  int32_t nsplit, split_tiles;   // pieces of the keys, and key tiles of a piece
   int32_t vec;                   // all tensors and strides are 16-byte aligned and rows are whole 16-byte pieces
 };
 
+// How a forward call of the bf16 kernels is cut; depends on sizes alone.
+struct SeqPlan {
+  bool few;             // tiles of 32 query rows instead of 128
+  int nsplit, split_tiles;
+  int64_t workspace;    // bytes
+};
+SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu);
+hipError_t launch_seq_fwd(SeqParams p, const SeqPlan& s, hipStream_t st);
 hipError_t launch_seq_generic_fwd(const SeqParams& p, int dtype, hipStream_t st);
 hipError_t launch_seq_generic_bwd(const SeqParams& p, int dtype, hipStream_t st);
 

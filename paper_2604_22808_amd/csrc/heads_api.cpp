@@ -281,6 +281,9 @@ freqattn_status seq_params(const char* who, const freqattn_sequence_shape* s, co
   return FREQATTN_OK;
 }
 
+// Eight rows lie within 2^32 bytes, as one copy of the bf16 kernels takes them.
+bool near(const HeadsPtr& v) { return v.ts >= 0 && v.ts < ((int64_t)1 << 27); }
+
 bool pieces16(const freqattn_heads* h, int size) {
   return (uintptr_t)h->data % 16 == 0 && h->batch_stride * size % 16 == 0 && h->row_stride * size % 16 == 0 && h->head_stride * size % 16 == 0;
 }
@@ -290,7 +293,7 @@ bool pieces16(const freqattn_heads* h, int size) {
 extern "C" int64_t freqattn_sequence_attention_workspace(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows) {
   SeqParams p;
   if (guarded([&] { return seq_params("freqattn_sequence_attention_workspace", s, rows, p); }) != FREQATTN_OK) return 0;
-  return 0;
+  return s->dtype == FREQATTN_BF16 ? seq_fwd_plan(p, compute_units()).workspace : 0;
 }
 
 extern "C" freqattn_status freqattn_sequence_attention(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows, const freqattn_heads* q,
@@ -313,9 +316,12 @@ extern "C" freqattn_status freqattn_sequence_attention(const freqattn_sequence_s
       p.vec = p.vec && pieces16(k, size) && pieces16(v, size);
     }
     p.lse = lse;
-    (void)workspace;
-    (void)workspace_bytes;
-    return launched(launch_seq_generic_fwd(p, s->dtype, (hipStream_t)stream), who);
+    if (s->dtype != FREQATTN_BF16) return launched(launch_seq_generic_fwd(p, s->dtype, (hipStream_t)stream), who);
+    const SeqPlan plan = seq_fwd_plan(p, compute_units());
+    if (plan.workspace > 0 && (!workspace || workspace_bytes < plan.workspace)) return fail(FREQATTN_EINVAL, who, "workspace too small");
+    if (plan.workspace > 0 && (uintptr_t)workspace % 16) return fail(FREQATTN_EINVAL, who, "workspace must be 16-byte aligned");
+    p.part = (float*)workspace;
+    return launched(p.vec && near(p.k) && near(p.v) ? launch_seq_fwd(p, plan, (hipStream_t)stream) : launch_seq_generic_fwd(p, s->dtype, (hipStream_t)stream), who);
   });
 }
 

@@ -1,0 +1,424 @@
+// Attention over sequences, bf16, forward: one pass over the keys with a running maximum and sum.
+//
+// A workgroup takes 32 * NW query rows of a sequence and key head (rows: tokens x heads of the group) and walks the key tiles that its rows see.
+// Scores are kept transposed, S^T = K Q^T, so that a lane owns one query: maximum and sum of a row take one exchange between the two lane
+// halves, and the accumulator registers, rounded to bf16, are the second operand of O^T += V^T P^T as they stand (rows of V come in that order
+// from transposing LDS reads).  K and V tiles are copied into the other half of LDS while this half is used.
+// Probabilities are rounded to bf16 for the product; their sum is taken before the rounding, in fp32, as lse needs it.
+//
+// Few rows (a token of each of some sequences): tiles of 32 rows, one wave a workgroup, and the keys are cut into pieces of `split_tiles` tiles
+// that run as workgroups of their own; their normalised results and log sums are joined by k_seq_join.
+#include "seq_mfma.h"
+
+namespace fa {
+
+using namespace seq;
+
+namespace {
+
+// Masked probabilities are exactly zero, but zero times a value that is not finite is not.  Run where a row's result came out not finite: the tile's
+// such values are added to the rows that see them, and taken out of the tile before the product.
+template <int D, int KT, typename F>
+__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], uint16_t* tile, int g, F&& seen) {
+  uint32_t* t32 = (uint32_t*)tile;
+  bool odd = false;
+  for (int i = threadIdx.x; i < KT * D / 2; i += blockDim.x) odd = odd || !finite_bf16x2(t32[i]);
+  if (!uniform(__syncthreads_or(odd))) return;
+#pragma nounroll
+  for (int i = 0; i < KT; ++i) {
+    const bool s = seen(i);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint2v x = *(const uint2v*)(tile + i * D + (((4 * dt + q) ^ swizzle<D, COLS>(i)) << 3) + 4 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float v = __uint_as_float((j & 1) ? (x[j >> 1] & 0xffff0000u) : (x[j >> 1] << 16));
+          if (s && !(fabsf(v) <= 3.4028235e38f)) acc[dt][4 * q + j] += v;
+        }
+      }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < KT * D / 2; i += blockDim.x) {
+    const uint32_t x = t32[i];
+    t32[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : (x & 0xffffu)) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : (x & 0xffff0000u));
+  }
+  __syncthreads();
+}
+
+template <int D, int NW, int KT>
+__global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
+  constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW;
+  // One wave has one K and one V tile: the next K tile is requested when the scores are done, the next V tile when the product is, and other
+  // workgroups of the compute unit (nine at D = 128) fill the wait.  More waves share two of each.
+  constexpr bool ONE = NW == 1;
+  constexpr int NB = ONE ? 1 : 2;
+  __shared__ __attribute__((aligned(16))) uint16_t Ks[NB][KT * D];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[NB][KT * D];
+  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // key heads fastest, then pieces of the keys, then tiles from the last: under the causal mask the longest come first
+  unsigned id = blockIdx.x;
+  const int kvh = (int)(id % (unsigned)p.hk);
+  id /= (unsigned)p.hk;
+  const int split = (int)(id % (unsigned)p.nsplit);
+  int seq_i, tile_i;
+  seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, p.slots - 1 - (int)(id / (unsigned)p.nsplit), seq_i, tile_i);
+  seq_i = uniform(seq_i);
+  tile_i = uniform(tile_i);
+  const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(p.k_off, p.k_len, p.k_rows, seq_i));
+  const int rows = q.n * p.group, r_first = tile_i * TILE;
+  if ((int64_t)tile_i * TILE >= rows) return;
+  const Row row = query_row(p, kvh, r_first + wave * 32 + nn, q.n, k.n);
+  // the last keys seen by the first and the last row of the workgroup and of the wave
+  const int rl = min(r_first + TILE, rows) - 1;
+  const int wg_first = last_key(p.causal, r_first / p.group, q.n, k.n), wg_last = last_key(p.causal, rl / p.group, q.n, k.n);
+  const int w0 = r_first + wave * 32;
+  const bool wave_live = w0 < rows;
+  const int wave_first = wave_live ? last_key(p.causal, w0 / p.group, q.n, k.n) : -1;
+  const int wave_last = wave_live ? last_key(p.causal, min(w0 + 31, rows - 1) / p.group, q.n, k.n) : -1;
+  // dead rows of a live wave act as its last one: their scores are zeros, nothing of them is stored
+  const int my_last = row.live ? row.last : wave_last;
+
+  const int t_all = (wg_last + KT) / KT;                       // tiles the workgroup's rows see (0: none)
+  const int t0 = split * p.split_tiles, t1 = p.nsplit > 1 ? min(t0 + p.split_tiles, t_all) : t_all;
+  if (p.nsplit > 1 && t0 >= t_all && split > 0) return;        // (piece 0 of a row that sees nothing stores that)
+
+  const int chunks = p.d >> 3;
+  bf16x8 Q[DK];
+  {
+    const uint16_t* src = (const uint16_t*)p.q.p + (int64_t)q.seq * p.q.bs + (int64_t)(q.base + row.token) * p.q.ts + (int64_t)row.head * p.q.hs;
+#pragma unroll
+    for (int s = 0; s < DK; ++s) {
+      uint4v x = {0u, 0u, 0u, 0u};
+      if (row.live && 2 * s + g < chunks) x = *(const uint4v*)(src + s * 16 + g * 8);
+      Q[s] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  const float c2 = p.scale * LOG2E;
+
+  RowRead<D> kr;
+  kr.template set<ROWS>(nn, g);
+  ColRead<D> vr;
+  vr.set(lane);
+  TileCopy<D, NW, KT, ROWS> kc;
+  TileCopy<D, NW, KT, COLS> vc;
+  const int64_t k_bytes = p.k.ts * 2, v_bytes = p.v.ts * 2;
+  kc.set(k_bytes, wave, lane);
+  vc.set(v_bytes, wave, lane);
+  const char* kb = p.k.p + 2 * ((int64_t)k.seq * p.k.bs + (int64_t)k.base * p.k.ts + (int64_t)kvh * p.k.hs);
+  const char* vb = p.v.p + 2 * ((int64_t)k.seq * p.v.bs + (int64_t)k.base * p.v.ts + (int64_t)kvh * p.v.hs);
+  const unsigned k_lds = lds_address(Ks[0]), v_lds = lds_address(Vs[0]);
+  constexpr int NI = TileCopy<D, NW, KT, ROWS>::NI, TB = KT * D * 2;
+  // the copies of tile t, in order: K (even) and V (odd)
+  using KC = typename TileCopy<D, NW, KT, ROWS>::Cursor;
+  using VC = typename TileCopy<D, NW, KT, COLS>::Cursor;
+  auto k_begin = [&](int t) { return kc.begin(kb + (int64_t)t * KT * k_bytes, k_bytes, wave); };
+  auto v_begin = [&](int t) { return vc.begin(vb + (int64_t)t * KT * v_bytes, v_bytes, wave); };
+  auto copy = [&](KC& kcur, VC& vcur, int buf, int i) {
+    if ((i & 1) == 0) kc.whole(kcur, k_bytes, k_lds + buf * TB, wave, i >> 1);
+    else vc.whole(vcur, v_bytes, v_lds + buf * TB, wave, i >> 1);
+  };
+  auto is_whole = [&](int t) { return (t + 1) * KT <= k.n && chunks == D / 8; };
+  auto copy_k = [&](int t, int buf) {
+    KC cur = k_begin(t);
+    if (is_whole(t)) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) kc.whole(cur, k_bytes, k_lds + buf * TB, wave, i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) kc.part(cur, k_bytes, k_lds + buf * TB, wave, lane, i, k.n - t * KT, chunks);
+    }
+  };
+  auto copy_v = [&](int t, int buf) {
+    VC cur = v_begin(t);
+    if (is_whole(t)) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) vc.whole(cur, v_bytes, v_lds + buf * TB, wave, i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) vc.part(cur, v_bytes, v_lds + buf * TB, wave, lane, i, k.n - t * KT, chunks);
+    }
+  };
+  auto wait_copies = [&](bool all) {    // all but the last NI, or all; and this wave's LDS reads
+    if (all) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NI) : "memory");
+  };
+
+  float16v O[DT];
+  float m, l;
+  // careful: the second pass of a workgroup whose result was not finite (see set_aside)
+  auto run = [&](auto careful) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) O[dt] = zero16();
+    m = -INFINITY;
+    l = 0.f;
+    auto next_tile = [&] {
+      if (!ONE) { wait_copies(true); __syncthreads(); }
+    };
+    if (t0 < t1) { copy_k(t0, 0); copy_v(t0, 0); }
+    next_tile();
+    for (int t = t0; t < t1; ++t, next_tile()) {
+      const int buf = ONE ? 0 : (t - t0) & 1, key0 = t * KT;
+      const uint16_t* Kt = Ks[buf];
+      uint16_t* Vt = Vs[buf];
+      const bool more = t + 1 < t1;
+      auto aside = [&] {
+        if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT>(O, Vt, g, [&](int i) { return row.live && key0 + i <= row.last; });
+      };
+      if (!ONE) aside();
+      if (!ONE && key0 > wave_last) {   // (uniform over the wave) none of its rows sees the tile
+        if (more) { copy_k(t + 1, buf ^ 1); copy_v(t + 1, buf ^ 1); }
+        continue;
+      }
+      if (ONE) wait_copies(false);
+      const bool mask = key0 + KT - 1 > wave_first;
+      // ---- S^T = K Q^T; the next tile's copies are spread over the products
+      float16v S[T2];
+      __builtin_amdgcn_s_setprio(1);
+      auto scores = [&](auto copies) {
+        constexpr int NS = T2 * DK, PF = NS < 8 ? NS : 8;
+        KC kcur{nullptr};
+        VC vcur{nullptr};
+        if (copies.value) { kcur = k_begin(t + 1); vcur = v_begin(t + 1); }
+        bf16x8 A[PF];
+#pragma unroll
+        for (int i = 0; i < PF; ++i) A[i] = kr.get(Kt, i / DK, i % DK);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const bf16x8 a = A[i % PF];
+          if (i + PF < NS) A[i % PF] = kr.get(Kt, (i + PF) / DK, (i + PF) % DK);
+          S[i / DK] = mfma(a, Q[i % DK], i % DK == 0 ? zero16() : S[i / DK]);
+          if (copies.value) {
+#pragma unroll
+            for (int c = i * (2 * NI) / NS; c < (i + 1) * (2 * NI) / NS; ++c) copy(kcur, vcur, buf ^ 1, c);
+          }
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, PF, 0);   // PF reads up front, then one read per product
+#pragma unroll
+        for (int i = 0; i < NS - PF; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, PF, 0);
+      };
+      if (!ONE && more && is_whole(t + 1)) scores(std::bool_constant<!ONE>{});
+      else {
+        if (!ONE && more) { copy_k(t + 1, buf ^ 1); copy_v(t + 1, buf ^ 1); }
+        scores(std::false_type{});
+      }
+      __builtin_amdgcn_s_setprio(0);
+      if (ONE && more) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        copy_k(t + 1, 0);
+      }
+      // ---- mask, running softmax.  m (in units of log2) is a reference, not the exact maximum: it moves when a score exceeds it by more than
+      // 2^8, so that probabilities stay within [0, 256], exact relative to their sum, and the accumulator is rarely rescaled.
+      constexpr float BUMP = 8.f;
+      if (mask) {
+        const int lim = my_last - key0 - 4 * g;
+#pragma unroll
+        for (int t2 = 0; t2 < T2; ++t2)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) S[t2][r] = t2 * 32 + 8 * (r >> 2) + (r & 3) <= lim ? S[t2][r] : -INFINITY;
+      }
+      float mc[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int t2 = 0; t2 < T2; ++t2)
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) mc[(r >> 1) & 3] = __builtin_fmaxf(__builtin_fmaxf(mc[(r >> 1) & 3], S[t2][r]), S[t2][r + 1]);
+      const float mx = max_halves(fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3]))) * c2;
+      const bool bump = m == -INFINITY ? mx > -INFINITY : mx > m + BUMP;
+      if (__builtin_amdgcn_ballot_w64(bump) != 0) {
+        const float mn = bump ? mx : m;
+        // (a row that saw nothing before has zeros to scale, or what set_aside just added, which 0 would spoil)
+        const float alpha = bump && m != -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+      }
+      const float nref = m == -INFINITY ? 0.f : -m;
+      bf16x8 P[T2][2];
+      float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t2 = 0; t2 < T2; ++t2)
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+          uint4v pk;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j], c2, nref));
+            const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j + 1], c2, nref));
+            ls[j] += a;
+            ls[j] += b;
+            pk[j] = pack2(a, b);
+          }
+          P[t2][s2] = __builtin_bit_cast(bf16x8, pk);
+        }
+      l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+      if (ONE) {
+        wait_copies(!more);
+        aside();
+      }
+      // ---- O^T += V^T P^T
+      {
+        constexpr int NS = 2 * T2 * DT, PF = NS < 8 ? NS : 8;
+        bf16x8 A[PF];
+#pragma unroll
+        for (int i = 0; i < PF; ++i) A[i] = vr.get(Vt, i % DT, i / DT);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const bf16x8 a = A[i % PF];
+          if (i + PF < NS) A[i % PF] = vr.get(Vt, (i + PF) % DT, (i + PF) / DT);
+          O[i % DT] = mfma(a, P[i / DT >> 1][i / DT & 1], O[i % DT]);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * PF, 0);   // PF operands up front, then one operand (two reads) per product
+#pragma unroll
+        for (int i = 0; i < NS - PF; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, PF, 0);
+      }
+      if (ONE && more) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        copy_v(t + 1, 0);
+      }
+    }
+  };
+  run(std::false_type{});
+  if (p.causal) {
+    // a value that is not finite may have come from a key that its row does not see
+    float probe = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) probe = __builtin_fmaf(O[dt][r], 0.f, probe);
+    if (uniform(__syncthreads_or(row.live && probe != 0.f))) run(std::true_type{});   // (NaN where any is not finite)
+  }
+
+  // ---- normalise and store.  Per 16 channels a lane holds two groups of four that interleave with its partner's: after swapping one each it has 8
+  // consecutive channels.
+  l += other_half(l);
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
+  const float lse2 = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY;
+  uint16_t* dst = (uint16_t*)const_cast<char*>(p.o.p) + (int64_t)q.seq * p.o.bs + (int64_t)(q.base + row.token) * p.o.ts + (int64_t)row.head * p.o.hs;
+  float* part = p.part + ((int64_t)split * p.hq * p.lse_rows + at) * p.d;
+  if (row.live && g == 0) {
+    if (p.nsplit > 1) p.part[(int64_t)p.nsplit * p.hq * p.lse_rows * p.d + (int64_t)split * p.hq * p.lse_rows + at] = lse2;
+    else if (p.lse) p.lse[at] = lse2 * LN2;
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float o[8];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(O[dt][8 * j + b] * inv), __float_as_uint(O[dt][8 * j + 4 + b] * inv), false, false);
+        o[b] = __uint_as_float(sw[0]);
+        o[4 + b] = __uint_as_float(sw[1]);
+      }
+      const int c = dt * 32 + j * 16 + g * 8;
+      if (row.live && c < p.d) {
+        if (p.nsplit > 1) {
+          *(float4v*)(part + c) = float4v{o[0], o[1], o[2], o[3]};
+          *(float4v*)(part + c + 4) = float4v{o[4], o[5], o[6], o[7]};
+        } else {
+          *(uint4v*)(dst + c) = uint4v{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
+        }
+      }
+    }
+}
+
+// Joins the pieces of a row: out = sum_s 2^(lse_s - top) out_s / sum_s 2^(lse_s - top).  A wave takes one row, a lane two channels.
+__global__ void __launch_bounds__(256) k_seq_join(SeqParams p, int piece_keys) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
+  int seq_i, tile_i;
+  seq_slot(p.q_off, p.q_rows, p.nseq, p.group, 4, (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i);
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq_i), k = seq_range(p.k_off, p.k_len, p.k_rows, seq_i);
+  const Row row = query_row(p, kvh, tile_i * 4 + wave, q.n, k.n);
+  if ((int64_t)tile_i * 4 + wave >= (int64_t)q.n * p.group) return;
+  const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
+  const int64_t all = (int64_t)p.hq * p.lse_rows;
+  const float* lse = p.part + p.nsplit * all * p.d;
+  const int n = row.last < 0 ? 0 : row.last / piece_keys + 1;    // pieces that hold keys of this row
+  float top = -INFINITY;
+  for (int s = lane; s < n; s += 64) top = fmaxf(top, lse[s * all + at]);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, a = 0.f, b = 0.f;
+  const int c = 2 * lane;
+  for (int s = 0; s < n; ++s) {
+    const float w = __builtin_amdgcn_exp2f(lse[s * all + at] - ref);
+    if (w == 0.f) continue;     // (a piece that the row sees no key of)
+    sum += w;
+    if (c < p.d) {
+      const float2v x = *(const float2v*)(p.part + (s * all + at) * p.d + c);
+      a += w * x[0];
+      b += w * x[1];
+    }
+  }
+  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+  if (c < p.d) {
+    uint16_t* dst = (uint16_t*)const_cast<char*>(p.o.p) + (int64_t)q.seq * p.o.bs + (int64_t)(q.base + row.token) * p.o.ts + (int64_t)row.head * p.o.hs;
+    *(uint32_t*)(dst + c) = pack2(a * inv, b * inv);
+  }
+  if (lane == 0 && p.lse) p.lse[at] = sum > 0.f || sum != sum ? (ref + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
+}
+
+template <int D, int NW, int KT>
+hipError_t go(const SeqParams& p, hipStream_t st) {
+  hipLaunchKernelGGL((k_seq_fwd<D, NW, KT>), dim3((unsigned)p.slots * (unsigned)p.nsplit * (unsigned)p.hk), dim3(64 * NW), 0, st, p);
+  return hipGetLastError();
+}
+
+constexpr int FEW_KT = 32, MANY_KT = 64;
+
+}  // namespace
+
+// How a forward call is cut.
+SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu) {
+  SeqPlan s;
+  const bool packed = p.q_off != nullptr;
+  // rows of an average sequence and key head
+  const int64_t all = (int64_t)p.q_rows * p.group, mean = packed ? (p.nseq ? all / p.nseq : 0) : all;
+  s.few = mean <= 32;
+  const int tile_rows = s.few ? 32 : 128, kt = s.few ? FEW_KT : MANY_KT;
+  const int64_t slots = seq_slots(packed, p.q_rows, p.nseq, p.group, tile_rows), groups = slots * p.hk, key_tiles = ((int64_t)p.k_rows + kt - 1) / kt;
+  s.nsplit = 1;
+  s.split_tiles = (int)(key_tiles > 0 ? key_tiles : 1);
+  const int64_t target = (int64_t)num_cu * (s.few ? 16 : 4);
+  if (groups > 0 && groups < target / 2 && key_tiles > 1) {
+    int64_t n = target / groups;
+    if (n > key_tiles) n = key_tiles;
+    if (n > 256) n = 256;
+    s.split_tiles = (int)((key_tiles + n - 1) / n);
+    s.nsplit = (int)((key_tiles + s.split_tiles - 1) / s.split_tiles);
+  }
+  s.workspace = s.nsplit > 1 ? (int64_t)s.nsplit * p.hq * p.lse_rows * (p.d + 1) * 4 : 0;
+  return s;
+}
+
+hipError_t launch_seq_fwd(SeqParams p, const SeqPlan& s, hipStream_t st) {
+  p.nsplit = s.nsplit;
+  p.split_tiles = s.split_tiles;
+  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, s.few ? 32 : 128);
+  if (p.slots == 0) return hipSuccess;
+  hipError_t e;
+  if (s.few) e = p.d <= 64 ? go<64, 1, FEW_KT>(p, st) : go<128, 1, FEW_KT>(p, st);
+  else e = p.d <= 64 ? go<64, 4, MANY_KT>(p, st) : go<128, 4, MANY_KT>(p, st);
+  if (e != hipSuccess || s.nsplit == 1) return e;
+  const int64_t slots = seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 4);
+  hipLaunchKernelGGL(k_seq_join, dim3((unsigned)(slots * p.hk)), dim3(256), 0, st, p, s.split_tiles * (s.few ? FEW_KT : MANY_KT));
+  return hipGetLastError();
+}
+
+}  // namespace fa

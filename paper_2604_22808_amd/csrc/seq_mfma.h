@@ -1,0 +1,180 @@
+// What the bf16 kernels of attention over sequences share: operand types, tiles in LDS and the copies that fill them.
+//
+// A tile is KT rows of D channels, row-major without padding.  Rows are copied straight from global memory into LDS, 16 bytes a lane; lane
+// l of a copy fills bytes 16 l of 1 KB, so that the order inside LDS is fixed and bank conflicts are avoided through the global address: 16-byte
+// chunk c of row r sits at position c ^ f(r).  Two kinds of operands are read from a tile:
+//   rows     lane = row (32 of them), 8 consecutive channels           (one 16-byte read)
+//   columns  lane = channel (32), 8 rows in the order of a product's accumulator registers   (two transposing reads, ds_read_b64_tr_b16)
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "seq_common.h"
+
+namespace fa {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef unsigned int uint4v __attribute__((ext_vector_type(4)));
+typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+namespace seq {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// 16 bytes of zeros that copies of rows and channels that do not exist read.
+static __device__ const uint4v zero_piece = {0u, 0u, 0u, 0u};
+
+// (values that every lane holds alike, said to the compiler)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const void* uniform(const void* x) {
+  const uint64_t v = (uint64_t)x;
+  return (const void*)(((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)(uint32_t)v));
+}
+__device__ __forceinline__ SeqRange uniform(SeqRange r) { return SeqRange{uniform(r.seq), uniform(r.base), uniform(r.n)}; }
+
+// One wave-wide copy, 16 bytes a lane, to LDS bytes dst + 16 lane (dst wave-uniform).  Written as assembly because the compiler orders every LDS
+// read behind a copy of this kind that it knows of; the kernels wait for their copies themselves (vmcnt) in front of the barrier that publishes a tile.
+__device__ __forceinline__ void copy16(const void* base, unsigned off, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(uniform(base)), "s"(uniform((int)dst))
+               : "memory", "m0");
+}
+__device__ __forceinline__ void copy16_any(const void* addr, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(uniform((int)dst)) : "memory", "m0");
+}
+__device__ __forceinline__ unsigned lds_address(const uint16_t* p) {
+  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) uint16_t*)p;
+}
+
+__device__ __forceinline__ float16v zero16() {
+  float16v z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a, b}, bf16x2));   // v_cvt_pk_bf16_f32: to nearest, ties to even
+}
+__device__ __forceinline__ float16v mfma(const bf16x8& a, const bf16x8& b, const float16v& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float other_half(float x) {   // the value of lane ^ 32
+  const uint32_t b = __float_as_uint(x);
+  const auto sw = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return __uint_as_float((threadIdx.x & 32) ? sw[0] : sw[1]);
+}
+__device__ __forceinline__ float max_halves(float x) {
+  const uint32_t b = __float_as_uint(x);
+  const auto sw = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+
+// Where 16-byte chunk c of row r sits.  ROWS tiles are read as row operands by 16 consecutive rows at a time, COLS tiles through transposing
+// reads, which hand lane i of a 16-lane group, for k = 0..3, element i % 4 of the 8-byte piece named by lane 4 k + i / 4: four rows of 32 bytes.
+enum { ROWS = 0, COLS = 1 };
+template <int D, int USE>
+__device__ __forceinline__ int swizzle(int r) {
+  if (USE == ROWS) return D == 128 ? (r & 15) : ((r >> 1) & 7);
+  return D == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2);
+}
+
+// Copies of KT rows into a tile by NW waves.
+template <int D, int NW, int KT, int USE>
+struct TileCopy {
+  static constexpr int CPR = D / 8, RPI = 64 / CPR, NI = KT / (RPI * NW);   // chunks a row, rows a copy, copies a wave
+  static_assert(NI >= 1, "");
+  // (the swizzle of a row repeats after 16 rows at most, so copies whose first rows agree modulo 16 use the same lane offsets)
+  static constexpr int NOFF = USE == COLS ? 1 : (16 / RPI < NI ? 16 / RPI : NI);
+  unsigned off[NOFF];
+  __device__ __forceinline__ void set(int64_t row_bytes, int wave, int lane) {
+    const int lr = lane / CPR, c = lane % CPR;
+#pragma unroll
+    for (int i = 0; i < NOFF; ++i) off[i] = (unsigned)(lr * row_bytes) + ((c ^ swizzle<D, USE>((wave * NI + i) * RPI + lr)) << 4);
+  }
+  // The copies of one tile, in order: a cursor steps through the tensor with the scalar unit.  (The empty assembly keeps the compiler from holding one
+  // address per copy in registers over the whole loop.)
+  struct Cursor {
+    const char* at;
+    __device__ __forceinline__ void step(int64_t bytes) {
+      at = (const char*)uniform(at + bytes);
+      asm("" : "+s"(at));
+    }
+  };
+  __device__ __forceinline__ Cursor begin(const char* tile, int64_t row_bytes, int wave) const {
+    return Cursor{(const char*)uniform(tile + (int64_t)(wave * NI * RPI) * row_bytes)};
+  }
+  // copy i of this wave, all rows and channels exist
+  __device__ __forceinline__ void whole(Cursor& cur, int64_t row_bytes, unsigned dst, int wave, int i) const {
+    copy16(cur.at, off[i % NOFF], dst + (wave * NI + i) * RPI * D * 2);
+    cur.step(RPI * row_bytes);
+  }
+  // the same where rows of the tile from n on, or chunks from `chunks` on, do not exist: they become zero
+  __device__ __forceinline__ void part(Cursor& cur, int64_t row_bytes, unsigned dst, int wave, int lane, int i, int n, int chunks) const {
+    asm volatile("" : "+v"(lane));
+    const int row = (wave * NI + i) * RPI, lr = lane / CPR, c = (lane % CPR) ^ swizzle<D, USE>(row + lr);
+    const char* at = cur.at + (int64_t)lr * row_bytes + (c << 4);
+    copy16_any(row + lr < n && c < chunks ? at : (const char*)&zero_piece, dst + row * D * 2);
+    cur.step(RPI * row_bytes);
+  }
+};
+
+// Operand addresses (elements) of a lane in a tile.
+template <int D>
+struct RowRead {    // rows 32 t + nn, channels 16 s + 8 g .. + 7
+  int row, x[D / 16];
+  template <int USE> __device__ __forceinline__ void set(int nn, int g) {
+    row = nn * D;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) x[s] = ((2 * s + g) ^ swizzle<D, USE>(nn)) << 3;   // (the swizzle of row 32 t + nn is that of nn)
+  }
+  __device__ __forceinline__ bf16x8 get(const uint16_t* tile, int t, int s) const { return *(const bf16x8*)(tile + t * 32 * D + row + x[s]); }
+};
+// channels 32 dt + nn, rows 16 s + 8 h + 4 g + 0..3 for h = 0, 1: the rows that a lane half g holds in registers 8 (s % 2) .. + 7 of the product
+// over rows 32 (s / 2) .. + 31.
+template <int D>
+struct ColRead {
+  int row, x[D / 32];
+  // (swizzles of ROWS tiles depend on more bits of the row than a transposing read's four rows: see get)
+  __device__ __forceinline__ void set(int lane) {
+    const int g = lane >> 5, sl = lane & 15, g1 = (lane >> 4) & 1;
+    row = (4 * g + (sl >> 2)) * D + (sl & 1) * 4;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) x[dt] = ((4 * dt + 2 * g1 + ((sl & 3) >> 1)) ^ swizzle<D, COLS>(sl >> 2)) << 3;
+  }
+  __device__ __forceinline__ bf16x8 get(const uint16_t* tile, int dt, int s) const {
+    uint4v r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint16_t* p = tile + (s * 16 + 8 * h) * D + row + x[dt];
+      const uint2v u = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)p));
+      r[2 * h] = u[0];
+      r[2 * h + 1] = u[1];
+    }
+    return __builtin_bit_cast(bf16x8, r);
+  }
+};
+
+__device__ __forceinline__ bool finite_bf16x2(uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; }
+
+struct Row { bool live; int token, head, last; };   // last: the last key the row sees, -1 none
+
+__device__ __forceinline__ int last_key(int causal, int token, int nq, int nk) {
+  return causal ? (token + nk - nq < nk - 1 ? token + nk - nq : nk - 1) : nk - 1;
+}
+__device__ __forceinline__ Row query_row(const SeqParams& p, int kvh, int r, int nq, int nk) {
+  Row w;
+  w.live = r < nq * p.group;
+  w.token = w.live ? (int)((unsigned)r / (unsigned)p.group) : 0;
+  w.head = kvh * p.group + (w.live ? r - w.token * p.group : 0);
+  w.last = w.live ? last_key(p.causal, w.token, nq, nk) : -1;
+  return w;
+}
+
+}  // namespace seq
+}  // namespace fa
