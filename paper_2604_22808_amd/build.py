@@ -15,7 +15,7 @@ SOURCES = ["mfma_wh_0.hip", "mfma_wh_1.hip", "mfma_wh_2.hip", "mfma_wh_3.hip", "
            "mfma_dct_scatter.hip",
            "mfma_dct_scatter_en.hip", "mfma_dct_gather.hip", "mfma_attn.hip", "mfma_vsum.hip", "mfma_gemm.hip", "api.cpp", "tables.cpp", "generic_kernels.hip",
            "generic_attn.hip", "generic_axis.hip", "mfma_dct.hip",
-           "heads_api.cpp", "qk_norm.hip", "seq_generic.hip", "seq_fwd.hip"]
+           "heads_api.cpp", "qk_norm.hip", "seq_generic.hip", "seq_fwd.hip", "seq_bwd.hip"]
 
 
 # Kernels that keep rows requested steps ahead in registers: a spilled register's reload would wait behind all of them.

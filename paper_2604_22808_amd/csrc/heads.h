@@ -46,7 +46,7 @@ hipError_t launch_qk_backward(const QkParams& p, const RotTable& t, int dtype, f
 struct SeqParams {
   HeadsPtr q, k, v, o, dout, dq, dk, dv;
   float* lse;
-  float* delta;                  // [q_heads][lse_rows] row sums of dout * out (backward)
+  float* delta;                  // backward: [q_heads][lse_rows] row sums of dout * out, or pairs (lse in units of log2, row sum)
   float* part;                   // split keys: partial results
   const int32_t *q_off, *k_off, *q_len, *k_len;
   int32_t nseq, hq, hk, group, d, q_rows, k_rows, causal;
@@ -65,6 +65,7 @@ struct SeqPlan {
 };
 SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu);
 hipError_t launch_seq_fwd(SeqParams p, const SeqPlan& s, hipStream_t st);
+hipError_t launch_seq_bwd(const SeqParams& p, hipStream_t st);
 hipError_t launch_seq_generic_fwd(const SeqParams& p, int dtype, hipStream_t st);
 hipError_t launch_seq_generic_bwd(const SeqParams& p, int dtype, hipStream_t st);
 

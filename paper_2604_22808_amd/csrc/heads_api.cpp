@@ -328,7 +328,7 @@ extern "C" freqattn_status freqattn_sequence_attention(const freqattn_sequence_s
 extern "C" int64_t freqattn_sequence_attention_backward_workspace(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows) {
   SeqParams p;
   if (guarded([&] { return seq_params("freqattn_sequence_attention_backward_workspace", s, rows, p); }) != FREQATTN_OK) return 0;
-  return (int64_t)p.hq * p.lse_rows * 4;
+  return (int64_t)p.hq * p.lse_rows * 8;   // (lse, delta) of every row
 }
 
 extern "C" freqattn_status freqattn_sequence_attention_backward(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows,
@@ -360,6 +360,7 @@ extern "C" freqattn_status freqattn_sequence_attention_backward(const freqattn_s
     }
     p.lse = const_cast<float*>(lse);
     p.delta = (float*)workspace;
-    return launched(launch_seq_generic_bwd(p, s->dtype, (hipStream_t)stream), who);
+    const bool fast = s->dtype == FREQATTN_BF16 && p.vec && near(p.q) && near(p.dout) && near(p.k) && near(p.v);
+    return launched(fast ? launch_seq_bwd(p, (hipStream_t)stream) : launch_seq_generic_bwd(p, s->dtype, (hipStream_t)stream), who);
   });
 }

@@ -16,37 +16,6 @@ using namespace seq;
 
 namespace {
 
-// Masked probabilities are exactly zero, but zero times a value that is not finite is not.  Run where a row's result came out not finite: the tile's
-// such values are added to the rows that see them, and taken out of the tile before the product.
-template <int D, int KT, typename F>
-__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], uint16_t* tile, int g, F&& seen) {
-  uint32_t* t32 = (uint32_t*)tile;
-  bool odd = false;
-  for (int i = threadIdx.x; i < KT * D / 2; i += blockDim.x) odd = odd || !finite_bf16x2(t32[i]);
-  if (!uniform(__syncthreads_or(odd))) return;
-#pragma nounroll
-  for (int i = 0; i < KT; ++i) {
-    const bool s = seen(i);
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint2v x = *(const uint2v*)(tile + i * D + (((4 * dt + q) ^ swizzle<D, COLS>(i)) << 3) + 4 * g);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float v = __uint_as_float((j & 1) ? (x[j >> 1] & 0xffff0000u) : (x[j >> 1] << 16));
-          if (s && !(fabsf(v) <= 3.4028235e38f)) acc[dt][4 * q + j] += v;
-        }
-      }
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < KT * D / 2; i += blockDim.x) {
-    const uint32_t x = t32[i];
-    t32[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : (x & 0xffffu)) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : (x & 0xffff0000u));
-  }
-  __syncthreads();
-}
-
 template <int D, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
   constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW;
@@ -101,7 +70,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
   RowRead<D> kr;
   kr.template set<ROWS>(nn, g);
   ColRead<D> vr;
-  vr.set(lane);
+  vr.template set<COLS>(lane);
   TileCopy<D, NW, KT, ROWS> kc;
   TileCopy<D, NW, KT, COLS> vc;
   const int64_t k_bytes = p.k.ts * 2, v_bytes = p.v.ts * 2;
@@ -165,7 +134,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
       uint16_t* Vt = Vs[buf];
       const bool more = t + 1 < t1;
       auto aside = [&] {
-        if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT>(O, Vt, g, [&](int i) { return row.live && key0 + i <= row.last; });
+        if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, COLS>(O, Vt, g, [&](int i) { return row.live && key0 + i <= row.last; });
       };
       if (!ONE) aside();
       if (!ONE && key0 > wave_last) {   // (uniform over the wave) none of its rows sees the tile
@@ -293,16 +262,10 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
   run(std::false_type{});
   if (p.causal) {
     // a value that is not finite may have come from a key that its row does not see
-    float probe = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) probe = __builtin_fmaf(O[dt][r], 0.f, probe);
-    if (uniform(__syncthreads_or(row.live && probe != 0.f))) run(std::true_type{});   // (NaN where any is not finite)
+    if (uniform(__syncthreads_or(row.live && any_odd(O)))) run(std::true_type{});
   }
 
-  // ---- normalise and store.  Per 16 channels a lane holds two groups of four that interleave with its partner's: after swapping one each it has 8
-  // consecutive channels.
+  // ---- normalise and store
   l += other_half(l);
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
   const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
@@ -313,27 +276,15 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
     if (p.nsplit > 1) p.part[(int64_t)p.nsplit * p.hq * p.lse_rows * p.d + (int64_t)split * p.hq * p.lse_rows + at] = lse2;
     else if (p.lse) p.lse[at] = lse2 * LN2;
   }
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float o[8];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(O[dt][8 * j + b] * inv), __float_as_uint(O[dt][8 * j + 4 + b] * inv), false, false);
-        o[b] = __uint_as_float(sw[0]);
-        o[4 + b] = __uint_as_float(sw[1]);
-      }
-      const int c = dt * 32 + j * 16 + g * 8;
-      if (row.live && c < p.d) {
-        if (p.nsplit > 1) {
-          *(float4v*)(part + c) = float4v{o[0], o[1], o[2], o[3]};
-          *(float4v*)(part + c + 4) = float4v{o[4], o[5], o[6], o[7]};
-        } else {
-          *(uint4v*)(dst + c) = uint4v{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
-        }
-      }
+  each_piece(O, inv, g, [&](int c, const float (&o)[8]) {
+    if (!row.live || c >= p.d) return;
+    if (p.nsplit > 1) {
+      *(float4v*)(part + c) = float4v{o[0], o[1], o[2], o[3]};
+      *(float4v*)(part + c + 4) = float4v{o[4], o[5], o[6], o[7]};
+    } else {
+      *(uint4v*)(dst + c) = pack8(o);
     }
+  });
 }
 
 // Joins the pieces of a row: out = sum_s 2^(lse_s - top) out_s / sum_s 2^(lse_s - top).  A wave takes one row, a lane two channels.

@@ -75,13 +75,15 @@ __device__ __forceinline__ float max_halves(float x) {
   return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
 }
 
-// Where 16-byte chunk c of row r sits.  ROWS tiles are read as row operands by 16 consecutive rows at a time, COLS tiles through transposing
+// Where 16-byte chunk c of row r sits.  ROWS tiles are read as row operands, by 16 consecutive rows at a time.  COLS tiles are read through transposing
 // reads, which hand lane i of a 16-lane group, for k = 0..3, element i % 4 of the 8-byte piece named by lane 4 k + i / 4: four rows of 32 bytes.
-enum { ROWS = 0, COLS = 1 };
+// BOTH serves both without conflicts: 16 rows in 16 places, four neighbouring ones 64 bytes apart.
+enum { ROWS = 0, COLS = 1, BOTH = 2 };
 template <int D, int USE>
 __device__ __forceinline__ int swizzle(int r) {
   if (USE == ROWS) return D == 128 ? (r & 15) : ((r >> 1) & 7);
-  return D == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2);
+  const int apart = D == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2);
+  return USE == COLS ? apart : apart | ((r >> 2) & 3);
 }
 
 // Copies of KT rows into a tile by NW waves.
@@ -139,19 +141,21 @@ struct RowRead {    // rows 32 t + nn, channels 16 s + 8 g .. + 7
 // over rows 32 (s / 2) .. + 31.
 template <int D>
 struct ColRead {
-  int row, x[D / 32];
-  // (swizzles of ROWS tiles depend on more bits of the row than a transposing read's four rows: see get)
-  __device__ __forceinline__ void set(int lane) {
+  int row, x[D / 32], flip;
+  template <int USE> __device__ __forceinline__ void set(int lane) {
+    static_assert(USE != ROWS, "");
     const int g = lane >> 5, sl = lane & 15, g1 = (lane >> 4) & 1;
     row = (4 * g + (sl >> 2)) * D + (sl & 1) * 4;
+    // row 16 s + 8 h + 4 g + sl / 4: of a BOTH tile's swizzle h changes one bit, by which two chunks change places
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) x[dt] = ((4 * dt + 2 * g1 + ((sl & 3) >> 1)) ^ swizzle<D, COLS>(sl >> 2)) << 3;
+    for (int dt = 0; dt < D / 32; ++dt) x[dt] = ((4 * dt + 2 * g1 + ((sl & 3) >> 1)) ^ swizzle<D, USE>(4 * g + (sl >> 2))) << 3;
+    flip = USE == BOTH ? ((x[0] & 16) ? -16 : 16) : 0;
   }
   __device__ __forceinline__ bf16x8 get(const uint16_t* tile, int dt, int s) const {
     uint4v r;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint16_t* p = tile + (s * 16 + 8 * h) * D + row + x[dt];
+      const uint16_t* p = tile + (s * 16 + 8 * h) * D + row + x[dt] + (h ? flip : 0);   // (x[dt] & 16 is alike for all dt)
       const uint2v u = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)p));
       r[2 * h] = u[0];
       r[2 * h + 1] = u[1];
@@ -160,7 +164,66 @@ struct ColRead {
   }
 };
 
-__device__ __forceinline__ bool finite_bf16x2(uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; }
+// Masked probabilities are exactly zero, but zero times a value that is not finite is not.  Run where a result came out not finite: the tile's such
+// values are added to the rows that see them, and taken out of the tile before the product.
+template <int D, int KT, int USE, typename F>
+__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], uint16_t* tile, int g, F&& seen) {
+  uint32_t* t32 = (uint32_t*)tile;
+  bool odd = false;
+  for (int i = threadIdx.x; i < KT * D / 2; i += blockDim.x) odd = odd || (t32[i] & 0x7f80u) == 0x7f80u || (t32[i] & 0x7f800000u) == 0x7f800000u;
+  if (!uniform(__syncthreads_or(odd))) return;
+#pragma nounroll
+  for (int i = 0; i < KT; ++i) {
+    const bool s = seen(i);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint2v x = *(const uint2v*)(tile + i * D + (((4 * dt + q) ^ swizzle<D, USE>(i)) << 3) + 4 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float v = __uint_as_float((j & 1) ? (x[j >> 1] & 0xffff0000u) : (x[j >> 1] << 16));
+          if (s && !(fabsf(v) <= 3.4028235e38f)) acc[dt][4 * q + j] += v;
+        }
+      }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < KT * D / 2; i += blockDim.x) {
+    const uint32_t x = t32[i];
+    t32[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : (x & 0xffffu)) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : (x & 0xffff0000u));
+  }
+  __syncthreads();
+}
+// Not zero where any of the values is not finite.
+template <int N>
+__device__ __forceinline__ bool any_odd(const float16v (&x)[N]) {
+  float probe = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) probe = __builtin_fmaf(x[i][r], 0.f, probe);
+  return probe != 0.f;
+}
+
+// Stores a row of which two lane halves hold the channels as accumulators, times f.  Per 16 channels a lane holds two groups of four that interleave with its
+// partner's: after swapping one each it has 8 consecutive channels.  put(c, o): channels c .. c + 7.
+template <int DT, typename F>
+__device__ __forceinline__ void each_piece(const float16v (&acc)[DT], float f, int g, F&& put) {
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float o[8];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[dt][8 * j + b] * f), __float_as_uint(acc[dt][8 * j + 4 + b] * f), false, false);
+        o[b] = __uint_as_float(sw[0]);
+        o[4 + b] = __uint_as_float(sw[1]);
+      }
+      put(dt * 32 + j * 16 + g * 8, o);
+    }
+}
+__device__ __forceinline__ uint4v pack8(const float (&o)[8]) { return uint4v{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])}; }
 
 struct Row { bool live; int token, head, last; };   // last: the last key the row sees, -1 none
 
