@@ -50,7 +50,7 @@ struct SeqParams {
   float* part;                   // split keys: partial results
   const int32_t *q_off, *k_off, *q_len, *k_len;
   int32_t nseq, hq, hk, group, d, q_rows, k_rows, causal;
-  int64_t lse_rows;              // columns of lse
+  int64_t lse_rows, lse_k;       // columns of lse; the same count for the keys (rows of k and v over all sequences)
   float scale;
   int32_t slots;                 // tiles of the launch per key head (upper bound)
   int32_t nsplit, split_tiles;   // pieces of the keys, and key tiles of a piece
@@ -62,10 +62,12 @@ struct SeqPlan {
   bool few;             // tiles of 32 query rows instead of 128
   int nsplit, split_tiles;
   int64_t workspace;    // bytes
+  int64_t part_at;      // backward: where the partial sums start in it
 };
 SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu);
 hipError_t launch_seq_fwd(SeqParams p, const SeqPlan& s, hipStream_t st);
-hipError_t launch_seq_bwd(const SeqParams& p, hipStream_t st);
+SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu);
+hipError_t launch_seq_bwd(SeqParams p, const SeqPlan& s, hipStream_t st);
 hipError_t launch_seq_generic_fwd(const SeqParams& p, int dtype, hipStream_t st);
 hipError_t launch_seq_generic_bwd(const SeqParams& p, int dtype, hipStream_t st);
 

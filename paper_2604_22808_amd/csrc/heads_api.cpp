@@ -274,6 +274,7 @@ freqattn_status seq_params(const char* who, const freqattn_sequence_shape* s, co
   if (rows) { p.q_off = rows->q_offsets; p.k_off = rows->k_offsets; p.q_len = rows->q_lengths; p.k_len = rows->k_lengths; }
   const int64_t qr = p.q_off ? s->q_rows : (int64_t)s->sequences * s->q_rows, kr = p.k_off ? s->k_rows : (int64_t)s->sequences * s->k_rows;
   p.lse_rows = qr;
+  p.lse_k = kr;
   // row indices of one sequence's group and launch sizes stay within 31 bits
   if ((int64_t)s->q_rows * p.group >= ((int64_t)1 << 30) || s->k_rows >= (1 << 30) ||
       (qr * p.group / 32 + s->sequences) * p.hk >= MAX_BLOCKS || (kr / 32 + s->sequences) * p.hk >= MAX_BLOCKS)
@@ -328,7 +329,7 @@ extern "C" freqattn_status freqattn_sequence_attention(const freqattn_sequence_s
 extern "C" int64_t freqattn_sequence_attention_backward_workspace(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows) {
   SeqParams p;
   if (guarded([&] { return seq_params("freqattn_sequence_attention_backward_workspace", s, rows, p); }) != FREQATTN_OK) return 0;
-  return (int64_t)p.hq * p.lse_rows * 8;   // (lse, delta) of every row
+  return s->dtype == FREQATTN_BF16 ? seq_bwd_plan(p, compute_units()).workspace : (int64_t)p.hq * p.lse_rows * 4;
 }
 
 extern "C" freqattn_status freqattn_sequence_attention_backward(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows,
@@ -361,6 +362,8 @@ extern "C" freqattn_status freqattn_sequence_attention_backward(const freqattn_s
     p.lse = const_cast<float*>(lse);
     p.delta = (float*)workspace;
     const bool fast = s->dtype == FREQATTN_BF16 && p.vec && near(p.q) && near(p.dout) && near(p.k) && near(p.v);
-    return launched(fast ? launch_seq_bwd(p, (hipStream_t)stream) : launch_seq_generic_bwd(p, s->dtype, (hipStream_t)stream), who);
+    const SeqPlan plan = seq_bwd_plan(p, compute_units());
+    p.part = (float*)((char*)workspace + plan.part_at);
+    return launched(fast ? launch_seq_bwd(p, plan, (hipStream_t)stream) : launch_seq_generic_bwd(p, s->dtype, (hipStream_t)stream), who);
   });
 }

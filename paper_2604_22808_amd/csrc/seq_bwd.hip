@@ -23,11 +23,32 @@ __device__ __forceinline__ void copy4_any(const void* addr, unsigned dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(addr), "s"(uniform((int)dst)) : "memory", "m0");
 }
 
+// The units of query rows that see keys from key0 on: tiles tile0 .. of each head of the group, `per_head` of them.
+struct DkvUnits { int tile0, per_head, all; };
+__device__ __forceinline__ DkvUnits dkv_units(const SeqParams& p, int nq, int nk, int key0, int rows_u) {
+  int first = p.causal ? key0 - (nk - nq) : 0;     // the first token that sees key0
+  if (first < 0) first = 0;
+  DkvUnits u;
+  u.tile0 = first / rows_u;
+  u.per_head = nq > first ? (nq + rows_u - 1) / rows_u - u.tile0 : 0;
+  u.all = u.per_head * p.group;
+  return u;
+}
+// Units of a piece: the longest sequence's, divided by the number of pieces (an even number of them).
+__device__ __forceinline__ int dkv_piece_units(const SeqParams& p, int rows_u, int lane) {
+  int most = 0;
+  for (int i = lane; i < p.nseq; i += 64) most = max(most, seq_range(p.q_off, p.q_len, p.q_rows, i).n);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o));
+  const int units = (most + rows_u - 1) / rows_u * p.group;
+  return max(2, ((units + p.nsplit - 1) / p.nsplit + 1) & ~1);
+}
+
 template <int D, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
   constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW;
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[2][KT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[2][KT * D];
+  __shared__ __attribute__((aligned(256))) uint16_t Ks[2][KT * D];
+  __shared__ __attribute__((aligned(256))) uint16_t Vs[2][KT * D];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6);
   const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
   int seq_i, tile_i;
@@ -79,8 +100,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
 
   RowRead<D> rr;
   rr.template set<BOTH>(nn, g);
-  ColRead<D> cr;
-  cr.template set<BOTH>(lane);
+  ColRead<D, BOTH> cr;
+  cr.set(lane);
   using Copy = TileCopy<D, NW, KT, BOTH>;
   Copy kc, vc;
   const int64_t k_bytes = p.k.ts * 2, v_bytes = p.v.ts * 2;
@@ -120,9 +141,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
     next_tile();
     for (int t = 0; t < tiles; ++t, next_tile()) {
       const int buf = t & 1, key0 = t * KT;
-      uint16_t* Kt = Ks[buf];
-      const uint16_t* Vt = Vs[buf];
-      if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, BOTH>(A, Kt, g, [&](int i) { return row.live && key0 + i <= row.last; });
+      const unsigned Kt = k_lds + buf * TB, Vt = v_lds + buf * TB;
+      if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, BOTH>(A, Ks[buf], g, [&](int i) { return row.live && key0 + i <= row.last; });
       if (t + 1 < tiles) copy_tile(t + 1, buf ^ 1);
       if (key0 > wave_last) continue;
 #pragma unroll
@@ -160,32 +180,44 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
   });
 }
 
-// 32 * NW keys, over all query rows of the group's heads that see any of them, QT rows of one head at a time.
-// V stays in LDS at D = 128: with it in registers too, a wave would need more than the 256 that two waves per SIMD leave it.
-template <int D, int NW, int QT>
-__global__ void __launch_bounds__(64 * NW, 2) k_seq_dkv(SeqParams p) {
-  constexpr int DT = D / 32, DK = D / 16, T2 = QT / 32, TILE = 32 * NW;
+// 64 keys, over the query rows of the group's heads that see any of them, in units of 32 * UT rows of one head.  Four waves: two for the keys (32
+// each) times two for the units, which take every other one; at the end the two add their sums up through LDS.  Units come two at a time, double
+// buffered; each wave copies one tensor of one unit.  Accumulators for dK and dV take half of the registers that two waves per SIMD leave a
+// wave; at D = 128 V's operands stay in LDS but for the last step's (the two workgroups of a compute unit have 80 KB each).
+template <int D, int UT>
+__global__ void __launch_bounds__(256, 2) k_seq_dkv(SeqParams p) {
+  constexpr int DT = D / 32, DK = D / 16, ROWS_U = 32 * UT, TILE = 64, TB = ROWS_U * D * 2;
   constexpr bool V_LDS = D == 128;
-  __shared__ __attribute__((aligned(16))) uint16_t Qs[2][QT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Gs[2][QT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[V_LDS ? TILE * D : 8];
-  __shared__ __attribute__((aligned(16))) float St[2][2 * QT];     // (lse, delta) of the tile's rows
-  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6);
-  // key heads fastest; tiles from the first: under the causal mask the first keys are seen by the most rows
-  const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
+  constexpr int VS = V_LDS ? DK - 1 : 0, VROW = 2 * (DK - 1) * 16;    // steps of V in LDS, bytes of a row there
+  __shared__ __attribute__((aligned(256))) uint16_t Buf[2][2][2][TB / 2];   // [copy][unit][Q, dO]
+  __shared__ __attribute__((aligned(256))) char Vs[V_LDS ? TILE * VROW : 16];
+  __shared__ __attribute__((aligned(256))) float St[2][2][2 * ROWS_U];      // [copy][unit] (lse, delta) of its rows
+  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6), kw = wave & 1, us = wave >> 1;
+  // key heads fastest, then pieces; tiles from the first: under the causal mask the first keys are seen by the most rows
+  unsigned id = blockIdx.x;
+  const int kvh = (int)(id % (unsigned)p.hk);
+  id /= (unsigned)p.hk;
+  const int piece = (int)(id % (unsigned)p.nsplit);
   int seq_i, tile_i;
-  seq_slot(p.k_off, p.k_rows, p.nseq, 1, TILE, (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i);
+  seq_slot(p.k_off, p.k_rows, p.nseq, 1, TILE, (int)(id / (unsigned)p.nsplit), seq_i, tile_i);
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(p.k_off, p.k_len, p.k_rows, seq_i));
   if (tile_i >= (k.n + TILE - 1) / TILE) return;
-  const int key0 = tile_i * TILE, key = key0 + wave * 32 + nn, chunks = p.d >> 3;
+  const int key0 = tile_i * TILE, key = key0 + kw * 32 + nn, chunks = p.d >> 3;
   const bool live = key < k.n;
-  const int wave_last = key0 + wave * 32 + 31, wg_last = key0 + TILE - 1;     // last keys of the wave and of the workgroup (dead ones too)
+  const int wave_last = key0 + kw * 32 + 31;     // last key of the wave (dead ones too)
+  const DkvUnits un = dkv_units(p, q.n, k.n, key0, ROWS_U);
+  const int cap = p.nsplit > 1 ? uniform(dkv_piece_units(p, ROWS_U, lane)) : un.all, u0 = piece * cap, u1 = min(u0 + cap, un.all);
+  const bool whole_sum = un.all <= cap;
+  if (piece > 0 && u0 >= un.all) return;
 
   const uint16_t* ks = (const uint16_t*)p.k.p + (int64_t)k.seq * p.k.bs + (int64_t)(k.base + (live ? key : 0)) * p.k.ts + (int64_t)kvh * p.k.hs;
   const uint16_t* vs = (const uint16_t*)p.v.p + (int64_t)k.seq * p.v.bs + (int64_t)(k.base + (live ? key : 0)) * p.v.ts + (int64_t)kvh * p.v.hs;
-  bf16x8 K[DK], V[V_LDS ? 1 : DK];
+  // chunk c of V's row r lies at chunk c + (r / 8) % 2 of 14: 16 rows in 16 places modulo 256 bytes
+  const unsigned v_row = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)Vs + (kw * 32 + nn) * VROW;
+  auto v_at = [&](int c) { const int at = c + ((nn >> 3) & 1); return v_row + (at == 2 * (DK - 1) ? 0 : at) * 16; };
+  bf16x8 K[DK], V[DK - VS];
 #pragma unroll
   for (int s = 0; s < DK; ++s) {
     uint4v x = {0u, 0u, 0u, 0u}, y = x;
@@ -194,46 +226,38 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dkv(SeqParams p) {
       y = *(const uint4v*)(vs + s * 16 + g * 8);
     }
     K[s] = __builtin_bit_cast(bf16x8, x);
-    if constexpr (V_LDS) *(uint4v*)(Vs + (wave * 32 + nn) * D + (((2 * s + g) ^ swizzle<D, ROWS>(nn)) << 3)) = y;
-    else V[s] = __builtin_bit_cast(bf16x8, y);
+    if (s < VS) *(__attribute__((address_space(3))) uint4v*)(uintptr_t)v_at(2 * s + g) = y;   // (both waves of the keys write the same)
+    else V[s - VS] = __builtin_bit_cast(bf16x8, y);
   }
+  const unsigned v_first = v_at(g), v_last = v_at(2 * (VS - 1) + g);   // (steps in between follow the first)
 
-  RowRead<D> rr, vr;
+  RowRead<D> rr;
   rr.template set<BOTH>(nn, g);
-  vr.template set<ROWS>(nn, g);
-  ColRead<D> cr;
-  cr.template set<BOTH>(lane);
-  using Copy = TileCopy<D, NW, QT, BOTH>;
-  Copy qc, gc;
-  const int64_t q_bytes = p.q.ts * 2, g_bytes = p.dout.ts * 2;
-  qc.set(q_bytes, wave, lane);
-  gc.set(g_bytes, wave, lane);
-  const unsigned q_lds = lds_address(Qs[0]), g_lds = lds_address(Gs[0]), s_lds = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) float*)St[0];
-  constexpr int NI = Copy::NI, TB = QT * D * 2;
-  // query tiles: those of the first token that sees the first key and on, for one head of the group after the other
-  int first = p.causal ? key0 - (k.n - q.n) : 0;
-  if (first < 0) first = 0;
-  const int tile0 = first / QT, per_head = q.n > first ? (q.n + QT - 1) / QT - tile0 : 0, all = per_head * p.group;
-  auto copy_tile = [&](int head, int tile, int buf) {
-    const int row0 = tile * QT, h = kvh * p.group + head;
-    auto qcur = qc.begin(p.q.p + 2 * ((int64_t)q.seq * p.q.bs + (int64_t)(q.base + row0) * p.q.ts + (int64_t)h * p.q.hs), q_bytes, wave);
-    auto gcur = gc.begin(p.dout.p + 2 * ((int64_t)q.seq * p.dout.bs + (int64_t)(q.base + row0) * p.dout.ts + (int64_t)h * p.dout.hs), g_bytes, wave);
-    if (row0 + QT <= q.n && chunks == D / 8) {
+  ColRead<D, BOTH> cr;
+  cr.set(lane);
+  // this wave copies Q (kw 0) or dO (kw 1) of its own unit
+  using Copy = TileCopy<D, 1, ROWS_U, BOTH>;
+  Copy cp;
+  const HeadsPtr& src = kw ? p.dout : p.q;
+  const int64_t src_bytes = src.ts * 2;
+  cp.set(src_bytes, 0, lane);
+  const char* src0 = src.p + 2 * ((int64_t)q.seq * src.bs + (int64_t)q.base * src.ts + (int64_t)kvh * p.group * src.hs);
+  const unsigned buf_lds = lds_address(Buf[0][0][0]), st_lds = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) float*)St[0][0];
+  auto copy_unit = [&](int head, int tile, int buf) {
+    const int row0 = tile * ROWS_U;
+    auto cur = cp.begin(src0 + 2 * ((int64_t)row0 * src.ts + (int64_t)head * src.hs), src_bytes, 0);
+    const unsigned dst = buf_lds + ((buf * 2 + us) * 2 + kw) * TB;
+    if (row0 + ROWS_U <= q.n && chunks == D / 8) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        qc.whole(qcur, q_bytes, q_lds + buf * TB, wave, i);
-        gc.whole(gcur, g_bytes, g_lds + buf * TB, wave, i);
-      }
+      for (int i = 0; i < Copy::NI; ++i) cp.whole(cur, src_bytes, dst, 0, i);
     } else {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) qc.part(qcur, q_bytes, q_lds + buf * TB, wave, lane, i, q.n - row0, chunks);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) gc.part(gcur, g_bytes, g_lds + buf * TB, wave, lane, i, q.n - row0, chunks);
+      for (int i = 0; i < Copy::NI; ++i) cp.part(cur, src_bytes, dst, 0, lane, i, q.n - row0, chunks);
     }
-    if (wave < 2 * QT / 64) {
-      const int i = wave * 64 + lane;     // (two floats a row)
-      const int64_t at = (int64_t)h * p.lse_rows + (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row0;
-      copy4_any(row0 + (i >> 1) < q.n ? p.delta + 2 * at + i : no_row + (i & 1), s_lds + buf * (2 * QT * 4) + wave * 256);
+    if (kw < UT) {
+      const int i = kw * 64 + lane;     // (two floats a row)
+      const int64_t at = (int64_t)(kvh * p.group + head) * p.lse_rows + (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row0;
+      copy4_any(row0 + (i >> 1) < q.n ? p.delta + 2 * at + i : no_row + (i & 1), st_lds + ((buf * 2 + us) * 2 * ROWS_U + kw * 64) * 4);
     }
   };
 
@@ -242,36 +266,48 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dkv(SeqParams p) {
   auto run = [&](auto careful) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) { dK[dt] = zero16(); dV[dt] = zero16(); }
-    int head = 0, tile = tile0;
-    if (all > 0) copy_tile(0, tile0, 0);
-    auto next_tile = [&] {
+    // the wave's next unit to copy, as head and tile
+    int u = u0 + us, head = un.per_head ? u / un.per_head : 0, tile = un.tile0 + u - head * un.per_head;
+    auto advance = [&] {
+      u += 2;
+      tile += 2;
+      while (tile >= un.tile0 + un.per_head) { tile -= un.per_head; ++head; }
+    };
+    auto next_units = [&] {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __syncthreads();
     };
-    next_tile();
-    for (int t = 0; t < all; ++t, next_tile()) {
-      const int buf = t & 1, row0 = tile * QT;
-      uint16_t* Qt = Qs[buf];
-      uint16_t* Gt = Gs[buf];
-      // the last key that row i of the tile sees is shift + i
-      const int shift = p.causal ? row0 + k.n - q.n : 1 << 29;
-      if (careful.value && (shift < wg_last || row0 + QT > q.n)) {
-        auto seen = [&](int i) { return live && row0 + i < q.n && key <= shift + i; };
-        set_aside<D, QT, BOTH>(dV, Gt, g, seen);
-        set_aside<D, QT, BOTH>(dK, Qt, g, seen);
-      }
-      if (++tile == tile0 + per_head) { tile = tile0; ++head; }
-      if (t + 1 < all) copy_tile(head, tile, buf ^ 1);
+    if (u < u1) copy_unit(head, tile, 0);
+    next_units();
+    for (int t = u0; t < u1; t += 2, next_units()) {
+      const int buf = ((t - u0) >> 1) & 1, row0 = tile * ROWS_U;
+      const bool has = u < u1;                                     // (the last unit may be the other waves' alone)
+      const int shift = p.causal ? row0 + k.n - q.n : 1 << 29;     // the last key that row i of the unit sees is shift + i
+      if (careful.value) {
 #pragma unroll
-      for (int t2 = 0; t2 < T2; ++t2) {
-        if (shift + t2 * 32 + 31 < key0 + wave * 32) continue;    // (uniform) no row of the half sees a key of the wave
+        for (int w = 0; w < 2; ++w) {
+          if (t + w >= u1) continue;
+          auto seen = [&](int i) { return w == us && live && row0 + i < q.n && key <= shift + i; };
+          set_aside<D, ROWS_U, BOTH>(dV, Buf[buf][w][1], g, seen);
+          set_aside<D, ROWS_U, BOTH>(dK, Buf[buf][w][0], g, seen);
+        }
+      }
+      if (un.all > 0) advance();
+      if (u < u1) copy_unit(head, tile, buf ^ 1);
+      if (!has) continue;
+      const unsigned Qt = buf_lds + (buf * 2 + us) * 2 * TB, Gt = Qt + TB;
+#pragma unroll
+      for (int t2 = 0; t2 < UT; ++t2) {
+        if (shift + t2 * 32 + 31 < key0 + kw * 32) continue;    // (uniform) no row sees a key of the wave
         float16v S = zero16(), dP = zero16();
 #pragma unroll
         for (int s = 0; s < DK; ++s) S = mfma(rr.get(Qt, t2, s), K[s], S);
 #pragma unroll
         for (int s = 0; s < DK; ++s) {
-          if constexpr (V_LDS) dP = mfma(rr.get(Gt, t2, s), vr.get(Vs, wave, s), dP);
-          else dP = mfma(rr.get(Gt, t2, s), V[s], dP);
+          bf16x8 v;
+          if (s < VS) v = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(s == VS - 1 ? v_last : v_first + 32 * s);
+          else v = V[s - VS];
+          dP = mfma(rr.get(Gt, t2, s), v, dP);
         }
         const bool mask = shift + t2 * 32 < wave_last;
         const int lim = key - shift - t2 * 32 - 4 * g;     // row 8 (r / 4) + 4 g + r % 4 sees the lane's key where that is lim or more
@@ -280,7 +316,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dkv(SeqParams p) {
           uint4v pp, ps;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float* st = St[buf] + 2 * (t2 * 32 + 8 * (2 * s2 + i) + 4 * g);
+            const float* st = St[buf][us] + 2 * (t2 * 32 + 8 * (2 * s2 + i) + 4 * g);
             const float4v a = *(const float4v*)st, b = *(const float4v*)(st + 4);
             const float lse[4] = {a[0], a[2], b[0], b[2]}, del[4] = {a[1], a[3], b[1], b[3]};
             float x[4], y[4];
@@ -310,29 +346,94 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dkv(SeqParams p) {
   };
   run(std::false_type{});
   if (p.causal && uniform(__syncthreads_or(live && (any_odd(dK) || any_odd(dV))))) run(std::true_type{});
-  auto out = [&](const HeadsPtr& v) { return (uint16_t*)const_cast<char*>(v.p) + (int64_t)k.seq * v.bs + (int64_t)(k.base + (live ? key : 0)) * v.ts + (int64_t)kvh * v.hs; };
-  uint16_t *dk = out(p.dk), *dv = out(p.dv);
-  each_piece(dK, p.scale, g, [&](int c, const float (&o)[8]) {
-    if (live && c < p.d) *(uint4v*)(dk + c) = pack8(o);
-  });
-  each_piece(dV, 1.f, g, [&](int c, const float (&o)[8]) {
-    if (live && c < p.d) *(uint4v*)(dv + c) = pack8(o);
+  // the waves of the first units take dK's sum, those of the second dV's (every wave is past its last read of the tiles: next_units)
+  float* ex = (float*)Buf + wave * (DT * 16 * 64);
+  const float* from = (const float*)Buf + (wave ^ 2) * (DT * 16 * 64);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ex[(dt * 16 + r) * 64 + lane] = us ? dK[dt][r] : dV[dt][r];
+  __syncthreads();
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float o = from[(dt * 16 + r) * 64 + lane];
+      dK[dt][r] = us ? o + dV[dt][r] : dK[dt][r] + o;     // (units in their order in both sums)
+    }
+  const HeadsPtr& to = us ? p.dv : p.dk;
+  uint16_t* dst = (uint16_t*)const_cast<char*>(to.p) + (int64_t)k.seq * to.bs + (int64_t)(k.base + (live ? key : 0)) * to.ts + (int64_t)kvh * to.hs;
+  float* part = p.part + (((int64_t)piece * 2 + us) * p.hk * p.lse_k + (int64_t)kvh * p.lse_k + (p.k_off ? (int64_t)k.base : (int64_t)seq_i * p.k_rows) + key) * p.d;
+  each_piece(dK, us ? 1.f : p.scale, g, [&](int c, const float (&o)[8]) {
+    if (!live || c >= p.d) return;
+    if (whole_sum) {
+      *(uint4v*)(dst + c) = pack8(o);
+    } else {
+      *(float4v*)(part + c) = float4v{o[0], o[1], o[2], o[3]};
+      *(float4v*)(part + c + 4) = float4v{o[4], o[5], o[6], o[7]};
+    }
   });
 }
 
-template <int D, int QT>
+// Adds the pieces of dK and dV up, in their order, where a tile of keys has several.  A wave takes a key, a lane two channels.
+__global__ void __launch_bounds__(256) k_seq_dkv_join(SeqParams p, int rows_u) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
+  int seq_i, tile_i;
+  seq_slot(p.k_off, p.k_rows, p.nseq, 1, 4, (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i);
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq_i), k = seq_range(p.k_off, p.k_len, p.k_rows, seq_i);
+  if ((int64_t)tile_i * 4 + wave >= k.n) return;
+  const int key = tile_i * 4 + wave, cap = dkv_piece_units(p, rows_u, lane), all = dkv_units(p, q.n, k.n, key / 64 * 64, rows_u).all;
+  const int c = 2 * lane;
+  if (all <= cap || c >= p.d) return;
+  const int64_t rows = (int64_t)p.hk * p.lse_k, at = (int64_t)kvh * p.lse_k + (p.k_off ? (int64_t)k.base : (int64_t)seq_i * p.k_rows) + key;
+  for (int w = 0; w < 2; ++w) {
+    float a = 0.f, b = 0.f;
+    for (int s = 0; s * cap < all; ++s) {
+      const float2v x = *(const float2v*)(p.part + (((int64_t)s * 2 + w) * rows + at) * p.d + c);
+      a += x[0];
+      b += x[1];
+    }
+    const HeadsPtr& to = w ? p.dv : p.dk;
+    uint16_t* dst = (uint16_t*)const_cast<char*>(to.p) + (int64_t)k.seq * to.bs + (int64_t)(k.base + key) * to.ts + (int64_t)kvh * to.hs;
+    *(uint32_t*)(dst + c) = pack2(a, b);
+  }
+}
+
+template <int D, int UT>
 hipError_t go(SeqParams p, hipStream_t st) {
   p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 128);
   if (p.slots > 0) hipLaunchKernelGGL((k_seq_dq<D, 4, 64>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  p.slots = (int)seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 128);
-  if (p.slots > 0) hipLaunchKernelGGL((k_seq_dkv<D, 4, QT>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
+  p.slots = (int)seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 64);
+  if (p.slots == 0) return hipSuccess;
+  hipLaunchKernelGGL((k_seq_dkv<D, UT>), dim3((unsigned)p.slots * (unsigned)p.nsplit * (unsigned)p.hk), dim3(256), 0, st, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const int64_t slots = seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 4);
+  hipLaunchKernelGGL(k_seq_dkv_join, dim3((unsigned)(slots * p.hk)), dim3(256), 0, st, p, 32 * UT);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_seq_bwd(const SeqParams& p, hipStream_t st) { return p.d <= 64 ? go<64, 64>(p, st) : go<128, 32>(p, st); }
+// How a backward call is cut: pieces of the query rows that a tile of keys is summed over, where there are few tiles.
+SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu) {
+  SeqPlan s = {};
+  const int64_t blocks = seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 64) * p.hk;
+  const int64_t units = ((int64_t)p.q_rows + 31) / 32 * p.group;      // the most that a tile of keys can have
+  s.nsplit = 1;
+  if (p.k_rows > 0 && units >= 32) s.nsplit = blocks >= 4 * num_cu ? 1 : blocks >= 2 * num_cu ? 2 : 4;
+  const int64_t stats = ((int64_t)p.hq * p.lse_rows * 8 + 255) / 256 * 256;
+  s.part_at = stats;
+  s.workspace = stats + (s.nsplit > 1 ? (int64_t)s.nsplit * 2 * p.hk * p.lse_k * p.d * 4 : 0);
+  return s;
+}
+
+hipError_t launch_seq_bwd(SeqParams p, const SeqPlan& s, hipStream_t st) {
+  p.nsplit = s.nsplit;
+  return p.d <= 64 ? go<64, 2>(p, st) : go<128, 1>(p, st);
+}
 
 }  // namespace fa

@@ -23,8 +23,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
   // workgroups of the compute unit (nine at D = 128) fill the wait.  More waves share two of each.
   constexpr bool ONE = NW == 1;
   constexpr int NB = ONE ? 1 : 2;
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[NB][KT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[NB][KT * D];
+  __shared__ __attribute__((aligned(256))) uint16_t Ks[NB][KT * D];
+  __shared__ __attribute__((aligned(256))) uint16_t Vs[NB][KT * D];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // key heads fastest, then pieces of the keys, then tiles from the last: under the causal mask the longest come first
@@ -69,8 +69,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
 
   RowRead<D> kr;
   kr.template set<ROWS>(nn, g);
-  ColRead<D> vr;
-  vr.template set<COLS>(lane);
+  ColRead<D, COLS> vr;
+  vr.set(lane);
   TileCopy<D, NW, KT, ROWS> kc;
   TileCopy<D, NW, KT, COLS> vc;
   const int64_t k_bytes = p.k.ts * 2, v_bytes = p.v.ts * 2;
@@ -130,11 +130,10 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
     next_tile();
     for (int t = t0; t < t1; ++t, next_tile()) {
       const int buf = ONE ? 0 : (t - t0) & 1, key0 = t * KT;
-      const uint16_t* Kt = Ks[buf];
-      uint16_t* Vt = Vs[buf];
+      const unsigned Kt = k_lds + buf * TB, Vt = v_lds + buf * TB;
       const bool more = t + 1 < t1;
       auto aside = [&] {
-        if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, COLS>(O, Vt, g, [&](int i) { return row.live && key0 + i <= row.last; });
+        if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, COLS>(O, Vs[buf], g, [&](int i) { return row.live && key0 + i <= row.last; });
       };
       if (!ONE) aside();
       if (!ONE && key0 > wave_last) {   // (uniform over the wave) none of its rows sees the tile

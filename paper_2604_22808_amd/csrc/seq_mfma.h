@@ -126,37 +126,32 @@ struct TileCopy {
   }
 };
 
-// Operand addresses (elements) of a lane in a tile.
+// Operand addresses (LDS bytes) of a lane in a tile that starts at a multiple of a row.  The swizzles are exclusive-ors, so that one register holds the
+// address and a constant flips the bits of step, channel tile and half.
 template <int D>
 struct RowRead {    // rows 32 t + nn, channels 16 s + 8 g .. + 7
-  int row, x[D / 16];
-  template <int USE> __device__ __forceinline__ void set(int nn, int g) {
-    row = nn * D;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) x[s] = ((2 * s + g) ^ swizzle<D, USE>(nn)) << 3;   // (the swizzle of row 32 t + nn is that of nn)
+  unsigned at;
+  template <int USE> __device__ __forceinline__ void set(int nn, int g) { at = nn * D * 2 + ((g ^ swizzle<D, USE>(nn)) << 4); }   // (row 32 t + nn has nn's swizzle)
+  __device__ __forceinline__ bf16x8 get(unsigned tile, int t, int s) const {
+    return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(((tile + at) ^ (s << 5)) + t * 32 * D * 2);
   }
-  __device__ __forceinline__ bf16x8 get(const uint16_t* tile, int t, int s) const { return *(const bf16x8*)(tile + t * 32 * D + row + x[s]); }
 };
 // channels 32 dt + nn, rows 16 s + 8 h + 4 g + 0..3 for h = 0, 1: the rows that a lane half g holds in registers 8 (s % 2) .. + 7 of the product
 // over rows 32 (s / 2) .. + 31.
-template <int D>
+template <int D, int USE>
 struct ColRead {
-  int row, x[D / 32], flip;
-  template <int USE> __device__ __forceinline__ void set(int lane) {
-    static_assert(USE != ROWS, "");
-    const int g = lane >> 5, sl = lane & 15, g1 = (lane >> 4) & 1;
-    row = (4 * g + (sl >> 2)) * D + (sl & 1) * 4;
-    // row 16 s + 8 h + 4 g + sl / 4: of a BOTH tile's swizzle h changes one bit, by which two chunks change places
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) x[dt] = ((4 * dt + 2 * g1 + ((sl & 3) >> 1)) ^ swizzle<D, USE>(4 * g + (sl >> 2))) << 3;
-    flip = USE == BOTH ? ((x[0] & 16) ? -16 : 16) : 0;
+  static_assert(USE != ROWS, "");
+  unsigned at;
+  __device__ __forceinline__ void set(int lane) {
+    const int g = lane >> 5, sl = lane & 15, g1 = (lane >> 4) & 1, row = 4 * g + (sl >> 2);
+    at = row * D * 2 + (sl & 1) * 8 + (((2 * g1 + ((sl & 3) >> 1)) ^ swizzle<D, USE>(row)) << 4);
   }
-  __device__ __forceinline__ bf16x8 get(const uint16_t* tile, int dt, int s) const {
+  __device__ __forceinline__ bf16x8 get(unsigned tile, int dt, int s) const {
     uint4v r;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint16_t* p = tile + (s * 16 + 8 * h) * D + row + x[dt] + (h ? flip : 0);   // (x[dt] & 16 is alike for all dt)
-      const uint2v u = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)p));
+    for (int h = 0; h < 2; ++h) {   // (eight rows on, a BOTH tile's swizzle has one more bit)
+      const unsigned p = ((tile + at) ^ ((dt << 6) | (USE == BOTH ? h << 5 : 0))) + (s * 16 + 8 * h) * D * 2;
+      const uint2v u = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(uintptr_t)p));
       r[2 * h] = u[0];
       r[2 * h + 1] = u[1];
     }
