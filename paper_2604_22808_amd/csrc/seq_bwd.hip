@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6);
   const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
   int seq_i, tile_i;
-  seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, p.slots - 1 - (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i);
+  if (!seq_query_tile(p, TILE, lane, (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i)) return;
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(p.k_off, p.k_len, p.k_rows, seq_i));
@@ -193,13 +193,13 @@ __global__ void __launch_bounds__(256, 2) k_seq_dkv(SeqParams p) {
   __shared__ __attribute__((aligned(256))) char Vs[V_LDS ? TILE * VROW : 16];
   __shared__ __attribute__((aligned(256))) float St[2][2][2 * ROWS_U];      // [copy][unit] (lse, delta) of its rows
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6), kw = wave & 1, us = wave >> 1;
-  // key heads fastest, then pieces; tiles from the first: under the causal mask the first keys are seen by the most rows
+  // key heads fastest, then pieces, then tiles, the longest first
   unsigned id = blockIdx.x;
   const int kvh = (int)(id % (unsigned)p.hk);
   id /= (unsigned)p.hk;
   const int piece = (int)(id % (unsigned)p.nsplit);
   int seq_i, tile_i;
-  seq_slot(p.k_off, p.k_rows, p.nseq, 1, TILE, (int)(id / (unsigned)p.nsplit), seq_i, tile_i);
+  if (!seq_key_tile(p, TILE, lane, (int)(id / (unsigned)p.nsplit), seq_i, tile_i)) return;
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(p.k_off, p.k_len, p.k_rows, seq_i));

@@ -27,13 +27,14 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
   __shared__ __attribute__((aligned(256))) uint16_t Vs[NB][KT * D];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // key heads fastest, then pieces of the keys, then tiles from the last: under the causal mask the longest come first
+  // key heads fastest, then pieces of the keys, then tiles, the longest first
   unsigned id = blockIdx.x;
   const int kvh = (int)(id % (unsigned)p.hk);
   id /= (unsigned)p.hk;
   const int split = (int)(id % (unsigned)p.nsplit);
   int seq_i, tile_i;
-  seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, p.slots - 1 - (int)(id / (unsigned)p.nsplit), seq_i, tile_i);
+  if (ONE) seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, (int)(id / (unsigned)p.nsplit), seq_i, tile_i);
+  else if (!seq_query_tile(p, TILE, lane, (int)(id / (unsigned)p.nsplit), seq_i, tile_i)) return;
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(p.k_off, p.k_len, p.k_rows, seq_i));
