@@ -46,7 +46,7 @@ __device__ __forceinline__ int dkv_piece_units(const SeqParams& p, int rows_u, i
 
 template <int D, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
-  constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW;
+  constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW, PF = 4;
   __shared__ __attribute__((aligned(256))) uint16_t Ks[2][KT * D];
   __shared__ __attribute__((aligned(256))) uint16_t Vs[2][KT * D];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6);
@@ -149,10 +149,12 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
       for (int t2 = 0; t2 < T2; ++t2) {
         const int first = key0 + t2 * 32;
         float16v S = zero16(), dP = zero16();
-#pragma unroll
-        for (int s = 0; s < DK; ++s) S = mfma(rr.get(Kt, t2, s), Q[s], S);
-#pragma unroll
-        for (int s = 0; s < DK; ++s) dP = mfma(rr.get(Vt, t2, s), G[s], dP);
+        products<2 * DK, PF>([&](int i) { return rr.get(i < DK ? Kt : Vt, t2, i % DK); },
+                             [&](int i, const bf16x8& a) {
+                               if (i < DK) S = mfma(a, Q[i], S);
+                               else dP = mfma(a, G[i - DK], dP);
+                             });
+        in_turn<2 * DK, PF, 1>();
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse2)) * (dP[r] - delta);
         if (first + 31 > wave_first) {
@@ -160,15 +162,17 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) S[r] = 8 * (r >> 2) + (r & 3) <= lim ? S[r] : 0.f;
         }
+        bf16x8 dS[2];
 #pragma unroll
         for (int s2 = 0; s2 < 2; ++s2) {
           uint4v pk;
 #pragma unroll
           for (int j = 0; j < 4; ++j) pk[j] = pack2(S[s2 * 8 + 2 * j], S[s2 * 8 + 2 * j + 1]);
-          const bf16x8 dS = __builtin_bit_cast(bf16x8, pk);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) A[dt] = mfma(cr.get(Kt, dt, 2 * t2 + s2), dS, A[dt]);
+          dS[s2] = __builtin_bit_cast(bf16x8, pk);
         }
+        products<2 * DT, PF>([&](int i) { return cr.get(Kt, i % DT, 2 * t2 + i / DT); },
+                             [&](int i, const bf16x8& a) { A[i % DT] = mfma(a, dS[i / DT], A[i % DT]); });
+        in_turn<2 * DT, PF, 2>();
       }
     }
   };
@@ -186,8 +190,9 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
 // wave; at D = 128 V's operands stay in LDS but for the last step's (the two workgroups of a compute unit have 80 KB each).
 template <int D, int UT>
 __global__ void __launch_bounds__(256, 2) k_seq_dkv(SeqParams p) {
-  constexpr int DT = D / 32, DK = D / 16, ROWS_U = 32 * UT, TILE = 64, TB = ROWS_U * D * 2;
+  constexpr int DT = D / 32, DK = D / 16, ROWS_U = 32 * UT, TILE = 64, TB = ROWS_U * D * 2, PF = 4;
   constexpr bool V_LDS = D == 128;
+  constexpr int PV = V_LDS ? 2 : PF;      // (with two operands each, more do not fit)
   constexpr int VS = V_LDS ? DK - 1 : 0, VROW = 2 * (DK - 1) * 16;    // steps of V in LDS, bytes of a row there
   __shared__ __attribute__((aligned(256))) uint16_t Buf[2][2][2][TB / 2];   // [copy][unit][Q, dO]
   __shared__ __attribute__((aligned(256))) char Vs[V_LDS ? TILE * VROW : 16];
@@ -300,15 +305,19 @@ __global__ void __launch_bounds__(256, 2) k_seq_dkv(SeqParams p) {
       for (int t2 = 0; t2 < UT; ++t2) {
         if (shift + t2 * 32 + 31 < key0 + kw * 32) continue;    // (uniform) no row sees a key of the wave
         float16v S = zero16(), dP = zero16();
-#pragma unroll
-        for (int s = 0; s < DK; ++s) S = mfma(rr.get(Qt, t2, s), K[s], S);
-#pragma unroll
-        for (int s = 0; s < DK; ++s) {
-          bf16x8 v;
-          if (s < VS) v = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(s == VS - 1 ? v_last : v_first + 32 * s);
-          else v = V[s - VS];
-          dP = mfma(rr.get(Gt, t2, s), v, dP);
-        }
+        products<DK, PF>([&](int i) { return rr.get(Qt, t2, i); }, [&](int i, const bf16x8& a) { S = mfma(a, K[i], S); });
+        in_turn<DK, PF, 1>();
+        struct Two { bf16x8 g, v; };
+        products<DK, PV>([&](int i) {
+                           Two x;
+                           x.g = rr.get(Gt, t2, i);
+                           if (i < VS) x.v = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(i == VS - 1 ? v_last : v_first + 32 * i);
+                           else x.v = V[i - VS];
+                           return x;
+                         },
+                         [&](int i, const Two& a) { dP = mfma(a.g, a.v, dP); });
+        in_turn<DK, PV, V_LDS ? 2 : 1>();
+        bf16x8 P[2], dS[2];
         const bool mask = shift + t2 * 32 < wave_last;
         const int lim = key - shift - t2 * 32 - 4 * g;     // row 8 (r / 4) + 4 g + r % 4 sees the lane's key where that is lim or more
 #pragma unroll
@@ -334,13 +343,16 @@ __global__ void __launch_bounds__(256, 2) k_seq_dkv(SeqParams p) {
             pp[2 * i] = pack2(x[0], x[1]); pp[2 * i + 1] = pack2(x[2], x[3]);
             ps[2 * i] = pack2(y[0], y[1]); ps[2 * i + 1] = pack2(y[2], y[3]);
           }
-          const bf16x8 P = __builtin_bit_cast(bf16x8, pp), dS = __builtin_bit_cast(bf16x8, ps);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            dV[dt] = mfma(cr.get(Gt, dt, 2 * t2 + s2), P, dV[dt]);
-            dK[dt] = mfma(cr.get(Qt, dt, 2 * t2 + s2), dS, dK[dt]);
-          }
+          P[s2] = __builtin_bit_cast(bf16x8, pp);
+          dS[s2] = __builtin_bit_cast(bf16x8, ps);
         }
+        products<4 * DT, PF>([&](int i) { return cr.get(i & 1 ? Qt : Gt, (i >> 1) % DT, 2 * t2 + (i >> 1) / DT); },
+                             [&](int i, const bf16x8& a) {
+                               const int dt = (i >> 1) % DT, s2 = (i >> 1) / DT;
+                               if (i & 1) dK[dt] = mfma(a, dS[s2], dK[dt]);
+                               else dV[dt] = mfma(a, P[s2], dV[dt]);
+                             });
+        in_turn<4 * DT, PF, 2>();
       }
     }
   };

@@ -200,6 +200,31 @@ __device__ __forceinline__ bool any_odd(const float16v (&x)[N]) {
   return probe != 0.f;
 }
 
+// N products of which product i takes an operand load(i), requested PF products ahead.
+template <int N, int PF, typename L, typename M>
+__device__ __forceinline__ void products(L&& load, M&& mul) {
+  decltype(load(0)) A[PF];
+#pragma unroll
+  for (int i = 0; i < PF; ++i) A[i] = load(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const auto a = A[i % PF];
+    if (i + PF < N) A[i % PF] = load(i + PF);
+    mul(i, a);
+  }
+}
+// The order of such a run: the reads of PF operands, then one product and one operand's reads in turn.
+template <int N, int PF, int READS>
+__device__ __forceinline__ void in_turn() {
+  __builtin_amdgcn_sched_group_barrier(0x100, PF * READS, 0);
+#pragma unroll
+  for (int i = 0; i < N - PF; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, PF, 0);
+}
+
 // Stores a row of which two lane halves hold the channels as accumulators, times f.  Per 16 channels a lane holds two groups of four that interleave with its
 // partner's: after swapping one each it has 8 consecutive channels.  put(c, o): channels c .. c + 7.
 template <int DT, typename F>
