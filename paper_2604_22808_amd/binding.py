@@ -398,79 +398,89 @@ def route_fixed(heads, n_low, n_mid, n_high):
 # They need no context.  A tensor of heads is [batch, rows, heads, head_dim] (packed sequences: [rows, heads, head_dim]) with adjacent
 # channels and any other strides: a head-major tensor is passed as x.transpose(1, 2), a part of a fused projection as the slice that it is.
 
+_Tensor = None     # torch.Tensor and the two I/O types, once torch is there (these calls are short: what they look up counts)
+
+
+def _torch_names():
+    global _Tensor, _BF16, _F32, _INT32, _device, _raw_stream
+    import torch
+    _BF16, _F32, _INT32 = torch.bfloat16, torch.float32, torch.int32
+    _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    _Tensor = torch.Tensor
+
+
 def _heads(who, name, t, like=None, shape=None, written=False):
     """The freqattn_heads of a tensor, after the checks that the library cannot make on an address."""
-    import torch
-    if not isinstance(t, torch.Tensor):
+    if _Tensor is None:
+        _torch_names()
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{who}: {name} must be a torch tensor")
     if not t.is_cuda:
         raise ValueError(f"{who}: {name} must be a device tensor")
-    dim, sh, st = t.dim(), t.shape, t.stride()
+    sh, st, dtype = t.shape, t.stride(), t.dtype
+    dim = len(st)
     if dim != 3 and dim != 4:
         raise ValueError(f"{who}: {name} must be [batch, rows, heads, head_dim] or [rows, heads, head_dim], got {tuple(sh)}")
     if like is None:
-        if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
-            raise ValueError(f"{who}: {name} has dtype {t.dtype}, expected bfloat16 or float32")
-    else:
-        if t.dtype is not like.dtype:
-            raise ValueError(f"{who}: {name} has dtype {t.dtype}, expected {like.dtype}")
-        if t.device != like.device:
-            raise ValueError(f"{who}: {name} is on {t.device}, expected {like.device}")
+        if dtype is not _BF16 and dtype is not _F32:
+            raise ValueError(f"{who}: {name} has dtype {dtype}, expected bfloat16 or float32")
+    elif dtype is not like.dtype:
+        raise ValueError(f"{who}: {name} has dtype {dtype}, expected {like.dtype}")
+    elif t.device != like.device:
+        raise ValueError(f"{who}: {name} is on {t.device}, expected {like.device}")
     if shape is not None and sh != shape:
         raise ValueError(f"{who}: {name} has shape {tuple(sh)}, expected {tuple(shape)}")
     if st[-1] != 1 and sh[-1] > 1:
         raise ValueError(f"{who}: the channels of {name} must be adjacent")
-    if written and any(s == 0 and n > 1 for s, n in zip(st, sh)):
+    if written and 0 in st and any(s == 0 and n > 1 for s, n in zip(st, sh)):
         raise ValueError(f"{who}: {name} is written and must not be expanded")
     return Heads(t.data_ptr(), st[0] if dim == 4 else 0, st[-3], st[-2])
 
 
 def _int32(who, name, t, like, *shapes):
     """Address of a contiguous int32 device tensor of one of the shapes; None passes."""
-    import torch
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.device != like.device or not t.is_contiguous() or tuple(t.shape) not in shapes:
+    if not isinstance(t, _Tensor) or t.dtype is not _INT32 or t.device != like.device or not t.is_contiguous() or t.shape not in shapes:
         raise ValueError(f"{who}: {name} must be a contiguous int32 tensor on {like.device} of shape {' or '.join(map(str, shapes))}")
     return t.data_ptr()
 
 
 def _vector(who, name, t, like, n, dtype):
-    import torch
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != like.device or not t.is_contiguous() or tuple(t.shape) != (n,):
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.device != like.device or not t.is_contiguous() or t.shape != (n,):
         raise ValueError(f"{who}: {name} must be a contiguous {dtype} tensor of shape {(n,)} on {like.device}")
     return t.data_ptr()
 
 
 def _call(fn, t, *args):
     """fn(*args, stream) on the device of t, with its current stream; raises on failure."""
-    import torch
-    if t.device.index == torch.cuda.current_device():
-        st = fn(*args, _stream())
+    index = t.get_device()
+    if index == _device():
+        st = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(t.device):
-            st = fn(*args, _stream())
+        import torch
+        with torch.cuda.device(index):
+            st = fn(*args, _raw_stream(index))
     if st != OK:
         raise FreqAttnError(st, lib().freqattn_last_error(None).decode())
 
 
 def _workspace(who, t, need, like):
     """Address and size of the caller's workspace, or of one from torch's allocator (on the stream that the call uses)."""
-    import torch
     if need == 0:
         return None, 0, None
     if t is None:
+        import torch
         t = torch.empty(need, dtype=torch.uint8, device=like.device)
-    elif not isinstance(t, torch.Tensor) or t.device != like.device or not t.is_contiguous():
+    elif not isinstance(t, _Tensor) or t.device != like.device or not t.is_contiguous():
         raise ValueError(f"{who}: workspace must be a contiguous tensor on {like.device}")
     return t.data_ptr(), t.numel() * t.element_size(), t
 
 
 def _io(t):
-    import torch
-    return BF16 if t.dtype is torch.bfloat16 else F32
+    return BF16 if t.dtype is _BF16 else F32
 
 
 class Rotary:
@@ -521,7 +531,7 @@ def _positions(who, rotary, positions, batch, tokens, like):
         each.append((batch, tokens))
         one.append((tokens,))
     at = _int32(who, "positions", positions, like, *each, *one)
-    return rotary._h, at, tokens * n if at is not None and tuple(positions.shape) in each else 0
+    return rotary._h, at, tokens * n if at is not None and positions.shape in each else 0
 
 
 def rotary_apply(rotary, x, out, positions=None, inverse=False):
@@ -571,14 +581,13 @@ def qk_norm(q, k, wq, wk, q_out, k_out, eps=1e-6, rotary=None, positions=None):
 
 def qk_norm_backward(q, k, wq, wk, dq_out, dk_out, dq, dk, dwq=None, dwk=None, eps=1e-6, rotary=None, positions=None, workspace=None):
     """freqattn_qk_norm_backward: q, k, wq, wk, rotary, positions as in qk_norm; dwq, dwk fp32 [head_dim] or None."""
-    import torch
     who = "qk_norm_backward"
     shape, rot, hq, hk, w = _qk_args(who, q, k, wq, wk, eps, rotary, positions)
     yq, xq = _heads(who, "dq_out", dq_out, q, q.shape), _heads(who, "dq", dq, q, q.shape, True)
     yk = xk = None
     if k is not None:
         yk, xk = _heads(who, "dk_out", dk_out, q, k.shape), _heads(who, "dk", dk, q, k.shape, True)
-    dw = [_vector(who, name, x, q, q.shape[3], torch.float32) for name, x in (("dwq", dwq), ("dwk", dwk))]
+    dw = [_vector(who, name, x, q, q.shape[3], _F32) for name, x in (("dwq", dwq), ("dwk", dwk))]
     need = 0 if dwq is None and dwk is None else lib().freqattn_qk_norm_workspace(q.shape[3])
     ws, size, keep = _workspace(who, workspace, need, q)
     _call(lib().freqattn_qk_norm_backward, q, shape, *rot, hq, hk, *w, yq, yk, xq, xk, *dw, ws, size)
@@ -605,11 +614,9 @@ def _sequence_args(who, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths,
 
 
 def _lse(who, lse, q, q_offsets, heads):
-    import torch
-    cols = q.shape[0] if q_offsets is not None else q.shape[0] * q.shape[1]
-    if not isinstance(lse, torch.Tensor) or lse.dtype is not torch.float32 or lse.device != q.device or not lse.is_contiguous() \
-            or tuple(lse.shape) != (heads, cols):
-        raise ValueError(f"{who}: lse must be a contiguous float32 tensor of shape {(heads, cols)} on {q.device}")
+    shape = (heads, q.shape[0] if q_offsets is not None else q.shape[0] * q.shape[1])
+    if not isinstance(lse, _Tensor) or lse.dtype is not _F32 or lse.device != q.device or not lse.is_contiguous() or lse.shape != shape:
+        raise ValueError(f"{who}: lse must be a contiguous float32 tensor of shape {shape} on {q.device}")
     return lse.data_ptr()
 
 

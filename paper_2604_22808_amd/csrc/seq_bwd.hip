@@ -91,13 +91,6 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
     }
     delta += other_half(delta);
   }
-  const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
-  float lse2 = row.live ? p.lse[at] * LOG2E : 0.f;
-  // A row that sees no key (lse -inf) has no probabilities; one whose scores hold +inf has no finite ones.
-  if (lse2 == -INFINITY) { lse2 = INFINITY; delta = 0.f; }
-  else if (lse2 == INFINITY) lse2 = __builtin_nanf("");
-  if (row.live && g == 0) *(float2v*)(p.delta + 2 * at) = float2v{lse2, delta};
-
   RowRead<D> rr;
   rr.template set<BOTH>(nn, g);
   ColRead<D, BOTH> cr;
@@ -128,18 +121,56 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
     }
   };
 
+  const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
+  float lse2 = row.live ? p.lse[at] * LOG2E : 0.f;
+  // A row that sees no key (lse -inf) has no probabilities; one whose scores hold +inf has no finite ones.
+  if (lse2 == -INFINITY) { lse2 = INFINITY; delta = 0.f; }
+  else if (lse2 == INFINITY) lse2 = __builtin_nanf("");
   const float c2 = p.scale * LOG2E;
+  auto arrived = [&] {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  // scores and dO V^T of 32 keys
+  auto both = [&](unsigned Kt, unsigned Vt, int t2, float16v& S, float16v& dP) {
+    S = zero16();
+    dP = zero16();
+    products<2 * DK, PF>([&](int i) { return rr.get(i < DK ? Kt : Vt, t2, i % DK); },
+                         [&](int i, const bf16x8& a) {
+                           if (i < DK) S = mfma(a, Q[i], S);
+                           else dP = mfma(a, G[i - DK], dP);
+                         });
+    in_turn<2 * DK, PF, 1>();
+  };
+  if (tiles == 1) {
+    // Rows of few keys have large gradients, and the rounding of out to bf16 is a share of them: up to KT keys, delta is summed from the probabilities
+    // themselves, sum_j P_j (dO V^T)_j, instead.  (Over n keys out is smaller than v by sqrt(n), and its rounding with it.)
+    copy_tile(0, 0);
+    arrived();
+    float sum = 0.f;
+#pragma nounroll
+    for (int t2 = 0; t2 < T2; ++t2) {
+      float16v S, dP;
+      both(k_lds, v_lds, t2, S, dP);
+      const int lim = row.last - t2 * 32 - 4 * g;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse2)) * dP[r];
+        sum += 8 * (r >> 2) + (r & 3) <= lim ? x : 0.f;
+      }
+    }
+    delta = sum + other_half(sum);
+    __syncthreads();
+  }
+  if (row.live && g == 0) *(float2v*)(p.delta + 2 * at) = float2v{lse2, delta};
+
   float16v A[DT];
   auto run = [&](auto careful) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) A[dt] = zero16();
     if (tiles > 0) copy_tile(0, 0);
-    auto next_tile = [&] {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      __syncthreads();
-    };
-    next_tile();
-    for (int t = 0; t < tiles; ++t, next_tile()) {
+    arrived();
+    for (int t = 0; t < tiles; ++t, arrived()) {
       const int buf = t & 1, key0 = t * KT;
       const unsigned Kt = k_lds + buf * TB, Vt = v_lds + buf * TB;
       if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, BOTH>(A, Ks[buf], g, [&](int i) { return row.live && key0 + i <= row.last; });
@@ -148,13 +179,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
 #pragma unroll
       for (int t2 = 0; t2 < T2; ++t2) {
         const int first = key0 + t2 * 32;
-        float16v S = zero16(), dP = zero16();
-        products<2 * DK, PF>([&](int i) { return rr.get(i < DK ? Kt : Vt, t2, i % DK); },
-                             [&](int i, const bf16x8& a) {
-                               if (i < DK) S = mfma(a, Q[i], S);
-                               else dP = mfma(a, G[i - DK], dP);
-                             });
-        in_turn<2 * DK, PF, 1>();
+        float16v S, dP;
+        both(Kt, Vt, t2, S, dP);
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse2)) * (dP[r] - delta);
         if (first + 31 > wave_first) {
@@ -189,7 +215,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
 // buffered; each wave copies one tensor of one unit.  Accumulators for dK and dV take half of the registers that two waves per SIMD leave a
 // wave; at D = 128 V's operands stay in LDS but for the last step's (the two workgroups of a compute unit have 80 KB each).
 template <int D, int UT>
-__global__ void __launch_bounds__(256, 2) k_seq_dkv(SeqParams p) {
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
   constexpr int DT = D / 32, DK = D / 16, ROWS_U = 32 * UT, TILE = 64, TB = ROWS_U * D * 2, PF = 4;
   constexpr bool V_LDS = D == 128;
   constexpr int PV = V_LDS ? 2 : PF;      // (with two operands each, more do not fit)
@@ -445,7 +471,7 @@ SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu) {
 
 hipError_t launch_seq_bwd(SeqParams p, const SeqPlan& s, hipStream_t st) {
   p.nsplit = s.nsplit;
-  return p.d <= 64 ? go<64, 2>(p, st) : go<128, 1>(p, st);
+  return p.d <= 64 ? go<64, 1>(p, st) : go<128, 1>(p, st);
 }
 
 }  // namespace fa

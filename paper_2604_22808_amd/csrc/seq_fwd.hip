@@ -17,7 +17,7 @@ using namespace seq;
 namespace {
 
 template <int D, int NW, int KT>
-__global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
+__global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams p) {
   constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW;
   // One wave has one K and one V tile: the next K tile is requested when the scores are done, the next V tile when the product is, and other
   // workgroups of the compute unit (nine at D = 128) fill the wait.  More waves share two of each.
@@ -287,38 +287,52 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_fwd(SeqParams p) {
   });
 }
 
-// Joins the pieces of a row: out = sum_s 2^(lse_s - top) out_s / sum_s 2^(lse_s - top).  A wave takes one row, a lane two channels.
+// Joins the pieces of a row: out = sum_s 2^(lse_s - top) out_s / sum_s 2^(lse_s - top).  A wave takes one row, a lane two channels; the weights are found one
+// piece a lane and handed round through LDS, so that the loads of the pieces do not wait for each other.
+enum { MAX_PIECES = 256 };
 __global__ void __launch_bounds__(256) k_seq_join(SeqParams p, int piece_keys) {
+  __shared__ float weights[4][MAX_PIECES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
   int seq_i, tile_i;
   seq_slot(p.q_off, p.q_rows, p.nseq, p.group, 4, (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i);
   const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq_i), k = seq_range(p.k_off, p.k_len, p.k_rows, seq_i);
+  if ((int64_t)tile_i * 4 + wave >= (int64_t)q.n * p.group) return;      // (the whole wave; nothing here waits for another wave)
   const Row row = query_row(p, kvh, tile_i * 4 + wave, q.n, k.n);
-  if ((int64_t)tile_i * 4 + wave >= (int64_t)q.n * p.group) return;
   const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
   const int64_t all = (int64_t)p.hq * p.lse_rows;
   const float* lse = p.part + p.nsplit * all * p.d;
   const int n = row.last < 0 ? 0 : row.last / piece_keys + 1;    // pieces that hold keys of this row
-  float top = -INFINITY;
-  for (int s = lane; s < n; s += 64) top = fmaxf(top, lse[s * all + at]);
+  float w[MAX_PIECES / 64], top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < MAX_PIECES / 64; ++i) {
+    w[i] = i * 64 + lane < n ? lse[(i * 64 + lane) * all + at] : -INFINITY;
+    top = fmaxf(top, w[i]);
+  }
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, a = 0.f, b = 0.f;
-  const int c = 2 * lane;
-  for (int s = 0; s < n; ++s) {
-    const float w = __builtin_amdgcn_exp2f(lse[s * all + at] - ref);
-    if (w == 0.f) continue;     // (a piece that the row sees no key of)
-    sum += w;
-    if (c < p.d) {
-      const float2v x = *(const float2v*)(p.part + (s * all + at) * p.d + c);
-      a += w * x[0];
-      b += w * x[1];
-    }
+#pragma unroll
+  for (int i = 0; i < MAX_PIECES / 64; ++i) {
+    const float x = __builtin_amdgcn_exp2f(w[i] - ref);
+    sum += x;
+    weights[wave][i * 64 + lane] = x;
   }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (a wave reads its own weights)
   const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+  const int c = 2 * lane;
   if (c < p.d) {
+    const float* src = p.part + at * p.d + c;
+    float a = 0.f, b = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < n; ++s) {
+      const float2v x = *(const float2v*)(src + s * all * p.d);
+      const float y = weights[wave][s];
+      a += y == 0.f ? 0.f : y * x[0];
+      b += y == 0.f ? 0.f : y * x[1];
+    }
     uint16_t* dst = (uint16_t*)const_cast<char*>(p.o.p) + (int64_t)q.seq * p.o.bs + (int64_t)(q.base + row.token) * p.o.ts + (int64_t)row.head * p.o.hs;
     *(uint32_t*)(dst + c) = pack2(a * inv, b * inv);
   }
@@ -350,7 +364,7 @@ SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu) {
   if (groups > 0 && groups < target / 2 && key_tiles > 1) {
     int64_t n = target / groups;
     if (n > key_tiles) n = key_tiles;
-    if (n > 256) n = 256;
+    if (n > MAX_PIECES) n = MAX_PIECES;
     s.split_tiles = (int)((key_tiles + n - 1) / n);
     s.nsplit = (int)((key_tiles + s.split_tiles - 1) / s.split_tiles);
   }

@@ -7,9 +7,11 @@
 // A wave owns 32 rows - query rows in the forward and dQ kernels, key rows in the dK / dV kernel - as columns of transposed products: S^T = K Q^T
 // leaves a column (a query) on two lanes, whose accumulator registers are then the B operand of O^T += V^T P^T as they stand: step
 // r of v_mfma_f32_32x32x2 takes k = 8 (r / 4) + r % 4 + 4 g from lane half g, which is where register r of the product before it lies.
-// The other side passes through LDS in tiles of 32 rows, widened to fp32.  The sums over keys (dQ) and over queries (dK, dV) are taken by
+// The other side passes through LDS in tiles of 32 rows, widened to fp32.  A workgroup owns 32 rows; its waves take the other side's tiles in turn, each through
+// LDS of its own (no barrier until their sums are joined at the end), with the next tile's loads under way in registers: fp32 products are slow
+// enough that a tile per 32 rows is no burden on the caches, and short sequences still give every wave something to do.  The sums over keys (dQ) and over queries (dK, dV) are taken by
 // different kernels, each by one workgroup in a fixed order, instead of by atomics: 7 products instead of 5, equal bits every time.
-// Bound by the fp32 matrix rate (157 TFLOP/s peak) less the tile loads, which are not overlapped.
+// Bound by the fp32 matrix rate (157 TFLOP/s peak), short sequences by the longest row's chain of tiles.
 #include <hip/hip_runtime.h>
 
 #include "seq_common.h"
@@ -37,6 +39,9 @@ __device__ __forceinline__ float16v zero16() {
   for (int r = 0; r < 16; ++r) z[r] = 0.f;
   return z;
 }
+
+// A wave's LDS writes are done before what follows reads them (LDS of one wave needs no barrier).
+__device__ __forceinline__ void wave_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 template <typename T>
 __device__ __forceinline__ const T* row_of(const HeadsPtr& v, int seq, int64_t row, int head) {
@@ -101,10 +106,11 @@ __device__ __forceinline__ void accumulate(float16v (&acc)[D / 32], const float*
 // tile has masked pairs and values that are not finite, those values are added to the rows that do see them and taken out of the tile.  Rare:
 // tiles without them pay one comparison per value.  `seen(i)`: does the lane's row see row i of the tile.
 template <int D, typename F>
-__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], float* tile, int nn, int g, F&& seen) {
+__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], float* tile, int lane, int g, F&& seen) {
   bool odd = false;
-  for (int i = threadIdx.x; i < TR * D; i += blockDim.x) odd = odd || !(fabsf(tile[i / D * (D + 4) + i % D]) <= 3.4028235e38f);
-  if (!__syncthreads_or(odd)) return;
+  for (int i = lane; i < TR * D; i += 64) odd = odd || !(fabsf(tile[i / D * (D + 4) + i % D]) <= 3.4028235e38f);
+  if (__builtin_amdgcn_ballot_w64(odd) == 0) return;
+#pragma nounroll
   for (int i = 0; i < TR; ++i) {
     const bool s = seen(i);
 #pragma unroll
@@ -115,12 +121,12 @@ __device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], float* tile, 
         if (s && !(fabsf(x) <= 3.4028235e38f)) acc[dt][r] += x;
       }
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < TR * D; i += blockDim.x) {
+  wave_lds();
+  for (int i = lane; i < TR * D; i += 64) {
     float& x = tile[i / D * (D + 4) + i % D];
     if (!(fabsf(x) <= 3.4028235e38f)) x = 0.f;
   }
-  __syncthreads();
+  wave_lds();
 }
 
 // What a query row is: token, head, and the last key it sees.
@@ -135,60 +141,87 @@ __device__ __forceinline__ Row query_row(const SeqParams& p, int kvh, int r, int
   return w;
 }
 
+// 32 rows of the other side on their way into the wave's tile; row(i) gives the address of row i, nullptr where there is none.
 template <typename T, int D>
-__device__ __forceinline__ void load_tile(float* dst, const HeadsPtr& v, int seq, int base, int row0, int n, int head, int d, int vec) {
-  for (int i = threadIdx.x; i < TR * D / 4; i += blockDim.x) {
-    const int r = i / (D / 4), c = i % (D / 4) * 4;
-    const bool live = row0 + r < n;
-    *(float4v*)(dst + r * (D + 4) + c) = chunk(live ? row_of<T>(v, seq, base + row0 + r, head) : nullptr, c, d, live, vec);
+struct Fetch {
+  float4v x[TR * D / 256];
+  template <typename F> __device__ __forceinline__ void load(int lane, int d, int vec, F&& row) {
+#pragma unroll
+    for (int j = 0; j < TR * D / 256; ++j) {
+      const int i = j * 64 + lane, r = i / (D / 4), c = i % (D / 4) * 4;
+      const T* at = row(r);
+      x[j] = chunk(at, c, d, at != nullptr, vec);
+    }
   }
-}
+  __device__ __forceinline__ void store(float* tile, int lane) {
+#pragma unroll
+    for (int j = 0; j < TR * D / 256; ++j) {
+      const int i = j * 64 + lane, r = i / (D / 4), c = i % (D / 4) * 4;
+      *(float4v*)(tile + r * (D + 4) + c) = x[j];
+    }
+  }
+};
 
-template <typename T, int D>
-__device__ __forceinline__ void store_row(T* row, const float16v (&acc)[D / 32], float f, int g, int d) {
+// Waves of a workgroup: by the LDS that their tiles take, and for dK and dV by the registers of two accumulators and two operands.
+template <int D> constexpr int waves() { return D == 64 ? 8 : 4; }
+enum { DKV_WAVES = 4 };
+template <int D> constexpr int tile_floats() { return TR * (D + 4); }
+
+// Adds the waves' accumulators up in the order of the waves, each wave a share of the registers, and hands the sums out: put(register, sum) with
+// register dt * 16 + r.  `weight(w)`: factor of wave w's values (nothing is added where it is 0).  lds holds waves * D * 32 floats.
+template <int D, int NW, typename W, typename P>
+__device__ __forceinline__ void join_waves(const float16v (&acc)[D / 32], float* lds, int wave, int lane, W&& weight, P&& put) {
+  constexpr int N = D / 2;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int c = dt * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-      if (c < d) put(row + c, acc[dt][r] * f);
+    for (int r = 0; r < 16; ++r) lds[(wave * N + dt * 16 + r) * 64 + lane] = acc[dt][r];
+  __syncthreads();
+  for (int i = wave * (N / NW); i < (wave + 1) * (N / NW); ++i) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = weight(w);
+      s += f == 0.f ? 0.f : f * lds[(w * N + i) * 64 + lane];
     }
+    put(i, s);
+  }
 }
-
-// Which tile a workgroup takes: key heads fastest (they share nothing, and go to different XCDs), tiles from the last, so that under the causal
-// mask the longest come first.
-struct Work { int kvh, seq, tile; };
-__device__ __forceinline__ Work work_of(const SeqParams& p, const int32_t* off, int rows, int mult, int tile_rows) {
-  Work w;
-  w.kvh = (int)(blockIdx.x % (unsigned)p.hk);
-  seq_slot(off, rows, p.nseq, mult, tile_rows, p.slots - 1 - (int)(blockIdx.x / (unsigned)p.hk), w.seq, w.tile);
-  return w;
-}
+__device__ __forceinline__ int channel_of(int reg, int g) { return (reg >> 4) * 32 + 8 * ((reg & 15) >> 2) + 4 * g + (reg & 3); }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 1) k_seq_generic_fwd(SeqParams p) {
-  __shared__ float Ks[TR * (D + 4)], Vs[TR * (D + 4)];
+__global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_fwd(SeqParams p) {
+  constexpr int NW = waves<D>(), TF = tile_floats<D>();
+  __shared__ __attribute__((aligned(16))) float tiles[NW][2 * TF];
+  __shared__ float ms[NW][64], ls[NW][64];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
-  const Work w = work_of(p, p.q_off, p.q_rows, p.group, 128);
-  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, w.seq), k = seq_range(p.k_off, p.k_len, p.k_rows, w.seq);
-  if ((int64_t)w.tile * 128 >= (int64_t)q.n * p.group) return;
-  const Row row = query_row(p, w.kvh, w.tile * 128 + wave * 32 + nn, q.n, k.n);
+  const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
+  int seq, tile;
+  if (!seq_query_tile(p, TR, lane, (int)(blockIdx.x / (unsigned)p.hk), seq, tile)) return;
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq), k = seq_range(p.k_off, p.k_len, p.k_rows, seq);
+  if ((int64_t)tile * TR >= (int64_t)q.n * p.group) return;
+  const Row row = query_row(p, kvh, tile * TR + nn, q.n, k.n);
   RowOperand<T, D> Q;
   Q.load(row_of<T>(p.q, q.seq, q.base + row.token, row.head), g, p.d, row.live, p.vec);
-  const int last_row = min(w.tile * 128 + 127, q.n * p.group - 1);
-  const int last = query_row(p, w.kvh, last_row, q.n, k.n).last;    // of the whole tile: the last row sees the most
+  const int last = query_row(p, kvh, min(tile * TR + TR - 1, q.n * p.group - 1), q.n, k.n).last;    // of the tile: its last row sees the most
+  const int first_last = query_row(p, kvh, tile * TR, q.n, k.n).last;
   const float c2 = p.scale * LOG2E;
+  float *Ks = tiles[wave], *Vs = tiles[wave] + TF;
+  Fetch<T, D> fk, fv;
+  auto fetch = [&](int key0) {
+    fk.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.k, k.seq, k.base + key0 + r, kvh) : nullptr; });
+    fv.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.v, k.seq, k.base + key0 + r, kvh) : nullptr; });
+  };
   float16v O[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) O[dt] = zero16();
   float m = -INFINITY, l = 0.f;
-  for (int key0 = 0; key0 <= last; key0 += TR) {
-    __syncthreads();
-    load_tile<T, D>(Ks, p.k, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
-    load_tile<T, D>(Vs, p.v, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
-    __syncthreads();
-    if (p.causal && key0 + TR - 1 > query_row(p, w.kvh, w.tile * 128, q.n, k.n).last)
-      set_aside<D>(O, Vs, nn, g, [&](int i) { return key0 + i <= row.last; });
+  if (wave * TR <= last) fetch(wave * TR);
+  for (int key0 = wave * TR; key0 <= last; key0 += NW * TR) {
+    fk.store(Ks, lane);
+    fv.store(Vs, lane);
+    wave_lds();
+    if (key0 + NW * TR <= last) fetch(key0 + NW * TR);
     float16v S = product<T, D>(Ks, Q, nn, g);
     float mx = -INFINITY;
 #pragma unroll
@@ -199,7 +232,7 @@ __global__ void __launch_bounds__(256, 1) k_seq_generic_fwd(SeqParams p) {
     }
     mx = fmaxf(mx, __shfl_xor(mx, 32));
     const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
-    const float alpha = __builtin_amdgcn_exp2f(m - ref);
+    const float alpha = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - ref);
     m = mn;
     l *= alpha;
 #pragma unroll
@@ -212,24 +245,44 @@ __global__ void __launch_bounds__(256, 1) k_seq_generic_fwd(SeqParams p) {
       S[r] = key <= row.last ? __builtin_amdgcn_exp2f(S[r] - ref) : 0.f;
       l += S[r];
     }
+    if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(O, Vs, lane, g, [&](int i) { return key0 + i <= row.last; });
     accumulate<D>(O, Vs, S, nn, g);
+    wave_lds();
   }
   l += __shfl_xor(l, 32);
-  if (!row.live) return;
-  store_row<T, D>(row_of_out<T>(p.o, q.seq, q.base + row.token, row.head), O, row.last < 0 ? 0.f : 1.f / l, g, p.d);
-  if (p.lse && g == 0)
-    p.lse[(int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)w.seq * p.q_rows) + row.token] = row.last < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+  ms[wave][lane] = m;
+  ls[wave][lane] = l;
+  __syncthreads();
+  float top = -INFINITY, sum = 0.f, w[NW];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) top = fmaxf(top, ms[i][lane]);
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    w[i] = ls[i][lane] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[i][lane] - top);
+    sum += w[i] * ls[i][lane];
+  }
+  T* dst = row_of_out<T>(p.o, q.seq, q.base + row.token, row.head);
+  const float inv = row.last < 0 ? 0.f : 1.f / sum;
+  join_waves<D, NW>(O, tiles[0], wave, lane, [&](int i) { return w[i]; }, [&](int i, float x) {
+    const int c = channel_of(i, g);
+    if (row.live && c < p.d) put(dst + c, x * inv);
+  });
+  if (row.live && p.lse && g == 0 && wave == 0)
+    p.lse[(int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)seq * p.q_rows) + row.token] = row.last < 0 ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 // dQ, and the row sums delta that the other kernel reads.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 1) k_seq_generic_dq(SeqParams p) {
-  __shared__ float Ks[TR * (D + 4)], Vs[TR * (D + 4)];
+__global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dq(SeqParams p) {
+  constexpr int NW = waves<D>(), TF = tile_floats<D>();
+  __shared__ __attribute__((aligned(16))) float tiles[NW][2 * TF];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
-  const Work w = work_of(p, p.q_off, p.q_rows, p.group, 128);
-  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, w.seq), k = seq_range(p.k_off, p.k_len, p.k_rows, w.seq);
-  if ((int64_t)w.tile * 128 >= (int64_t)q.n * p.group) return;
-  const Row row = query_row(p, w.kvh, w.tile * 128 + wave * 32 + nn, q.n, k.n);
+  const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
+  int seq, tile;
+  if (!seq_query_tile(p, TR, lane, (int)(blockIdx.x / (unsigned)p.hk), seq, tile)) return;
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq), k = seq_range(p.k_off, p.k_len, p.k_rows, seq);
+  if ((int64_t)tile * TR >= (int64_t)q.n * p.group) return;
+  const Row row = query_row(p, kvh, tile * TR + nn, q.n, k.n);
   RowOperand<T, D> Q, dO;
   Q.load(row_of<T>(p.q, q.seq, q.base + row.token, row.head), g, p.d, row.live, p.vec);
   dO.load(row_of<T>(p.dout, q.seq, q.base + row.token, row.head), g, p.d, row.live, p.vec);
@@ -244,19 +297,27 @@ __global__ void __launch_bounds__(256, 1) k_seq_generic_dq(SeqParams p) {
     }
     delta += __shfl_xor(delta, 32);
   }
-  const int64_t at = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)w.seq * p.q_rows) + row.token;
-  if (row.live && g == 0) p.delta[at] = delta;
+  const int64_t at = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)seq * p.q_rows) + row.token;
+  if (row.live && g == 0 && wave == 0) p.delta[at] = delta;
   const float lse2 = row.live && row.last >= 0 ? p.lse[at] * LOG2E : 0.f;
-  const int last = query_row(p, w.kvh, min(w.tile * 128 + 127, q.n * p.group - 1), q.n, k.n).last;
+  const int last = query_row(p, kvh, min(tile * TR + TR - 1, q.n * p.group - 1), q.n, k.n).last;
+  const int first_last = query_row(p, kvh, tile * TR, q.n, k.n).last;
   const float c2 = p.scale * LOG2E;
+  float *Ks = tiles[wave], *Vs = tiles[wave] + TF;
+  Fetch<T, D> fk, fv;
+  auto fetch = [&](int key0) {
+    fk.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.k, k.seq, k.base + key0 + r, kvh) : nullptr; });
+    fv.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.v, k.seq, k.base + key0 + r, kvh) : nullptr; });
+  };
   float16v A[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) A[dt] = zero16();
-  for (int key0 = 0; key0 <= last; key0 += TR) {
-    __syncthreads();
-    load_tile<T, D>(Ks, p.k, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
-    load_tile<T, D>(Vs, p.v, k.seq, k.base, key0, k.n, w.kvh, p.d, p.vec);
-    __syncthreads();
+  if (wave * TR <= last) fetch(wave * TR);
+  for (int key0 = wave * TR; key0 <= last; key0 += NW * TR) {
+    fk.store(Ks, lane);
+    fv.store(Vs, lane);
+    wave_lds();
+    if (key0 + NW * TR <= last) fetch(key0 + NW * TR);
     float16v S = product<T, D>(Ks, Q, nn, g);
     const float16v dP = product<T, D>(Vs, dO, nn, g);
 #pragma unroll
@@ -264,88 +325,118 @@ __global__ void __launch_bounds__(256, 1) k_seq_generic_dq(SeqParams p) {
       const int key = key0 + 8 * (r >> 2) + 4 * g + (r & 3);
       S[r] = key <= row.last ? __builtin_amdgcn_exp2f(S[r] * c2 - lse2) * (dP[r] - delta) : 0.f;
     }
-    if (p.causal && key0 + TR - 1 > query_row(p, w.kvh, w.tile * 128, q.n, k.n).last) {
-      set_aside<D>(A, Ks, nn, g, [&](int i) { return key0 + i <= row.last; });
-    }
+    if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(A, Ks, lane, g, [&](int i) { return key0 + i <= row.last; });
     accumulate<D>(A, Ks, S, nn, g);
+    wave_lds();
   }
-  if (row.live) store_row<T, D>(row_of_out<T>(p.dq, q.seq, q.base + row.token, row.head), A, p.scale, g, p.d);
+  __syncthreads();
+  T* dst = row_of_out<T>(p.dq, q.seq, q.base + row.token, row.head);
+  join_waves<D, NW>(A, tiles[0], wave, lane, [](int) { return 1.f; }, [&](int i, float x) {
+    const int c = channel_of(i, g);
+    if (row.live && c < p.d) put(dst + c, x * p.scale);
+  });
 }
 
-// dK and dV of 128 keys, over all query rows of the sequence and group that see any of them.
+// dK and dV of 32 keys, over all query rows of the sequence and group that see any of them.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 1) k_seq_generic_dkv(SeqParams p) {
-  __shared__ float Qs[TR * (D + 4)], Gs[TR * (D + 4)], Ls[TR], Ds[TR];
-  __shared__ int Last[TR];
+__global__ void __launch_bounds__(64 * DKV_WAVES, 1) k_seq_generic_dkv(SeqParams p) {
+  constexpr int NW = DKV_WAVES, TF = tile_floats<D>();
+  constexpr bool AHEAD = D == 64;     // (at D = 128 the registers are full without the next tile's rows)
+  __shared__ __attribute__((aligned(16))) float tiles[NW][2 * TF];
+  __shared__ float Ls[NW][TR], Ds[NW][TR];
+  __shared__ int Last[NW][TR];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
-  const Work w = work_of(p, p.k_off, p.k_rows, 1, 128);
-  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, w.seq), k = seq_range(p.k_off, p.k_len, p.k_rows, w.seq);
-  if (w.tile * 128 >= k.n) return;
-  const int key = w.tile * 128 + wave * 32 + nn;
+  const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
+  int seq, tile;
+  if (!seq_key_tile(p, TR, lane, (int)(blockIdx.x / (unsigned)p.hk), seq, tile)) return;
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq), k = seq_range(p.k_off, p.k_len, p.k_rows, seq);
+  if ((int64_t)tile * TR >= k.n) return;
+  const int key = tile * TR + nn;
   const bool live = key < k.n;
   RowOperand<T, D> K, V;
-  K.load(row_of<T>(p.k, k.seq, k.base + (live ? key : 0), w.kvh), g, p.d, live, p.vec);
-  V.load(row_of<T>(p.v, k.seq, k.base + (live ? key : 0), w.kvh), g, p.d, live, p.vec);
+  K.load(row_of<T>(p.k, k.seq, k.base + (live ? key : 0), kvh), g, p.d, live, p.vec);
+  V.load(row_of<T>(p.v, k.seq, k.base + (live ? key : 0), kvh), g, p.d, live, p.vec);
   float16v dK[D / 32], dV[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) { dK[dt] = zero16(); dV[dt] = zero16(); }
   const float c2 = p.scale * LOG2E;
-  const int rows = q.n * p.group;
+  const int64_t rows = (int64_t)q.n * p.group;
   // the first token that sees the tile's first key
-  int first = p.causal ? w.tile * 128 - (k.n - q.n) : 0;
+  int first = p.causal ? tile * TR - (k.n - q.n) : 0;
   if (first < 0) first = 0;
-  const int last_key = min(w.tile * 128 + 127, k.n - 1);
-  for (int64_t r0 = (int64_t)first * p.group / TR * TR; r0 < rows; r0 += TR) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < TR * D / 4; i += blockDim.x) {
-      const int r = i / (D / 4), c = i % (D / 4) * 4;
-      const Row row = query_row(p, w.kvh, (int)r0 + r, q.n, k.n);
-      *(float4v*)(Qs + r * (D + 4) + c) = chunk(row_of<T>(p.q, q.seq, q.base + row.token, row.head), c, p.d, row.live, p.vec);
-      *(float4v*)(Gs + r * (D + 4) + c) = chunk(row_of<T>(p.dout, q.seq, q.base + row.token, row.head), c, p.d, row.live, p.vec);
-      if (c == 0) {
-        const int64_t at = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)w.seq * p.q_rows) + row.token;
-        Ls[r] = row.live && row.last >= 0 ? p.lse[at] * LOG2E : 0.f;
-        Ds[r] = row.live && row.last >= 0 ? p.delta[at] : 0.f;
-        Last[r] = row.last;
-      }
-    }
-    __syncthreads();
+  const int last_key = min(tile * TR + TR - 1, k.n - 1);
+  float *Qs = tiles[wave], *Gs = tiles[wave] + TF;
+  Fetch<T, D> fq, fg;
+  float lse2 = 0.f, delta = 0.f;
+  int row_last = -1;
+  auto fetch = [&](int r0) {
+    const auto at = [&](const HeadsPtr& v, int r) -> const T* {
+      const Row row = query_row(p, kvh, r0 + r, q.n, k.n);
+      return row.live ? row_of<T>(v, q.seq, q.base + row.token, row.head) : nullptr;
+    };
+    fq.load(lane, p.d, p.vec, [&](int r) { return at(p.q, r); });
+    fg.load(lane, p.d, p.vec, [&](int r) { return at(p.dout, r); });
+    const Row row = query_row(p, kvh, r0 + nn, q.n, k.n);
+    const int64_t i = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)seq * p.q_rows) + row.token;
+    const bool some = row.live && row.last >= 0;
+    lse2 = some ? p.lse[i] * LOG2E : 0.f;
+    delta = some ? p.delta[i] : 0.f;
+    row_last = row.last;
+  };
+  const int64_t start = (int64_t)first * p.group / TR * TR + wave * TR;
+  if (AHEAD && start < rows) fetch((int)start);
+  for (int64_t r0 = start; r0 < rows; r0 += NW * TR) {
+    if (!AHEAD) fetch((int)r0);
+    fq.store(Qs, lane);
+    fg.store(Gs, lane);
+    if (g == 0) { Ls[wave][nn] = lse2; Ds[wave][nn] = delta; Last[wave][nn] = row_last; }
+    wave_lds();
+    if (AHEAD && r0 + NW * TR < rows) fetch((int)(r0 + NW * TR));
     float16v S = product<T, D>(Qs, K, nn, g);
     float16v dP = product<T, D>(Gs, V, nn, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int i = 8 * (r >> 2) + 4 * g + (r & 3);
-      const bool seen = live && key <= Last[i];
-      S[r] = seen ? __builtin_amdgcn_exp2f(S[r] * c2 - Ls[i]) : 0.f;
-      dP[r] = seen ? S[r] * (dP[r] - Ds[i]) : 0.f;
+      const bool seen = live && key <= Last[wave][i];
+      S[r] = seen ? __builtin_amdgcn_exp2f(S[r] * c2 - Ls[wave][i]) : 0.f;
+      dP[r] = seen ? S[r] * (dP[r] - Ds[wave][i]) : 0.f;
     }
-    if (Last[0] < last_key || Last[TR - 1] < last_key) {   // (uniform) some pair is masked: queries before the diagonal, rows behind the last query
-      set_aside<D>(dV, Gs, nn, g, [&](int i) { return live && key <= Last[i]; });
-      set_aside<D>(dK, Qs, nn, g, [&](int i) { return live && key <= Last[i]; });
+    if (Last[wave][0] < last_key || Last[wave][TR - 1] < last_key) {   // some pair is masked: queries before the diagonal, rows behind the last query
+      set_aside<D>(dV, Gs, lane, g, [&](int i) { return live && key <= Last[wave][i]; });
+      set_aside<D>(dK, Qs, lane, g, [&](int i) { return live && key <= Last[wave][i]; });
     }
     accumulate<D>(dV, Gs, S, nn, g);
     accumulate<D>(dK, Qs, dP, nn, g);
+    wave_lds();
   }
-  if (!live) return;
-  store_row<T, D>(row_of_out<T>(p.dk, k.seq, k.base + key, w.kvh), dK, p.scale, g, p.d);
-  store_row<T, D>(row_of_out<T>(p.dv, k.seq, k.base + key, w.kvh), dV, 1.f, g, p.d);
+  __syncthreads();
+  const auto store = [&](const HeadsPtr& v, const float16v (&acc)[D / 32], float f) {
+    T* dst = row_of_out<T>(v, k.seq, k.base + (live ? key : 0), kvh);
+    join_waves<D, NW>(acc, tiles[0], wave, lane, [](int) { return 1.f; }, [&](int i, float x) {
+      const int c = channel_of(i, g);
+      if (live && c < p.d) put(dst + c, x * f);
+    });
+  };
+  store(p.dk, dK, p.scale);
+  __syncthreads();
+  store(p.dv, dV, 1.f);
 }
 
 template <typename T, int D>
 hipError_t fwd(SeqParams p, hipStream_t st) {
-  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 128);
+  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, TR);
   if (p.slots == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_seq_generic_fwd<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((k_seq_generic_fwd<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(64 * waves<D>()), 0, st, p);
   return hipGetLastError();
 }
 template <typename T, int D>
 hipError_t bwd(SeqParams p, hipStream_t st) {
-  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 128);
-  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dq<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
+  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, TR);
+  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dq<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(64 * waves<D>()), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  p.slots = (int)seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 128);
-  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dkv<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
+  p.slots = (int)seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, TR);
+  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dkv<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(64 * DKV_WAVES), 0, st, p);
   return hipGetLastError();
 }
 
