@@ -360,7 +360,7 @@ SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu) {
   const int64_t slots = seq_slots(packed, p.q_rows, p.nseq, p.group, tile_rows), groups = slots * p.hk, key_tiles = ((int64_t)p.k_rows + kt - 1) / kt;
   s.nsplit = 1;
   s.split_tiles = (int)(key_tiles > 0 ? key_tiles : 1);
-  const int64_t target = (int64_t)num_cu * (s.few ? 16 : 4);
+  const int64_t target = (int64_t)num_cu * (s.few ? 16 : 2);
   if (groups > 0 && groups < target / 2 && key_tiles > 1) {
     int64_t n = target / groups;
     if (n > key_tiles) n = key_tiles;
