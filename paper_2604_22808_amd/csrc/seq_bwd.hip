@@ -34,14 +34,21 @@ __device__ __forceinline__ DkvUnits dkv_units(const SeqParams& p, int nq, int nk
   u.all = u.per_head * p.group;
   return u;
 }
-// Units of a piece: the longest sequence's, divided by the number of pieces (an even number of them).
+// Units of a piece (an even number): the longest sequence's divided by the number of pieces, but not less than what leaves `split_tiles` pieces in all.
 __device__ __forceinline__ int dkv_piece_units(const SeqParams& p, int rows_u, int lane) {
   int most = 0;
-  for (int i = lane; i < p.nseq; i += 64) most = max(most, seq_range(p.q_off, p.q_len, p.q_rows, i).n);
+  float all = 0.f;
+  for (int i = lane; i < p.nseq; i += 64) {
+    const int nq = seq_range(p.q_off, p.q_len, p.q_rows, i).n, nk = seq_range(p.k_off, p.k_len, p.k_rows, i).n;
+    most = max(most, nq);
+    all += (float)nq * (p.causal ? fmaxf((float)nk - 0.5f * (float)nq, 0.5f * (float)nk) : (float)nk);
+  }
+  most = lane_max(most);
 #pragma unroll
-  for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o));
+  for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
   const int units = (most + rows_u - 1) / rows_u * p.group;
-  return max(2, ((units + p.nsplit - 1) / p.nsplit + 1) & ~1);
+  const int least = (int)(all * (float)p.hq / (64.f * (float)rows_u * (float)p.split_tiles));
+  return max(max(2, least & ~1), ((units + p.nsplit - 1) / p.nsplit + 1) & ~1);
 }
 
 template <int D, int NW, int KT>
@@ -224,13 +231,13 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
   __shared__ __attribute__((aligned(256))) char Vs[V_LDS ? TILE * VROW : 16];
   __shared__ __attribute__((aligned(256))) float St[2][2][2 * ROWS_U];      // [copy][unit] (lse, delta) of its rows
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6), kw = wave & 1, us = wave >> 1;
-  // key heads fastest, then pieces, then tiles, the longest first
+  // key heads fastest, then tiles, the longest first, then pieces (pieces that do not exist would leave the XCDs that they fall on idle if they were between tiles)
   unsigned id = blockIdx.x;
   const int kvh = (int)(id % (unsigned)p.hk);
   id /= (unsigned)p.hk;
-  const int piece = (int)(id % (unsigned)p.nsplit);
+  const int piece = (int)(id / (unsigned)p.slots);
   int seq_i, tile_i;
-  if (!seq_key_tile(p, TILE, lane, (int)(id / (unsigned)p.nsplit), seq_i, tile_i)) return;
+  if (!seq_key_tile(p, TILE, lane, (int)(id % (unsigned)p.slots), seq_i, tile_i)) return;
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(p.k_off, p.k_len, p.k_rows, seq_i));
@@ -462,7 +469,8 @@ SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu) {
   const int64_t blocks = seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 64) * p.hk;
   const int64_t units = ((int64_t)p.q_rows + 31) / 32 * p.group;      // the most that a tile of keys can have
   s.nsplit = 1;
-  if (p.k_rows > 0 && units >= 32) s.nsplit = blocks >= 4 * num_cu ? 1 : blocks >= 2 * num_cu ? 2 : 4;
+  if (p.k_rows > 0 && units >= 32 && blocks < 4 * num_cu) s.nsplit = 4;
+  s.split_tiles = 8 * num_cu;
   const int64_t stats = ((int64_t)p.hq * p.lse_rows * 8 + 255) / 256 * 256;
   s.part_at = stats;
   s.workspace = stats + (s.nsplit > 1 ? (int64_t)s.nsplit * 2 * p.hk * p.lse_k * p.d * 4 : 0);
@@ -471,6 +479,7 @@ SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu) {
 
 hipError_t launch_seq_bwd(SeqParams p, const SeqPlan& s, hipStream_t st) {
   p.nsplit = s.nsplit;
+  p.split_tiles = s.split_tiles;
   return p.d <= 64 ? go<64, 1>(p, st) : go<128, 1>(p, st);
 }
 

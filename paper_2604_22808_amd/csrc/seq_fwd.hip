@@ -27,14 +27,15 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
   __shared__ __attribute__((aligned(256))) uint16_t Vs[NB][KT * D];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // key heads fastest, then pieces of the keys, then tiles, the longest first
+  // key heads fastest, then tiles, the longest first, then pieces of the keys (pieces that do not exist would leave the XCDs that they fall on idle if they
+  // were between tiles)
   unsigned id = blockIdx.x;
   const int kvh = (int)(id % (unsigned)p.hk);
   id /= (unsigned)p.hk;
-  const int split = (int)(id % (unsigned)p.nsplit);
+  const int split = (int)(id / (unsigned)p.slots), slot = (int)(id % (unsigned)p.slots);
   int seq_i, tile_i;
-  if (ONE) seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, (int)(id / (unsigned)p.nsplit), seq_i, tile_i);
-  else if (!seq_query_tile(p, TILE, lane, (int)(id / (unsigned)p.nsplit), seq_i, tile_i)) return;
+  if (ONE) seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, slot, seq_i, tile_i);
+  else if (!seq_query_tile(p, TILE, lane, slot, seq_i, tile_i)) return;
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(p.k_off, p.k_len, p.k_rows, seq_i));
