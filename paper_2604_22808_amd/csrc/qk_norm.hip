@@ -16,6 +16,7 @@ namespace fa {
 
 typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
 typedef unsigned int uint4v __attribute__((ext_vector_type(4)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 struct Bf16 { uint16_t u; };
@@ -108,9 +109,12 @@ __device__ __forceinline__ Pairs load_pairs(const T* row, const Place<HALF, SCAL
 #pragma unroll
       for (int j = 0; j < 4; ++j) { x.a[j] = __uint_as_float(v[j] << 16); x.b[j] = __uint_as_float(v[j] & 0xffff0000u); }
     } else {
-      const float4v lo = *(const float4v*)(row + pl.ca[0]), hi = *(const float4v*)(row + pl.cb[0]);
-      x.a[0] = lo[0]; x.b[0] = lo[1]; x.a[1] = lo[2]; x.b[1] = lo[3];
-      x.a[2] = hi[0]; x.b[2] = hi[1]; x.a[3] = hi[2]; x.b[3] = hi[3];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2v v = *(const float2v*)(row + pl.ca[0] + 2 * j);
+        x.a[j] = v[0];
+        x.b[j] = v[1];
+      }
     }
   }
   return x;
@@ -127,16 +131,36 @@ __device__ __forceinline__ void store_pairs(T* row, const Place<HALF, SCALAR>& p
   } else if constexpr (sizeof(T) == 2) {
     *(uint4v*)(row + pl.ca[0]) = uint4v{pack_bf16(x.a[0], x.b[0]), pack_bf16(x.a[1], x.b[1]), pack_bf16(x.a[2], x.b[2]), pack_bf16(x.a[3], x.b[3])};
   } else {
-    *(float4v*)(row + pl.ca[0]) = float4v{x.a[0], x.b[0], x.a[1], x.b[1]};
-    *(float4v*)(row + pl.cb[0]) = float4v{x.a[2], x.b[2], x.a[3], x.b[3]};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *(float2v*)(row + pl.ca[0] + 2 * j) = float2v{x.a[j], x.b[j]};
   }
 }
 
+// Sum over the LPR lanes of a head, on all of them.  Lanes of a quad, then of eight and sixteen (mirrored: the other half holds one value), then across.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
 template <int LPR>
 __device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-  for (int o = 1; o < LPR; o <<= 1) x += __shfl_xor(x, o);
+  x += dpp<0xb1>(x);
+  x += dpp<0x4e>(x);
+  if (LPR >= 8) x += dpp<0x141>(x);
+  if (LPR >= 16) x += dpp<0x140>(x);
+  if (LPR >= 32) {
+    const auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
+  if (LPR >= 64) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
   return x;
+}
+// (mean + eps)^-1/2: the instruction is within one step, the scaled argument is a normal number unless mean and eps are both about zero
+__device__ __forceinline__ float inv_norm(float ss, float inv_d, float eps) {
+  const float m = __builtin_fmaf(ss, inv_d, eps);
+  return m < 1e-30f ? 1.f / sqrtf(m) : __builtin_amdgcn_rsqf(m);
 }
 
 // The rotation of a lane's pairs at one token.
@@ -203,20 +227,20 @@ __device__ __forceinline__ Pairs load_weight(const void* w, const Place<HALF, SC
   return x;
 }
 
-// How a launch cuts the work: an item is `tpw` tokens x `64 / LPR * STEPS` heads (one wave).
-struct Items { int tpw, head_groups; uint32_t n; };
+// How a launch cuts the work.  An item (one wave) is a token - or `tpw` tokens, where a token has fewer heads than a wave has rows - and 64 / LPR * STEPS heads of
+// each tensor.  Head groups are slowest: neighbouring waves take neighbouring tokens of the same heads.
+struct Items { int tpw, head_groups; uint32_t n, per_group; };
 enum : int64_t { MAX_ITEMS = (int64_t)1 << 25 };   // a launch has fewer than 2^32 threads
 
 template <typename T, int LPR, bool HALF, bool SCALAR, int STEPS>
 __global__ void __launch_bounds__(256) k_qk(QkParams p, const RotTable t, Items it) {
   constexpr int RPW = 64 / LPR;
   const int lane = threadIdx.x & 63, unit = lane % LPR, hr = lane / LPR;
-  const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
+  const uint32_t item = blockIdx.x * 4u + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (item >= it.n) return;
-  const uint32_t tg = item / (uint32_t)it.head_groups;
-  const int heads = p.heads[0] + p.heads[1];
-  // rows of the wave: several tokens' heads where a token has fewer heads than the wave has rows
-  const int sub = it.tpw > 1 ? hr / heads : 0, h_first = (it.tpw > 1 ? hr - sub * heads : (int)(item % (uint32_t)it.head_groups) * RPW * STEPS + hr);
+  const uint32_t hg = item / it.per_group, tg = item - hg * it.per_group;
+  const int most = p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1];
+  const int sub = it.tpw > 1 ? hr / most : 0, h_base = (int)hg * RPW * STEPS, h_lane = it.tpw > 1 ? hr - sub * most : h_base + hr;
   const int64_t token = (int64_t)tg * it.tpw + sub;
   const int valid_pairs = p.d / 2 - unit * 4;
   const int valid = valid_pairs < 0 ? 0 : valid_pairs > 4 ? 4 : valid_pairs;
@@ -226,46 +250,51 @@ __global__ void __launch_bounds__(256) k_qk(QkParams p, const RotTable t, Items 
   pl.set(unit, t.half);
   const LaneRot lr = lane_rot(t, unit);
 
-  Pairs x[STEPS];
+  // all loads first (a step whose heads do not exist is skipped by the whole wave)
+  Pairs x[2][STEPS];
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int h = h_first + s * RPW;
-    if (live && h < heads) {
-      const int w = h >= p.heads[0];
-      const HeadsPtr& v = p.in[w];
-      x[s] = load_pairs<T, HALF, SCALAR>((const T*)v.p + (int64_t)b * v.bs + (int64_t)n * v.ts + (int64_t)(h - (w ? p.heads[0] : 0)) * v.hs, pl, valid);
-    } else {
+  for (int w = 0; w < 2; ++w)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[s].a[j] = x[s].b[j] = 0.f;
-    }
-  }
-  Pairs wq, wk;
-  if (p.norm) {
-    wq = load_weight<T, HALF, SCALAR>(p.w[0], pl, valid, live);
-    wk = load_weight<T, HALF, SCALAR>(p.w[1], pl, valid, live);
-  }
-  Turn tn;
-  if (t.half > 0) tn = turn_at(p, t, lr, b, n);
-  const float sign = p.inverse ? -1.f : 1.f;
+    for (int s = 0; s < STEPS; ++s) {
+      if (h_base + s * RPW >= p.heads[w]) continue;
+      const int h = h_lane + s * RPW;
+      if (live && h < p.heads[w]) {
+        const HeadsPtr& v = p.in[w];
+        x[w][s] = load_pairs<T, HALF, SCALAR>((const T*)v.p + (int64_t)b * v.bs + (int64_t)n * v.ts + (int64_t)h * v.hs, pl, valid);
+      } else {
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int h = h_first + s * RPW;
-    const int w = h >= p.heads[0];
-    if (p.norm) {
-      float ss = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) ss += x[s].a[j] * x[s].a[j] + x[s].b[j] * x[s].b[j];
-      const float r = 1.f / sqrtf(row_sum<LPR>(ss) / (float)p.d + p.eps);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[s].a[j] *= r * (w ? wk.a[j] : wq.a[j]);
-        x[s].b[j] *= r * (w ? wk.b[j] : wq.b[j]);
+        for (int j = 0; j < 4; ++j) x[w][s].a[j] = x[w][s].b[j] = 0.f;
       }
     }
-    if (live && h < heads) {
-      if (t.half > 0) rotate(x[s], tn, lr, sign);
-      const HeadsPtr& v = p.out[w];
-      store_pairs<T, HALF, SCALAR>((T*)v.p + (int64_t)b * v.bs + (int64_t)n * v.ts + (int64_t)(h - (w ? p.heads[0] : 0)) * v.hs, pl, valid, x[s]);
+  Turn tn;
+  if (t.half > 0) tn = turn_at(p, t, lr, b, n);
+  const float sign = p.inverse ? -1.f : 1.f, inv_d = 1.f / (float)p.d;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    if (h_base >= p.heads[w]) continue;
+    Pairs wt;
+    if (p.norm) wt = load_weight<T, HALF, SCALAR>(p.w[w], pl, valid, live);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      if (h_base + s * RPW >= p.heads[w]) continue;
+      const int h = h_lane + s * RPW;
+      Pairs& y = x[w][s];
+      if (p.norm) {
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ss += y.a[j] * y.a[j] + y.b[j] * y.b[j];
+        const float r = inv_norm(row_sum<LPR>(ss), inv_d, p.eps);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y.a[j] *= r * wt.a[j];
+          y.b[j] *= r * wt.b[j];
+        }
+      }
+      if (live && h < p.heads[w]) {
+        if (t.half > 0) rotate(y, tn, lr, sign);
+        const HeadsPtr& v = p.out[w];
+        store_pairs<T, HALF, SCALAR>((T*)v.p + (int64_t)b * v.bs + (int64_t)n * v.ts + (int64_t)h * v.hs, pl, valid, y);
+      }
     }
   }
 }
@@ -291,10 +320,11 @@ __global__ void __launch_bounds__(256) k_qk_backward(QkParams p, const RotTable 
 #pragma unroll
   for (int j = 0; j < 4; ++j) dw.a[j] = dw.b[j] = 0.f;
   const int sub = it.tpw > 1 ? hr / heads : 0;
+  const float inv_d = 1.f / (float)p.d;
 
   for (uint32_t item = 4u * (blockIdx.x - (which ? first_k : 0)) + wave; item < it.n; item += waves) {
-    const uint32_t tg = item / (uint32_t)it.head_groups;
-    const int h_first = it.tpw > 1 ? hr - sub * heads : (int)(item - tg * (uint32_t)it.head_groups) * RPW * STEPS + hr;
+    const uint32_t hg = item / it.per_group, tg = item - hg * it.per_group;
+    const int h_first = it.tpw > 1 ? hr - sub * heads : (int)hg * RPW * STEPS + hr;
     const int64_t token = (int64_t)tg * it.tpw + sub;
     const bool live = valid > 0 && sub < it.tpw && token < (int64_t)p.batch * p.tokens;
     const int b = live ? (int)(token / p.tokens) : 0, n = live ? (int)(token - (int64_t)b * p.tokens) : 0;
@@ -324,8 +354,8 @@ __global__ void __launch_bounds__(256) k_qk_backward(QkParams p, const RotTable 
       }
       ss = row_sum<LPR>(ss);
       gx = row_sum<LPR>(gx);
-      const float r = 1.f / sqrtf(ss / (float)p.d + p.eps);
-      const float m = r * r * (gx / (float)p.d);
+      const float r = inv_norm(ss, inv_d, p.eps);
+      const float m = r * r * (gx * inv_d);
       if (live && h < heads) {
         Pairs o;
 #pragma unroll
@@ -385,23 +415,25 @@ static Items make_items(int64_t tokens, int heads, int rpw, int steps) {
   Items it;
   it.tpw = heads < rpw ? rpw / heads : 1;
   it.head_groups = it.tpw > 1 ? 1 : (heads + rpw * steps - 1) / (rpw * steps);
-  const int64_t n = (tokens + it.tpw - 1) / it.tpw * it.head_groups;
+  const int64_t groups = (tokens + it.tpw - 1) / it.tpw, n = groups * it.head_groups;
+  it.per_group = groups > 0 && n <= MAX_ITEMS ? (uint32_t)groups : 1u;
   it.n = n <= MAX_ITEMS ? (uint32_t)n : ~0u;
   return it;
 }
 
 template <typename T, int LPR, bool HALF, bool SCALAR, int STEPS>
 static hipError_t fwd_s(const QkParams& p, const RotTable& t, hipStream_t st) {
-  const Items it = make_items((int64_t)p.batch * p.tokens, p.heads[0] + p.heads[1], 64 / LPR, STEPS);
+  const Items it = make_items((int64_t)p.batch * p.tokens, p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1], 64 / LPR, STEPS);
   if (it.n == ~0u) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_qk<T, LPR, HALF, SCALAR, STEPS>), dim3((it.n + 3) / 4), dim3(256), 0, st, p, t, it);
   return hipGetLastError();
 }
 template <typename T, int LPR, bool HALF, bool SCALAR>
 static hipError_t fwd(const QkParams& p, const RotTable& t, int num_cu, hipStream_t st) {
-  // Four steps share a token's sines and have four loads in flight; where that leaves fewer than 8 waves per compute unit, one step per wave.
-  const int64_t rows = (int64_t)p.batch * p.tokens * (p.heads[0] + p.heads[1]);
-  if (p.heads[0] + p.heads[1] <= 64 / LPR || rows < (int64_t)num_cu * 8 * 4 * (64 / LPR)) return fwd_s<T, LPR, HALF, SCALAR, 1>(p, t, st);
+  // Four steps of each tensor share a token's sines and have their loads in flight together; where that leaves fewer than 8 waves per compute unit, one
+  // step per wave.
+  const int64_t tokens = (int64_t)p.batch * p.tokens, most = p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1];
+  if (most <= 64 / LPR || tokens * ((most + 4 * (64 / LPR) - 1) / (4 * (64 / LPR))) < (int64_t)num_cu * 8) return fwd_s<T, LPR, HALF, SCALAR, 1>(p, t, st);
   return fwd_s<T, LPR, HALF, SCALAR, 4>(p, t, st);
 }
 template <typename T, int LPR, bool HALF, bool SCALAR>
@@ -409,7 +441,7 @@ static hipError_t bwd(const QkParams& p, const RotTable& t, float* const dw[2], 
   constexpr int STEPS = 2;
   const int64_t tokens = (int64_t)p.batch * p.tokens;
   const Items iq = make_items(tokens, p.heads[0], 64 / LPR, STEPS);
-  Items ik = {1, 1, 0};
+  Items ik = {1, 1, 0, 1};
   if (p.heads[1] > 0) ik = make_items(tokens, p.heads[1], 64 / LPR, STEPS);
   if (iq.n == ~0u || ik.n == ~0u) return hipErrorInvalidConfiguration;
   // resident blocks, dealt to q and k by their items
