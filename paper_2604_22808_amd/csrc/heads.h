@@ -31,14 +31,14 @@ struct QkParams {
   const void* w[2];
   const int32_t* pos;             // nullptr: from the token index
   int64_t pos_bs;
-  float* part;                    // backward: [blocks][d] partial weight gradients
+  float* part;                    // backward: [blocks][2][d] partial weight gradients
   int32_t batch, tokens, heads[2], d;
   int32_t norm, inverse;
   float eps;
 };
 
 hipError_t launch_qk(const QkParams& p, const RotTable& t, int dtype, int num_cu, hipStream_t st);
-// blocks of the backward launch per tensor; the workspace holds QK_BWD_BLOCKS rows of head_dim floats
+// most blocks of the backward launch; the workspace holds two rows of head_dim floats for each
 enum { QK_BWD_BLOCKS = 1024 };
 hipError_t launch_qk_backward(const QkParams& p, const RotTable& t, int dtype, float* const dw[2], int num_cu, hipStream_t st);
 

@@ -212,7 +212,7 @@ extern "C" freqattn_status freqattn_qk_norm(const freqattn_qk_shape* s, const fr
 }
 
 extern "C" int64_t freqattn_qk_norm_workspace(int32_t head_dim) {
-  return head_dim < 2 || head_dim > 512 ? 0 : (int64_t)QK_BWD_BLOCKS * head_dim * 4;
+  return head_dim < 2 || head_dim > 512 ? 0 : (int64_t)QK_BWD_BLOCKS * 2 * head_dim * 4;
 }
 
 extern "C" freqattn_status freqattn_qk_norm_backward(const freqattn_qk_shape* s, const freqattn_rotary* rot, const int32_t* positions,

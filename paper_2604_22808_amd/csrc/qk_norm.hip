@@ -167,10 +167,11 @@ __device__ __forceinline__ float inv_norm(float ss, float inv_d, float eps) {
 struct Turn { float s[4], c[4]; };
 
 // What a lane knows of its pairs' rotation, fixed for the launch.
-struct LaneRot { uint32_t lo[4], hi[4]; int axis[4]; bool on[4]; };
+struct LaneRot { uint32_t lo[4], hi[4], axis; bool on[4]; };    // axis: a byte each
 
 __device__ __forceinline__ LaneRot lane_rot(const RotTable& t, int unit) {
   LaneRot l;
+  l.axis = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int i = unit * 4 + j;
@@ -178,7 +179,7 @@ __device__ __forceinline__ LaneRot lane_rot(const RotTable& t, int unit) {
     const int at = l.on[j] ? i : 0;
     l.lo[j] = (uint32_t)t.turn[at];
     l.hi[j] = (uint32_t)(t.turn[at] >> 32);
-    l.axis[j] = t.axis[at];
+    l.axis |= (uint32_t)t.axis[at] << (8 * j);
   }
   return l;
 }
@@ -201,7 +202,8 @@ __device__ __forceinline__ Turn turn_at(const QkParams& p, const RotTable& t, co
   Turn r;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const int pos = l.axis[j] == 0 ? at[0] : l.axis[j] == 1 ? at[1] : l.axis[j] == 2 ? at[2] : at[3];
+    const uint32_t axis = l.axis >> (8 * j) & 3u;
+    const int pos = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
     const uint32_t u = __umulhi((uint32_t)pos, l.lo[j]) + (uint32_t)pos * l.hi[j] - (pos < 0 ? l.lo[j] : 0u);
     sincos_turns(u, t.amplitude, r.s[j], r.c[j]);
   }
@@ -217,6 +219,45 @@ __device__ __forceinline__ void rotate(Pairs& x, const Turn& t, const LaneRot& l
       x.b[j] = b * t.c[j] + a * s;
     }
 }
+
+// A lane's pairs as they lie in memory (loads that nothing waits for yet).
+template <typename T, bool HALF, bool SCALAR>
+struct Raw {
+  Pairs x;    // fp32 and single values: as they are
+  __device__ __forceinline__ void load(const T* row, const Place<HALF, SCALAR>& pl, int valid) { x = load_pairs<T, HALF, SCALAR>(row, pl, valid); }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.a[j] = x.b[j] = 0.f;
+  }
+  __device__ __forceinline__ Pairs get() const { return x; }
+};
+template <bool HALF>
+struct Raw<Bf16, HALF, false> {
+  uint4v v;
+  __device__ __forceinline__ void load(const Bf16* row, const Place<HALF, false>& pl, int) {
+    if (HALF) {
+      const uint2v a = *(const uint2v*)(row + pl.ca[0]), b = *(const uint2v*)(row + pl.cb[0]);
+      v = uint4v{a[0], a[1], b[0], b[1]};
+    } else {
+      v = *(const uint4v*)(row + pl.ca[0]);
+    }
+  }
+  __device__ __forceinline__ void zero() { v = uint4v{0u, 0u, 0u, 0u}; }
+  __device__ __forceinline__ Pairs get() const {
+    Pairs x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (HALF) {
+        x.a[j] = __uint_as_float((j & 1) ? (v[j >> 1] & 0xffff0000u) : (v[j >> 1] << 16));
+        x.b[j] = __uint_as_float((j & 1) ? (v[2 + (j >> 1)] & 0xffff0000u) : (v[2 + (j >> 1)] << 16));
+      } else {
+        x.a[j] = __uint_as_float(v[j] << 16);
+        x.b[j] = __uint_as_float(v[j] & 0xffff0000u);
+      }
+    }
+    return x;
+  }
+};
 
 template <typename T, bool HALF, bool SCALAR>
 __device__ __forceinline__ Pairs load_weight(const void* w, const Place<HALF, SCALAR>& pl, int valid, bool live) {
@@ -299,104 +340,135 @@ __global__ void __launch_bounds__(256) k_qk(QkParams p, const RotTable t, Items 
   }
 }
 
-// Backward: the blocks are dealt to the two tensors by `first_k`; a wave walks items of its tensor and keeps its lanes' sums of dw in
-// registers.  A block adds its waves' sums in a fixed order and stores one row of partial sums; k_qk_weights adds the rows.
+// Backward: waves walk items, cut as the forward pass cuts them, and keep their lanes' sums of dw in registers.  A block adds its waves' sums in a fixed order and
+// stores one row of partial sums per tensor; k_qk_weights adds the rows.
 template <typename T, int LPR, bool HALF, bool SCALAR, int STEPS>
-__global__ void __launch_bounds__(256) k_qk_backward(QkParams p, const RotTable t, Items iq, Items ik, int first_k) {
+__global__ void __launch_bounds__(256, 3) k_qk_backward(QkParams p, const RotTable t, Items it) {
   constexpr int RPW = 64 / LPR;
-  const int lane = threadIdx.x & 63, unit = lane % LPR, hr = lane / LPR, wave = threadIdx.x >> 6;
-  const int which = (int)blockIdx.x >= first_k;
-  const Items it = which ? ik : iq;
-  const uint32_t waves = 4u * (which ? gridDim.x - first_k : first_k);
-  const int heads = p.heads[which];
-  const HeadsPtr vx = p.in[which], vy = p.dy[which], vo = p.out[which];
+  const int lane = threadIdx.x & 63, unit = lane % LPR, hr = lane / LPR, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int most = p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1];
   const int valid_pairs = p.d / 2 - unit * 4;
   const int valid = valid_pairs < 0 ? 0 : valid_pairs > 4 ? 4 : valid_pairs;
   Place<HALF, SCALAR> pl;
   pl.set(unit, t.half);
   const LaneRot lr = lane_rot(t, unit);
-  const Pairs w = load_weight<T, HALF, SCALAR>(p.w[which], pl, valid, valid > 0);
-  Pairs dw;
+  Pairs dw[2];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) dw.a[j] = dw.b[j] = 0.f;
-  const int sub = it.tpw > 1 ? hr / heads : 0;
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dw[w].a[j] = dw[w].b[j] = 0.f;
+  const int sub = it.tpw > 1 ? hr / most : 0;
   const float inv_d = 1.f / (float)p.d;
 
-  for (uint32_t item = 4u * (blockIdx.x - (which ? first_k : 0)) + wave; item < it.n; item += waves) {
+  // The rows of the next tensor or item are requested before the present ones are worked on.
+  struct At { int h_base, h_lane, b, n; bool live; };
+  auto place = [&](uint32_t item) {
     const uint32_t hg = item / it.per_group, tg = item - hg * it.per_group;
-    const int h_first = it.tpw > 1 ? hr - sub * heads : (int)hg * RPW * STEPS + hr;
     const int64_t token = (int64_t)tg * it.tpw + sub;
-    const bool live = valid > 0 && sub < it.tpw && token < (int64_t)p.batch * p.tokens;
-    const int b = live ? (int)(token / p.tokens) : 0, n = live ? (int)(token - (int64_t)b * p.tokens) : 0;
-    Pairs x[STEPS], g[STEPS];
+    At at;
+    at.h_base = (int)hg * RPW * STEPS;
+    at.h_lane = it.tpw > 1 ? hr - sub * most : at.h_base + hr;
+    at.live = valid > 0 && sub < it.tpw && token < (int64_t)p.batch * p.tokens;
+    at.b = at.live ? (int)(token / p.tokens) : 0;
+    at.n = at.live ? (int)(token - (int64_t)at.b * p.tokens) : 0;
+    return at;
+  };
+  auto row = [&](const HeadsPtr& v, const At& at, int h) { return (T*)const_cast<char*>(v.p) + (int64_t)at.b * v.bs + (int64_t)at.n * v.ts + (int64_t)h * v.hs; };
+  Raw<T, HALF, SCALAR> rx[2][STEPS], rg[2][STEPS];
+  auto request = [&](const At& at, int w) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      const int h = h_first + s * RPW;
-      if (live && h < heads) {
-        x[s] = load_pairs<T, HALF, SCALAR>((const T*)vx.p + (int64_t)b * vx.bs + (int64_t)n * vx.ts + (int64_t)h * vx.hs, pl, valid);
-        g[s] = load_pairs<T, HALF, SCALAR>((const T*)vy.p + (int64_t)b * vy.bs + (int64_t)n * vy.ts + (int64_t)h * vy.hs, pl, valid);
+      if (at.h_base + s * RPW >= p.heads[w]) continue;
+      const int h = at.h_lane + s * RPW;
+      if (at.live && h < p.heads[w]) {
+        rx[w][s].load(row(p.in[w], at, h), pl, valid);
+        rg[w][s].load(row(p.dy[w], at, h), pl, valid);
       } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[s].a[j] = x[s].b[j] = g[s].a[j] = g[s].b[j] = 0.f;
+        rx[w][s].zero();
+        rg[w][s].zero();
       }
     }
-    Turn tn;
-    if (t.half > 0) tn = turn_at(p, t, lr, b, n);
+  };
+  auto work = [&](const At& at, int w, const Turn& tn) {
+    if (at.h_base >= p.heads[w]) return;
+    const Pairs wt = load_weight<T, HALF, SCALAR>(p.w[w], pl, valid, valid > 0);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      const int h = h_first + s * RPW;
-      if (t.half > 0) rotate(g[s], tn, lr, -1.f);
+      if (at.h_base + s * RPW >= p.heads[w]) continue;
+      const int h = at.h_lane + s * RPW;
+      const Pairs x = rx[w][s].get();
+      Pairs g = rg[w][s].get(), gw;
+      if (t.half > 0) rotate(g, tn, lr, -1.f);
       float ss = 0.f, gx = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        ss += x[s].a[j] * x[s].a[j] + x[s].b[j] * x[s].b[j];
-        gx += g[s].a[j] * w.a[j] * x[s].a[j] + g[s].b[j] * w.b[j] * x[s].b[j];
+        gw.a[j] = g.a[j] * wt.a[j];
+        gw.b[j] = g.b[j] * wt.b[j];
+        ss += x.a[j] * x.a[j] + x.b[j] * x.b[j];
+        gx += gw.a[j] * x.a[j] + gw.b[j] * x.b[j];
       }
       ss = row_sum<LPR>(ss);
       gx = row_sum<LPR>(gx);
       const float r = inv_norm(ss, inv_d, p.eps);
       const float m = r * r * (gx * inv_d);
-      if (live && h < heads) {
+      if (at.live && h < p.heads[w]) {
         Pairs o;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          dw.a[j] += g[s].a[j] * (x[s].a[j] * r);
-          dw.b[j] += g[s].b[j] * (x[s].b[j] * r);
-          o.a[j] = r * (g[s].a[j] * w.a[j] - x[s].a[j] * m);
-          o.b[j] = r * (g[s].b[j] * w.b[j] - x[s].b[j] * m);
+          dw[w].a[j] += g.a[j] * (x.a[j] * r);
+          dw[w].b[j] += g.b[j] * (x.b[j] * r);
+          o.a[j] = r * (gw.a[j] - x.a[j] * m);
+          o.b[j] = r * (gw.b[j] - x.b[j] * m);
         }
-        store_pairs<T, HALF, SCALAR>((T*)vo.p + (int64_t)b * vo.bs + (int64_t)n * vo.ts + (int64_t)h * vo.hs, pl, valid, o);
+        store_pairs<T, HALF, SCALAR>(row(p.out[w], at, h), pl, valid, o);
       }
     }
+  };
+  uint32_t item = 4u * blockIdx.x + wave;
+  At at = {};
+  if (item < it.n) { at = place(item); request(at, 0); }
+  for (; item < it.n; item += 4u * gridDim.x) {
+    const At now = at;
+    request(now, 1);
+    Turn tn;
+    if (t.half > 0) tn = turn_at(p, t, lr, now.b, now.n);
+    work(now, 0, tn);
+    if (item + 4u * gridDim.x < it.n) { at = place(item + 4u * gridDim.x); request(at, 0); }
+    work(now, 1, tn);
   }
   if (!p.part) return;
-  __shared__ float sums[4][8 * LPR];
+  __shared__ float sums[2][4][8 * LPR];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int w = 0; w < 2; ++w)
 #pragma unroll
-    for (int o = LPR; o < 64; o <<= 1) { dw.a[j] += __shfl_xor(dw.a[j], o); dw.b[j] += __shfl_xor(dw.b[j], o); }
-    if (hr == 0) { sums[wave][unit * 8 + j] = dw.a[j]; sums[wave][unit * 8 + 4 + j] = dw.b[j]; }
-  }
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int o = LPR; o < 64; o <<= 1) { dw[w].a[j] += __shfl_xor(dw[w].a[j], o); dw[w].b[j] += __shfl_xor(dw[w].b[j], o); }
+      if (hr == 0) { sums[w][wave][unit * 8 + j] = dw[w].a[j]; sums[w][wave][unit * 8 + 4 + j] = dw[w].b[j]; }
+    }
   __syncthreads();
   // back to channel order: slot unit*8 + j is channel a[j], + 4 its partner b[j]
-  for (int i = threadIdx.x; i < p.d; i += 256) {
+  for (int i = threadIdx.x; i < 2 * p.d; i += 256) {
+    const int w = i >= p.d, c = i - w * p.d;
     int pair, second;
-    if (HALF && i < 2 * t.half) { second = i >= t.half; pair = i - second * t.half; }
-    else if (!HALF || SCALAR) { pair = i >> 1; second = i & 1; }
-    else { pair = (i >> 3) * 4 + (i & 3); second = (i >> 2) & 1; }   // (aligned pieces behind the rotated channels of the HALF layout)
+    if (HALF && c < 2 * t.half) { second = c >= t.half; pair = c - second * t.half; }
+    else if (!HALF || SCALAR) { pair = c >> 1; second = c & 1; }
+    else { pair = (c >> 3) * 4 + (c & 3); second = (c >> 2) & 1; }   // (aligned pieces behind the rotated channels of the HALF layout)
     const int slot = (pair >> 2) * 8 + (pair & 3) + 4 * second;
-    p.part[(int64_t)blockIdx.x * p.d + i] = (sums[0][slot] + sums[1][slot]) + (sums[2][slot] + sums[3][slot]);
+    p.part[(int64_t)blockIdx.x * 2 * p.d + i] = (sums[w][0][slot] + sums[w][1][slot]) + (sums[w][2][slot] + sums[w][3][slot]);
   }
 }
 
-// dw[c] = sum over rows first..last - 1 of the partial sums; a block adds 32 channels, 32 threads a channel.
-__global__ void __launch_bounds__(1024) k_qk_weights(const float* __restrict__ part, int d, int first_k, int blocks, float* dwq, float* dwk) {
+// dw[c] = sum over the blocks' rows; a block adds 32 channels of one tensor, 32 threads a channel.
+__global__ void __launch_bounds__(1024) k_qk_weights(const float* __restrict__ part, int d, int blocks, float* dwq, float* dwk) {
   float* dst = blockIdx.y ? dwk : dwq;
   if (!dst) return;   // (uniform over the block)
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
   float s = 0.f;
-  if (c < d)
-    for (int i = (blockIdx.y ? first_k : 0) + row; i < (blockIdx.y ? blocks : first_k); i += 32) s += part[(int64_t)i * d + c];
+  if (c < d) {
+#pragma unroll 8
+    for (int i = row; i < blocks; i += 32) s += part[((int64_t)i * 2 + blockIdx.y) * d + c];
+  }
   __shared__ float acc[32][33];
   acc[row][threadIdx.x & 31] = s;
   __syncthreads();
@@ -438,30 +510,17 @@ static hipError_t fwd(const QkParams& p, const RotTable& t, int num_cu, hipStrea
 }
 template <typename T, int LPR, bool HALF, bool SCALAR>
 static hipError_t bwd(const QkParams& p, const RotTable& t, float* const dw[2], int num_cu, hipStream_t st) {
-  constexpr int STEPS = 2;
-  const int64_t tokens = (int64_t)p.batch * p.tokens;
-  const Items iq = make_items(tokens, p.heads[0], 64 / LPR, STEPS);
-  Items ik = {1, 1, 0, 1};
-  if (p.heads[1] > 0) ik = make_items(tokens, p.heads[1], 64 / LPR, STEPS);
-  if (iq.n == ~0u || ik.n == ~0u) return hipErrorInvalidConfiguration;
-  // resident blocks, dealt to q and k by their items
-  int64_t total = ((int64_t)iq.n + ik.n + 3) / 4;
-  if (total > 4 * num_cu) total = 4 * num_cu;
-  if (total > QK_BWD_BLOCKS) total = QK_BWD_BLOCKS;
-  if (total < 1) total = 1;
-  int first_k = (int)total, blocks = (int)total;
-  if (ik.n) {
-    if (total < 2) total = 2;
-    first_k = (int)(total * iq.n / ((int64_t)iq.n + ik.n));
-    if (first_k < 1) first_k = 1;
-    if (first_k > total - 1) first_k = (int)total - 1;
-    blocks = (int)total;
-  }
-  hipLaunchKernelGGL((k_qk_backward<T, LPR, HALF, SCALAR, STEPS>), dim3((unsigned)blocks), dim3(256), 0, st, p, t, iq, ik, first_k);
+  constexpr int STEPS = SCALAR ? 1 : sizeof(T) == 2 ? 4 : 2;    // (rows in flight, by the registers that they take)
+  const Items it = make_items((int64_t)p.batch * p.tokens, p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1], 64 / LPR, STEPS);
+  if (it.n == ~0u) return hipErrorInvalidConfiguration;
+  int64_t blocks = ((int64_t)it.n + 3) / 4;     // as many as are resident, at most (see launch bounds)
+  if (blocks > 3 * num_cu) blocks = 3 * num_cu;
+  if (blocks > QK_BWD_BLOCKS) blocks = QK_BWD_BLOCKS;
+  if (blocks < 1) blocks = 1;
+  hipLaunchKernelGGL((k_qk_backward<T, LPR, HALF, SCALAR, STEPS>), dim3((unsigned)blocks), dim3(256), 0, st, p, t, it);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.part) return e;
-  hipLaunchKernelGGL(k_qk_weights, dim3((unsigned)((p.d + 31) / 32), p.heads[1] > 0 ? 2u : 1u), dim3(1024), 0, st, p.part, p.d, first_k, blocks,
-                     dw[0], dw[1]);
+  hipLaunchKernelGGL(k_qk_weights, dim3((unsigned)((p.d + 31) / 32), p.heads[1] > 0 ? 2u : 1u), dim3(1024), 0, st, p.part, p.d, (int)blocks, dw[0], dw[1]);
   return hipGetLastError();
 }
 
