@@ -416,6 +416,18 @@ freqattn_status freqattn_sequence_attention_backward(const freqattn_sequence_sha
                                                      const freqattn_heads* dq, const freqattn_heads* dk, const freqattn_heads* dv,
                                                      void* workspace, int64_t workspace_bytes, void* stream);
 
+/* freqattn_forward from projections as they leave a linear layer: q, k, v are views [batch][N][heads][head_dim] of any strides (one fused tensor, say);
+ * queries and keys get their norms and rotation on the way into the layout of freqattn_forward, values are laid out alike.
+ *   w_q, w_k  DEVICE [head_dim] of the context's dtype or NULL; eps < 0: no norms
+ *   rotary, positions, positions_stride  as in freqattn_qk_norm; rotary NULL: none
+ *   band_cfg, head_alloc, out, stream    as in freqattn_forward; out must not overlap q, k, v
+ * The context keeps three tensors of its shape for this, allocated at the first call (so a call that is captured into a HIP graph comes after an
+ * eager one).  head_dim must be even and at most 512 (EUNSUPPORTED).  Errors as in freqattn_forward and freqattn_qk_norm. */
+freqattn_status freqattn_forward_tokens(freqattn_ctx* ctx, const freqattn_heads* q, const freqattn_heads* k, const freqattn_heads* v,
+                                        const void* w_q, const void* w_k, float eps, const freqattn_rotary* rotary, const int32_t* positions,
+                                        int64_t positions_stride, const freqattn_band_cfg* band_cfg, const int32_t* head_alloc, void* out,
+                                        void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -99,6 +99,7 @@ EXPORTS = {
     "freqattn_workspace_bytes": (C.c_int64, [C.c_void_p]),
     "freqattn_check_range": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.c_void_p]),
     "freqattn_measure_peaks": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_void_p]),
+    "freqattn_forward_tokens": (C.c_int, [_P, _H, _H, _H, _P, _P, C.c_float] + _ROT + [C.POINTER(BandCfg), C.POINTER(C.c_int32), _P, _P]),
     "freqattn_rotary_create": (C.c_int, [C.POINTER(RotaryCfg), C.POINTER(_P)]),
     "freqattn_rotary_destroy": (None, [_P]),
     "freqattn_rotary_frequencies": (C.c_int, [_P, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
@@ -210,6 +211,25 @@ class Context:
         cfg = cfg or self.cfg
         self._check(lib().freqattn_forward(self._h, _ptr(q), _ptr(k), _ptr(v), C.byref(cfg),
                                            ha.ctypes.data_as(C.POINTER(C.c_int32)), _ptr(out), _stream()))
+        return out
+
+    def forward_tokens(self, q, k, v, head_alloc, out, wq=None, wk=None, eps=1e-6, rotary=None, positions=None, cfg=None):
+        """freqattn_forward_tokens: q, k, v [batch, N, heads, head_dim] with adjacent channels (views of a fused projection, say), out as in
+        forward; eps None: no norms."""
+        who = "forward_tokens"
+        self._check_tensors(who, out=out)
+        s = self.shape
+        want = (s.batch, s.T * s.H * s.W, s.heads, s.head_dim)
+        hq, hk, hv = (_heads(who, name, x, out, want) for name, x in (("q", q), ("k", k), ("v", v)))
+        wq, wk = (_vector(who, name, x, out, s.head_dim, out.dtype) for name, x in (("wq", wq), ("wk", wk)))
+        ha = np.ascontiguousarray(head_alloc, dtype=np.int32)
+        if ha.shape != (s.heads,):
+            raise ValueError(f"{who}: head_alloc must hold {s.heads} entries, got shape {ha.shape}")
+        if rotary is not None and isinstance(rotary, Rotary) and rotary.head_dim != s.head_dim:
+            raise ValueError(f"{who}: head_dim {s.head_dim}, the rotary was made for {rotary.head_dim}")
+        rot, at, stride = _positions(who, rotary, positions, want[0], want[1], out)
+        self._check(lib().freqattn_forward_tokens(self._h, hq, hk, hv, wq, wk, -1.0 if eps is None else float(eps), rot, at, stride,
+                                                  C.byref(cfg or self.cfg), ha.ctypes.data_as(C.POINTER(C.c_int32)), _ptr(out), _stream()))
         return out
 
     def forward_projected(self, x, wq, wk, wv, wo, head_alloc, out, cfg=None):

@@ -86,6 +86,7 @@ static void free_all(Ctx* c) {
   F(c->specQ); F(c->specK); F(c->specV); F(c->Y); F(c->tmp0); F(c->tmp1);
   F(c->lowQ); F(c->lowK); F(c->lowV); F(c->Cbuf); F(c->d_stats); F(c->d_range_flag); F(c->d_lists); F(c->d_energy_part);
   F(c->d_tot_part); F(c->d_wsum); F(c->d_vsum_part);
+  F(c->tokQ); F(c->tokK); F(c->tokV);
   F(c->projX); F(c->projZ); F(c->projWq); F(c->projWk); F(c->projWv); F(c->projWo); F(c->proj_ones);
   F(c->projWvN); F(c->projM); F(c->projPool); F(c->projCtmp);
   F(c->d_gemm_prob); F(c->d_gemm_seg);
@@ -1483,6 +1484,52 @@ extern "C" freqattn_status freqattn_forward(freqattn_ctx* c, const void* q, cons
   if (!c) return FREQATTN_EINVAL;
   return guarded(c, "freqattn_forward", [&]() -> freqattn_status {
     return forward_impl(c, q, k, v, band_cfg, head_alloc, out, (hipStream_t)stream, "freqattn_forward");
+  });
+}
+
+// ------------------------------------------------------------------------------------------------ from token-major projections
+extern "C" freqattn_status freqattn_forward_tokens(freqattn_ctx* c, const freqattn_heads* q, const freqattn_heads* k, const freqattn_heads* v,
+                                                   const void* w_q, const void* w_k, float eps, const freqattn_rotary* rotary,
+                                                   const int32_t* positions, int64_t positions_stride, const freqattn_band_cfg* band_cfg,
+                                                   const int32_t* head_alloc, void* out, void* stream) {
+  if (!c) return FREQATTN_EINVAL;
+  const char* who = "freqattn_forward_tokens";
+  return guarded(c, who, [&]() -> freqattn_status {
+    if (!q || !k || !v || !head_alloc) return fail(c, FREQATTN_EINVAL, std::string(who) + ": NULL argument");
+    freqattn_status fs = check_forward_args(c, q->data, k->data, v->data, band_cfg, out, who);
+    if (fs != FREQATTN_OK) return fs;
+    for (int h = 0; h < c->shape.heads; ++h)
+      if (head_alloc[h] < 0 || head_alloc[h] >= (1 << c->nb)) return fail(c, FREQATTN_EINVAL, std::string(who) + ": head_alloc entry out of range");
+    if (c->d % 2 || c->d > 512) return fail(c, FREQATTN_EUNSUPPORTED, std::string(who) + ": head_dim must be even and at most 512");
+    if (eps != eps) return fail(c, FREQATTN_EINVAL, std::string(who) + ": eps must not be NaN");
+    hipStream_t st = (hipStream_t)stream;
+    const size_t bytes = (size_t)c->slices * (size_t)c->N * (size_t)c->d * (c->shape.dtype == FREQATTN_BF16 ? 2 : 4);
+    for (void** p : {&c->tokQ, &c->tokK, &c->tokV})
+      if (!*p) {
+        const hipError_t e = dev_alloc_bytes(*c, p, bytes);
+        if (e != hipSuccess) {
+          (void)hipGetLastError();
+          *p = nullptr;
+          return fail(c, e == hipErrorOutOfMemory ? FREQATTN_ENOMEM : FREQATTN_EHIP, std::string(who) + ": " + hipGetErrorString(e));
+        }
+      }
+    const int64_t nd = c->N * c->d;
+    auto slab = [&](void* p) { return freqattn_heads{p, nd * c->shape.heads, c->d, nd}; };
+    const freqattn_heads hq = slab(c->tokQ), hk = slab(c->tokK), hv = slab(c->tokV);
+    const int B = c->shape.batch, N = (int)c->N, heads = c->shape.heads, dtype = c->shape.dtype;
+    if (eps >= 0.f) {
+      const freqattn_qk_shape s = {B, N, heads, heads, c->d, dtype, eps};
+      fs = freqattn_qk_norm(&s, rotary, positions, positions_stride, q, k, w_q, w_k, &hq, &hk, stream);
+    } else if (rotary) {
+      fs = freqattn_rotary_apply(rotary, dtype, B, N, heads, q, positions, positions_stride, 0, &hq, stream);
+      if (fs == FREQATTN_OK) fs = freqattn_rotary_apply(rotary, dtype, B, N, heads, k, positions, positions_stride, 0, &hk, stream);
+    } else {
+      HIP_TRY(c, copy_heads(dtype, B, N, heads, c->d, *q, hq, st));
+      HIP_TRY(c, copy_heads(dtype, B, N, heads, c->d, *k, hk, st));
+    }
+    if (fs != FREQATTN_OK) return fail(c, fs, std::string(who) + ": " + context_free_error());
+    HIP_TRY(c, copy_heads(dtype, B, N, heads, c->d, *v, hv, st));
+    return forward_impl(c, c->tokQ, c->tokK, c->tokV, band_cfg, head_alloc, out, st, who);
   });
 }
 

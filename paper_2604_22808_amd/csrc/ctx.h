@@ -149,6 +149,7 @@ struct Ctx {
   int64_t timed_steps = 0;                        // timed forwards since timing was switched on
   bool ev_created = false;
 
+  void* tokQ = nullptr; void* tokK = nullptr; void* tokV = nullptr;   // freqattn_forward_tokens: q, k, v in the layout of a forward, allocated at its first call
   // Projected forward (freqattn_forward_projected): buffers allocated at its first call for a model width
   int proj_d_model = 0;
   void* projX = nullptr; void* projZ = nullptr;           // X~ and the projected spectral output, [batch][N][d_model] fp16, band-major rows

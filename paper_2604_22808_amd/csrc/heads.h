@@ -37,6 +37,9 @@ struct QkParams {
   float eps;
 };
 
+// A copy of x into the order of out (heads_api.cpp).
+hipError_t copy_heads(int dtype, int batch, int tokens, int heads, int d, const freqattn_heads& x, const freqattn_heads& out, hipStream_t st);
+
 hipError_t launch_qk(const QkParams& p, const RotTable& t, int dtype, int num_cu, hipStream_t st);
 // most blocks of the backward launch; the workspace holds two rows of head_dim floats for each
 enum { QK_BWD_BLOCKS = 1024 };

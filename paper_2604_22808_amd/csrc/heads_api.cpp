@@ -171,6 +171,17 @@ const RotTable no_rotation = {};
 
 }  // namespace
 
+hipError_t fa::copy_heads(int dtype, int batch, int tokens, int heads, int d, const freqattn_heads& x, const freqattn_heads& out, hipStream_t st) {
+  QkParams p = {};
+  p.batch = batch;
+  p.tokens = tokens;
+  p.heads[0] = heads;
+  p.d = d;
+  p.in[0] = ptr(&x);
+  p.out[0] = ptr(&out);
+  return launch_qk(p, no_rotation, dtype, compute_units(), st);
+}
+
 extern "C" freqattn_status freqattn_rotary_apply(const freqattn_rotary* rot, int32_t dtype, int32_t batch, int32_t tokens, int32_t heads,
                                                  const freqattn_heads* x, const int32_t* positions, int64_t positions_stride, int32_t inverse,
                                                  const freqattn_heads* out, void* stream) {

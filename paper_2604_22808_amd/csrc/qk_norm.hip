@@ -16,7 +16,6 @@ namespace fa {
 
 typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
 typedef unsigned int uint4v __attribute__((ext_vector_type(4)));
-typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 struct Bf16 { uint16_t u; };
@@ -43,7 +42,7 @@ __device__ __forceinline__ void sincos_turns(uint32_t u, float amp, float& s, fl
 }
 
 // The eight channels of a lane, as four pairs (a[j], b[j]).
-struct Pairs { float a[4], b[4]; };
+struct Pairs { float4v a, b; };
 
 // Where a lane's channels lie.  SCALAR: pair by pair, for rows that are not made of aligned pieces; else two pieces of four (HALF) or one of eight.
 template <bool HALF, bool SCALAR>
@@ -66,11 +65,9 @@ struct Place {
 };
 
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
+__device__ __forceinline__ void load4(const T* p, float4v& x) {
   if constexpr (sizeof(T) == 4) {
-    const float4v v = *(const float4v*)p;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = v[j];
+    x = *(const float4v*)p;
   } else {
     const uint2v v = *(const uint2v*)p;
 #pragma unroll
@@ -81,9 +78,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return (uint32_t)narrow<Bf16>(a).u | ((uint32_t)narrow<Bf16>(b).u << 16);
 }
 template <typename T>
-__device__ __forceinline__ void store4(T* p, const float (&x)[4]) {
+__device__ __forceinline__ void store4(T* p, const float4v& x) {
   if constexpr (sizeof(T) == 4) {
-    *(float4v*)p = float4v{x[0], x[1], x[2], x[3]};
+    *(float4v*)p = x;
   } else {
     *(uint2v*)p = uint2v{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
   }
@@ -109,12 +106,9 @@ __device__ __forceinline__ Pairs load_pairs(const T* row, const Place<HALF, SCAL
 #pragma unroll
       for (int j = 0; j < 4; ++j) { x.a[j] = __uint_as_float(v[j] << 16); x.b[j] = __uint_as_float(v[j] & 0xffff0000u); }
     } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2v v = *(const float2v*)(row + pl.ca[0] + 2 * j);
-        x.a[j] = v[0];
-        x.b[j] = v[1];
-      }
+      const float4v lo = *(const float4v*)(row + pl.ca[0]), hi = *(const float4v*)(row + pl.cb[0]);
+      x.a = float4v{lo[0], lo[2], hi[0], hi[2]};
+      x.b = float4v{lo[1], lo[3], hi[1], hi[3]};
     }
   }
   return x;
@@ -131,8 +125,8 @@ __device__ __forceinline__ void store_pairs(T* row, const Place<HALF, SCALAR>& p
   } else if constexpr (sizeof(T) == 2) {
     *(uint4v*)(row + pl.ca[0]) = uint4v{pack_bf16(x.a[0], x.b[0]), pack_bf16(x.a[1], x.b[1]), pack_bf16(x.a[2], x.b[2]), pack_bf16(x.a[3], x.b[3])};
   } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) *(float2v*)(row + pl.ca[0] + 2 * j) = float2v{x.a[j], x.b[j]};
+    *(float4v*)(row + pl.ca[0]) = float4v{x.a[0], x.b[0], x.a[1], x.b[1]};
+    *(float4v*)(row + pl.cb[0]) = float4v{x.a[2], x.b[2], x.a[3], x.b[3]};
   }
 }
 

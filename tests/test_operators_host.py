@@ -170,3 +170,18 @@ def test_binding_refuses_sequences():
             go(**kw)
     with pytest.raises(ValueError, match="lse"):
         B.sequence_attention_backward(q, q, k, k, q, None, q, k, k, q_offsets=off, k_offsets=off)
+
+
+def test_forward_tokens_refuses():
+    ctx = B.Context(1, 2, 64, (4, 8, 8), B.BF16, B.make_cfg(mid_block=16, mid_stride=4, high_window=32, n_summary=4), path=B.PATH_TABLES_ONLY)
+    L, cfg = B.lib(), C.byref(ctx.cfg)
+    ha = (C.c_int32 * 2)(1, 4)
+    go = lambda c=ctx._h, q=H, v=H, alloc=ha, out=32: L.freqattn_forward_tokens(c, q, H, v, None, None, 1e-6, None, None, 0, cfg, alloc, out, None)   # noqa: E731
+    assert go(c=None) == B.EINVAL and go(q=None) == B.EINVAL and go(v=B.Heads(None, 0, 0, 0)) == B.EINVAL and go(alloc=None) == B.EINVAL and go(out=None) == B.EINVAL
+    assert go() == B.EUNSUPPORTED and b"tables-only" in L.freqattn_last_error(ctx._h)
+    q, out = dev(1, 256, 2, 64), dev(1, 2, 256, 64)
+    for kw, match in ((dict(q=dev(1, 2, 256, 64)), "shape"), (dict(out=dev(1, 256, 2, 64)), "shape"), (dict(head_alloc=[1]), "head_alloc"), (dict(wq=dev(32)), "wq"),
+                      (dict(rotary=B.Rotary(32, [32])), "made for"), (dict(positions=dev(256, dtype=torch.int32)), "without a rotary"),
+                      (dict(v=dev(1, 256, 2, 64, dtype=torch.float32)), "dtype")):
+        with pytest.raises(ValueError, match=match):
+            ctx.forward_tokens(**{**dict(q=q, k=q, v=q, head_alloc=[1, 4], out=out), **kw})
