@@ -191,6 +191,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse2)) * (dP[r] - delta);
         if (first + 31 > wave_first) {
+          really_branch();
           const int lim = my_last - first - 4 * g;
 #pragma unroll
           for (int r = 0; r < 16; ++r) S[r] = 8 * (r >> 2) + (r & 3) <= lim ? S[r] : 0.f;
@@ -354,27 +355,33 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
         const bool mask = shift + t2 * 32 < wave_last;
         const int lim = key - shift - t2 * 32 - 4 * g;     // row 8 (r / 4) + 4 g + r % 4 sees the lane's key where that is lim or more
 #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* st = St[buf][us] + 2 * (t2 * 32 + 8 * i + 4 * g);
+          const float4v a = *(const float4v*)st, b = *(const float4v*)(st + 4);
+          const float lse[4] = {a[0], a[2], b[0], b[2]}, del[4] = {a[1], a[3], b[1], b[3]};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = 4 * i + j;
+            S[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse[j]));
+            dP[r] = S[r] * (dP[r] - del[j]);
+          }
+        }
+        if (mask) {
+          really_branch();
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const bool seen = 8 * (r >> 2) + (r & 3) >= lim;
+            S[r] = seen ? S[r] : 0.f;
+            dP[r] = seen ? dP[r] : 0.f;
+          }
+        }
+#pragma unroll
         for (int s2 = 0; s2 < 2; ++s2) {
           uint4v pp, ps;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float* st = St[buf][us] + 2 * (t2 * 32 + 8 * (2 * s2 + i) + 4 * g);
-            const float4v a = *(const float4v*)st, b = *(const float4v*)(st + 4);
-            const float lse[4] = {a[0], a[2], b[0], b[2]}, del[4] = {a[1], a[3], b[1], b[3]};
-            float x[4], y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int r = 8 * s2 + 4 * i + j;
-              x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse[j]));
-              y[j] = x[j] * (dP[r] - del[j]);
-              if (mask) {
-                const bool seen = 8 * (r >> 2) + (r & 3) >= lim;
-                x[j] = seen ? x[j] : 0.f;
-                y[j] = seen ? y[j] : 0.f;
-              }
-            }
-            pp[2 * i] = pack2(x[0], x[1]); pp[2 * i + 1] = pack2(x[2], x[3]);
-            ps[2 * i] = pack2(y[0], y[1]); ps[2 * i + 1] = pack2(y[2], y[3]);
+          for (int j = 0; j < 4; ++j) {
+            pp[j] = pack2(S[8 * s2 + 2 * j], S[8 * s2 + 2 * j + 1]);
+            ps[j] = pack2(dP[8 * s2 + 2 * j], dP[8 * s2 + 2 * j + 1]);
           }
           P[s2] = __builtin_bit_cast(bf16x8, pp);
           dS[s2] = __builtin_bit_cast(bf16x8, ps);

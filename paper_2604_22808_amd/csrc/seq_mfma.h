@@ -52,6 +52,9 @@ __device__ __forceinline__ unsigned lds_address(const uint16_t* p) {
   return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) uint16_t*)p;
 }
 
+// Stands at the start of a branch that is rarely taken: without it the compiler turns a branch of selects into selects for everyone.
+__device__ __forceinline__ void really_branch() { asm volatile(""); }
+
 __device__ __forceinline__ float16v zero16() {
   float16v z;
 #pragma unroll
