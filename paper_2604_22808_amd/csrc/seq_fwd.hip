@@ -183,53 +183,58 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         copy_k(t + 1, 0);
       }
-      // ---- mask, running softmax.  m (in units of log2) is a reference, not the exact maximum: it moves when a score exceeds it by more than
-      // 2^8, so that probabilities stay within [0, 256], exact relative to their sum, and the accumulator is rarely rescaled.
-      constexpr float BUMP = 8.f;
+      // ---- mask, running softmax.  m (in units of log2) is a reference, not the exact maximum.  bf16 has the range of fp32, so a probability above one
+      // loses nothing: the reference stays while a lane's probabilities of the tile add up to less than 2^40 (exact relative to their sum), and most
+      // tiles take no maximum at all.  Where they do not, or the row has no probabilities yet, the tile's maximum becomes the reference.
       if (mask) {
+        really_branch();
         const int lim = my_last - key0 - 4 * g;
 #pragma unroll
         for (int t2 = 0; t2 < T2; ++t2)
 #pragma unroll
           for (int r = 0; r < 16; ++r) S[t2][r] = t2 * 32 + 8 * (r >> 2) + (r & 3) <= lim ? S[t2][r] : -INFINITY;
       }
-      float mc[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      bf16x8 P[T2][2];
+      auto probabilities = [&]() -> float {
+        const float nref = m == -INFINITY ? 0.f : -m;
+        float ls[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t2 = 0; t2 < T2; ++t2)
+        for (int t2 = 0; t2 < T2; ++t2)
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) mc[(r >> 1) & 3] = __builtin_fmaxf(__builtin_fmaxf(mc[(r >> 1) & 3], S[t2][r]), S[t2][r + 1]);
-      const float mx = max_halves(fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3]))) * c2;
-      const bool bump = m == -INFINITY ? mx > -INFINITY : mx > m + BUMP;
-      if (__builtin_amdgcn_ballot_w64(bump) != 0) {
-        const float mn = bump ? mx : m;
+          for (int s2 = 0; s2 < 2; ++s2) {
+            uint4v pk;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j], c2, nref));
+              const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j + 1], c2, nref));
+              ls[j] += a;
+              ls[j] += b;
+              pk[j] = pack2(a, b);
+            }
+            P[t2][s2] = __builtin_bit_cast(bf16x8, pk);
+          }
+        return (ls[0] + ls[1]) + (ls[2] + ls[3]);
+      };
+      float psum = probabilities();
+      if (__builtin_amdgcn_ballot_w64(!(psum < 1.0995116e12f) || !(l > 0.f)) != 0) {   // (also where they are not numbers)
+        float mc[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int t2 = 0; t2 < T2; ++t2)
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) mc[(r >> 1) & 3] = __builtin_fmaxf(__builtin_fmaxf(mc[(r >> 1) & 3], S[t2][r]), S[t2][r + 1]);
+        const float mx = max_halves(fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3]))) * c2;
+        const float mn = fmaxf(m, mx);
         // (a row that saw nothing before has zeros to scale, or what set_aside just added, which 0 would spoil)
-        const float alpha = bump && m != -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
+        const float alpha = mn > m && m != -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
         m = mn;
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
           for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+        psum = probabilities();
       }
-      const float nref = m == -INFINITY ? 0.f : -m;
-      bf16x8 P[T2][2];
-      float ls[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t2 = 0; t2 < T2; ++t2)
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-          uint4v pk;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j], c2, nref));
-            const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j + 1], c2, nref));
-            ls[j] += a;
-            ls[j] += b;
-            pk[j] = pack2(a, b);
-          }
-          P[t2][s2] = __builtin_bit_cast(bf16x8, pk);
-        }
-      l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+      l += psum;
       if (ONE) {
         wait_copies(!more);
         aside();
