@@ -8,6 +8,8 @@
 // Both keep their products transposed as the forward pass does (the owned row on the lane), so that P and dS, rounded to bf16 in the accumulator
 // registers, are the second operand of the products that follow.  k_seq_dq reads K by rows (S) and by columns (dQ), V by rows (dO V^T); k_seq_dkv
 // reads Q and dO both ways.  k_seq_dq goes first and leaves (lse, delta) of every row, lse in units of log2, in the workspace.
+#include <algorithm>
+
 #include "seq_mfma.h"
 
 namespace fa {
@@ -476,7 +478,10 @@ SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu) {
   const int64_t blocks = seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 64) * p.hk;
   const int64_t units = ((int64_t)p.q_rows + 31) / 32 * p.group;      // the most that a tile of keys can have
   s.nsplit = 1;
-  if (p.k_rows > 0 && units >= 32 && blocks < 4 * num_cu) s.nsplit = 4;
+  // Pieces so that there are four workgroups for each compute unit, eight pieces at most.  us of the backward pass with 2 / 4 / 8 pieces (more pieces: shorter chains,
+  // more partial sums): 640 tiles (16 heads x 2500 rows) 176 / 189 / 236, 290 tiles (32 / 4 heads, 4500 rows) 465 / 389 / 381, 64 tiles (8 / 1 heads of 64,
+  // 4096 rows) 343 / 218 / 159.
+  if (p.k_rows > 0 && units >= 32 && blocks < 4 * num_cu) s.nsplit = (int)std::min<int64_t>(8, (4 * num_cu + blocks - 1) / blocks);
   s.split_tiles = 8 * num_cu;
   const int64_t stats = ((int64_t)p.hq * p.lse_rows * 8 + 255) / 256 * 256;
   s.part_at = stats;

@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
 
 // Joins the pieces of a row: out = sum_s 2^(lse_s - top) out_s / sum_s 2^(lse_s - top).  A wave takes one row, a lane two channels; the weights are found one
 // piece a lane and handed round through LDS, so that the loads of the pieces do not wait for each other.
-enum { MAX_PIECES = 256 };
+enum { MAX_PIECES = 64 };
 __global__ void __launch_bounds__(256) k_seq_join(SeqParams p, int piece_keys) {
   __shared__ float weights[4][MAX_PIECES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
