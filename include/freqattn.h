@@ -385,7 +385,8 @@ freqattn_status freqattn_qk_norm_backward(const freqattn_qk_shape* shape, const 
  * A query that sees no key gets zeros, lse -inf, and gives no gradient.  Keys behind what a query sees reach it in no way, whatever they hold
  * (NaN and infinities too).
  * dtype of q, k, v, out: BF16 (products on the matrix cores from bf16 operands, sums and softmax fp32) or F32 (fp32 throughout).  head_dim 1..128.
- * softmax_scale <= 0 selects 1/sqrt(head_dim). */
+ * out must not overlap q, k, v.  softmax_scale <= 0 selects 1/sqrt(head_dim).
+ * BF16 rows that are not whole 16-byte pieces (addresses, strides, head_dim * 2 bytes), or lie 2^27 elements or more apart, take the fp32 kernels: several times slower. */
 typedef struct {
   int32_t sequences, q_heads, kv_heads, head_dim;
   int32_t q_rows, k_rows;

@@ -47,7 +47,10 @@ int compute_units() {
 bool known(int32_t dtype) { return dtype == FREQATTN_F32 || dtype == FREQATTN_BF16; }
 int size_of(int32_t dtype) { return dtype == FREQATTN_F32 ? 4 : 2; }
 
-HeadsPtr ptr(const freqattn_heads* h) { return HeadsPtr{(const char*)h->data, h->batch_stride, h->row_stride, h->head_stride}; }
+// The stride of an axis of one entry says nothing (and must not decide which kernel runs).
+HeadsPtr ptr(const freqattn_heads* h, int64_t batch, int64_t rows, int64_t heads) {
+  return HeadsPtr{(const char*)h->data, batch > 1 ? h->batch_stride : 0, rows > 1 ? h->row_stride : 0, heads > 1 ? h->head_stride : 0};
+}
 bool given(const freqattn_heads* h) { return h && h->data; }
 
 // The largest launch: workgroups of 256 threads, fewer than 2^32 threads.
@@ -177,8 +180,8 @@ hipError_t fa::copy_heads(int dtype, int batch, int tokens, int heads, int d, co
   p.tokens = tokens;
   p.heads[0] = heads;
   p.d = d;
-  p.in[0] = ptr(&x);
-  p.out[0] = ptr(&out);
+  p.in[0] = ptr(&x, batch, tokens, heads);
+  p.out[0] = ptr(&out, batch, tokens, heads);
   return launch_qk(p, no_rotation, dtype, compute_units(), st);
 }
 
@@ -193,8 +196,8 @@ extern "C" freqattn_status freqattn_rotary_apply(const freqattn_rotary* rot, int
     if (fs != FREQATTN_OK) return fs;
     if (batch == 0 || tokens == 0 || heads == 0) return FREQATTN_OK;
     if (!given(x) || !given(out)) return fail(FREQATTN_EINVAL, who, "NULL argument");
-    p.in[0] = ptr(x);
-    p.out[0] = ptr(out);
+    p.in[0] = ptr(x, batch, tokens, heads);
+    p.out[0] = ptr(out, batch, tokens, heads);
     p.inverse = inverse != 0;
     return launched(launch_qk(p, rot->t, dtype, compute_units(), (hipStream_t)stream), who);
   });
@@ -212,8 +215,9 @@ extern "C" freqattn_status freqattn_qk_norm(const freqattn_qk_shape* s, const fr
     if (fs != FREQATTN_OK) return fs;
     if (s->batch == 0 || s->tokens == 0 || s->q_heads + s->k_heads == 0) return FREQATTN_OK;
     if ((s->q_heads && (!given(q) || !given(q_out))) || (s->k_heads && (!given(k) || !given(k_out)))) return fail(FREQATTN_EINVAL, who, "NULL argument");
-    if (s->q_heads) { p.in[0] = ptr(q); p.out[0] = ptr(q_out); }
-    if (s->k_heads) { p.in[1] = ptr(k); p.out[1] = ptr(k_out); }
+    auto at = [&](const freqattn_heads* h, int heads) { return ptr(h, s->batch, s->tokens, heads); };
+    if (s->q_heads) { p.in[0] = at(q, s->q_heads); p.out[0] = at(q_out, s->q_heads); }
+    if (s->k_heads) { p.in[1] = at(k, s->k_heads); p.out[1] = at(k_out, s->k_heads); }
     p.w[0] = w_q;
     p.w[1] = w_k;
     p.norm = 1;
@@ -250,8 +254,9 @@ extern "C" freqattn_status freqattn_qk_norm_backward(const freqattn_qk_shape* s,
       return FREQATTN_OK;
     }
     // (with no rows the sums are still written: zeros)
-    if (any) { p.in[0] = ptr(q); p.dy[0] = ptr(dq_out); p.out[0] = ptr(dq); }
-    if (any && s->k_heads) { p.in[1] = ptr(k); p.dy[1] = ptr(dk_out); p.out[1] = ptr(dk); }
+    auto at = [&](const freqattn_heads* h, int heads) { return ptr(h, s->batch, s->tokens, heads); };
+    if (any) { p.in[0] = at(q, s->q_heads); p.dy[0] = at(dq_out, s->q_heads); p.out[0] = at(dq, s->q_heads); }
+    if (any && s->k_heads) { p.in[1] = at(k, s->k_heads); p.dy[1] = at(dk_out, s->k_heads); p.out[1] = at(dk, s->k_heads); }
     p.w[0] = w_q;
     p.w[1] = w_k;
     p.norm = 1;
@@ -296,9 +301,12 @@ freqattn_status seq_params(const char* who, const freqattn_sequence_shape* s, co
 // Eight rows lie within 2^32 bytes, as one copy of the bf16 kernels takes them.
 bool near(const HeadsPtr& v) { return v.ts >= 0 && v.ts < ((int64_t)1 << 27); }
 
-bool pieces16(const freqattn_heads* h, int size) {
-  return (uintptr_t)h->data % 16 == 0 && h->batch_stride * size % 16 == 0 && h->row_stride * size % 16 == 0 && h->head_stride * size % 16 == 0;
+bool pieces16(const HeadsPtr& v, int size) {
+  return (uintptr_t)v.p % 16 == 0 && v.bs * size % 16 == 0 && v.ts * size % 16 == 0 && v.hs * size % 16 == 0;
 }
+// A tensor of queries or of keys: the batch axis of a packed one is not used.
+HeadsPtr q_ptr(const SeqParams& p, const freqattn_heads* h) { return ptr(h, p.q_off ? 1 : p.nseq, p.q_rows, p.hq); }
+HeadsPtr k_ptr(const SeqParams& p, const freqattn_heads* h) { return ptr(h, p.k_off ? 1 : p.nseq, p.k_rows, p.hk); }
 
 }  // namespace
 
@@ -319,13 +327,13 @@ extern "C" freqattn_status freqattn_sequence_attention(const freqattn_sequence_s
     if (p.lse_rows == 0 || p.nseq == 0) return FREQATTN_OK;
     if (!given(q) || !given(out) || (p.k_rows > 0 && (!given(k) || !given(v)))) return fail(FREQATTN_EINVAL, who, "NULL argument");
     const int size = size_of(s->dtype);
-    p.vec = p.d * size % 16 == 0 && pieces16(q, size) && pieces16(out, size);
-    p.q = ptr(q);
-    p.o = ptr(out);
+    p.q = q_ptr(p, q);
+    p.o = q_ptr(p, out);
+    p.vec = p.d * size % 16 == 0 && pieces16(p.q, size) && pieces16(p.o, size);
     if (p.k_rows > 0) {
-      p.k = ptr(k);
-      p.v = ptr(v);
-      p.vec = p.vec && pieces16(k, size) && pieces16(v, size);
+      p.k = k_ptr(p, k);
+      p.v = k_ptr(p, v);
+      p.vec = p.vec && pieces16(p.k, size) && pieces16(p.v, size);
     }
     p.lse = lse;
     if (s->dtype != FREQATTN_BF16) return launched(launch_seq_generic_fwd(p, s->dtype, (hipStream_t)stream), who);
@@ -363,12 +371,12 @@ extern "C" freqattn_status freqattn_sequence_attention_backward(const freqattn_s
     const int size = size_of(s->dtype);
     p.vec = p.d * size % 16 == 0;
     if (any_q) {
-      p.dout = ptr(dout); p.q = ptr(q); p.o = ptr(out); p.dq = ptr(dq);
-      p.vec = p.vec && pieces16(dout, size) && pieces16(q, size) && pieces16(out, size) && pieces16(dq, size);
+      p.dout = q_ptr(p, dout); p.q = q_ptr(p, q); p.o = q_ptr(p, out); p.dq = q_ptr(p, dq);
+      p.vec = p.vec && pieces16(p.dout, size) && pieces16(p.q, size) && pieces16(p.o, size) && pieces16(p.dq, size);
     }
     if (any_k) {
-      p.k = ptr(k); p.v = ptr(v); p.dk = ptr(dk); p.dv = ptr(dv);
-      p.vec = p.vec && pieces16(k, size) && pieces16(v, size) && pieces16(dk, size) && pieces16(dv, size);
+      p.k = k_ptr(p, k); p.v = k_ptr(p, v); p.dk = k_ptr(p, dk); p.dv = k_ptr(p, dv);
+      p.vec = p.vec && pieces16(p.k, size) && pieces16(p.v, size) && pieces16(p.dk, size) && pieces16(p.dv, size);
     }
     p.lse = const_cast<float*>(lse);
     p.delta = (float*)workspace;

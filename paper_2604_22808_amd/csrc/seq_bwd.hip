@@ -49,7 +49,7 @@ __device__ __forceinline__ int dkv_piece_units(const SeqParams& p, int rows_u, i
 #pragma unroll
   for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
   const int units = (most + rows_u - 1) / rows_u * p.group;
-  const int least = (int)(all * (float)p.hq / (64.f * (float)rows_u * (float)p.split_tiles));
+  const int least = (int)fminf(all * (float)p.hq / (64.f * (float)rows_u * (float)p.split_tiles), 1e9f);
   return max(max(2, least & ~1), ((units + p.nsplit - 1) / p.nsplit + 1) & ~1);
 }
 

@@ -123,6 +123,32 @@ def test_packed_sequences(case, dtype, causal):
     c.check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_sequences_than_lanes(dtype):
+    """100 sequences: short ones (tiles of few rows), and with some long ones among them; packed and batched with lengths."""
+    short = [(7 * i) % 5 for i in range(100)]
+    mixed = [(7 * i) % 5 + (300 if i % 40 == 3 else 0) for i in range(100)]
+    for causal, lengths in ((True, short), (False, mixed), (True, mixed)):
+        c = Call(121, dtype, 4, 2, 64, sum(lengths) + 1, sum(lengths), q_offsets=offsets(*lengths), k_offsets=offsets(*lengths), causal=causal, spoil=True)
+        c.forward()
+        c.backward()
+        c.check()
+    c = Call(122, dtype, 2, 1, 64, 40, 50, batch=70, q_lengths=[i % 41 for i in range(70)], k_lengths=[50 - i % 51 for i in range(70)], causal=True, spoil=True)
+    c.forward()
+    c.backward()
+    c.check()
+
+
+def test_one_head_of_any_stride():
+    """The stride of an axis of one entry is not used: a single head sliced out of rows of 65 channels keeps to the aligned kernels' results."""
+    c = Call(131, "bf16", 1, 1, 64, 200, 200, q_offsets=[0, 200], k_offsets=[0, 200], causal=True)
+    for n, t in c.dev.items():
+        c.dev[n] = torch.as_strided(t, (200, 1, 64), (64, 65, 1))
+    c.forward()
+    c.backward()
+    c.check()
+
+
 @pytest.mark.parametrize("order", ["rows", "heads"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
