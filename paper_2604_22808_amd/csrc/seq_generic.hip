@@ -19,6 +19,7 @@
 namespace fa {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef int int4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
 
@@ -241,8 +242,7 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_fwd(SeqParam
       for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int key = key0 + 8 * (r >> 2) + 4 * g + (r & 3);
-      S[r] = key <= row.last ? __builtin_amdgcn_exp2f(S[r] - ref) : 0.f;
+      S[r] = __builtin_amdgcn_exp2f(S[r] - ref);      // (0 where masked)
       l += S[r];
     }
     if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(O, Vs, lane, g, [&](int i) { return key0 + i <= row.last; });
@@ -323,7 +323,8 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dq(SeqParams
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int key = key0 + 8 * (r >> 2) + 4 * g + (r & 3);
-      S[r] = key <= row.last ? __builtin_amdgcn_exp2f(S[r] * c2 - lse2) * (dP[r] - delta) : 0.f;
+      const float x = __builtin_amdgcn_exp2f(S[r] * c2 - lse2) * (dP[r] - delta);
+      S[r] = key <= row.last ? x : 0.f;
     }
     if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(A, Ks, lane, g, [&](int i) { return key0 + i <= row.last; });
     accumulate<D>(A, Ks, S, nn, g);
@@ -343,8 +344,8 @@ __global__ void __launch_bounds__(64 * DKV_WAVES, 1) k_seq_generic_dkv(SeqParams
   constexpr int NW = DKV_WAVES, TF = tile_floats<D>();
   constexpr bool AHEAD = D == 64;     // (at D = 128 the registers are full without the next tile's rows)
   __shared__ __attribute__((aligned(16))) float tiles[NW][2 * TF];
-  __shared__ float Ls[NW][TR], Ds[NW][TR];
-  __shared__ int Last[NW][TR];
+  __shared__ __attribute__((aligned(16))) float Ls[NW][TR], Ds[NW][TR];
+  __shared__ __attribute__((aligned(16))) int Last[NW][TR];
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
   const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
   int seq, tile;
@@ -369,14 +370,26 @@ __global__ void __launch_bounds__(64 * DKV_WAVES, 1) k_seq_generic_dkv(SeqParams
   Fetch<T, D> fq, fg;
   float lse2 = 0.f, delta = 0.f;
   int row_last = -1;
+  const float per_group = 1.f / (float)p.group;
   auto fetch = [&](int r0) {
+    // tokens of the tile's rows from the first row's: what is left to divide is below group + 32
+    const int t0 = __builtin_amdgcn_readfirstlane((int)((unsigned)r0 / (unsigned)p.group)), rem = r0 - t0 * p.group;
+    const auto row_at = [&](int r) {
+      const int up = (int)(((float)(rem + r) + 0.5f) * per_group);
+      Row w;
+      w.live = r0 + r < rows;
+      w.token = t0 + up;
+      w.head = kvh * p.group + rem + r - up * p.group;
+      w.last = !w.live ? -1 : p.causal ? min(w.token + k.n - q.n, k.n - 1) : k.n - 1;
+      return w;
+    };
     const auto at = [&](const HeadsPtr& v, int r) -> const T* {
-      const Row row = query_row(p, kvh, r0 + r, q.n, k.n);
+      const Row row = row_at(r);
       return row.live ? row_of<T>(v, q.seq, q.base + row.token, row.head) : nullptr;
     };
     fq.load(lane, p.d, p.vec, [&](int r) { return at(p.q, r); });
     fg.load(lane, p.d, p.vec, [&](int r) { return at(p.dout, r); });
-    const Row row = query_row(p, kvh, r0 + nn, q.n, k.n);
+    const Row row = row_at(nn);
     const int64_t i = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)seq * p.q_rows) + row.token;
     const bool some = row.live && row.last >= 0;
     lse2 = some ? p.lse[i] * LOG2E : 0.f;
@@ -395,11 +408,17 @@ __global__ void __launch_bounds__(64 * DKV_WAVES, 1) k_seq_generic_dkv(SeqParams
     float16v S = product<T, D>(Qs, K, nn, g);
     float16v dP = product<T, D>(Gs, V, nn, g);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int i = 8 * (r >> 2) + 4 * g + (r & 3);
-      const bool seen = live && key <= Last[wave][i];
-      S[r] = seen ? __builtin_amdgcn_exp2f(S[r] * c2 - Ls[wave][i]) : 0.f;
-      dP[r] = seen ? S[r] * (dP[r] - Ds[wave][i]) : 0.f;
+    for (int i = 0; i < 4; ++i) {
+      const float4v lse = *(const float4v*)&Ls[wave][8 * i + 4 * g], del = *(const float4v*)&Ds[wave][8 * i + 4 * g];
+      const int4v last = *(const int4v*)&Last[wave][8 * i + 4 * g];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 4 * i + j;
+        const float x = __builtin_amdgcn_exp2f(S[r] * c2 - lse[j]), y = x * (dP[r] - del[j]);
+        const bool seen = live && key <= last[j];
+        S[r] = seen ? x : 0.f;
+        dP[r] = seen ? y : 0.f;
+      }
     }
     if (Last[wave][0] < last_key || Last[wave][TR - 1] < last_key) {   // some pair is masked: queries before the diagonal, rows behind the last query
       set_aside<D>(dV, Gs, lane, g, [&](int i) { return live && key <= Last[wave][i]; });
