@@ -364,7 +364,7 @@ freqattn_status freqattn_qk_norm(const freqattn_qk_shape* shape, const freqattn_
 /* Gradients of freqattn_qk_norm: q, k, w_q, w_k, positions as in that call (q and k before the norm), dq_out, dk_out the gradients of its
  * outputs; dq, dk of dtype (may be dq_out and dk_out themselves); dw_q, dw_k DEVICE fp32 [head_dim], summed over batch, tokens and heads in a fixed
  * order (equal calls give equal bits), NULL: not wanted.  workspace DEVICE, freqattn_qk_norm_workspace(head_dim) bytes, 16-byte aligned, its
- * content does not matter; NULL is fine where both dw are NULL.  EINVAL as above, also a workspace that is too small. */
+ * content does not matter; NULL is fine where both dw are NULL.  EINVAL as above, also q_heads < 1 and a workspace that is too small. */
 int64_t freqattn_qk_norm_workspace(int32_t head_dim);
 freqattn_status freqattn_qk_norm_backward(const freqattn_qk_shape* shape, const freqattn_rotary* rotary, const int32_t* positions, int64_t positions_stride,
                                           const freqattn_heads* q, const freqattn_heads* k, const void* w_q, const void* w_k,

@@ -7,7 +7,8 @@
 // fp32 atomics whose order changes from run to run.
 // Both keep their products transposed as the forward pass does (the owned row on the lane), so that P and dS, rounded to bf16 in the accumulator
 // registers, are the second operand of the products that follow.  k_seq_dq reads K by rows (S) and by columns (dQ), V by rows (dO V^T); k_seq_dkv
-// reads Q and dO both ways.  k_seq_dq goes first and leaves (lse, delta) of every row, lse in units of log2, in the workspace.
+// reads Q and dO both ways.  8 heads x 8192 x 128, full: k_seq_dq 390 us (1.06 PFLOP/s, matrix cores busy 58 % at 1.72 GHz: power), k_seq_dkv 550 (1.0);
+// 16,384 rows x 8 heads of 64: 826 (1.0) and 1161 (0.95), where exponentials take as long as products.  k_seq_dq goes first and leaves (lse, delta) of every row, lse in units of log2, in the workspace.
 #include <algorithm>
 
 #include "seq_mfma.h"
@@ -26,18 +27,19 @@ __device__ __forceinline__ void copy4_any(const void* addr, unsigned dst) {
 }
 
 // The units of query rows that see keys from key0 on: tiles tile0 .. of each head of the group, `per_head` of them.
+constexpr int UNIT = 32;
 struct DkvUnits { int tile0, per_head, all; };
-__device__ __forceinline__ DkvUnits dkv_units(const SeqParams& p, int nq, int nk, int key0, int rows_u) {
+__device__ __forceinline__ DkvUnits dkv_units(const SeqParams& p, int nq, int nk, int key0) {
   int first = p.causal ? key0 - (nk - nq) : 0;     // the first token that sees key0
   if (first < 0) first = 0;
   DkvUnits u;
-  u.tile0 = first / rows_u;
-  u.per_head = nq > first ? (nq + rows_u - 1) / rows_u - u.tile0 : 0;
+  u.tile0 = first / UNIT;
+  u.per_head = nq > first ? (nq + UNIT - 1) / UNIT - u.tile0 : 0;
   u.all = u.per_head * p.group;
   return u;
 }
 // Units of a piece (an even number): the longest sequence's divided by the number of pieces, but not less than what leaves `split_tiles` pieces in all.
-__device__ __forceinline__ int dkv_piece_units(const SeqParams& p, int rows_u, int lane) {
+__device__ __forceinline__ int dkv_piece_units(const SeqParams& p, int lane) {
   int most = 0;
   float all = 0.f;
   for (int i = lane; i < p.nseq; i += 64) {
@@ -48,8 +50,8 @@ __device__ __forceinline__ int dkv_piece_units(const SeqParams& p, int rows_u, i
   most = lane_max(most);
 #pragma unroll
   for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
-  const int units = (most + rows_u - 1) / rows_u * p.group;
-  const int least = (int)fminf(all * (float)p.hq / (64.f * (float)rows_u * (float)p.split_tiles), 1e9f);
+  const int units = (most + UNIT - 1) / UNIT * p.group;
+  const int least = (int)fminf(all * (float)p.hq / (64.f * (float)UNIT * (float)p.split_tiles), 1e9f);
   return max(max(2, least & ~1), ((units + p.nsplit - 1) / p.nsplit + 1) & ~1);
 }
 
@@ -220,13 +222,15 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
   });
 }
 
-// 64 keys, over the query rows of the group's heads that see any of them, in units of 32 * UT rows of one head.  Four waves: two for the keys (32
+// 64 keys, over the query rows of the group's heads that see any of them, in units of 32 rows of one head.  Four waves: two for the keys (32
 // each) times two for the units, which take every other one; at the end the two add their sums up through LDS.  Units come two at a time, double
-// buffered; each wave copies one tensor of one unit.  Accumulators for dK and dV take half of the registers that two waves per SIMD leave a
+// buffered; each wave copies one tensor of one unit.  (128 keys and one unit at a time: half as many, longer workgroups; 16,384 causal rows, 32 / 8 heads of
+// 128: whole backward pass 10.3 ms instead of 7.9.)  Accumulators for dK and dV take half of the registers that two waves per SIMD leave a
 // wave; at D = 128 V's operands stay in LDS but for the last step's (the two workgroups of a compute unit have 80 KB each).
-template <int D, int UT>
+// (D = 64 fits three waves per SIMD: 1482 -> 1359 us for 16,384 rows x 8 heads)
+template <int D>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
-  constexpr int DT = D / 32, DK = D / 16, ROWS_U = 32 * UT, TILE = 64, TB = ROWS_U * D * 2, PF = 4;
+  constexpr int DT = D / 32, DK = D / 16, ROWS_U = UNIT, TILE = 64, TB = ROWS_U * D * 2, PF = 4;
   constexpr bool V_LDS = D == 128;
   constexpr int PV = V_LDS ? 2 : PF;      // (with two operands each, more do not fit)
   constexpr int VS = V_LDS ? DK - 1 : 0, VROW = 2 * (DK - 1) * 16;    // steps of V in LDS, bytes of a row there
@@ -248,8 +252,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
   const int key0 = tile_i * TILE, key = key0 + kw * 32 + nn, chunks = p.d >> 3;
   const bool live = key < k.n;
   const int wave_last = key0 + kw * 32 + 31;     // last key of the wave (dead ones too)
-  const DkvUnits un = dkv_units(p, q.n, k.n, key0, ROWS_U);
-  const int cap = p.nsplit > 1 ? uniform(dkv_piece_units(p, ROWS_U, lane)) : un.all, u0 = piece * cap, u1 = min(u0 + cap, un.all);
+  const DkvUnits un = dkv_units(p, q.n, k.n, key0);
+  const int cap = p.nsplit > 1 ? uniform(dkv_piece_units(p, lane)) : un.all, u0 = piece * cap, u1 = min(u0 + cap, un.all);
   const bool whole_sum = un.all <= cap;
   if (piece > 0 && u0 >= un.all) return;
 
@@ -295,10 +299,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
 #pragma unroll
       for (int i = 0; i < Copy::NI; ++i) cp.part(cur, src_bytes, dst, 0, lane, i, q.n - row0, chunks);
     }
-    if (kw < UT) {
-      const int i = kw * 64 + lane;     // (two floats a row)
+    if (kw == 0) {
+      const int i = lane;     // (two floats a row)
       const int64_t at = (int64_t)(kvh * p.group + head) * p.lse_rows + (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row0;
-      copy4_any(row0 + (i >> 1) < q.n ? p.delta + 2 * at + i : no_row + (i & 1), st_lds + ((buf * 2 + us) * 2 * ROWS_U + kw * 64) * 4);
+      copy4_any(row0 + (i >> 1) < q.n ? p.delta + 2 * at + i : no_row + (i & 1), st_lds + (buf * 2 + us) * 2 * ROWS_U * 4);
     }
   };
 
@@ -337,65 +341,62 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
       if (u < u1) copy_unit(head, tile, buf ^ 1);
       if (!has) continue;
       const unsigned Qt = buf_lds + (buf * 2 + us) * 2 * TB, Gt = Qt + TB;
+      if (shift + 31 < key0 + kw * 32) continue;    // (uniform) no row sees a key of the wave
+      float16v S = zero16(), dP = zero16();
+      products<DK, PF>([&](int i) { return rr.get(Qt, 0, i); }, [&](int i, const bf16x8& a) { S = mfma(a, K[i], S); });
+      in_turn<DK, PF, 1>();
+      struct Two { bf16x8 g, v; };
+      products<DK, PV>([&](int i) {
+                         Two x;
+                         x.g = rr.get(Gt, 0, i);
+                         if (i < VS) x.v = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(i == VS - 1 ? v_last : v_first + 32 * i);
+                         else x.v = V[i - VS];
+                         return x;
+                       },
+                       [&](int i, const Two& a) { dP = mfma(a.g, a.v, dP); });
+      in_turn<DK, PV, V_LDS ? 2 : 1>();
+      bf16x8 P[2], dS[2];
+      const bool mask = shift < wave_last;
+      const int lim = key - shift - 4 * g;     // row 8 (r / 4) + 4 g + r % 4 sees the lane's key where that is lim or more
 #pragma unroll
-      for (int t2 = 0; t2 < UT; ++t2) {
-        if (shift + t2 * 32 + 31 < key0 + kw * 32) continue;    // (uniform) no row sees a key of the wave
-        float16v S = zero16(), dP = zero16();
-        products<DK, PF>([&](int i) { return rr.get(Qt, t2, i); }, [&](int i, const bf16x8& a) { S = mfma(a, K[i], S); });
-        in_turn<DK, PF, 1>();
-        struct Two { bf16x8 g, v; };
-        products<DK, PV>([&](int i) {
-                           Two x;
-                           x.g = rr.get(Gt, t2, i);
-                           if (i < VS) x.v = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(i == VS - 1 ? v_last : v_first + 32 * i);
-                           else x.v = V[i - VS];
-                           return x;
-                         },
-                         [&](int i, const Two& a) { dP = mfma(a.g, a.v, dP); });
-        in_turn<DK, PV, V_LDS ? 2 : 1>();
-        bf16x8 P[2], dS[2];
-        const bool mask = shift + t2 * 32 < wave_last;
-        const int lim = key - shift - t2 * 32 - 4 * g;     // row 8 (r / 4) + 4 g + r % 4 sees the lane's key where that is lim or more
+      for (int i = 0; i < 4; ++i) {
+        const float* st = St[buf][us] + 2 * (8 * i + 4 * g);
+        const float4v a = *(const float4v*)st, b = *(const float4v*)(st + 4);
+        const float lse[4] = {a[0], a[2], b[0], b[2]}, del[4] = {a[1], a[3], b[1], b[3]};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float* st = St[buf][us] + 2 * (t2 * 32 + 8 * i + 4 * g);
-          const float4v a = *(const float4v*)st, b = *(const float4v*)(st + 4);
-          const float lse[4] = {a[0], a[2], b[0], b[2]}, del[4] = {a[1], a[3], b[1], b[3]};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = 4 * i + j;
-            S[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse[j]));
-            dP[r] = S[r] * (dP[r] - del[j]);
-          }
+        for (int j = 0; j < 4; ++j) {
+          const int r = 4 * i + j;
+          S[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse[j]));
+          dP[r] = S[r] * (dP[r] - del[j]);
         }
-        if (mask) {
-          really_branch();
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const bool seen = 8 * (r >> 2) + (r & 3) >= lim;
-            S[r] = seen ? S[r] : 0.f;
-            dP[r] = seen ? dP[r] : 0.f;
-          }
-        }
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-          uint4v pp, ps;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            pp[j] = pack2(S[8 * s2 + 2 * j], S[8 * s2 + 2 * j + 1]);
-            ps[j] = pack2(dP[8 * s2 + 2 * j], dP[8 * s2 + 2 * j + 1]);
-          }
-          P[s2] = __builtin_bit_cast(bf16x8, pp);
-          dS[s2] = __builtin_bit_cast(bf16x8, ps);
-        }
-        products<4 * DT, PF>([&](int i) { return cr.get(i & 1 ? Qt : Gt, (i >> 1) % DT, 2 * t2 + (i >> 1) / DT); },
-                             [&](int i, const bf16x8& a) {
-                               const int dt = (i >> 1) % DT, s2 = (i >> 1) / DT;
-                               if (i & 1) dK[dt] = mfma(a, dS[s2], dK[dt]);
-                               else dV[dt] = mfma(a, P[s2], dV[dt]);
-                             });
-        in_turn<4 * DT, PF, 2>();
       }
+      if (mask) {
+        really_branch();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool seen = 8 * (r >> 2) + (r & 3) >= lim;
+          S[r] = seen ? S[r] : 0.f;
+          dP[r] = seen ? dP[r] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        uint4v pp, ps;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          pp[j] = pack2(S[8 * s2 + 2 * j], S[8 * s2 + 2 * j + 1]);
+          ps[j] = pack2(dP[8 * s2 + 2 * j], dP[8 * s2 + 2 * j + 1]);
+        }
+        P[s2] = __builtin_bit_cast(bf16x8, pp);
+        dS[s2] = __builtin_bit_cast(bf16x8, ps);
+      }
+      products<4 * DT, PF>([&](int i) { return cr.get(i & 1 ? Qt : Gt, (i >> 1) % DT, (i >> 1) / DT); },
+                           [&](int i, const bf16x8& a) {
+                             const int dt = (i >> 1) % DT, s2 = (i >> 1) / DT;
+                             if (i & 1) dK[dt] = mfma(a, dS[s2], dK[dt]);
+                             else dV[dt] = mfma(a, P[s2], dV[dt]);
+                           });
+      in_turn<4 * DT, PF, 2>();
     }
   };
   run(std::false_type{});
@@ -430,14 +431,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
 }
 
 // Adds the pieces of dK and dV up, in their order, where a tile of keys has several.  A wave takes a key, a lane two channels.
-__global__ void __launch_bounds__(256) k_seq_dkv_join(SeqParams p, int rows_u) {
+__global__ void __launch_bounds__(256) k_seq_dkv_join(SeqParams p) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
   int seq_i, tile_i;
   seq_slot(p.k_off, p.k_rows, p.nseq, 1, 4, (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i);
   const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq_i), k = seq_range(p.k_off, p.k_len, p.k_rows, seq_i);
   if ((int64_t)tile_i * 4 + wave >= k.n) return;
-  const int key = tile_i * 4 + wave, cap = dkv_piece_units(p, rows_u, lane), all = dkv_units(p, q.n, k.n, key / 64 * 64, rows_u).all;
+  const int key = tile_i * 4 + wave, cap = dkv_piece_units(p, lane), all = dkv_units(p, q.n, k.n, key / 64 * 64).all;
   const int c = 2 * lane;
   if (all <= cap || c >= p.d) return;
   const int64_t rows = (int64_t)p.hk * p.lse_k, at = (int64_t)kvh * p.lse_k + (p.k_off ? (int64_t)k.base : (int64_t)seq_i * p.k_rows) + key;
@@ -454,7 +455,7 @@ __global__ void __launch_bounds__(256) k_seq_dkv_join(SeqParams p, int rows_u) {
   }
 }
 
-template <int D, int UT>
+template <int D>
 hipError_t go(SeqParams p, hipStream_t st) {
   p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 128);
   if (p.slots > 0) hipLaunchKernelGGL((k_seq_dq<D, 4, 64>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(256), 0, st, p);
@@ -462,11 +463,11 @@ hipError_t go(SeqParams p, hipStream_t st) {
   if (e != hipSuccess) return e;
   p.slots = (int)seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 64);
   if (p.slots == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_seq_dkv<D, UT>), dim3((unsigned)p.slots * (unsigned)p.nsplit * (unsigned)p.hk), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((k_seq_dkv<D>), dim3((unsigned)p.slots * (unsigned)p.nsplit * (unsigned)p.hk), dim3(256), 0, st, p);
   e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const int64_t slots = seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, 4);
-  hipLaunchKernelGGL(k_seq_dkv_join, dim3((unsigned)(slots * p.hk)), dim3(256), 0, st, p, 32 * UT);
+  hipLaunchKernelGGL(k_seq_dkv_join, dim3((unsigned)(slots * p.hk)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
@@ -492,7 +493,7 @@ SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu) {
 hipError_t launch_seq_bwd(SeqParams p, const SeqPlan& s, hipStream_t st) {
   p.nsplit = s.nsplit;
   p.split_tiles = s.split_tiles;
-  return p.d <= 64 ? go<64, 1>(p, st) : go<128, 1>(p, st);
+  return p.d <= 64 ? go<64>(p, st) : go<128>(p, st);
 }
 
 }  // namespace fa

@@ -8,6 +8,10 @@
 //
 // Few rows (a token of each of some sequences): tiles of 32 rows, one wave a workgroup, and the keys are cut into pieces of `split_tiles` tiles
 // that run as workgroups of their own; their normalised results and log sums are joined by k_seq_join.
+//
+// Bound: long rows by the matrix cores at the clock that power leaves them (32,768 causal rows, 4 / 1 heads of 128: 1.04 ms, 1.06 PFLOP/s, busy 51 % at
+// 1.74 GHz), at head_dim 64 as much by the exponentials (16,384 rows x 8 heads: 0.68 ms, 0.81 PFLOP/s); few rows by memory (32 tokens against caches
+// of 200 to 16,384 rows, 32 / 8 heads of 128: 217 us, 4.9 TB/s).
 #include "seq_mfma.h"
 
 namespace fa {
@@ -16,6 +20,7 @@ using namespace seq;
 
 namespace {
 
+// (D = 64 fits three waves per SIMD: 720 -> 691 us for 16,384 rows x 8 heads)
 template <int D, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams p) {
   constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW;
@@ -359,13 +364,17 @@ constexpr int FEW_KT = 32, MANY_KT = 64;
 SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu) {
   SeqPlan s;
   const bool packed = p.q_off != nullptr;
-  // rows of an average sequence and key head
+  // By the rows of an average sequence and key head: more than 32 would take several one-wave tiles, each reading all keys.
   const int64_t all = (int64_t)p.q_rows * p.group, mean = packed ? (p.nseq ? all / p.nseq : 0) : all;
   s.few = mean <= 32;
   const int tile_rows = s.few ? 32 : 128, kt = s.few ? FEW_KT : MANY_KT;
   const int64_t slots = seq_slots(packed, p.q_rows, p.nseq, p.group, tile_rows), groups = slots * p.hk, key_tiles = ((int64_t)p.k_rows + kt - 1) / kt;
   s.nsplit = 1;
   s.split_tiles = (int)(key_tiles > 0 ? key_tiles : 1);
+  // Few rows: 16 one-wave workgroups for each compute unit (nine are resident); with 8 a batch whose caches are filled to an eighth of their rows is left with
+  // too few (32 tokens, 2000 of 16,384 rows: 73 us instead of 47), full ones gain 2 %.  Many rows: two workgroups for each where there is less than one; with
+  // four where there are less than two, joining costs more than the shorter chains give (16 heads x 2500 rows 64 us instead of 70, 4 sequences of 64
+  // rows against 4096 keys 36 instead of 48).
   const int64_t target = (int64_t)num_cu * (s.few ? 16 : 2);
   if (groups > 0 && groups < target / 2 && key_tiles > 1) {
     int64_t n = target / groups;
