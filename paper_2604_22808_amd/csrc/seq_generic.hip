@@ -8,11 +8,11 @@
 // leaves a column (a query) on two lanes, whose accumulator registers are then the B operand of O^T += V^T P^T as they stand: step
 // r of v_mfma_f32_32x32x2 takes k = 8 (r / 4) + r % 4 + 4 g from lane half g, which is where register r of the product before it lies.
 // The other side passes through LDS in tiles of 32 rows, widened to fp32.  A workgroup owns 32 rows; its waves take the other side's tiles in turn, each through
-// LDS of its own (no barrier until their sums are joined at the end), with the next tile's loads under way in registers: fp32 products are slow
+// LDS of its own (no barrier until their sums are joined at the end), in the forward and dQ kernels with the next tile's loads under way in registers: fp32 products are slow
 // enough that a tile per 32 rows is no burden on the caches, and short sequences still give every wave something to do.  The sums over keys (dQ) and over queries (dK, dV) are taken by
 // different kernels, each by one workgroup in a fixed order, instead of by atomics: 7 products instead of 5, equal bits every time.
 // Bound by the fp32 matrix rate (157 TFLOP/s peak), short sequences by the longest row's chain of tiles
-// (three sequences of 701, 333 and 100 rows, 6 / 3 heads of 48: forward 29 us, dQ 35, dK and dV 89).
+// (three sequences of 701, 333 and 100 rows, 6 / 3 heads of 48: forward 29 us, dQ 35, dK and dV 70; with four waves and the next rows in registers dK and dV took 89).
 #include <hip/hip_runtime.h>
 
 #include "seq_common.h"
@@ -164,9 +164,8 @@ struct Fetch {
   }
 };
 
-// Waves of a workgroup: by the LDS that their tiles take, and for dK and dV by the registers of two accumulators and two operands.
+// Waves of a workgroup, by the LDS that their tiles take.
 template <int D> constexpr int waves() { return D == 64 ? 8 : 4; }
-enum { DKV_WAVES = 4 };
 template <int D> constexpr int tile_floats() { return TR * (D + 4); }
 
 // Adds the waves' accumulators up in the order of the waves, each wave a share of the registers, and hands the sums out: put(register, sum) with
@@ -341,9 +340,8 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dq(SeqParams
 
 // dK and dV of 32 keys, over all query rows of the sequence and group that see any of them.
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * DKV_WAVES, 1) k_seq_generic_dkv(SeqParams p) {
-  constexpr int NW = DKV_WAVES, TF = tile_floats<D>();
-  constexpr bool AHEAD = D == 64;     // (at D = 128 the registers are full without the next tile's rows)
+__global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dkv(SeqParams p) {
+  constexpr int NW = waves<D>(), TF = tile_floats<D>();
   __shared__ __attribute__((aligned(16))) float tiles[NW][2 * TF];
   __shared__ __attribute__((aligned(16))) float Ls[NW][TR], Ds[NW][TR];
   __shared__ __attribute__((aligned(16))) int Last[NW][TR];
@@ -368,9 +366,6 @@ __global__ void __launch_bounds__(64 * DKV_WAVES, 1) k_seq_generic_dkv(SeqParams
   if (first < 0) first = 0;
   const int last_key = min(tile * TR + TR - 1, k.n - 1);
   float *Qs = tiles[wave], *Gs = tiles[wave] + TF;
-  Fetch<T, D> fq, fg;
-  float lse2 = 0.f, delta = 0.f;
-  int row_last = -1;
   const float per_group = 1.f / (float)p.group;
   auto fetch = [&](int r0) {
     // tokens of the tile's rows from the first row's: what is left to divide is below group + 32
@@ -388,24 +383,24 @@ __global__ void __launch_bounds__(64 * DKV_WAVES, 1) k_seq_generic_dkv(SeqParams
       const Row row = row_at(r);
       return row.live ? row_of<T>(v, q.seq, q.base + row.token, row.head) : nullptr;
     };
-    fq.load(lane, p.d, p.vec, [&](int r) { return at(p.q, r); });
-    fg.load(lane, p.d, p.vec, [&](int r) { return at(p.dout, r); });
+    Fetch<T, D> f;
+    f.load(lane, p.d, p.vec, [&](int r) { return at(p.q, r); });
+    f.store(Qs, lane);
+    f.load(lane, p.d, p.vec, [&](int r) { return at(p.dout, r); });
+    f.store(Gs, lane);
     const Row row = row_at(nn);
     const int64_t i = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)seq * p.q_rows) + row.token;
     const bool some = row.live && row.last >= 0;
-    lse2 = some ? p.lse[i] * LOG2E : 0.f;
-    delta = some ? p.delta[i] : 0.f;
-    row_last = row.last;
+    if (g == 0) {
+      Ls[wave][nn] = some ? p.lse[i] * LOG2E : 0.f;
+      Ds[wave][nn] = some ? p.delta[i] : 0.f;
+      Last[wave][nn] = row.last;
+    }
   };
   const int64_t start = (int64_t)first * p.group / TR * TR + wave * TR;
-  if (AHEAD && start < rows) fetch((int)start);
   for (int64_t r0 = start; r0 < rows; r0 += NW * TR) {
-    if (!AHEAD) fetch((int)r0);
-    fq.store(Qs, lane);
-    fg.store(Gs, lane);
-    if (g == 0) { Ls[wave][nn] = lse2; Ds[wave][nn] = delta; Last[wave][nn] = row_last; }
+    fetch((int)r0);      // (the registers are full without the next tile's rows; the other waves fill the wait)
     wave_lds();
-    if (AHEAD && r0 + NW * TR < rows) fetch((int)(r0 + NW * TR));
     float16v S = product<T, D>(Qs, K, nn, g);
     float16v dP = product<T, D>(Gs, V, nn, g);
 #pragma unroll
@@ -456,7 +451,7 @@ hipError_t bwd(SeqParams p, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   p.slots = (int)seq_slots(p.k_off != nullptr, p.k_rows, p.nseq, 1, TR);
-  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dkv<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(64 * DKV_WAVES), 0, st, p);
+  if (p.slots > 0) hipLaunchKernelGGL((k_seq_generic_dkv<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(64 * waves<D>()), 0, st, p);
   return hipGetLastError();
 }
 
