@@ -277,11 +277,11 @@ __global__ void __launch_bounds__(256) k_qk(QkParams p, const RotTable t, Items 
   const uint32_t hg = item / it.per_group, tg = item - hg * it.per_group;
   const int most = p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1];
   const int sub = it.tpw > 1 ? hr / most : 0, h_base = (int)hg * RPW * STEPS, h_lane = it.tpw > 1 ? hr - sub * most : h_base + hr;
-  const int64_t token = (int64_t)tg * it.tpw + sub;
+  const uint32_t token = tg * (uint32_t)it.tpw + (uint32_t)sub;    // (2^25 items of at most 64 tokens)
   const int valid_pairs = p.d / 2 - unit * 4;
   const int valid = valid_pairs < 0 ? 0 : valid_pairs > 4 ? 4 : valid_pairs;
-  const bool live = valid > 0 && sub < it.tpw && token < (int64_t)p.batch * p.tokens;
-  const int b = live ? (int)(token / p.tokens) : 0, n = live ? (int)(token - (int64_t)b * p.tokens) : 0;
+  const bool live = valid > 0 && sub < it.tpw && token < (uint32_t)p.batch * (uint32_t)p.tokens;
+  const int b = live ? (int)(token / (uint32_t)p.tokens) : 0, n = live ? (int)(token - (uint32_t)b * (uint32_t)p.tokens) : 0;
   Place<HALF, SCALAR> pl;
   pl.set(unit, t.half);
   const LaneRot lr = lane_rot(t, unit);
@@ -359,13 +359,13 @@ __global__ void __launch_bounds__(256, 3) k_qk_backward(QkParams p, const RotTab
   struct At { int h_base, h_lane, b, n; bool live; };
   auto place = [&](uint32_t item) {
     const uint32_t hg = item / it.per_group, tg = item - hg * it.per_group;
-    const int64_t token = (int64_t)tg * it.tpw + sub;
+    const uint32_t token = tg * (uint32_t)it.tpw + (uint32_t)sub;
     At at;
     at.h_base = (int)hg * RPW * STEPS;
     at.h_lane = it.tpw > 1 ? hr - sub * most : at.h_base + hr;
-    at.live = valid > 0 && sub < it.tpw && token < (int64_t)p.batch * p.tokens;
-    at.b = at.live ? (int)(token / p.tokens) : 0;
-    at.n = at.live ? (int)(token - (int64_t)at.b * p.tokens) : 0;
+    at.live = valid > 0 && sub < it.tpw && token < (uint32_t)p.batch * (uint32_t)p.tokens;
+    at.b = at.live ? (int)(token / (uint32_t)p.tokens) : 0;
+    at.n = at.live ? (int)(token - (uint32_t)at.b * (uint32_t)p.tokens) : 0;
     return at;
   };
   auto row = [&](const HeadsPtr& v, const At& at, int h) { return (T*)const_cast<char*>(v.p) + (int64_t)at.b * v.bs + (int64_t)at.n * v.ts + (int64_t)h * v.hs; };
