@@ -18,8 +18,8 @@ SOURCES = ["mfma_wh_0.hip", "mfma_wh_1.hip", "mfma_wh_2.hip", "mfma_wh_3.hip", "
            "heads_api.cpp", "qk_norm.hip", "seq_generic.hip", "seq_fwd.hip", "seq_bwd.hip"]
 
 
-# Kernels that keep rows requested steps ahead in registers: a spilled register's reload would wait behind all of them.
-NO_SCRATCH = ("mfma_wh_0.hip", "mfma_wh_1.hip", "mfma_wh_2.hip", "mfma_wh_3.hip")
+# Kernels that keep rows requested steps ahead in registers, or copies into LDS under way: a spilled register's reload would wait behind all of them.
+NO_SCRATCH = ("mfma_wh_0.hip", "mfma_wh_1.hip", "mfma_wh_2.hip", "mfma_wh_3.hip", "seq_fwd.hip", "seq_bwd.hip")
 
 
 def hipcc() -> str:
