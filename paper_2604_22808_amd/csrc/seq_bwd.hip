@@ -153,17 +153,19 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
                          });
     in_turn<2 * DK, PF, 1>();
   };
-  if (tiles == 1) {
-    // Rows of few keys have large gradients, and the rounding of out to bf16 is a share of them: up to KT keys, delta is summed from the probabilities
+  if (tiles == 1 || tiles == 2) {
+    // Rows of few keys have large gradients, and the rounding of out to bf16 is a share of them: up to two tiles of keys, delta is summed from the probabilities
     // themselves, sum_j P_j (dO V^T)_j, instead.  (Over n keys out is smaller than v by sqrt(n), and its rounding with it.)
     copy_tile(0, 0);
+    if (tiles == 2) copy_tile(1, 1);
     arrived();
     float sum = 0.f;
 #pragma nounroll
-    for (int t2 = 0; t2 < T2; ++t2) {
+    for (int i = 0; i < tiles * T2; ++i) {
+      const int buf = i / T2, t2 = i % T2;
       float16v S, dP;
-      both(k_lds, v_lds, t2, S, dP);
-      const int lim = row.last - t2 * 32 - 4 * g;
+      both(k_lds + buf * TB, v_lds + buf * TB, t2, S, dP);
+      const int lim = row.last - i * 32 - 4 * g;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], c2, -lse2)) * dP[r];
