@@ -358,8 +358,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
                        [&](int i, const Two& a) { dP = mfma(a.g, a.v, dP); });
       in_turn<DK, PV, V_LDS ? 2 : 1>();
       bf16x8 P[2], dS[2];
-      const bool mask = shift < wave_last;
-      const int lim = key - shift - 4 * g;     // row 8 (r / 4) + 4 g + r % 4 sees the lane's key where that is lim or more
+      // row 8 (r / 4) + 4 g + r % 4 of the unit sees the lane's key where that is lim or more, and exists where it is less than rows (zeros of rows that do not
+      // exist times an infinity of the key would be NaN)
+      const bool mask = shift < wave_last || row0 + ROWS_U > q.n;
+      const int lim = key - shift - 4 * g, rows = q.n - row0 - 4 * g;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float* st = St[buf][us] + 2 * (8 * i + 4 * g);
@@ -376,7 +378,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
         really_branch();
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const bool seen = 8 * (r >> 2) + (r & 3) >= lim;
+          const bool seen = 8 * (r >> 2) + (r & 3) >= lim && 8 * (r >> 2) + (r & 3) < rows;
           S[r] = seen ? S[r] : 0.f;
           dP[r] = seen ? dP[r] : 0.f;
         }

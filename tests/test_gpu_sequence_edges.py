@@ -1,0 +1,53 @@
+"""Attention over sequences where values are not finite, very large, or cancel: what a pair that is seen, or not seen, gives."""
+import math
+
+import pytest
+import torch
+
+from tests.test_gpu_sequence_attention import Call
+
+pytestmark = pytest.mark.gpu
+N, AT = 300, 150
+
+
+def pair_of_calls(seed, dtype, n=N, heads=2, kv_heads=1, d=64, causal=True, **change):
+    """Two calls of the same inputs; `change` [name: function of the tensor] is made in both, so that it can make scores one-sided."""
+    out = []
+    for _ in range(2):
+        c = Call(seed, dtype, heads, kv_heads, d, n, n, q_offsets=[0, n], k_offsets=[0, n], causal=causal)
+        for name, f in change.items():
+            c.dev[name].copy_(f(c.dev[name]))
+        out.append(c)
+    return out
+
+
+def positive(channel):
+    def f(t):
+        t = t.clone()
+        t[..., channel] = t[..., channel].abs() + 0.5
+        return t
+    return f
+
+
+def run(*calls):
+    for c in calls:
+        c.forward()
+        c.backward()
+
+
+def same(a, b, what):
+    assert torch.equal(a, b), (what, float((a.float() - b.float()).abs().nan_to_num(1e30).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_key_without_probability_gets_no_gradient(dtype):
+    """Channel 5 of one key is -inf and of all queries positive: its scores are -inf, its probabilities zero, as they are exactly where that channel is -1e5
+    (scores thousands below the row's others).  Out, lse, dk and dv keep their bits, also where the queries do not fill their last tile."""
+    clean, bad = pair_of_calls(200, dtype, causal=False, q=positive(5))
+    clean.dev["k"][AT, :, 5] = -1e5
+    bad.dev["k"][AT, :, 5] = -math.inf
+    run(clean, bad)
+    for n in ("out", "dk", "dv"):
+        same(bad.out[n], clean.out[n], n)
+    same(bad.lse, clean.lse, "lse")
+    assert float(bad.out["dk"][AT].abs().sum()) == 0 and float(bad.out["dv"][AT].abs().sum()) == 0
