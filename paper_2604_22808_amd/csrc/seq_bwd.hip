@@ -186,9 +186,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
     for (int t = 0; t < tiles; ++t, arrived()) {
       const int buf = t & 1, key0 = t * KT;
       const unsigned Kt = k_lds + buf * TB, Vt = v_lds + buf * TB;
-      if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, BOTH>(A, Ks[buf], g, [&](int i) { return row.live && key0 + i <= row.last; });
       if (t + 1 < tiles) copy_tile(t + 1, buf ^ 1);
-      if (key0 > wave_last) continue;
+      if (!careful.value && key0 > wave_last) continue;     // (set_aside needs every wave; all pairs of such a wave are masked below)
 #pragma unroll
       for (int t2 = 0; t2 < T2; ++t2) {
         const int first = key0 + t2 * 32;
@@ -210,6 +209,9 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
           for (int j = 0; j < 4; ++j) pk[j] = pack2(S[s2 * 8 + 2 * j], S[s2 * 8 + 2 * j + 1]);
           dS[s2] = __builtin_bit_cast(bf16x8, pk);
         }
+        // (the scores need K as it is)
+        if (careful.value && key0 + KT - 1 > wg_first)
+          set_aside<D, 32, BOTH>(A, Ks[buf] + t2 * 32 * D, g, [&](int i) { return row.live && first + i <= row.last; });
         products<2 * DT, PF>([&](int i) { return cr.get(Kt, i % DT, 2 * t2 + i / DT); },
                              [&](int i, const bf16x8& a) { A[i % DT] = mfma(a, dS[i / DT], A[i % DT]); });
         in_turn<2 * DT, PF, 2>();
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
   cp.set(src_bytes, 0, lane);
   const char* src0 = src.p + 2 * ((int64_t)q.seq * src.bs + (int64_t)q.base * src.ts + (int64_t)kvh * p.group * src.hs);
   const unsigned buf_lds = lds_address(Buf[0][0][0]), st_lds = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) float*)St[0][0];
-  auto copy_unit = [&](int head, int tile, int buf) {
+  auto copy_unit = [&](auto careful, int head, int tile, int buf) {
     const int row0 = tile * ROWS_U;
     auto cur = cp.begin(src0 + 2 * ((int64_t)row0 * src.ts + (int64_t)head * src.hs), src_bytes, 0);
     const unsigned dst = buf_lds + ((buf * 2 + us) * 2 + kw) * TB;
@@ -302,7 +304,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
       for (int i = 0; i < Copy::NI; ++i) cp.part(cur, src_bytes, dst, 0, lane, i, q.n - row0, chunks);
     }
     if (kw == 0) {
-      const int i = lane;     // (two floats a row)
+      int i = lane;     // (two floats a row)
+      if (careful.value) asm volatile("" : "+v"(i));     // (addresses made anew each time: the second pass has no registers to keep them)
       const int64_t at = (int64_t)(kvh * p.group + head) * p.lse_rows + (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row0;
       copy4_any(row0 + (i >> 1) < q.n ? p.delta + 2 * at + i : no_row + (i & 1), st_lds + (buf * 2 + us) * 2 * ROWS_U * 4);
     }
@@ -324,26 +327,17 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __syncthreads();
     };
-    if (u < u1) copy_unit(head, tile, 0);
+    if (u < u1) copy_unit(careful, head, tile, 0);
     next_units();
     for (int t = u0; t < u1; t += 2, next_units()) {
       const int buf = ((t - u0) >> 1) & 1, row0 = tile * ROWS_U;
-      const bool has = u < u1;                                     // (the last unit may be the other waves' alone)
+      bool idle = u >= u1;                                         // (the last unit may be the other waves' alone)
       const int shift = p.causal ? row0 + k.n - q.n : 1 << 29;     // the last key that row i of the unit sees is shift + i
-      if (careful.value) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          if (t + w >= u1) continue;
-          auto seen = [&](int i) { return w == us && live && row0 + i < q.n && key <= shift + i; };
-          set_aside<D, ROWS_U, BOTH>(dV, Buf[buf][w][1], g, seen);
-          set_aside<D, ROWS_U, BOTH>(dK, Buf[buf][w][0], g, seen);
-        }
-      }
       if (un.all > 0) advance();
-      if (u < u1) copy_unit(head, tile, buf ^ 1);
-      if (!has) continue;
+      if (u < u1) copy_unit(careful, head, tile, buf ^ 1);
+      idle = idle || shift + 31 < key0 + kw * 32;                  // (uniform) no row sees a key of the wave
+      if (!careful.value && idle) continue;
       const unsigned Qt = buf_lds + (buf * 2 + us) * 2 * TB, Gt = Qt + TB;
-      if (shift + 31 < key0 + kw * 32) continue;    // (uniform) no row sees a key of the wave
       float16v S = zero16(), dP = zero16();
       products<DK, PF>([&](int i) { return rr.get(Qt, 0, i); }, [&](int i, const bf16x8& a) { S = mfma(a, K[i], S); });
       in_turn<DK, PF, 1>();
@@ -393,6 +387,16 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
         }
         P[s2] = __builtin_bit_cast(bf16x8, pp);
         dS[s2] = __builtin_bit_cast(bf16x8, ps);
+      }
+      if (careful.value) {     // (every wave is here, and the scores need Q and dO as they are)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          if (t + w >= u1) continue;
+          auto seen = [&](int i) { return w == us && live && row0 + i < q.n && key <= shift + i; };
+          set_aside<D, ROWS_U, BOTH>(dV, Buf[buf][w][1], g, seen);
+          set_aside<D, ROWS_U, BOTH>(dK, Buf[buf][w][0], g, seen);
+        }
+        if (idle) continue;
       }
       products<4 * DT, PF>([&](int i) { return cr.get(i & 1 ? Qt : Gt, (i >> 1) % DT, (i >> 1) / DT); },
                            [&](int i, const bf16x8& a) {

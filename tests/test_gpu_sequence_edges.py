@@ -51,3 +51,42 @@ def test_a_key_without_probability_gets_no_gradient(dtype):
         same(bad.out[n], clean.out[n], n)
     same(bad.lse, clean.lse, "lse")
     assert float(bad.out["dk"][AT].abs().sum()) == 0 and float(bad.out["dv"][AT].abs().sum()) == 0
+
+
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_seen_key_with_an_infinite_channel(dtype, causal):
+    """As above: everything keeps its bits but channel 5 of dq, which is not finite for the rows that see the key."""
+    clean, bad = pair_of_calls(201, dtype, causal=causal, q=positive(5))
+    clean.dev["k"][AT, :, 5] = -1e5
+    bad.dev["k"][AT, :, 5] = -math.inf
+    run(clean, bad)
+    first = AT if causal else 0
+    dq, want = bad.out["dq"].clone(), clean.out["dq"].clone()
+    assert not bool(torch.isfinite(dq[first:, :, 5]).any())
+    dq[first:, :, 5] = want[first:, :, 5] = 0
+    same(dq, want, "dq")
+    for n in ("out", "dk", "dv"):
+        same(bad.out[n], clean.out[n], n)
+    same(bad.lse, clean.lse, "lse")
+    assert bool(torch.isfinite(want.float()).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_infinite_gradient_of_a_row(dtype):
+    """Channel 3 of one row of dout is +inf and that channel of v positive: the row's dP and delta are +inf, its dS is NaN.  dv gets +inf in that channel from every key that
+    the row sees, dk is NaN there, and keys that it does not see keep their bits."""
+    clean, bad = pair_of_calls(202, dtype, v=positive(3))
+    bad.dev["dout"][AT, 1, 3] = math.inf
+    run(clean, bad)
+    seen = AT + 1
+    assert bool(torch.isnan(bad.out["dk"][:seen]).all())
+    dv, want = bad.out["dv"].clone(), clean.out["dv"].clone()
+    assert bool((dv[:seen, :, 3] == math.inf).all())
+    dv[:seen, :, 3] = want[:seen, :, 3] = 0
+    same(dv, want, "dv")
+    same(bad.out["dk"][seen:], clean.out["dk"][seen:], "dk")
+    assert bool(torch.isnan(bad.out["dq"][AT, 1]).all())
+    rest = torch.ones(N, 2, dtype=torch.bool)
+    rest[AT, 1] = False
+    same(bad.out["dq"][rest], clean.out["dq"][rest], "dq")
