@@ -209,9 +209,9 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
           for (int j = 0; j < 4; ++j) pk[j] = pack2(S[s2 * 8 + 2 * j], S[s2 * 8 + 2 * j + 1]);
           dS[s2] = __builtin_bit_cast(bf16x8, pk);
         }
-        // (the scores need K as it is)
+        // (the scores need K as it is.  A key that is not finite has scores of +inf or NaN, and the row's sums are NaN anyway, or -inf: its dS is zero)
         if (careful.value && key0 + KT - 1 > wg_first)
-          set_aside<D, 32, BOTH>(A, Ks[buf] + t2 * 32 * D, g, [&](int i) { return row.live && first + i <= row.last; });
+          set_aside<D, BOTH>(A, Ks[buf] + t2 * 32 * D, g, ~0u, [&](int i) { return row.live && first + i <= row.last; });
         products<2 * DT, PF>([&](int i) { return cr.get(Kt, i % DT, 2 * t2 + i / DT); },
                              [&](int i, const bf16x8& a) { A[i % DT] = mfma(a, dS[i / DT], A[i % DT]); });
         in_turn<2 * DT, PF, 2>();
@@ -389,12 +389,13 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) k_seq_dkv(SeqParams p) {
         dS[s2] = __builtin_bit_cast(bf16x8, ps);
       }
       if (careful.value) {     // (every wave is here, and the scores need Q and dO as they are)
+        const uint32_t none = row_bits(g, [&](int r) { return !(P[r >> 3][r & 7] != (__bf16)0.f); });
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           if (t + w >= u1) continue;
           auto seen = [&](int i) { return w == us && live && row0 + i < q.n && key <= shift + i; };
-          set_aside<D, ROWS_U, BOTH>(dV, Buf[buf][w][1], g, seen);
-          set_aside<D, ROWS_U, BOTH>(dK, Buf[buf][w][0], g, seen);
+          set_aside<D, BOTH>(dV, Buf[buf][w][1], g, none, seen);
+          set_aside<D, BOTH>(dK, Buf[buf][w][0], g, ~0u, seen);      // (of a query that is not finite every dS is zero or NaN, as in dQ)
         }
         if (idle) continue;
       }

@@ -139,11 +139,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
       const int buf = ONE ? 0 : (t - t0) & 1, key0 = t * KT;
       const unsigned Kt = k_lds + buf * TB, Vt = v_lds + buf * TB;
       const bool more = t + 1 < t1;
-      auto aside = [&] {
-        if (careful.value && key0 + KT - 1 > wg_first) set_aside<D, KT, COLS>(O, Vs[buf], g, [&](int i) { return row.live && key0 + i <= row.last; });
-      };
-      if (!ONE) aside();
-      if (!ONE && key0 > wave_last) {   // (uniform over the wave) none of its rows sees the tile
+      if (!careful.value && !ONE && key0 > wave_last) {   // (uniform over the wave) none of its rows sees the tile (set_aside needs every wave: all masked below)
         if (more) { copy_k(t + 1, buf ^ 1); copy_v(t + 1, buf ^ 1); }
         continue;
       }
@@ -242,7 +238,13 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
       l += psum;
       if (ONE) {
         wait_copies(!more);
-        aside();
+      }
+      if (careful.value && key0 + KT - 1 > wg_first) {
+#pragma unroll
+        for (int t2 = 0; t2 < T2; ++t2) {
+          const uint32_t none = row_bits(g, [&](int r) { return !(P[t2][r >> 3][r & 7] != (__bf16)0.f); });
+          set_aside<D, COLS>(O, Vs[buf] + t2 * 32 * D, g, none, [&](int i) { return row.live && key0 + t2 * 32 + i <= row.last; });
+        }
       }
       // ---- O^T += V^T P^T
       {

@@ -105,22 +105,30 @@ __device__ __forceinline__ void accumulate(float16v (&acc)[D / 32], const float*
 }
 
 // A product of a probability that is exactly zero and a value that is not finite is NaN on the matrix core, but a masked pair contributes nothing.  So where a
-// tile has masked pairs and values that are not finite, those values are added to the rows that do see them and taken out of the tile.  Rare:
-// tiles without them pay one comparison per value.  `seen(i)`: does the lane's row see row i of the tile.
+// tile has masked pairs and values that are not finite, their products are added to the rows that do see them and they are taken out of the tile.  Rare:
+// tiles without them pay one comparison per value.  `seen(i)`: does the lane's row see row i of the tile.  w: the products' factors; an infinity
+// stays what it is where its factor is positive, and becomes NaN where it is zero - or `zero` says so of all: a key or a query that is not finite has scores of +inf
+// or NaN, whose row is NaN anyway, or of -inf, and dS zero.  (Factors that are NaN spoil the product itself.)
 template <int D, typename F>
-__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], float* tile, int lane, int g, F&& seen) {
+__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], float* tile, int lane, int g, const float16v& w, bool zero, F&& seen) {
   bool odd = false;
   for (int i = lane; i < TR * D; i += 64) odd = odd || !(fabsf(tile[i / D * (D + 4) + i % D]) <= 3.4028235e38f);
   if (__builtin_amdgcn_ballot_w64(odd) == 0) return;
+  uint32_t none = 0;     // bit i: row i's factor is zero (the lane halves hold four rows each in turn)
+#pragma unroll
+  for (int r = 0; r < 16; ++r) none |= zero || !(w[r] != 0.f) ? 1u << (8 * (r >> 2) + (r & 3)) : 0u;
+  none <<= 4 * g;
+  none |= (uint32_t)__shfl_xor((int)none, 32);
 #pragma nounroll
   for (int i = 0; i < TR; ++i) {
     const bool s = seen(i);
+    const float f = (none >> i & 1) ? 0.f : 1.f;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float x = tile[i * (D + 4) + dt * 32 + 8 * (r >> 2) + 4 * g + (r & 3)];
-        if (s && !(fabsf(x) <= 3.4028235e38f)) acc[dt][r] += x;
+        if (s && !(fabsf(x) <= 3.4028235e38f)) acc[dt][r] += f * x;
       }
   }
   wave_lds();
@@ -245,7 +253,7 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_fwd(SeqParam
       S[r] = __builtin_amdgcn_exp2f(S[r] - ref);      // (0 where masked)
       l += S[r];
     }
-    if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(O, Vs, lane, g, [&](int i) { return key0 + i <= row.last; });
+    if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(O, Vs, lane, g, S, false, [&](int i) { return key0 + i <= row.last; });
     accumulate<D>(O, Vs, S, nn, g);
     wave_lds();
   }
@@ -326,7 +334,7 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dq(SeqParams
       const float x = __builtin_amdgcn_exp2f(S[r] * c2 - lse2) * (dP[r] - delta);
       S[r] = key <= row.last ? x : 0.f;
     }
-    if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(A, Ks, lane, g, [&](int i) { return key0 + i <= row.last; });
+    if (p.causal && key0 + TR - 1 > first_last) set_aside<D>(A, Ks, lane, g, S, true, [&](int i) { return key0 + i <= row.last; });
     accumulate<D>(A, Ks, S, nn, g);
     wave_lds();
   }
@@ -417,8 +425,8 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dkv(SeqParam
       }
     }
     if (Last[wave][0] < last_key || Last[wave][TR - 1] < last_key) {   // some pair is masked: queries before the diagonal, rows behind the last query
-      set_aside<D>(dV, Gs, lane, g, [&](int i) { return live && key <= Last[wave][i]; });
-      set_aside<D>(dK, Qs, lane, g, [&](int i) { return live && key <= Last[wave][i]; });
+      set_aside<D>(dV, Gs, lane, g, S, false, [&](int i) { return live && key <= Last[wave][i]; });
+      set_aside<D>(dK, Qs, lane, g, dP, true, [&](int i) { return live && key <= Last[wave][i]; });
     }
     accumulate<D>(dV, Gs, S, nn, g);
     accumulate<D>(dK, Qs, dP, nn, g);

@@ -162,10 +162,23 @@ struct ColRead {
   }
 };
 
-// Masked probabilities are exactly zero, but zero times a value that is not finite is not.  Run where a result came out not finite: the tile's such
-// values are added to the rows that see them, and taken out of the tile before the product.
-template <int D, int KT, int USE, typename F>
-__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], uint16_t* tile, int g, F&& seen) {
+// Bit i: does f hold of row i of 32, rows as two lane halves hold them in the registers of a product (f(r): of register r, row 8 (r / 4) + 4 g + r % 4).
+template <typename F>
+__device__ __forceinline__ uint32_t row_bits(int g, F&& f) {
+  uint32_t b = 0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) b |= f(r) ? 1u << (8 * (r >> 2) + (r & 3)) : 0u;
+  b <<= 4 * g;
+  const auto sw = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return sw[0] | sw[1];
+}
+
+// Masked probabilities are exactly zero, but zero times a value that is not finite is not.  Run where a result came out not finite: the products of 32 rows' such
+// values are added for the pairs that are seen, and the values taken out of the tile before its product.  The rows' factors are `none` (row_bits) zero, and
+// positive elsewhere: an infinity stays what it is, or becomes NaN.  (Factors that are NaN spoil the product itself.)
+template <int D, int USE, typename F>
+__device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], uint16_t* tile, int g, uint32_t none, F&& seen) {
+  constexpr int KT = 32;
   uint32_t* t32 = (uint32_t*)tile;
   bool odd = false;
   for (int i = threadIdx.x; i < KT * D / 2; i += blockDim.x) odd = odd || (t32[i] & 0x7f80u) == 0x7f80u || (t32[i] & 0x7f800000u) == 0x7f800000u;
@@ -173,6 +186,7 @@ __device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], uint16_t* til
 #pragma nounroll
   for (int i = 0; i < KT; ++i) {
     const bool s = seen(i);
+    const float zero = (none >> i & 1) ? 0.f : 1.f;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -181,7 +195,7 @@ __device__ __forceinline__ void set_aside(float16v (&acc)[D / 32], uint16_t* til
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float v = __uint_as_float((j & 1) ? (x[j >> 1] & 0xffff0000u) : (x[j >> 1] << 16));
-          if (s && !(fabsf(v) <= 3.4028235e38f)) acc[dt][4 * q + j] += v;
+          if (s && !(fabsf(v) <= 3.4028235e38f)) acc[dt][4 * q + j] += zero * v;
         }
       }
   }

@@ -90,3 +90,29 @@ def test_an_infinite_gradient_of_a_row(dtype):
     rest = torch.ones(N, 2, dtype=torch.bool)
     rest[AT, 1] = False
     same(bad.out["dq"][rest], clean.out["dq"][rest], "dq")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_infinite_value_of_a_key_without_probability(dtype):
+    """The scores of one key are -inf and a channel of its value +inf: zero times infinity is NaN in that channel of the rows that see it, on the diagonal as elsewhere."""
+    clean, bad = pair_of_calls(203, dtype, q=positive(5))
+    clean.dev["k"][AT, :, 5] = -1e5
+    bad.dev["k"][AT, :, 5] = -math.inf
+    bad.dev["v"][AT, :, 3] = math.inf
+    clean.forward()
+    bad.forward()
+    out, want = bad.out["out"].clone(), clean.out["out"].clone()
+    assert bool(torch.isnan(out[AT:, :, 3]).all())
+    out[AT:, :, 3] = want[AT:, :, 3] = 0
+    same(out, want, "out")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_channel_of_an_infinite_key_that_is_seen(dtype):
+    """Its probabilities are zero, and zero times infinity is NaN in that channel of dq: of the rows that see the key, in and behind the tile on the diagonal, and of no others."""
+    clean, bad = pair_of_calls(208, dtype, q=positive(5))
+    bad.dev["k"][AT, :, 5] = -math.inf
+    run(clean, bad)
+    assert bool(torch.isnan(bad.out["dq"][AT:, :, 5]).all())
+    same(bad.out["dq"][:AT], clean.out["dq"][:AT], "dq")
+    assert bool(torch.isfinite(bad.out["dq"][..., :5].float()).all())
