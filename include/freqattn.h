@@ -382,7 +382,7 @@ freqattn_status freqattn_qk_norm_backward(const freqattn_qk_shape* shape, const 
  * give wrong results, never an access outside.
  * Heads: q_heads a multiple of kv_heads; query head h reads key head h / (q_heads / kv_heads).
  * causal: the last query sees all keys, query i of a sequence with nq queries and nk keys sees keys j <= i + nk - nq.
- * A query that sees no key gets zeros, lse -inf, and gives no gradient.  Keys behind what a query sees reach it in no way, whatever they hold
+ * A query that sees no key gets zeros, lse -inf, and gives no gradient; one that sees keys and whose scores are all -inf gets NaN, lse -inf.  Keys behind what a query sees reach it in no way, whatever they hold
  * (NaN and infinities too).
  * dtype of q, k, v, out: BF16 (products on the matrix cores from bf16 operands, sums and softmax fp32) or F32 (fp32 throughout).  head_dim 1..128.
  * out must not overlap q, k, v.  softmax_scale <= 0 selects 1/sqrt(head_dim).

@@ -134,9 +134,9 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
 
   const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
   float lse2 = row.live ? p.lse[at] * LOG2E : 0.f;
-  // A row that sees no key (lse -inf) has no probabilities; one whose scores hold +inf has no finite ones.
-  if (lse2 == -INFINITY) { lse2 = INFINITY; delta = 0.f; }
-  else if (lse2 == INFINITY) lse2 = __builtin_nanf("");
+  // A row that sees no key has no probabilities; one whose scores hold +inf, or are all -inf, has no finite ones.
+  if (row.last < 0) { lse2 = INFINITY; delta = 0.f; }
+  else if (!(fabsf(lse2) < INFINITY)) lse2 = __builtin_nanf("");
   const float c2 = p.scale * LOG2E;
   auto arrived = [&] {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");

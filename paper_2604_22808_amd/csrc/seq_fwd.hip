@@ -280,7 +280,8 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
 
   // ---- normalise and store
   l += other_half(l);
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  // (a sum of zero: the row sees nothing, or all its scores are -inf and it has no softmax; of a piece, the join tells)
+  const float inv = l > 0.f || l != l ? 1.f / l : p.nsplit == 1 && row.last >= 0 ? __builtin_nanf("") : 0.f;
   const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
   const float lse2 = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY;
   uint16_t* dst = (uint16_t*)const_cast<char*>(p.o.p) + (int64_t)q.seq * p.o.bs + (int64_t)(q.base + row.token) * p.o.ts + (int64_t)row.head * p.o.hs;
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(256) k_seq_join(SeqParams p, int piece_keys) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (a wave reads its own weights)
-  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+  const float inv = sum > 0.f || sum != sum ? 1.f / sum : row.last >= 0 ? __builtin_nanf("") : 0.f;
   const int c = 2 * lane;
   if (c < p.d) {
     const float* src = p.part + at * p.d + c;

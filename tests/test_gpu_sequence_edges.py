@@ -116,3 +116,42 @@ def test_the_channel_of_an_infinite_key_that_is_seen(dtype):
     assert bool(torch.isnan(bad.out["dq"][AT:, :, 5]).all())
     same(bad.out["dq"][:AT], clean.out["dq"][:AT], "dq")
     assert bool(torch.isfinite(bad.out["dq"][..., :5].float()).all())
+
+
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_row_whose_scores_are_all_minus_infinity(dtype, causal):
+    """It sees keys, so its softmax is not that of a row that sees none: out and its gradients are NaN, lse -inf; other rows, and keys that it does not see, keep their bits."""
+    clean, bad = pair_of_calls(204, dtype, causal=causal, k=positive(5))
+    bad.dev["q"][AT, 0, 5] = -math.inf
+    run(clean, bad)
+    assert bool(torch.isnan(bad.out["out"][AT, 0]).all()) and float(bad.lse[0, AT]) == -math.inf
+    assert bool(torch.isnan(bad.out["dq"][AT, 0]).all())
+    seen = AT + 1 if causal else N
+    rest = torch.ones(N, 2, dtype=torch.bool)
+    rest[AT, 0] = False
+    for n in ("out", "dq"):
+        same(bad.out[n][rest], clean.out[n][rest], n)
+    for n in ("dk", "dv"):
+        assert bool(torch.isnan(bad.out[n][:seen]).all()), n
+        same(bad.out[n][seen:], clean.out[n][seen:], n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_token_whose_scores_are_minus_infinity_over_a_long_cache(dtype):
+    """All of them: NaN and lse -inf, from pieces of the keys too.  Those of the first 1500 keys alone: as without these keys.  A cache that holds none: zeros."""
+    calls = []
+    for _ in range(2):
+        c = Call(205, dtype, 4, 2, 64, 1, 5000, batch=3, k_lengths=[5000, 4000, 0], causal=True)
+        c.dev["q"].copy_(positive(5)(c.dev["q"]))
+        calls.append(c)
+    clean, bad = calls
+    clean.dev["k"][1, :1500, :, 5] = -1e5
+    bad.dev["k"][1, :1500, :, 5] = -math.inf
+    bad.dev["k"][0, :, :, 5] = -math.inf
+    for c in calls:
+        c.forward()
+    assert bool(torch.isnan(bad.out["out"][0]).all()) and bool((bad.lse[:, 0] == -math.inf).all())
+    same(bad.out["out"][1:], clean.out["out"][1:], "out")
+    same(bad.lse[:, 1:], clean.lse[:, 1:], "lse")
+    assert float(bad.out["out"][2].abs().sum()) == 0 and bool((bad.lse[:, 2] == -math.inf).all())
