@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
 
   float16v O[DT];
   float m, l;
-  // careful: the second pass of a workgroup whose result was not finite (see set_aside)
+  // careful: the second pass of a workgroup whose result was not finite, with values set aside (set_aside) and the maximum as the reference
   auto run = [&](auto careful) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) O[dt] = zero16();
@@ -185,8 +185,9 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
         copy_k(t + 1, 0);
       }
       // ---- mask, running softmax.  m (in units of log2) is a reference, not the exact maximum.  bf16 has the range of fp32, so a probability above one
-      // loses nothing: the reference stays while a lane's probabilities of the tile add up to less than 2^40 (exact relative to their sum), and most
-      // tiles take no maximum at all.  Where they do not, or the row has no probabilities yet, the tile's maximum becomes the reference.
+      // loses no precision: the reference stays while a lane's probabilities of the tile add up to less than 2^40 (exact relative to their sum), and most
+      // tiles take no maximum at all.  Where they do not, or the row has no probabilities yet, the tile's maximum becomes the reference.  Values above some
+      // 2^88 may overflow under such a reference: the second pass takes the maximum of every tile.
       if (mask) {
         really_branch();
         const int lim = my_last - key0 - 4 * g;
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
         return (ls[0] + ls[1]) + (ls[2] + ls[3]);
       };
       float psum = probabilities();
-      if (__builtin_amdgcn_ballot_w64(!(psum < 1.0995116e12f) || !(l > 0.f)) != 0) {   // (also where they are not numbers)
+      if (careful.value || __builtin_amdgcn_ballot_w64(!(psum < 1.0995116e12f) || !(l > 0.f)) != 0) {   // (also where they are not numbers)
         float mc[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int t2 = 0; t2 < T2; ++t2)
@@ -273,10 +274,8 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) k_seq_fwd(SeqParams 
     }
   };
   run(std::false_type{});
-  if (p.causal) {
-    // a value that is not finite may have come from a key that its row does not see
-    if (uniform(__syncthreads_or(row.live && any_odd(O)))) run(std::true_type{});
-  }
+  // a value that is not finite may have come from a key that its row does not see, or from large values times probabilities above one
+  if (uniform(__syncthreads_or(row.live && any_odd(O)))) run(std::true_type{});
 
   // ---- normalise and store
   l += other_half(l);

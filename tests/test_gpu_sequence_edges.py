@@ -155,3 +155,19 @@ def test_one_token_whose_scores_are_minus_infinity_over_a_long_cache(dtype):
     same(bad.out["out"][1:], clean.out["out"][1:], "out")
     same(bad.lse[:, 1:], clean.lse[:, 1:], "lse")
     assert float(bad.out["out"][2].abs().sum()) == 0 and bool((bad.lse[:, 2] == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("rows,keys,batch,heads", [(200, 700, 1, 2), (130, 200, 64, 4), (1, 200, 256, 8)])
+def test_values_of_1e30_under_growing_scores(rows, keys, batch, heads, causal, dtype):
+    """Scores that grow by some 24 along the keys, and values whose weighted sum is far below the type's largest while e^24 times one of them is above it."""
+    d = 64
+    c = Call(206, dtype, heads, heads, d, rows, keys, batch=batch, causal=causal, scale=1.0, spread=0.05)
+    c.host["q"][..., 0] = 1.0
+    c.host["k"][..., 0] = torch.linspace(0.0, 24.0, keys)[None, :, None].to(c.io)
+    c.host["v"] = (c.host["v"].double() * 1e30).to(c.io)
+    for n in "qkv":
+        c.dev[n].copy_(c.host[n])
+    c.forward()
+    c.check(train=False)
