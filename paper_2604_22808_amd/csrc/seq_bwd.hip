@@ -153,15 +153,14 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
                          });
     in_turn<2 * DK, PF, 1>();
   };
-  if (tiles == 1 || tiles == 2) {
-    // Rows of few keys have large gradients, and the rounding of out to bf16 is a share of them: up to two tiles of keys, delta is summed from the probabilities
-    // themselves, sum_j P_j (dO V^T)_j, instead.  (Over n keys out is smaller than v by sqrt(n), and its rounding with it.)
+  if (wg_first < SHORT_ROW && tiles > 0) {     // (its first row sees the fewest keys)
+    static_assert(SHORT_ROW == 2 * KT, "");
     copy_tile(0, 0);
-    if (tiles == 2) copy_tile(1, 1);
+    if (tiles > 1) copy_tile(1, 1);
     arrived();
     float sum = 0.f;
 #pragma nounroll
-    for (int i = 0; i < tiles * T2; ++i) {
+    for (int i = 0; i < min(tiles, 2) * T2; ++i) {
       const int buf = i / T2, t2 = i % T2;
       float16v S, dP;
       both(k_lds + buf * TB, v_lds + buf * TB, t2, S, dP);
@@ -172,7 +171,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_seq_dq(SeqParams p) {
         sum += 8 * (r >> 2) + (r & 3) <= lim ? x : 0.f;
       }
     }
-    delta = sum + other_half(sum);
+    sum += other_half(sum);
+    if (row.last < SHORT_ROW) delta = sum;
     __syncthreads();
   }
   if (row.live && g == 0) *(float2v*)(p.delta + 2 * at) = float2v{lse2, delta};

@@ -12,6 +12,11 @@
 
 namespace fa {
 
+// bf16, backward: delta = rowsum(dO O) of a row that sees up to SHORT_ROW keys is summed from the probabilities themselves, sum_j P_j (dO V^T)_j: the rounding of the
+// stored out to bf16 is a share of delta, and dS is what is left of dO V^T - delta.  Over n keys of about equal probability out is smaller than v by sqrt(n), and
+// its rounding with it; longer rows keep that error.
+constexpr int SHORT_ROW = 128;
+
 struct SeqRange {
   int seq;          // entry of the batch axis (0 for packed tensors)
   int base, n;      // first row and number of rows

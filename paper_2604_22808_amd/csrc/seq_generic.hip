@@ -306,7 +306,6 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dq(SeqParams
     delta += __shfl_xor(delta, 32);
   }
   const int64_t at = (int64_t)row.head * p.lse_rows + (p.q_off ? q.base : (int64_t)seq * p.q_rows) + row.token;
-  if (row.live && g == 0 && wave == 0) p.delta[at] = delta;
   const float lse2 = row.live && row.last >= 0 ? p.lse[at] * LOG2E : 0.f;
   const int last = query_row(p, kvh, min(tile * TR + TR - 1, q.n * p.group - 1), q.n, k.n).last;
   const int first_last = query_row(p, kvh, tile * TR, q.n, k.n).last;
@@ -317,6 +316,33 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dq(SeqParams
     fk.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.k, k.seq, k.base + key0 + r, kvh) : nullptr; });
     fv.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.v, k.seq, k.base + key0 + r, kvh) : nullptr; });
   };
+  if (sizeof(T) == 2 && first_last < SHORT_ROW && last >= 0) {    // short rows of bf16: delta from the probabilities
+    __shared__ float sums[NW][TR];
+    static_assert(NW * TR >= SHORT_ROW, "");
+    float sum = 0.f;
+    const int key0 = wave * TR;
+    if (key0 < SHORT_ROW && key0 <= last) {
+      fetch(key0);
+      fk.store(Ks, lane);
+      fv.store(Vs, lane);
+      wave_lds();
+      const float16v S = product<T, D>(Ks, Q, nn, g), dP = product<T, D>(Vs, dO, nn, g);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = __builtin_amdgcn_exp2f(S[r] * c2 - lse2) * dP[r];
+        sum += key0 + 8 * (r >> 2) + 4 * g + (r & 3) <= row.last ? x : 0.f;
+      }
+      sum += __shfl_xor(sum, 32);
+      wave_lds();
+    }
+    if (g == 0) sums[wave][nn] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < SHORT_ROW / TR; ++w) sum += sums[w][nn];
+    if (row.last < SHORT_ROW) delta = sum;
+  }
+  if (row.live && g == 0 && wave == 0) p.delta[at] = delta;
   float16v A[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) A[dt] = zero16();

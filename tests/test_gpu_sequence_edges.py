@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from tests import heads_util as U
 from tests.test_gpu_sequence_attention import Call
 
 pytestmark = pytest.mark.gpu
@@ -171,3 +172,53 @@ def test_values_of_1e30_under_growing_scores(rows, keys, batch, heads, causal, d
         c.dev[n].copy_(c.host[n])
     c.forward()
     c.check(train=False)
+
+
+def gradients_of_short_rows(q, k, v, dout, causal, scale, few=128):
+    """One sequence and head in 64 bits: dq and dk with bounds for a kernel that sums delta from the probabilities in rows of up to `few` keys, and takes it from the stored bf16 out in others."""
+    step, d = U.STEP[torch.bfloat16], q.shape[1]
+    nq, nk = q.shape[0], k.shape[0]
+    q, k, v, do = (t.double() for t in (q, k, v, dout))
+    seen = torch.ones(nq, nk, dtype=torch.bool)
+    if causal:
+        seen = torch.arange(nk)[None] <= torch.arange(nq)[:, None] + nk - nq
+    some = seen.any(1, keepdim=True)
+    s = (q @ k.T * scale).masked_fill(~seen, -math.inf)
+    lse = torch.where(some, torch.logsumexp(s, 1, keepdim=True), 0.0)
+    p = torch.where(seen, torch.exp(s - lse), 0.0)
+    out, dp = p @ v, do @ v.T
+    # as in heads_util.attend: errors of scores, of probabilities relative to themselves, of dO V^T
+    se = U.F32 * (d + 8) * torch.where(seen, q.abs() @ k.abs().T * scale + torch.where(seen, s, 0.0).abs(), 0.0).amax(1, keepdim=True)
+    pe = 2 * se + (nk + 16) * U.F32
+    dp_e = U.F32 * (d + 4) * (do.abs() @ v.abs().T)
+    delta = (p * dp).sum(1, keepdim=True)
+    exact = (p * dp_e).sum(1, keepdim=True) + (p * dp.abs()).sum(1, keepdim=True) * (pe + (nk + 4) * U.F32)
+    stored = (do.abs() * ((p @ v.abs()) * (pe + step + nk * U.F32) + step * out.abs())).sum(1, keepdim=True) + d * U.F32 * (do * out).abs().sum(1, keepdim=True)
+    delta_e = torch.where(seen.sum(1, keepdim=True) <= few, exact, stored)
+    ds = p * (dp - delta)
+    ds_e = p * (dp_e + delta_e) + ds.abs() * (pe + step + (nq + nk + 8) * U.F32)
+    dq, dk = scale * ds @ k, scale * ds.T @ q
+    return (dq, scale * ds_e @ k.abs() + step * dq.abs() * (1 + 2.0 ** -6) + 1e-30), (dk, scale * ds_e.T @ q.abs()), seen.sum(1)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,nq,nk,causal,pad", [
+    (1, 1, 64, 300, 200, True, 0), (4, 1, 64, 300, 340, True, 0), (2, 2, 128, 1, 128, False, 0), (2, 1, 128, 260, 270, True, 0),
+    (2, 1, 64, 100, 100, True, 1), (2, 2, 64, 70, 128, False, 1), (1, 1, 64, 300, 200, True, 1), (2, 1, 44, 130, 120, True, 0), (3, 1, 128, 90, 100, True, 1)])
+def test_gradients_of_rows_that_see_few_keys(heads, kv_heads, d, nq, nk, causal, pad):
+    """bf16, values far from zero: dS is what is left of dO V^T - delta, and half a step of out would be several times the bound.  Whatever other rows a workgroup holds, and whatever
+    the rows' alignment."""
+    c = Call(207, "bf16", heads, kv_heads, d, nq, nk, q_offsets=[0, nq], k_offsets=[0, nk], causal=causal, pad=pad)
+    c.host["v"] = (c.host["v"].double() + 64.0).to(c.io)
+    c.host["k"] = (c.host["k"].double() + 1.0).to(c.io)
+    for n in "kv":
+        c.dev[n].copy_(c.host[n][0])
+    run(c)
+    group = heads // kv_heads
+    dk, dk_b = torch.zeros(nk, kv_heads, d).double(), torch.zeros(nk, kv_heads, d).double()
+    for h in range(heads):
+        (dq, dq_b), (k1, k1_b), count = gradients_of_short_rows(*(c.host[n][0][:, h if n in ("q", "dout") else h // group] for n in ("q", "k", "v", "dout")), causal, c.scale)
+        few = count <= 128
+        U.check(("dq", h), c.out["dq"][:, h].cpu()[few], dq[few], dq_b[few])
+        dk[:, h // group] += k1
+        dk_b[:, h // group] += k1_b
+    U.check("dk", c.out["dk"], dk, dk_b + (U.STEP[torch.bfloat16] * (1 + 2.0 ** -6) + group * U.F32) * dk.abs() + 1e-30)
