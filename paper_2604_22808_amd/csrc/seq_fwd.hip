@@ -343,8 +343,8 @@ __global__ void __launch_bounds__(256) k_seq_join(SeqParams p, int piece_keys) {
     for (int s = 0; s < n; ++s) {
       const float2v x = *(const float2v*)(src + s * all * p.d);
       const float y = weights[wave][s];
-      a += y == 0.f ? 0.f : y * x[0];
-      b += y == 0.f ? 0.f : y * x[1];
+      a += y * x[0];     // (an infinity or NaN stays in the sum, whatever its weight)
+      b += y * x[1];
     }
     uint16_t* dst = (uint16_t*)const_cast<char*>(p.o.p) + (int64_t)q.seq * p.o.bs + (int64_t)(q.base + row.token) * p.o.ts + (int64_t)row.head * p.o.hs;
     *(uint32_t*)(dst + c) = pack2(a * inv, b * inv);

@@ -177,7 +177,7 @@ template <int D> constexpr int waves() { return D == 64 ? 8 : 4; }
 template <int D> constexpr int tile_floats() { return TR * (D + 4); }
 
 // Adds the waves' accumulators up in the order of the waves, each wave a share of the registers, and hands the sums out: put(register, sum) with
-// register dt * 16 + r.  `weight(w)`: factor of wave w's values (nothing is added where it is 0).  lds holds waves * D * 32 floats.
+// register dt * 16 + r.  `weight(w)`: factor of wave w's values.  lds holds waves * D * 32 floats.
 template <int D, int NW, typename W, typename P>
 __device__ __forceinline__ void join_waves(const float16v (&acc)[D / 32], float* lds, int wave, int lane, W&& weight, P&& put) {
   constexpr int N = D / 2;
@@ -189,10 +189,7 @@ __device__ __forceinline__ void join_waves(const float16v (&acc)[D / 32], float*
   for (int i = wave * (N / NW); i < (wave + 1) * (N / NW); ++i) {
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = weight(w);
-      s += f == 0.f ? 0.f : f * lds[(w * N + i) * 64 + lane];
-    }
+    for (int w = 0; w < NW; ++w) s += weight(w) * lds[(w * N + i) * 64 + lane];
     put(i, s);
   }
 }

@@ -222,3 +222,17 @@ def test_gradients_of_rows_that_see_few_keys(heads, kv_heads, d, nq, nk, causal,
         dk[:, h // group] += k1
         dk_b[:, h // group] += k1_b
     U.check("dk", c.out["dk"], dk, dk_b + (U.STEP[torch.bfloat16] * (1 + 2.0 ** -6) + group * U.F32) * dk.abs() + 1e-30)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("keys,far", [(200, (32, 64)), (5000, (0, 100)), (5000, (3000, 4000))])
+def test_an_infinite_value_far_below_the_others(keys, far, dtype):
+    """Scores thousands below the row's largest: probabilities of zero, times an infinity NaN, also where the key is in a piece of the keys of which nothing else counts."""
+    c = Call(209, dtype, 4, 2, 64, 1, keys, batch=2, causal=True)
+    c.dev["q"].copy_(positive(5)(c.dev["q"]))
+    c.dev["k"][0, far[0]:far[1], :, 5] = -1e5
+    c.dev["v"][0, far[0] + 20, :, 3] = math.inf
+    c.forward()
+    assert bool(torch.isnan(c.out["out"][0, :, :, 3]).all())
+    c.out["out"][0, :, :, 3] = 0
+    assert bool(torch.isfinite(c.out["out"].float()).all())
