@@ -429,6 +429,12 @@ def _torch_names():
     _Tensor = torch.Tensor
 
 
+def _count(who, name, n):
+    """The library counts in int32."""
+    if n > 0x7fffffff:
+        raise ValueError(f"{who}: {name} has an axis of 2^31 entries or more")
+
+
 def _heads(who, name, t, like=None, shape=None, written=False):
     """The freqattn_heads of a tensor, after the checks that the library cannot make on an address."""
     if _Tensor is None:
@@ -448,7 +454,9 @@ def _heads(who, name, t, like=None, shape=None, written=False):
         raise ValueError(f"{who}: {name} has dtype {dtype}, expected {like.dtype}")
     elif t.device != like.device:
         raise ValueError(f"{who}: {name} is on {t.device}, expected {like.device}")
-    if shape is not None and sh != shape:
+    if shape is None:
+        _count(who, name, max(sh))
+    elif sh != shape:
         raise ValueError(f"{who}: {name} has shape {tuple(sh)}, expected {tuple(shape)}")
     if st[-1] != 1 and sh[-1] > 1:
         raise ValueError(f"{who}: the channels of {name} must be adjacent")
@@ -581,6 +589,7 @@ def _qk_args(who, q, k, wq, wk, eps, rotary, positions):
         if getattr(k, "dim", lambda: 0)() != 4:
             raise ValueError(f"{who}: k must be [batch, tokens, heads, head_dim]")
         kh = k.shape[2]
+        _count(who, "k", kh)
         hk = _heads(who, "k", k, q, q.shape[:2] + (kh, d))
     w = [_vector(who, name, x, q, d, q.dtype) for name, x in (("wq", wq), ("wk", wk))]
     rot = _positions(who, rotary, positions, b, n, q)
@@ -625,6 +634,7 @@ def _sequence_args(who, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths,
     n = q.shape[0] if q_offsets is None else q_offsets.numel() - 1
     if (k.shape[0] if k_offsets is None else k_offsets.numel() - 1) != n or n < 0:
         raise ValueError(f"{who}: q and k must have the same number of sequences")
+    _count(who, "q_offsets", n)
     if q.shape[-1] != k.shape[-1]:
         raise ValueError(f"{who}: q and k must have the same head_dim")
     rows = SequenceRows(_int32(who, "q_offsets", q_offsets, q, (n + 1,)), _int32(who, "k_offsets", k_offsets, q, (n + 1,)),
