@@ -213,7 +213,7 @@ extern "C" freqattn_status freqattn_qk_norm(const freqattn_qk_shape* s, const fr
     QkParams p;
     fs = qk_common(who, rot, s->dtype, s->batch, s->tokens, s->q_heads, s->k_heads, s->head_dim, positions, positions_stride, p);
     if (fs != FREQATTN_OK) return fs;
-    if (s->batch == 0 || s->tokens == 0 || s->q_heads + s->k_heads == 0) return FREQATTN_OK;
+    if (s->batch == 0 || s->tokens == 0 || (s->q_heads == 0 && s->k_heads == 0)) return FREQATTN_OK;
     if ((s->q_heads && (!given(q) || !given(q_out))) || (s->k_heads && (!given(k) || !given(k_out)))) return fail(FREQATTN_EINVAL, who, "NULL argument");
     auto at = [&](const freqattn_heads* h, int heads) { return ptr(h, s->batch, s->tokens, heads); };
     if (s->q_heads) { p.in[0] = at(q, s->q_heads); p.out[0] = at(q_out, s->q_heads); }
@@ -292,7 +292,8 @@ freqattn_status seq_params(const char* who, const freqattn_sequence_shape* s, co
   p.lse_rows = qr;
   p.lse_k = kr;
   // row indices of one sequence's group and launch sizes stay within 31 bits
-  if ((int64_t)s->q_rows * p.group >= ((int64_t)1 << 30) || s->k_rows >= (1 << 30) ||
+  // (sequences first: what the products behind it can come to is below 2^63 then)
+  if ((int64_t)s->sequences * p.hk >= MAX_BLOCKS || (int64_t)s->q_rows * p.group >= ((int64_t)1 << 30) || s->k_rows >= (1 << 30) ||
       (qr * p.group / 32 + s->sequences) * p.hk >= MAX_BLOCKS || (kr / 32 + s->sequences) * p.hk >= MAX_BLOCKS)
     return fail(FREQATTN_EUNSUPPORTED, who, "too many rows for one call");
   return FREQATTN_OK;

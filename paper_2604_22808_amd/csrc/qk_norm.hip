@@ -481,10 +481,11 @@ static bool pieces(const HeadsPtr& v, int bytes, int size) {
 static Items make_items(int64_t tokens, int heads, int rpw, int steps) {
   Items it;
   it.tpw = heads < rpw ? rpw / heads : 1;
-  it.head_groups = it.tpw > 1 ? 1 : (heads + rpw * steps - 1) / (rpw * steps);
-  const int64_t groups = (tokens + it.tpw - 1) / it.tpw, n = groups * it.head_groups;
-  it.per_group = groups > 0 && n <= MAX_ITEMS ? (uint32_t)groups : 1u;
-  it.n = n <= MAX_ITEMS ? (uint32_t)n : ~0u;
+  it.head_groups = it.tpw > 1 ? 1 : (int)(((int64_t)heads + rpw * steps - 1) / (rpw * steps));
+  const int64_t groups = (tokens + it.tpw - 1) / it.tpw;
+  const bool fits = groups <= MAX_ITEMS / it.head_groups;     // (their product may pass 64 bits)
+  it.per_group = groups > 0 && fits ? (uint32_t)groups : 1u;
+  it.n = fits ? (uint32_t)(groups * it.head_groups) : ~0u;
   return it;
 }
 
@@ -500,7 +501,8 @@ static hipError_t fwd(const QkParams& p, const RotTable& t, int num_cu, hipStrea
   // Four steps of each tensor share a token's sines and have their loads in flight together; where that leaves fewer than 8 waves per compute unit, one
   // step per wave.
   const int64_t tokens = (int64_t)p.batch * p.tokens, most = p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1];
-  if (most <= 64 / LPR || tokens * ((most + 4 * (64 / LPR) - 1) / (4 * (64 / LPR))) < (int64_t)num_cu * 8) return fwd_s<T, LPR, HALF, SCALAR, 1>(p, t, st);
+  const int64_t groups = (most + 4 * (64 / LPR) - 1) / (4 * (64 / LPR));
+  if (most <= 64 / LPR || tokens < ((int64_t)num_cu * 8 + groups - 1) / groups) return fwd_s<T, LPR, HALF, SCALAR, 1>(p, t, st);
   return fwd_s<T, LPR, HALF, SCALAR, 4>(p, t, st);
 }
 template <typename T, int LPR, bool HALF, bool SCALAR>

@@ -34,3 +34,18 @@ def test_axes_beyond_32_bits():
     many = dev(BIG, dtype=torch.int32)
     with pytest.raises(ValueError, match="2\\^31"):
         B.sequence_attention(k, k, k, k, q_offsets=many, k_offsets=many)
+
+
+def test_counts_whose_products_pass_64_bits():
+    """Products of three sizes near 2^31 wrap around in 64 bits; they are too many all the same."""
+    L, h, top = B.lib(), B.Heads(16, 0, 64, 64), 2 ** 31 - 1
+    rot = B.Rotary(64, [64])
+    assert L.freqattn_rotary_apply(rot._h, B.BF16, top, top, top, h, None, 0, 0, h, None) == B.EUNSUPPORTED
+    s = B.QkShape(batch=top, tokens=top, q_heads=top, k_heads=top, head_dim=64, dtype=B.BF16, eps=1e-6)
+    assert L.freqattn_qk_norm(s, None, None, 0, h, h, None, None, h, h, None) == B.EUNSUPPORTED
+    assert L.freqattn_qk_norm_backward(s, None, None, 0, h, h, None, None, h, h, h, h, None, None, None, 0, None) == B.EUNSUPPORTED
+    q = B.SequenceShape(sequences=top, q_heads=256, kv_heads=256, head_dim=64, q_rows=2 ** 29, k_rows=2 ** 29, dtype=B.BF16, causal=1)
+    size = 1 << 62
+    assert L.freqattn_sequence_attention(q, None, h, h, h, h, None, 16, size, None) == B.EUNSUPPORTED
+    assert L.freqattn_sequence_attention_backward(q, None, h, h, h, h, h, 16, h, h, h, 16, size, None) == B.EUNSUPPORTED
+    assert L.freqattn_sequence_attention_workspace(q, None) == 0 and L.freqattn_sequence_attention_backward_workspace(q, None) == 0
