@@ -327,7 +327,7 @@ typedef struct {
                           coordinates of n (one entry per axis), or, without a grid and with one axis, at n */
   double base, factor; /* base > 1; factor > 0, >= 1 for BY_PARTS */
   double beta_fast, beta_slow; /* BY_PARTS: beta_fast > beta_slow >= 0 */
-  double amplitude;    /* 0: what the scaling says */
+  double amplitude;    /* 0: what the scaling says; finite in fp32 */
 } freqattn_rotary_cfg;
 typedef struct freqattn_rotary freqattn_rotary; /* opaque, host memory only, constant: usable from any thread, device and stream */
 

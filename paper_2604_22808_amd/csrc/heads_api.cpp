@@ -75,7 +75,7 @@ extern "C" freqattn_status freqattn_rotary_create(const freqattn_rotary_cfg* c, 
     if (c->scaling < FREQATTN_ROTARY_PLAIN || c->scaling > FREQATTN_ROTARY_BY_PARTS) return fail(FREQATTN_EINVAL, who, "unknown scaling");
     if (!(c->base > 1.0) || !std::isfinite(c->base)) return fail(FREQATTN_EINVAL, who, "base must be above 1");
     if (c->scaling != FREQATTN_ROTARY_PLAIN && !(c->factor > 0.0 && std::isfinite(c->factor))) return fail(FREQATTN_EINVAL, who, "factor must be positive");
-    if (!(c->amplitude >= 0.0) || !std::isfinite(c->amplitude)) return fail(FREQATTN_EINVAL, who, "amplitude must not be negative");
+    if (!(c->amplitude >= 0.0) || !std::isfinite((float)c->amplitude)) return fail(FREQATTN_EINVAL, who, "amplitude must not be negative, and finite in fp32");
     if (c->scaling == FREQATTN_ROTARY_BY_PARTS &&
         !(c->factor >= 1.0 && c->context > 0 && c->beta_slow >= 0.0 && c->beta_fast > c->beta_slow && std::isfinite(c->beta_fast)))
       return fail(FREQATTN_EINVAL, who, "scaling by parts needs factor >= 1, context > 0 and beta_fast > beta_slow >= 0");

@@ -49,3 +49,11 @@ def test_counts_whose_products_pass_64_bits():
     assert L.freqattn_sequence_attention(q, None, h, h, h, h, None, 16, size, None) == B.EUNSUPPORTED
     assert L.freqattn_sequence_attention_backward(q, None, h, h, h, h, h, 16, h, h, h, 16, size, None) == B.EUNSUPPORTED
     assert L.freqattn_sequence_attention_workspace(q, None) == 0 and L.freqattn_sequence_attention_backward_workspace(q, None) == 0
+
+
+def test_an_amplitude_beyond_fp32():
+    """The kernels scale in fp32: a larger amplitude would be infinite there, and NaN beside zeros."""
+    assert B.Rotary(64, [64], amplitude=3e38).frequencies()[1] == 3e38
+    with pytest.raises(B.FreqAttnError) as e:
+        B.Rotary(64, [64], amplitude=1e39)
+    assert e.value.status == B.EINVAL
