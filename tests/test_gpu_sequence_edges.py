@@ -4,8 +4,9 @@ import math
 import pytest
 import torch
 
+from paper_2604_22808_amd import binding as B
 from tests import heads_util as U
-from tests.test_gpu_sequence_attention import Call
+from tests.test_gpu_sequence_attention import MARK, Call, ints, offsets
 
 pytestmark = pytest.mark.gpu
 N, AT = 300, 150
@@ -236,3 +237,129 @@ def test_an_infinite_value_far_below_the_others(keys, far, dtype):
     assert bool(torch.isnan(c.out["out"][0, :, :, 3]).all())
     c.out["out"][0, :, :, 3] = 0
     assert bool(torch.isfinite(c.out["out"].float()).all())
+
+
+# ---- the second pass in the other cuts of a call: one-wave tiles, pieces of the keys, pieces of the query rows
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_last_key_that_only_the_last_token_sees(dtype):
+    """Four tokens against a long cache: the last row of keys and values is NaN."""
+    calls = [Call(210, dtype, 4, 2, 64, 4, 5000, batch=2, causal=True) for _ in range(2)]
+    clean, bad = calls
+    for n in "kv":
+        bad.dev[n][:, -1] = math.nan
+    run(*calls)
+    for n in ("out", "dq"):
+        same(bad.out[n][:, :3], clean.out[n][:, :3], n)
+        assert bool(torch.isnan(bad.out[n][:, 3]).all()), n
+    same(bad.lse.view(4, 2, 4)[..., :3], clean.lse.view(4, 2, 4)[..., :3], "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_late_key_under_pieces_of_the_keys(dtype):
+    n, nk, at = 300, 4096, 4000
+    calls = [Call(211, dtype, 2, 1, 64, n, nk, q_offsets=[0, n], k_offsets=[0, nk], causal=True) for _ in range(2)]
+    clean, bad = calls
+    bad.dev["v"][at, :, 7] = math.inf
+    bad.dev["k"][at + 20] = math.nan
+    for c in calls:
+        c.forward()
+    first = at - (nk - n)
+    same(bad.out["out"][:first], clean.out["out"][:first], "out")
+    assert bool((bad.out["out"][first:first + 20, :, 7] == math.inf).all()) and bool(torch.isnan(bad.out["out"][first + 20:]).all())
+    same(bad.lse[:, :first + 20], clean.lse[:, :first + 20], "lse")
+    rest = [i for i in range(64) if i != 7]
+    same(bad.out["out"][first:first + 20][..., rest], clean.out["out"][first:first + 20][..., rest], "other channels")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_early_queries_under_pieces_of_the_query_rows(dtype):
+    n = 1200
+    clean, bad = pair_of_calls(212, dtype, n=n)
+    bad.dev["q"][499] = math.nan
+    bad.dev["dout"][500, 0, 9] = math.inf
+    run(clean, bad)
+    for name in ("dk", "dv"):
+        same(bad.out[name][501:], clean.out[name][501:], name)
+        assert not bool(torch.isfinite(bad.out[name][:500].float()).all(-1).any()), name
+
+
+# ---- offsets and workspaces
+
+def wrong_offsets(n, rows, seed):
+    gen = torch.Generator().manual_seed(seed)
+    top = 2 ** 31 - 1
+    yield torch.randint(-2 ** 31, top, (n + 1,), generator=gen).tolist()
+    yield torch.randint(-rows, 2 * rows, (n + 1,), generator=gen).tolist()
+    yield torch.randint(0, rows + 1, (n + 1,), generator=gen).sort(descending=True).values.tolist()
+    yield [-2 ** 31, top] * ((n + 2) // 2) if n % 2 else [0] + [top] * n
+
+
+class Guarded:
+    """A tensor inside a larger one whose other elements hold `guard`."""
+    def __init__(self, shape, dtype, fill, guard, edge=8192):
+        n = math.prod(shape)
+        self.all, self.edge, self.n = torch.full((n + 2 * edge,), guard, dtype=dtype, device="cuda"), edge, n
+        self.x = self.all[edge:edge + n].view(shape)
+        self.x.copy_(fill) if isinstance(fill, torch.Tensor) else self.x.fill_(fill)
+        self.guard = self.all[:edge].clone()
+
+    def untouched(self):
+        return torch.equal(self.all[:self.edge], self.guard) and torch.equal(self.all[self.edge + self.n:], self.guard)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 2, 70])
+def test_wrong_offsets_read_and_write_inside_alone(n, dtype):
+    """Offsets that point outside, descend or overlap: outputs and workspaces keep the marks around them, and the NaN around the inputs reaches no result.  (Which results they are is open;
+    workspaces of zeros and marks of small numbers make them finite.)"""
+    rows, h, hk, d = 200, 4, 2, 64
+    io = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator().manual_seed(213)
+    for i, off in enumerate(wrong_offsets(n, rows, 214)):
+        src = {m: Guarded((rows, x, d), io, torch.randn(rows, x, d, generator=gen).to(io).cuda(), math.nan) for m, x in (("q", h), ("k", hk), ("v", hk), ("dout", h))}
+        dst = {m: Guarded((rows, x, d), io, 0.5, MARK) for m, x in (("out", h), ("dq", h), ("dk", hk), ("dv", hk))}
+        lse = Guarded((h, rows), torch.float32, 1.0, MARK)
+        how = dict(causal=i % 2 == 0, q_offsets=ints(off), k_offsets=ints(off if i == 1 else off[::-1]), q_lengths=ints([rows // 2] * n) if i == 2 else None)
+        shape = B.SequenceShape(n, h, hk, d, rows, rows, B.BF16 if dtype == "bf16" else B.F32, 0, 0.0)
+        which = B.SequenceRows(16, 16, None, None)
+        ws = [Guarded((max(16, f(shape, which)),), torch.uint8, 0, 90) for f in (B.lib().freqattn_sequence_attention_workspace, B.lib().freqattn_sequence_attention_backward_workspace)]
+        B.sequence_attention(*(src[m].x for m in "qkv"), dst["out"].x, lse=lse.x, workspace=ws[0].x, **how)
+        # a row that two sequences own may be left with the lse of the one in which it sees no key (-inf): the other's exp(score - lse) is not finite, so lse is given here
+        lse.x.fill_(1.0)
+        B.sequence_attention_backward(*(src[m].x for m in ("dout", "q", "k", "v")), dst["out"].x, lse.x, *(dst[m].x for m in ("dq", "dk", "dv")), workspace=ws[1].x, **how)
+        torch.cuda.synchronize()
+        for m, t in {**dst, "lse": lse, "workspace": ws[0], "backward workspace": ws[1]}.items():
+            assert t.untouched(), (n, i, m)
+        for m, t in dst.items():
+            assert bool(torch.isfinite(t.x.float()).all()), (n, i, m)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_rows,k_rows,causal", [(1, 5000, True), (300, 4096, True), (1500, 1500, False)])
+def test_what_a_workspace_holds_does_not_matter(q_rows, k_rows, causal, dtype):
+    c = Call(215, dtype, 4, 2, 64, q_rows, k_rows, batch=2, causal=causal, k_lengths=[k_rows, k_rows - 77])
+    run(c)
+    want = [t.clone() for t in (*c.out.values(), c.lse)]
+    lens = c.how["k_lengths"]
+    shape = B.SequenceShape(2, 4, 2, 64, q_rows, k_rows, B.BF16 if dtype == "bf16" else B.F32, int(causal), 0.0)
+    which = B.SequenceRows(None, None, None, lens.data_ptr())
+    need = max(f(shape, which) for f in (B.lib().freqattn_sequence_attention_workspace, B.lib().freqattn_sequence_attention_backward_workspace))
+    d, o = c.dev, c.out
+    for fill in (math.nan, math.inf):
+        ws = torch.full((need // 4 + 4,), fill, device="cuda")
+        B.sequence_attention(d["q"], d["k"], d["v"], o["out"], lse=c.lse, workspace=ws, **c.how)
+        ws.fill_(fill)
+        B.sequence_attention_backward(d["dout"], d["q"], d["k"], d["v"], o["out"], c.lse, o["dq"], o["dk"], o["dv"], workspace=ws, **c.how)
+        for got, w in zip((*o.values(), c.lse), want):
+            same(got, w, fill)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_tokens_against_packed_keys(dtype):
+    """One query row, or some, of each of 24 sequences whose keys lie behind each other: the keys are split by all rows there are, and sequences end inside pieces."""
+    kl = [(37 * i) % 700 + 1 for i in range(24)]
+    for ql in ([1] * 24, [(i * 5) % 3 for i in range(24)]):
+        c = Call(216, dtype, 4, 2, 64, sum(ql) + 2, sum(kl) + 5, q_offsets=offsets(*ql), k_offsets=offsets(*kl), causal=True, spoil=True)
+        run(c)
+        c.check()
