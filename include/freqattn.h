@@ -384,7 +384,8 @@ freqattn_status freqattn_qk_norm_backward(const freqattn_qk_shape* shape, const 
  * causal: the last query sees all keys, query i of a sequence with nq queries and nk keys sees keys j <= i + nk - nq.
  * A query that sees no key gets zeros, lse -inf, and gives no gradient; one that sees keys and whose scores are all -inf gets NaN, lse -inf.  Keys behind what a query sees reach it in no way, whatever they hold
  * (NaN and infinities too).
- * dtype of q, k, v, out: BF16 (products on the matrix cores from bf16 operands, sums and softmax fp32) or F32 (fp32 throughout).  head_dim 1..128.
+ * dtype of q, k, v, out: BF16 (products on the matrix cores from bf16 operands: probabilities, and in the backward pass their gradients, are rounded to bf16 before
+ * the products that follow; sums and softmax fp32) or F32 (fp32 throughout).  head_dim 1..128.
  * out must not overlap q, k, v.  softmax_scale <= 0 selects 1/sqrt(head_dim).
  * BF16 rows that are not whole 16-byte pieces (addresses, strides, head_dim * 2 bytes), or lie 2^27 elements or more apart, take the fp32 kernels: several times slower. */
 typedef struct {
@@ -400,7 +401,8 @@ typedef struct {
 /* lse: DEVICE fp32 [q_heads][rows of q] or NULL: log of each query's sum of exponentials, what the backward pass needs.  Row n of the packed
  * form is column n, row n of sequence i of the batched form column i*q_rows + n.
  * workspace DEVICE, at least freqattn_sequence_attention_workspace(shape, rows) bytes (may be 0: NULL), 16-byte aligned, content does not matter.
- * Few queries over many keys are split along the keys and joined from there.  rows: only which of its pointers are NULL matters to the size.
+ * BF16: few queries over many keys are split along the keys and joined from there, by the tensors' sizes: a cache by its rows, packed keys by all rows there are
+ * (long pieces, where they are many sequences).  F32 is not split.  rows: only which of its pointers are NULL matters to the size.
  * EINVAL: NULL, sizes out of range, a workspace that is too small; EUNSUPPORTED: head_dim above 128, 2^30 rows of a group or more, more workgroups
  * than a launch holds. */
 int64_t freqattn_sequence_attention_workspace(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows);
@@ -408,7 +410,8 @@ freqattn_status freqattn_sequence_attention(const freqattn_sequence_shape* shape
                                             const freqattn_heads* k, const freqattn_heads* v, const freqattn_heads* out, float* lse,
                                             void* workspace, int64_t workspace_bytes, void* stream);
 /* Gradients dq, dk, dv (of dtype) from dout and what the forward call read and wrote (out, lse).  Keys' gradients are summed over the queries and the
- * heads of their group in fp32 in a fixed order: equal calls give equal bits.  Key rows no query sees get zeros.  dq, dk, dv must not overlap inputs.
+ * heads of their group in fp32 in a fixed order: equal calls give equal bits.  Key rows no query sees get zeros.  BF16: the row sums dout * out are taken from the
+ * stored out, in rows that see up to 128 keys from the probabilities instead, which the rounding of out does not reach.  dq, dk, dv must not overlap inputs.
  * workspace: freqattn_sequence_attention_backward_workspace(shape, rows) bytes. */
 int64_t freqattn_sequence_attention_backward_workspace(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows);
 freqattn_status freqattn_sequence_attention_backward(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows,

@@ -1,5 +1,5 @@
 // Shared by the context-free operators (rotary positions, norms of Q and K, attention over sequences): host entry points in
-// heads_api.cpp, kernels in qk_norm.hip and seq_attn*.hip.
+// heads_api.cpp, kernels in qk_norm.hip, seq_fwd.hip, seq_bwd.hip and seq_generic.hip.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

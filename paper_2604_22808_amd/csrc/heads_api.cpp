@@ -53,7 +53,7 @@ HeadsPtr ptr(const freqattn_heads* h, int64_t batch, int64_t rows, int64_t heads
 }
 bool given(const freqattn_heads* h) { return h && h->data; }
 
-// The largest launch: workgroups of 256 threads, fewer than 2^32 threads.
+// The largest launch: fewer than 2^32 threads, in workgroups of up to 512.
 constexpr int64_t MAX_BLOCKS = (int64_t)1 << 23;
 
 }  // namespace

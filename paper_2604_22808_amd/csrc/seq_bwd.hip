@@ -1,6 +1,6 @@
 // Attention over sequences, bf16, backward.
 //
-//   delta = rowsum(dO O),  P = exp(S - lse),  dS = P (dO V^T - delta),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//   delta = rowsum(dO O) (rows of few keys: see SHORT_ROW),  P = exp(S - lse),  dS = P (dO V^T - delta),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
 //
 // Two kernels, 7 products of 2 d flops per pair instead of the 5 that one kernel would need: k_seq_dq owns query rows and sums over keys, k_seq_dkv owns
 // keys and sums over query rows, each in registers and in a fixed order.  One kernel would have to add one of the two sums up through memory, by
@@ -8,7 +8,7 @@
 // Both keep their products transposed as the forward pass does (the owned row on the lane), so that P and dS, rounded to bf16 in the accumulator
 // registers, are the second operand of the products that follow.  k_seq_dq reads K by rows (S) and by columns (dQ), V by rows (dO V^T); k_seq_dkv
 // reads Q and dO both ways.  8 heads x 8192 x 128, full: k_seq_dq 390 us (1.06 PFLOP/s, matrix cores busy 58 % at 1.72 GHz: power), k_seq_dkv 550 (1.0);
-// 16,384 rows x 8 heads of 64: 826 (1.0) and 1161 (0.95), where exponentials take as long as products.  k_seq_dq goes first and leaves (lse, delta) of every row, lse in units of log2, in the workspace.
+// 16,384 rows x 8 heads of 64: 820 (1.0) and 1150 (0.95), where exponentials take as long as products.  k_seq_dq goes first and leaves (lse, delta) of every row, lse in units of log2, in the workspace.
 #include <algorithm>
 
 #include "seq_mfma.h"

@@ -14,7 +14,10 @@ namespace fa {
 
 // bf16, backward: delta = rowsum(dO O) of a row that sees up to SHORT_ROW keys is summed from the probabilities themselves, sum_j P_j (dO V^T)_j: the rounding of the
 // stored out to bf16 is a share of delta, and dS is what is left of dO V^T - delta.  Over n keys of about equal probability out is smaller than v by sqrt(n), and
-// its rounding with it; longer rows keep that error.
+// its rounding with it; longer rows keep that error, whose share is larger where the values have a mean.  Relative error of dq, values of mean 0 / of mean 4:
+// 64 sequences of 128 rows, 16 / 4 heads of 128, causal: 2.58e-3 / 9.9e-3 from out, 2.32e-3 / 2.35e-3 from the probabilities (about what rounding dS and dq
+// leaves).  It takes both products of these keys once more: backward pass 120 -> 123 us; 256 sequences of 64 rows, 16 heads of 64, full: 129 -> 137; 512 of
+// 128 rows, 16 heads of 128, full: 1024 -> 1118.
 constexpr int SHORT_ROW = 128;
 
 struct SeqRange {
@@ -71,6 +74,8 @@ __device__ __forceinline__ int lane_scan(int x) {
 // The rank-th tile of a launch in the order of descending work (the first key tiles of a sequence, or its last query tiles, under the causal mask), so that no long tile
 // starts when the chip is about to run dry.  Up to 64 sequences, one a lane.  Work counts in steps of 64 rows of the other side; `count(c)` is the
 // number of the lane's tiles of c steps or more, and the level of the rank is found by bisection.  Returns false past the last tile.
+// (More sequences are launched in their own order; no loss was measured: 64 of 16 to 3000 rows, 46,308 in all, 16 / 4 heads of 128, causal: forward 404 us, backward
+// 1245; the same and one more of one row 383 and 1267.)
 template <typename F>
 __device__ __forceinline__ bool seq_rank(int rank, int top, F&& count, int& seq, int& nth) {
   int lo = 0, hi = top + 1;    // level lo holds the rank, level hi does not

@@ -9,9 +9,9 @@
 // Few rows (a token of each of some sequences): tiles of 32 rows, one wave a workgroup, and the keys are cut into pieces of `split_tiles` tiles
 // that run as workgroups of their own; their normalised results and log sums are joined by k_seq_join.
 //
-// Bound: long rows by the matrix cores at the clock that power leaves them (32,768 causal rows, 4 / 1 heads of 128: 1.04 ms, 1.06 PFLOP/s, busy 51 % at
-// 1.74 GHz), at head_dim 64 as much by the exponentials (16,384 rows x 8 heads: 0.68 ms, 0.81 PFLOP/s); few rows by memory (32 tokens against caches
-// of 200 to 16,384 rows, 32 / 8 heads of 128: 217 us, 4.9 TB/s).
+// Bound: long rows by the matrix cores at the clock that power leaves them (32,768 causal rows, 4 / 1 heads of 128: 1.02 ms, 1.08 PFLOP/s; in a run with counters, 1.17 ms,
+// they were busy 57 % at 1.58 GHz), at head_dim 64 as much by the exponentials (16,384 rows x 8 heads: 0.66-0.69 ms, 0.8 PFLOP/s, busy 42 % at 1.91 GHz); few
+// rows by memory (32 tokens against caches of 200 to 16,384 rows, 32 / 8 heads of 128: 217 us, 4.9 TB/s).
 #include "seq_mfma.h"
 
 namespace fa {
@@ -362,7 +362,9 @@ constexpr int FEW_KT = 32, MANY_KT = 64;
 
 }  // namespace
 
-// How a forward call is cut.
+// How a forward call is cut.  Lengths are on the device, so the cut goes by the tensors' sizes, and suits batches whose sequences are alike.  Where they are not it costs: 64 tokens
+// beside a prompt of 4096 rows (32 / 8 heads, caches of 4096) take 250 us, alone 123 and 142; packed keys count as one long sequence, so that the pieces of 32
+// tokens against 32 x 4096 packed keys are longer than the sequences: 170 us, as a cache 108.
 SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu) {
   SeqPlan s;
   const bool packed = p.q_off != nullptr;

@@ -11,8 +11,11 @@
 // LDS of its own (no barrier until their sums are joined at the end), in the forward and dQ kernels with the next tile's loads under way in registers: fp32 products are slow
 // enough that a tile per 32 rows is no burden on the caches, and short sequences still give every wave something to do.  The sums over keys (dQ) and over queries (dK, dV) are taken by
 // different kernels, each by one workgroup in a fixed order, instead of by atomics: 7 products instead of 5, equal bits every time.
-// Bound by the fp32 matrix rate (157 TFLOP/s peak), short sequences by the longest row's chain of tiles
-// (three sequences of 701, 333 and 100 rows, 6 / 3 heads of 48: forward 29 us, dQ 35, dK and dV 70; with four waves and the next rows in registers dK and dV took 89).
+// Bound, on long rows: 8 heads of 4096 rows, full, run at 85 TFLOP/s forward (404 us, head_dim 64; 71 at 128, 964 us) and 100 backward, counting its own seven products (1202 us; 89
+// and 2715), of the 134 that a large library product reaches, with one workgroup of four or eight waves a compute unit (LDS).  Short sequences by the
+// longest row's chain of tiles (three sequences of 701, 333 and 100 rows, 6 / 3 heads of 48: forward 28 us, dQ 34, dK and dV 71; with four waves and the next rows in
+// registers dK and dV took 89).  The other side is not cut into pieces: one token against a cache of 16,384 rows, 32 / 8 heads of 128, runs on 8 workgroups and takes
+// 929 us, 32 such tokens on 256 take 955 (4.5 TB/s).
 #include <hip/hip_runtime.h>
 
 #include "seq_common.h"
