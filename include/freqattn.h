@@ -432,6 +432,86 @@ freqattn_status freqattn_forward_tokens(freqattn_ctx* ctx, const freqattn_heads*
                                         int64_t positions_stride, const freqattn_band_cfg* band_cfg, const int32_t* head_alloc, void* out,
                                         void* stream);
 
+/* ---- on token rows: layer norm, products in 8-bit integers, caches held in 8 bits ----
+ * A device tensor [batch][rows][channels]: element (b, n, c) at b*batch_stride + n*row_stride + c, strides in elements, any element's alignment
+ * (16-byte aligned rows are faster); strides of outputs must keep rows apart. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, row_stride;
+} freqattn_rows;
+
+/* Layer norm, out = (x - mean_c x) (var_c x + eps)^-1/2 * w + b, var the mean of the centred squares.  w, b DEVICE of `dtype`, NULL: ones and zeros;
+ * [channels], or, with weights_per_batch != 0, [batch][channels]: scale and shift of their own for every batch entry, as conditioning gives them.  Sums are fp32; the
+ * mean's own rounding is taken out again, so rows far from zero keep their precision.  out may be x itself (same pointer and strides), else must not overlap it.
+ * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype, eps negative or not finite; EUNSUPPORTED: channels above 16384, 2^31 rows or more, more than 65535
+ * batch entries with weights of their own.  Nothing is launched where batch or rows is 0. */
+typedef struct {
+  int32_t batch, rows, channels;
+  int32_t dtype;             /* freqattn_dtype of x, w, b, out */
+  int32_t weights_per_batch; /* 0: one w and b */
+  float eps;                 /* >= 0 */
+} freqattn_norm_shape;
+freqattn_status freqattn_layer_norm(const freqattn_norm_shape* shape, const freqattn_rows* x, const void* w, const void* b, const freqattn_rows* out,
+                                    void* stream);
+/* Gradients of freqattn_layer_norm: dx of dtype from x (before the norm), w and dout; dx may be dout or x itself.  dw, db DEVICE fp32 [channels] or [batch][channels] as w is
+ * given, summed over the rows in a fixed order (equal calls give equal bits), zeros where there are no rows, NULL: not wanted.
+ * workspace DEVICE, freqattn_layer_norm_workspace(shape) bytes (may be 0: NULL), 16-byte aligned, content does not matter; not needed where both are NULL. */
+int64_t freqattn_layer_norm_workspace(const freqattn_norm_shape* shape);
+freqattn_status freqattn_layer_norm_backward(const freqattn_norm_shape* shape, const freqattn_rows* x, const void* w, const freqattn_rows* dout,
+                                             const freqattn_rows* dx, float* dw, float* db, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Rows in 8-bit integers with a scale each: a = max_c |x_c|, codes_c = 127 x_c / a to the nearest whole number, ties to even (exactly so for every
+ * input), scales = a / 127 in fp32 [batch*rows]; x is about scales * codes.  A row of zeros has codes and scale 0; one that holds an infinity or NaN has codes 0 and the
+ * scale NaN, which a product hands on to its results.  (Scales below 2^-126, of rows whose a is below 2^-119, are subnormal numbers and as coarse as those.)  dtype:
+ * freqattn_dtype of x; codes int8 rows of any stride.  Weights [outputs][channels] are coded by the same call, a scale for each output.
+ * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype; EUNSUPPORTED: channels above 131071, 2^31 rows or more. */
+freqattn_status freqattn_quantize_rows(int32_t dtype, int32_t batch, int32_t rows, int32_t channels, const freqattn_rows* x, const freqattn_rows* codes,
+                                       float* scales, void* stream);
+/* out[m][n] = a_scales[m] * w_scales[n] * sum_c a[m][c] w[n][c] + bias[n]: a linear layer on coded rows.  a int8 [rows][channels], w int8 [outputs][channels], row strides in
+ * elements, any codes -128..127; sums are exact 32-bit integers, scales and bias are applied in fp32, out is rounded once.  out [rows][outputs] and bias [outputs] (NULL: none) of
+ * `dtype`; scales DEVICE fp32.  out must not overlap the inputs.
+ * Rows of codes that are not whole 16-byte pieces (addresses, strides, channels) take a slower kernel.
+ * workspace DEVICE, freqattn_product_i8_workspace(shape) bytes (may be 0: NULL), 16-byte aligned, content does not matter.
+ * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype, a workspace that is too small; EUNSUPPORTED: channels above 131071, more tiles than a launch holds. */
+typedef struct {
+  int32_t rows, channels, outputs;
+  int32_t dtype; /* freqattn_dtype of out and bias */
+} freqattn_product_shape;
+int64_t freqattn_product_i8_workspace(const freqattn_product_shape* shape);
+freqattn_status freqattn_product_i8(const freqattn_product_shape* shape, const int8_t* a, int64_t a_stride, const float* a_scales, const int8_t* w,
+                                    int64_t w_stride, const float* w_scales, const void* bias, void* out, int64_t out_stride, void* workspace,
+                                    int64_t workspace_bytes, void* stream);
+
+/* Caches of keys and values held in 8 bits.  k, v: codes [sequences][k_rows][kv_heads][head_dim], one byte each in e4m3 (OCP: bias 7, largest value 448, NaN
+ * 0x7f and 0xff).  k_scales, v_scales: DEVICE bytes [sequences][blocks][kv_heads], blocks = k_rows / block_rows rounded up; the block_rows rows (16, 32, 64, 128 or 256) of a
+ * block and head have the scale 2^(byte - 127), byte 255: NaN.  A value is its code times its scale: exact in bf16 and fp32 for the bytes that append writes (10..247;
+ * values below 2^-126, which smaller bytes give, may count as zero).
+ * The calls take the shape and rows of freqattn_sequence_attention: the cache is the batched form of the keys, so k_offsets must be NULL, and k_lengths (NULL: k_rows) says
+ * how far each sequence is filled, appended rows included.  Lengths and offsets are held to the tensors' rows on the device. */
+typedef struct {
+  freqattn_heads k, v; /* codes: strides in bytes */
+  uint8_t *k_scales, *v_scales;
+  int32_t block_rows;
+} freqattn_cache8;
+/* New rows k, v (of dtype, packed by q_offsets or [sequences][q_rows][kv_heads][head_dim], cut by q_lengths) become the last rows of the filled part: sequence i's nq rows
+ * go to cache rows k_lengths[i] - nq .. k_lengths[i] - 1 (rows that would lie before row 0 are dropped).  A block's scale is the smallest that brings its largest
+ * new value to 448 or less, byte 10 at least; in a block that holds earlier rows it is that or the scale it has, whichever is larger, and where it grows the
+ * earlier rows' codes are rounded to it.  Codes are rounded to the nearest, ties to even; NaN and infinities become NaN and do not count for the scale.  Equal calls give
+ * equal bytes.  q_heads, causal and softmax_scale of the shape are ignored.  Other rows and blocks stay as they are. */
+freqattn_status freqattn_cache8_append(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows, const freqattn_heads* k,
+                                       const freqattn_heads* v, const freqattn_cache8* cache, void* stream);
+/* Values of the filled rows, k and v [sequences][k_rows][kv_heads][head_dim] of dtype; rows behind a sequence's length stay as they are. */
+freqattn_status freqattn_cache8_read(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows, const freqattn_cache8* cache,
+                                     const freqattn_heads* k, const freqattn_heads* v, void* stream);
+/* Attention over such a cache: freqattn_sequence_attention with the cache's values as keys and values, q, out and lse as there (dtype BF16 or F32; the order of
+ * causal queries, empty rows, NaN and infinities too).
+ * workspace: freqattn_cache8_attention_workspace(shape, rows) bytes.
+ * EINVAL, EUNSUPPORTED as there, also block_rows or k_offsets that no cache has. */
+int64_t freqattn_cache8_attention_workspace(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows);
+freqattn_status freqattn_cache8_attention(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows, const freqattn_heads* q,
+                                          const freqattn_cache8* cache, const freqattn_heads* out, float* lse, void* workspace, int64_t workspace_bytes,
+                                          void* stream);
+
 #ifdef __cplusplus
 }
 #endif

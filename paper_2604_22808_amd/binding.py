@@ -56,7 +56,25 @@ class SequenceRows(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q_offsets", "k_offsets", "q_lengths", "k_lengths")]
 
 
+class Rows(C.Structure):
+    """freqattn_rows: a device tensor [batch][rows][channels] by its address and strides (elements)."""
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class NormShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "rows", "channels", "dtype", "weights_per_batch")] + [("eps", C.c_float)]
+
+
+class ProductShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "channels", "outputs", "dtype")]
+
+
+class Cache8(C.Structure):
+    _fields_ = [("k", Heads), ("v", Heads), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("block_rows", C.c_int32)]
+
+
 _H, _P = C.POINTER(Heads), C.c_void_p
+_R, _N, _C8 = C.POINTER(Rows), C.POINTER(NormShape), C.POINTER(Cache8)
 _SEQ = [C.POINTER(SequenceShape), C.POINTER(SequenceRows)]
 _ROT = [_P, _P, C.c_int64]     # rotary, positions, positions_stride
 
@@ -111,6 +129,16 @@ EXPORTS = {
     "freqattn_sequence_attention": (C.c_int, _SEQ + [_H, _H, _H, _H, _P, _P, C.c_int64, _P]),
     "freqattn_sequence_attention_backward_workspace": (C.c_int64, _SEQ),
     "freqattn_sequence_attention_backward": (C.c_int, _SEQ + [_H] * 5 + [_P] + [_H] * 3 + [_P, C.c_int64, _P]),
+    "freqattn_layer_norm": (C.c_int, [_N, _R, _P, _P, _R, _P]),
+    "freqattn_layer_norm_workspace": (C.c_int64, [_N]),
+    "freqattn_layer_norm_backward": (C.c_int, [_N, _R, _P, _R, _R, _P, _P, _P, C.c_int64, _P]),
+    "freqattn_quantize_rows": (C.c_int, [C.c_int32] * 4 + [_R, _R, _P, _P]),
+    "freqattn_product_i8_workspace": (C.c_int64, [C.POINTER(ProductShape)]),
+    "freqattn_product_i8": (C.c_int, [C.POINTER(ProductShape), _P, C.c_int64, _P, _P, C.c_int64, _P, _P, _P, C.c_int64, _P, C.c_int64, _P]),
+    "freqattn_cache8_append": (C.c_int, _SEQ + [_H, _H, _C8, _P]),
+    "freqattn_cache8_read": (C.c_int, _SEQ + [_C8, _H, _H, _P]),
+    "freqattn_cache8_attention_workspace": (C.c_int64, _SEQ),
+    "freqattn_cache8_attention": (C.c_int, _SEQ + [_H, _C8, _H, _P, _P, C.c_int64, _P]),
 }
 
 _lib = None
@@ -422,9 +450,10 @@ _Tensor = None     # torch.Tensor and the two I/O types, once torch is there (th
 
 
 def _torch_names():
-    global _Tensor, _BF16, _F32, _INT32, _device, _raw_stream
+    global _Tensor, _BF16, _F32, _INT32, _INT8, _CODES, _BYTE, _device, _raw_stream
     import torch
-    _BF16, _F32, _INT32 = torch.bfloat16, torch.float32, torch.int32
+    _BF16, _F32, _INT32, _INT8, _BYTE = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
+    _CODES = (torch.float8_e4m3fn, torch.uint8)
     _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _Tensor = torch.Tensor
 
@@ -674,3 +703,226 @@ def sequence_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, causal=Fals
     ws, size, keep = _workspace(who, workspace, lib().freqattn_sequence_attention_backward_workspace(shape, rows), q)
     _call(lib().freqattn_sequence_attention_backward, q, shape, rows, hg, hq, hk, hv, ho, at, xq, xk, xv, ws, size)
     return dq, dk, dv
+
+
+# ---- on token rows: layer norm, products in 8-bit integers, caches held in 8 bits ---------------------------------------
+# A tensor of rows is [batch, rows, channels] or [rows, channels] with adjacent channels and any other strides.
+
+def _rows(who, name, t, like=None, shape=None, dtype=None, written=False):
+    """The freqattn_rows of a tensor and its sizes as three axes, after the checks that the library cannot make on an address."""
+    if _Tensor is None:
+        _torch_names()
+    if not isinstance(t, _Tensor):
+        raise TypeError(f"{who}: {name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{who}: {name} must be a device tensor")
+    sh, st = t.shape, t.stride()
+    dim = len(st)
+    if dim != 2 and dim != 3:
+        raise ValueError(f"{who}: {name} must be [batch, rows, channels] or [rows, channels], got {tuple(sh)}")
+    if dtype is not None:
+        if t.dtype is not dtype:
+            raise ValueError(f"{who}: {name} has dtype {t.dtype}, expected {dtype}")
+    elif t.dtype is not _BF16 and t.dtype is not _F32:
+        raise ValueError(f"{who}: {name} has dtype {t.dtype}, expected bfloat16 or float32")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{who}: {name} is on {t.device}, expected {like.device}")
+    if shape is None:
+        _count(who, name, max(sh))
+    elif sh != shape:
+        raise ValueError(f"{who}: {name} has shape {tuple(sh)}, expected {tuple(shape)}")
+    if st[-1] != 1 and sh[-1] > 1:
+        raise ValueError(f"{who}: the channels of {name} must be adjacent")
+    if written and 0 in st and any(s == 0 and n > 1 for s, n in zip(st, sh)):
+        raise ValueError(f"{who}: {name} is written and must not be expanded")
+    return Rows(t.data_ptr(), st[0] if dim == 3 else 0, st[-2])
+
+
+def _filled(who, name, t, like, dtype, shape):
+    """Address of a contiguous device tensor of the type and shape; None passes."""
+    if t is None:
+        return None
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.device != like.device or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"{who}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def _norm_args(who, x, w, eps, vectors):
+    """The shape and the freqattn_rows of x, and the addresses of `vectors` (name, tensor, type): all [channels] or all [batch, channels]."""
+    hx = _rows(who, "x", x)
+    sh = x.shape
+    b, n, c = sh if len(sh) == 3 else (1,) + tuple(sh)
+    each, at = None, []
+    for name, t, dtype in vectors:
+        if t is not None:
+            one = getattr(t, "dim", lambda: 0)() == 2 and len(sh) == 3
+            if each is not None and one != each:
+                raise ValueError(f"{who}: weights must be all [channels] or all [batch, channels]")
+            each = one
+            at.append(_filled(who, name, t, x, dtype, (b, c) if one else (c,)))
+        else:
+            at.append(None)
+    return NormShape(b, n, c, _io(x), 1 if each else 0, eps), hx, at
+
+
+def layer_norm(x, w, b, out, eps=1e-6):
+    """freqattn_layer_norm: x, out [batch, rows, channels] or [rows, channels]; w, b [channels] or [batch, channels], or None; out may be x."""
+    who = "layer_norm"
+    if _Tensor is None:
+        _torch_names()
+    dtype = getattr(x, "dtype", None)
+    shape, hx, at = _norm_args(who, x, w, eps, (("w", w, dtype), ("b", b, dtype)))
+    ho = _rows(who, "out", out, x, x.shape, dtype, True)
+    _call(lib().freqattn_layer_norm, x, shape, hx, *at, ho)
+    return out
+
+
+def layer_norm_backward(x, w, dout, dx, dw=None, db=None, eps=1e-6, workspace=None):
+    """freqattn_layer_norm_backward: x, w as in layer_norm; dw, db fp32 [channels] or [batch, channels] (as w, where there is one), or None."""
+    who = "layer_norm_backward"
+    if _Tensor is None:
+        _torch_names()
+    dtype = getattr(x, "dtype", None)
+    shape, hx, at = _norm_args(who, x, w, eps, (("w", w, dtype), ("dw", dw, _F32), ("db", db, _F32)))
+    hy, ho = _rows(who, "dout", dout, x, x.shape, dtype), _rows(who, "dx", dx, x, x.shape, dtype, True)
+    need = 0 if dw is None and db is None else lib().freqattn_layer_norm_workspace(shape)
+    ws, size, keep = _workspace(who, workspace, need, x)
+    _call(lib().freqattn_layer_norm_backward, x, shape, hx, at[0], hy, ho, at[1], at[2], ws, size)
+    return dx, dw, db
+
+
+def quantize_rows(x, codes, scales):
+    """freqattn_quantize_rows: x [batch, rows, channels] or [rows, channels], codes int8 of its shape, scales fp32 of its shape without the channels."""
+    who = "quantize_rows"
+    hx = _rows(who, "x", x)
+    hc = _rows(who, "codes", codes, x, x.shape, _INT8, True)
+    at = _filled(who, "scales", scales, x, _F32, x.shape[:-1])
+    if at is None:
+        raise ValueError(f"{who}: scales must be a tensor")
+    sh = x.shape
+    b, n, c = sh if len(sh) == 3 else (1,) + tuple(sh)
+    _call(lib().freqattn_quantize_rows, x, _io(x), b, n, c, hx, hc, at)
+    return codes, scales
+
+
+def _flat(who, name, t):
+    """Rows and row stride of a tensor whose leading axes are one axis of rows in memory."""
+    sh, st = t.shape, t.stride()
+    if len(sh) == 2:
+        return sh[0], st[0]
+    if sh[0] > 1 and sh[1] > 1 and st[0] != sh[1] * st[1]:
+        raise ValueError(f"{who}: the rows of {name} must lie at one stride")
+    return sh[0] * sh[1], st[1] if sh[1] > 1 else st[0]
+
+
+def product_i8(a, a_scales, w, w_scales, out, bias=None, workspace=None):
+    """freqattn_product_i8: a int8 [batch, rows, channels] or [rows, channels], w int8 [outputs, channels], a_scales and w_scales fp32 without the channels, out
+    bfloat16 or float32 of a's shape with the outputs in place of the channels, bias [outputs] of out's type or None."""
+    who = "product_i8"
+    if _Tensor is None:
+        _torch_names()
+    _rows(who, "a", a, None, None, _INT8)
+    hw = _rows(who, "w", w, a, None, _INT8)
+    if len(w.shape) != 2 or w.shape[1] != a.shape[-1]:
+        raise ValueError(f"{who}: w must be [outputs, {a.shape[-1]}], got {tuple(w.shape)}")
+    n = w.shape[0]
+    _rows(who, "out", out, a, a.shape[:-1] + (n,), None, True)
+    at = [_filled(who, "a_scales", a_scales, a, _F32, a.shape[:-1]), _filled(who, "w_scales", w_scales, a, _F32, (n,))]
+    if None in at:
+        raise ValueError(f"{who}: a_scales and w_scales must be tensors")
+    (rows, a_stride), (_, out_stride) = _flat(who, "a", a), _flat(who, "out", out)
+    _count(who, "a", rows)
+    shape = ProductShape(rows, a.shape[-1], n, _io(out))
+    ws, size, keep = _workspace(who, workspace, lib().freqattn_product_i8_workspace(shape), a)
+    _call(lib().freqattn_product_i8, a, shape, a.data_ptr(), a_stride, at[0], w.data_ptr(), hw.row_stride, at[1],
+          _filled(who, "bias", bias, a, out.dtype, (n,)), out.data_ptr(), out_stride, ws, size)
+    return out
+
+
+def _cache8(who, cache_k, cache_v, k_scales, v_scales, block):
+    """The freqattn_cache8 of a cache's tensors."""
+    if _Tensor is None:
+        _torch_names()
+    at = []
+    for name, t in (("cache_k", cache_k), ("cache_v", cache_v)):
+        if not isinstance(t, _Tensor):
+            raise TypeError(f"{who}: {name} must be a torch tensor")
+        if not t.is_cuda:
+            raise ValueError(f"{who}: {name} must be a device tensor")
+        if t.dtype not in _CODES or t.dim() != 4:
+            raise ValueError(f"{who}: {name} must be a float8_e4m3fn or uint8 tensor [sequences, rows, heads, head_dim], got {t.dtype} {tuple(t.shape)}")
+        if t.shape != cache_k.shape or t.device != cache_k.device:
+            raise ValueError(f"{who}: cache_k and cache_v must have one shape and device")
+        st = t.stride()
+        if st[3] != 1 and t.shape[3] > 1:
+            raise ValueError(f"{who}: the channels of {name} must be adjacent")
+        at.append(Heads(t.data_ptr(), st[0], st[1], st[2]))
+    _count(who, "cache_k", max(cache_k.shape))
+    n, rows, heads, _ = cache_k.shape
+    if block not in (16, 32, 64, 128, 256):
+        raise ValueError(f"{who}: block must be 16, 32, 64, 128 or 256")
+    for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+        at.append(_filled(who, name, t, cache_k, _BYTE, (n, -(-rows // block), heads)))
+        if at[-1] is None:
+            raise ValueError(f"{who}: {name} must be a tensor")
+    return Cache8(*at, block)
+
+
+def _apart(who, name, t):
+    if 0 in t.stride() and any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape)):
+        raise ValueError(f"{who}: {name} is written and must not be expanded")
+
+
+def cache8_append(k, v, cache_k, cache_v, k_scales, v_scales, block, q_offsets=None, q_lengths=None, k_lengths=None):
+    """freqattn_cache8_append: new rows k, v [rows, heads, head_dim] with q_offsets (packed sequences) or [sequences, rows, heads, head_dim] become the last of the
+    k_lengths filled rows of cache_k, cache_v [sequences, capacity, heads, head_dim]; k_scales, v_scales uint8 [sequences, blocks of `block` rows, heads]."""
+    who = "cache8_append"
+    cache = _cache8(who, cache_k, cache_v, k_scales, v_scales, block)
+    _apart(who, "cache_k", cache_k)
+    _apart(who, "cache_v", cache_v)
+    hk = _heads(who, "k", k)
+    hv = _heads(who, "v", v, k, k.shape)
+    n, rows, heads, d = cache_k.shape
+    if k.dim() != (4 if q_offsets is None else 3):
+        raise ValueError(f"{who}: k must be [rows, heads, head_dim] with q_offsets, [sequences, rows, heads, head_dim] without")
+    if k.device != cache_k.device or k.shape[-2:] != (heads, d) or (q_offsets is None and k.shape[0] != n):
+        raise ValueError(f"{who}: k has shape {tuple(k.shape)} on {k.device}, the cache {tuple(cache_k.shape)} on {cache_k.device}")
+    at = SequenceRows(_int32(who, "q_offsets", q_offsets, k, (n + 1,)), None, _int32(who, "q_lengths", q_lengths, k, (n,)),
+                      _int32(who, "k_lengths", k_lengths, k, (n,)))
+    shape = SequenceShape(n, heads, heads, d, k.shape[-3], rows, _io(k), 0, 0.0)
+    _call(lib().freqattn_cache8_append, k, shape, at, hk, hv, cache)
+
+
+def cache8_read(cache_k, cache_v, k_scales, v_scales, block, k, v, k_lengths=None):
+    """freqattn_cache8_read: the values of the filled rows into k, v of the cache's shape, bfloat16 or float32."""
+    who = "cache8_read"
+    cache = _cache8(who, cache_k, cache_v, k_scales, v_scales, block)
+    hk = _heads(who, "k", k, None, cache_k.shape, True)
+    hv = _heads(who, "v", v, k, cache_k.shape, True)
+    if k.device != cache_k.device:
+        raise ValueError(f"{who}: k is on {k.device}, expected {cache_k.device}")
+    n, rows, heads, d = cache_k.shape
+    at = SequenceRows(None, None, None, _int32(who, "k_lengths", k_lengths, k, (n,)))
+    _call(lib().freqattn_cache8_read, k, SequenceShape(n, heads, heads, d, 0, rows, _io(k), 0, 0.0), at, cache, hk, hv)
+    return k, v
+
+
+def cache8_attention(q, cache_k, cache_v, k_scales, v_scales, block, out, lse=None, causal=False, scale=0.0, q_offsets=None, q_lengths=None, k_lengths=None,
+                     workspace=None):
+    """freqattn_cache8_attention: q, out, lse, causal, scale as in sequence_attention, the cache as in cache8_append."""
+    who = "cache8_attention"
+    cache = _cache8(who, cache_k, cache_v, k_scales, v_scales, block)
+    hq = _heads(who, "q", q)
+    ho = _heads(who, "out", out, q, q.shape, True)
+    n, rows, heads, d = cache_k.shape
+    if q.dim() != (4 if q_offsets is None else 3):
+        raise ValueError(f"{who}: q must be [rows, heads, head_dim] with q_offsets, [sequences, rows, heads, head_dim] without")
+    if q.device != cache_k.device or q.shape[-1] != d or (q_offsets is None and q.shape[0] != n):
+        raise ValueError(f"{who}: q has shape {tuple(q.shape)} on {q.device}, the cache {tuple(cache_k.shape)} on {cache_k.device}")
+    at = SequenceRows(_int32(who, "q_offsets", q_offsets, q, (n + 1,)), None, _int32(who, "q_lengths", q_lengths, q, (n,)),
+                      _int32(who, "k_lengths", k_lengths, q, (n,)))
+    shape = SequenceShape(n, q.shape[-2], heads, d, q.shape[-3], rows, _io(q), 1 if causal else 0, scale)
+    where = None if lse is None else _lse(who, lse, q, q_offsets, shape.q_heads)
+    ws, size, keep = _workspace(who, workspace, lib().freqattn_cache8_attention_workspace(shape, at), q)
+    _call(lib().freqattn_cache8_attention, q, shape, at, hq, cache, ho, where, ws, size)
+    return out

@@ -1,0 +1,218 @@
+// Caches held in 8 bits: new rows appended, values read back.
+//
+// A block of 2^shift rows of a sequence and head has one scale 2^(e - 127), the smallest that brings its largest value to 448 or less (the largest e4m3 value); a code
+// is x 2^(127 - e) to the nearest e4m3 value, ties to even.  Scales are powers of two so that a value in e4m3 keeps its bits when a block's scale grows:
+// only values that fall among the subnormal codes are rounded again.  With no smaller byte than 10 every value is a normal number in fp32 and exact in bf16.
+//
+// Bound by memory.  A workgroup appends to one block of one head of K or V (nobody else writes there): largest value of the new rows, then codes; rows that the block
+// holds already are rewritten only where its scale has grown.
+#include "rows.h"
+#include "seq_common.h"
+#include "tokens.h"
+
+namespace fa {
+
+using namespace rows;
+
+namespace {
+
+constexpr int LEAST = 10;      // byte of the smallest scale
+constexpr uint32_t INF_BITS = 0x7f800000u;
+
+typedef float float2v __attribute__((ext_vector_type(2)));
+
+// The smallest byte e with top <= 448 * 2^(e - 127) = 1.75 * 2^(e - 119), top by its bits.
+__device__ __forceinline__ int least_byte(uint32_t top) {
+  const int e = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return e > LEAST ? e : LEAST;
+}
+
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  int x = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, x, true);
+}
+__device__ __forceinline__ float coded(float x, int e) {   // what is coded: infinities become NaN
+  return (__float_as_uint(x) & 0x7fffffffu) >= INF_BITS ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(x, 127 - e);
+}
+__device__ __forceinline__ void values4(uint32_t codes, float (&x)[4]) {
+  const float2v a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+  x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
+}
+
+// Eight channels c .. c + 7 of a row of d.
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int c, int d, float (&x)[8]) {
+  constexpr int N = 8 / PW<T>;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    Piece<T> p;
+    p.load(row, c + i * PW<T>, d);
+#pragma unroll
+    for (int j = 0; j < PW<T>; ++j) x[i * PW<T> + j] = p.get(j);
+  }
+}
+__device__ __forceinline__ uint2v load_codes(const uint8_t* row, int c, int d) {
+  uint2v x = {0u, 0u};
+  if (c + 8 <= d) return *(const uint2any*)(row + c);
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+    if (c + j < d) x[j >> 2] |= (uint32_t)row[c + j] << (8 * (j & 3));
+  return x;
+}
+__device__ __forceinline__ void store_codes(uint8_t* row, int c, int d, uint2v x) {
+  if (c + 8 <= d) { *(uint2any*)(row + c) = x; return; }
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+    if (c + j < d) row[c + j] = (uint8_t)(x[j >> 2] >> (8 * (j & 3)));
+}
+
+// Blocks that n new rows touch start at slot floor(offset / rows of a block) + 2 i of a launch: they are floor(n / rows) + 2 at most.
+__device__ __forceinline__ void touched(const Cache8Params& p, int slot, int& seq, int& nth) {
+  if (!p.q_off) {
+    const int per = ((p.q_rows + (1 << p.shift) - 2) >> p.shift) + 1;
+    seq = slot / per;
+    nth = slot - seq * per;
+    return;
+  }
+  int lo = 0, hi = p.nseq - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if ((seq_clamp(p.q_off[mid], 0, p.q_rows) >> p.shift) + 2 * mid <= slot) lo = mid; else hi = mid - 1;
+  }
+  seq = lo;
+  nth = slot - ((seq_clamp(p.q_off[lo], 0, p.q_rows) >> p.shift) + 2 * lo);
+}
+
+constexpr int THREADS = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS) k_cache8_append(Cache8Params p) {
+  __shared__ uint32_t tops[THREADS / 64];
+  unsigned id = blockIdx.x;
+  const int head = (int)(id % (unsigned)p.heads);
+  id /= (unsigned)p.heads;
+  const bool is_v = id & 1;
+  int seq, nth;
+  touched(p, (int)(id >> 1), seq, nth);
+  if (nth < 0) return;                                     // (offsets that do not ascend)
+  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq);
+  const int length = p.k_len ? seq_clamp(p.k_len[seq], 0, p.k_rows) : p.k_rows;
+  const int first = length - q.n, from = first > 0 ? first : 0;      // cache rows from .. length - 1 are new
+  const int block = (from >> p.shift) + nth, lo = block << p.shift;
+  if (q.n == 0 || lo >= length) return;
+  const int hi = min(lo + (1 << p.shift), length), start = max(lo, from);
+  const HeadsPtr& in = is_v ? p.v : p.k;
+  const HeadsPtr& out = is_v ? p.cv : p.ck;
+  uint8_t* scale = (is_v ? p.vs : p.ks) + ((int64_t)seq * p.blocks + block) * p.heads + head;
+  const int was = *scale, chunks = (p.d + 7) >> 3, items = (hi - start) * chunks;
+  const T* src = (const T*)in.p + (int64_t)q.seq * in.bs + (int64_t)head * in.hs;
+  uint8_t* dst = (uint8_t*)const_cast<char*>(out.p) + (int64_t)seq * out.bs + (int64_t)head * out.hs;
+  auto new_row = [&](int r) { return src + (int64_t)(q.base + start + r - first) * in.ts; };
+  uint32_t top = 0;
+  for (int i = threadIdx.x; i < items; i += THREADS) {
+    const int r = i / chunks;
+    float x[8];
+    load8(new_row(r), (i - r * chunks) * 8, p.d, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t b = __float_as_uint(x[j]) & 0x7fffffffu;
+      top = max(top, b < INF_BITS ? b : 0u);
+    }
+  }
+  top = __float_as_uint(over_lanes<64>(__uint_as_float(top), [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) top = max(top, tops[w]);
+  const int need = least_byte(top), e = start > lo ? max(was, need) : need;
+  for (int i = threadIdx.x; i < items; i += THREADS) {
+    const int r = i / chunks, c = (i - r * chunks) * 8;
+    float x[8];
+    load8(new_row(r), c, p.d, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = coded(x[j], e);
+    store_codes(dst + (int64_t)(start + r) * out.ts, c, p.d, uint2v{codes4(x[0], x[1], x[2], x[3]), codes4(x[4], x[5], x[6], x[7])});
+  }
+  if (start > lo && e != was) {
+    for (int i = threadIdx.x; i < (start - lo) * chunks; i += THREADS) {
+      const int r = i / chunks, c = (i - r * chunks) * 8;
+      uint8_t* row = dst + (int64_t)(lo + r) * out.ts;
+      const uint2v was_codes = load_codes(row, c, p.d);
+      uint2v now;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x[4];
+        values4(was_codes[h], x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_ldexpf(x[j], was - e);
+        now[h] = codes4(x[0], x[1], x[2], x[3]);
+      }
+      store_codes(row, c, p.d, now);
+    }
+  }
+  __syncthreads();      // (every wave has the byte that it found)
+  if (threadIdx.x == 0) *scale = (uint8_t)e;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS) k_cache8_read(Cache8Params p, int per) {
+  unsigned id = blockIdx.x;
+  const int part = (int)(id % (unsigned)per);
+  id /= (unsigned)per;
+  const bool is_v = id & 1;
+  const int seq = (int)(id >> 1);
+  const int length = p.k_len ? seq_clamp(p.k_len[seq], 0, p.k_rows) : p.k_rows;
+  const unsigned chunks = (unsigned)(p.d + 7) >> 3, row_items = chunks * (unsigned)p.heads;
+  const int64_t i = (int64_t)part * THREADS + threadIdx.x;
+  if (i >= (int64_t)length * row_items) return;
+  const int r = (int)(i / row_items);
+  const unsigned in_row = (unsigned)(i - (int64_t)r * row_items);
+  const int head = (int)(in_row / chunks), c = (int)(in_row - (unsigned)head * chunks) * 8;
+  const HeadsPtr& from = is_v ? p.cv : p.ck;
+  const HeadsPtr& to = is_v ? p.v : p.k;
+  const int e = (is_v ? p.vs : p.ks)[((int64_t)seq * p.blocks + (r >> p.shift)) * p.heads + head];
+  const uint2v codes = load_codes((const uint8_t*)from.p + (int64_t)seq * from.bs + (int64_t)r * from.ts + (int64_t)head * from.hs, c, p.d);
+  float x[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float y[4];
+    values4(codes[h], y);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[4 * h + j] = e == 255 ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(y[j], e - 127);
+  }
+  T* row = (T*)const_cast<char*>(to.p) + (int64_t)seq * to.bs + (int64_t)r * to.ts + (int64_t)head * to.hs;
+#pragma unroll
+  for (int h = 0; h < 8 / PW<T>; ++h) {
+    Piece<T> o;
+#pragma unroll
+    for (int j = 0; j < PW<T>; j += 2) o.set(j, x[h * PW<T> + j], x[h * PW<T> + j + 1]);
+    o.store(row, c + h * PW<T>, p.d);
+  }
+}
+
+constexpr int64_t MOST_BLOCKS = (int64_t)1 << 23;
+
+}  // namespace
+
+hipError_t launch_cache8_append(const Cache8Params& p, int dtype, hipStream_t st) {
+  const int64_t rows = (int64_t)1 << p.shift;
+  const int64_t slots = p.q_off ? p.q_rows / rows + 2 * (int64_t)p.nseq : (int64_t)p.nseq * ((p.q_rows + rows - 2) / rows + 1);
+  if (p.q_rows == 0 || slots == 0) return hipSuccess;
+  if (slots >= MOST_BLOCKS || slots * 2 * p.heads >= MOST_BLOCKS) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)(slots * 2 * p.heads));
+  if (dtype == FREQATTN_BF16) hipLaunchKernelGGL(k_cache8_append<Bf16>, grid, dim3(THREADS), 0, st, p);
+  else hipLaunchKernelGGL(k_cache8_append<float>, grid, dim3(THREADS), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache8_read(const Cache8Params& p, int dtype, hipStream_t st) {
+  const int64_t chunks = (p.d + 7) / 8, per = ((int64_t)p.k_rows * chunks * p.heads + THREADS - 1) / THREADS;
+  if (per == 0 || p.nseq == 0) return hipSuccess;
+  if (per >= MOST_BLOCKS || per * 2 * p.nseq >= MOST_BLOCKS) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)(per * 2 * p.nseq));
+  if (dtype == FREQATTN_BF16) hipLaunchKernelGGL(k_cache8_read<Bf16>, grid, dim3(THREADS), 0, st, p, (int)per);
+  else hipLaunchKernelGGL(k_cache8_read<float>, grid, dim3(THREADS), 0, st, p, (int)per);
+  return hipGetLastError();
+}
+
+}  // namespace fa

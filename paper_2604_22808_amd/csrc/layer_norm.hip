@@ -1,0 +1,315 @@
+// Layer norm over the channels of token rows, forward and backward.
+//
+//   m = mean_c x_c,  r = (mean_c (x_c - m)^2 + eps)^-1/2,  h = (x - m) r,  y = h w + b
+//   backward: g = dy w,  dx = r (g - mean g - h mean(g h)),  dw = sum over rows of dy h,  db = sum over rows of dy
+//
+// Bound by memory: the forward pass reads a row and writes one, the backward pass reads two and writes one.  A row lies in the registers of LPR lanes, or of W
+// waves where it is longer than one wave holds, so that mean and centred squares are taken one after the other from one read; the next row is requested before the
+// present one is worked on.  The mean as it comes out of fp32 is off by some of its steps, which rows far from zero would feel: the sum of the
+// centred values, taken beside their squares, puts that right.  A wave keeps the weights and, in the backward pass, its share of dw and db in registers over all its rows;
+// a workgroup adds its waves' shares in their order and stores one row of partial sums, k_norm_weights adds those: no atomics, equal calls give equal bits.
+#include "rows.h"
+#include "tokens.h"
+
+namespace fa {
+
+using namespace rows;
+
+namespace {
+
+// (var + eps)^-1/2 (the instruction is within one step; its argument is a normal number unless both are about zero)
+__device__ __forceinline__ float inv_root(float v) { return v < 1e-30f ? 1.f / sqrtf(v) : __builtin_amdgcn_rsqf(v); }
+
+// Sums of N values over a row's lanes; those of W waves meet in LDS, in the order of the waves.  `turn` alternates between two places, so that one barrier a sum
+// is enough.
+template <int LPR, int W, int N>
+__device__ __forceinline__ void row_sums(float (&x)[N], float (*lds)[W][4], int& turn, int wave) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = over_lanes<LPR>(x[i], add);
+  if constexpr (W > 1) {
+    float (*at)[4] = lds[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) at[wave][i] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float s = at[0][i];
+#pragma unroll
+      for (int w = 1; w < W; ++w) s += at[w][i];
+      x[i] = s;
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ T* row_at(const RowsPtr& v, const NormParams& p, int64_t i) {
+  return p.groups == 1 ? row_of<T>(v, p.rows, i) : (T*)v.p + (int64_t)blockIdx.y * v.bs + i * v.rs;
+}
+
+// Centred values d of a row's pieces (zero where there is no channel).
+template <typename T, int LPR, int W, int PT>
+__device__ __forceinline__ void centre(const Piece<T> (&x)[PT], float (&d)[PT][PW<T>], const Place<T, LPR, W, PT>& at, int n, float mean) {
+#pragma unroll
+  for (int i = 0; i < PT; ++i) {
+    const int c = at.channel(i);
+    const float m = c < n ? mean : 0.f;
+#pragma unroll
+    for (int j = 0; j < PW<T>; ++j) d[i][j] = x[i].get(j) - m;
+    if (c < n && c + PW<T> > n) {
+#pragma unroll
+      for (int j = 1; j < PW<T>; ++j) d[i][j] = c + j < n ? d[i][j] : 0.f;
+    }
+  }
+}
+
+template <typename T, int PT>
+__device__ __forceinline__ float sum_of(const Piece<T> (&x)[PT]) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < PT; ++i)
+#pragma unroll
+    for (int j = 0; j < PW<T>; ++j) s[j & 3] += x[i].get(j);
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+template <typename T, int LPR, int W, int PT>
+__global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm(NormParams p) {
+  using At = Place<T, LPR, W, PT>;
+  __shared__ float lds[2][W][4];
+  At at;
+  at.set();
+  const int n = p.channels, wave = threadIdx.x >> 6;
+  const float inv_n = 1.f / (float)n;
+  int turn = 0;
+  Piece<T> w[PT], b[PT], x[PT], next[PT];
+#pragma unroll
+  for (int i = 0; i < PT; ++i) {
+    const int c = at.channel(i);
+    w[i].load((const T*)p.w + (int64_t)blockIdx.y * n, c, p.w ? n : 0);
+    if (!p.w) {
+#pragma unroll
+      for (int j = 0; j < PW<T>; j += 2) w[i].set(j, 1.f, 1.f);
+    }
+    b[i].load((const T*)p.b + (int64_t)blockIdx.y * n, c, p.b ? n : 0);
+  }
+  auto request = [&](int64_t i) {
+    const T* row = row_at<T>(p.x, p, i < p.n ? i : 0);
+#pragma unroll
+    for (int k = 0; k < PT; ++k) next[k].load(row, at.channel(k), i < p.n ? n : 0);
+  };
+  const int64_t step = (int64_t)gridDim.x * At::STEP;
+  int64_t i = (int64_t)blockIdx.x * At::STEP;
+  if (At::AHEAD) request(i + at.row);
+  for (; i < p.n; i += step) {
+    if (!At::AHEAD) request(i + at.row);
+#pragma unroll
+    for (int k = 0; k < PT; ++k) x[k] = next[k];
+    if (At::AHEAD && i + step < p.n) request(i + step + at.row);
+    float s[1] = {sum_of<T, PT>(x)};
+    row_sums<LPR, W>(s, lds, turn, wave);
+    float d[PT][PW<T>];
+    centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n);
+    float q[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < PT; ++k)
+#pragma unroll
+      for (int j = 0; j < PW<T>; ++j) {
+        q[0] += d[k][j];
+        q[1] = __builtin_fmaf(d[k][j], d[k][j], q[1]);
+      }
+    row_sums<LPR, W>(q, lds, turn, wave);
+    const float dm = q[0] * inv_n, r = inv_root(__builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps), k0 = -dm * r;
+    if (i + at.row < p.n) {
+      T* row = row_at<T>(p.y, p, i + at.row);
+#pragma unroll
+      for (int k = 0; k < PT; ++k) {
+        Piece<T> o;
+#pragma unroll
+        for (int j = 0; j < PW<T>; j += 2)
+          o.set(j, __builtin_fmaf(__builtin_fmaf(d[k][j], r, k0), w[k].get(j), b[k].get(j)),
+                __builtin_fmaf(__builtin_fmaf(d[k][j + 1], r, k0), w[k].get(j + 1), b[k].get(j + 1)));
+        o.store(row, at.channel(k), n);
+      }
+    }
+  }
+}
+
+template <typename T, int LPR, int W, int PT>
+__global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_backward(NormParams p) {
+  using At = Place<T, LPR, W, PT>;
+  __shared__ float lds[2][W][4];
+  At at;
+  at.set();
+  const int n = p.channels, wave = threadIdx.x >> 6;
+  const float inv_n = 1.f / (float)n;
+  int turn = 0;
+  Piece<T> w[PT], x[PT], dy[PT], nx[PT], ny[PT];
+  float dw[PT][PW<T>], db[PT][PW<T>];
+#pragma unroll
+  for (int i = 0; i < PT; ++i) {
+    w[i].load((const T*)p.w + (int64_t)blockIdx.y * n, at.channel(i), p.w ? n : 0);
+    if (!p.w) {
+#pragma unroll
+      for (int j = 0; j < PW<T>; j += 2) w[i].set(j, 1.f, 1.f);
+    }
+#pragma unroll
+    for (int j = 0; j < PW<T>; ++j) dw[i][j] = db[i][j] = 0.f;
+  }
+  auto request = [&](int64_t i) {
+    const T *rx = row_at<T>(p.x, p, i < p.n ? i : 0), *ry = row_at<T>(p.dy, p, i < p.n ? i : 0);
+#pragma unroll
+    for (int k = 0; k < PT; ++k) {
+      nx[k].load(rx, at.channel(k), i < p.n ? n : 0);
+      ny[k].load(ry, at.channel(k), i < p.n ? n : 0);
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * At::STEP;
+  int64_t i = (int64_t)blockIdx.x * At::STEP;
+  if (At::AHEAD && i < p.n) request(i + at.row);
+  for (; i < p.n; i += step) {
+    if (!At::AHEAD) request(i + at.row);
+#pragma unroll
+    for (int k = 0; k < PT; ++k) { x[k] = nx[k]; dy[k] = ny[k]; }
+    if (At::AHEAD && i + step < p.n) request(i + step + at.row);
+    float s[1] = {sum_of<T, PT>(x)};
+    row_sums<LPR, W>(s, lds, turn, wave);
+    float d[PT][PW<T>];
+    centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n);
+    float q[4] = {0.f, 0.f, 0.f, 0.f};     // sums of d, d^2, g, g d
+#pragma unroll
+    for (int k = 0; k < PT; ++k)
+#pragma unroll
+      for (int j = 0; j < PW<T>; ++j) {
+        const float g = dy[k].get(j) * w[k].get(j);
+        q[0] += d[k][j];
+        q[1] = __builtin_fmaf(d[k][j], d[k][j], q[1]);
+        q[2] += g;
+        q[3] = __builtin_fmaf(g, d[k][j], q[3]);
+      }
+    row_sums<LPR, W>(q, lds, turn, wave);
+    const float dm = q[0] * inv_n, r = inv_root(__builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps), k0 = -dm * r;
+    const float mg = q[2] * inv_n, mgh = r * __builtin_fmaf(-dm, q[2], q[3]) * inv_n;
+    if (i + at.row < p.n) {
+      T* row = row_at<T>(p.dx, p, i + at.row);
+#pragma unroll
+      for (int k = 0; k < PT; ++k) {
+        Piece<T> o;
+        float v[PW<T>];
+#pragma unroll
+        for (int j = 0; j < PW<T>; ++j) {
+          const float y = dy[k].get(j), g = y * w[k].get(j), h = __builtin_fmaf(d[k][j], r, k0);
+          dw[k][j] = __builtin_fmaf(y, h, dw[k][j]);
+          db[k][j] += y;
+          v[j] = r * (g - __builtin_fmaf(h, mgh, mg));
+        }
+#pragma unroll
+        for (int j = 0; j < PW<T>; j += 2) o.set(j, v[j], v[j + 1]);
+        o.store(row, at.channel(k), n);
+      }
+    }
+  }
+  if (!p.dw && !p.db) return;
+  // the rows' lanes that hold the same channels, in their order: lanes of a wave, then waves
+  float* to[2] = {p.dw ? p.dw + (int64_t)blockIdx.y * n : nullptr, p.db ? p.db + (int64_t)blockIdx.y * n : nullptr};
+  if (p.blocks > 1) {
+    to[0] = p.part + ((int64_t)blockIdx.y * p.blocks + blockIdx.x) * 2 * n;
+    to[1] = to[0] + n;
+  }
+  __shared__ float sums[W == 1 ? 4 : 1][W == 1 ? PT * PW<T> * LPR : 1];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if constexpr (W == 1) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < PT; ++k)
+#pragma unroll
+        for (int j = 0; j < PW<T>; ++j) {
+          float v = which ? db[k][j] : dw[k][j];
+#pragma unroll
+          for (int o = LPR; o < 64; o <<= 1) v += __shfl_xor(v, o);
+          if ((threadIdx.x & 63) < LPR) sums[wave][(k * PW<T> + j) * LPR + at.lane] = v;
+        }
+      __syncthreads();
+      if (to[which]) {
+        for (int c = threadIdx.x; c < n; c += 256) {
+          const int piece = c / PW<T>, slot = (piece / LPR * PW<T> + c % PW<T>) * LPR + piece % LPR;
+          to[which][c] = (sums[0][slot] + sums[1][slot]) + (sums[2][slot] + sums[3][slot]);
+        }
+      }
+    } else if (to[which]) {
+#pragma unroll
+      for (int k = 0; k < PT; ++k)
+#pragma unroll
+        for (int j = 0; j < PW<T>; ++j)
+          if (at.channel(k) + j < n) to[which][at.channel(k) + j] = which ? db[k][j] : dw[k][j];
+    }
+  }
+}
+
+// dw[c], db[c] = sums over the workgroups' rows; a workgroup adds 32 columns of a group's 2 * channels, 32 threads a column.
+__global__ void __launch_bounds__(1024) k_norm_weights(NormParams p) {
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
+  const float* part = p.part + (int64_t)blockIdx.y * p.blocks * 2 * p.channels;
+  float s = 0.f;
+  if (c < 2 * p.channels) {
+#pragma unroll 8
+    for (int i = row; i < p.blocks; i += 32) s += part[(int64_t)i * 2 * p.channels + c];
+  }
+  __shared__ float acc[32][33];
+  acc[row][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (row == 0 && c < 2 * p.channels) {
+    float r = 0.f;
+    for (int i = 0; i < 32; ++i) r += acc[i][threadIdx.x & 31];
+    float* to = c < p.channels ? p.dw : p.db;
+    if (to) to[(int64_t)blockIdx.y * p.channels + (c < p.channels ? c : c - p.channels)] = r;
+  }
+}
+
+constexpr int FWD_WAVES = 16, BWD_WAVES = 8;
+
+}  // namespace
+
+int norm_backward_blocks(int64_t n, int64_t groups, int channels, int dtype, int num_cu) {
+  auto of = [&](auto l, auto w, auto) {
+    using At = Place<float, l.value, w.value, 1>;
+    const int64_t b = blocks_of(n, groups, At::STEP, At::THREADS, BWD_WAVES, num_cu);
+    return (int)(b < 1 ? 1 : b);
+  };
+  return dtype == FREQATTN_BF16 ? for_channels<Bf16>(channels, of) : for_channels<float>(channels, of);
+}
+
+template <typename T>
+static hipError_t forward(const NormParams& p, int num_cu, hipStream_t st) {
+  return for_channels<T>(p.channels, [&](auto l, auto w, auto pt) {
+    using At = Place<T, l.value, w.value, pt.value>;
+    const int64_t blocks = blocks_of(p.n, p.groups, At::STEP, At::THREADS, FWD_WAVES, num_cu);
+    hipLaunchKernelGGL((k_layer_norm<T, l.value, w.value, pt.value>), dim3((unsigned)blocks, (unsigned)p.groups), dim3(At::THREADS), 0, st, p);
+    return hipGetLastError();
+  });
+}
+template <typename T>
+static hipError_t backward(const NormParams& p, hipStream_t st) {
+  return for_channels<T>(p.channels, [&](auto l, auto w, auto pt) {
+    using At = Place<T, l.value, w.value, pt.value>;
+    hipLaunchKernelGGL((k_layer_norm_backward<T, l.value, w.value, pt.value>), dim3((unsigned)p.blocks, (unsigned)p.groups), dim3(At::THREADS), 0, st, p);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_layer_norm(NormParams p, int dtype, int num_cu, hipStream_t st) {
+  return dtype == FREQATTN_BF16 ? forward<Bf16>(p, num_cu, st) : forward<float>(p, num_cu, st);
+}
+
+hipError_t launch_layer_norm_backward(NormParams p, int dtype, int num_cu, hipStream_t st) {
+  p.blocks = norm_backward_blocks(p.n, p.groups, p.channels, dtype, num_cu);
+  const hipError_t e = dtype == FREQATTN_BF16 ? backward<Bf16>(p, st) : backward<float>(p, st);
+  if (e != hipSuccess || p.blocks == 1 || (!p.dw && !p.db)) return e;
+  hipLaunchKernelGGL(k_norm_weights, dim3((unsigned)((2 * p.channels + 31) / 32), (unsigned)p.groups), dim3(1024), 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace fa

@@ -19,6 +19,7 @@
 #include <hip/hip_runtime.h>
 
 #include "seq_common.h"
+#include "tokens.h"
 
 namespace fa {
 
@@ -30,7 +31,9 @@ typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
 namespace {
 
 struct Bf16 { uint16_t u; };
+struct E4m3 { uint8_t u; };    // a code of a cache held in 8 bits
 __device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(E4m3 x) { return __builtin_amdgcn_cvt_f32_fp8((int)x.u, 0); }
 __device__ __forceinline__ float widen(Bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(Bf16* p, float x) { p->u = __builtin_bit_cast(uint16_t, (__bf16)x); }
@@ -62,7 +65,7 @@ template <typename T>
 __device__ __forceinline__ float4v chunk(const T* row, int c, int d, bool live, int vec) {
   float4v x = {0.f, 0.f, 0.f, 0.f};
   if (!live || c >= d) return x;
-  if (vec) {
+  if (vec && sizeof(T) > 1) {
     if constexpr (sizeof(T) == 4) return *(const float4v*)(row + c);
     const uint2v u = *(const uint2v*)(row + c);
     return float4v{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
@@ -166,6 +169,15 @@ struct Fetch {
       x[j] = chunk(at, c, d, at != nullptr, vec);
     }
   }
+  // codes to values: times the scale 2^(byte - 127) of their row, by(r) the byte (255: NaN)
+  template <typename F> __device__ __forceinline__ void scale(int lane, F&& by) {
+#pragma unroll
+    for (int j = 0; j < TR * D / 256; ++j) {
+      const int e = by((j * 64 + lane) / (D / 4));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[j][k] = e == 255 ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(x[j][k], e - 127);
+    }
+  }
   __device__ __forceinline__ void store(float* tile, int lane) {
 #pragma unroll
     for (int j = 0; j < TR * D / 256; ++j) {
@@ -198,8 +210,9 @@ __device__ __forceinline__ void join_waves(const float16v (&acc)[D / 32], float*
 }
 __device__ __forceinline__ int channel_of(int reg, int g) { return (reg >> 4) * 32 + 8 * ((reg & 15) >> 2) + 4 * g + (reg & 3); }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_fwd(SeqParams p) {
+// KV: type of the keys and values; E4m3 takes them from a cache held in 8 bits with the scales `sc`.
+template <typename T, int D, typename KV = T>
+__global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_fwd(SeqParams p, Cache8Scales sc) {
   constexpr int NW = waves<D>(), TF = tile_floats<D>();
   __shared__ __attribute__((aligned(16))) float tiles[NW][2 * TF];
   __shared__ float ms[NW][64], ls[NW][64];
@@ -216,10 +229,16 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_fwd(SeqParam
   const int first_last = query_row(p, kvh, tile * TR, q.n, k.n).last;
   const float c2 = p.scale * LOG2E;
   float *Ks = tiles[wave], *Vs = tiles[wave] + TF;
-  Fetch<T, D> fk, fv;
+  Fetch<KV, D> fk, fv;
   auto fetch = [&](int key0) {
-    fk.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.k, k.seq, k.base + key0 + r, kvh) : nullptr; });
-    fv.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<T>(p.v, k.seq, k.base + key0 + r, kvh) : nullptr; });
+    fk.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<KV>(p.k, k.seq, k.base + key0 + r, kvh) : nullptr; });
+    fv.load(lane, p.d, p.vec, [&](int r) { return key0 + r < k.n ? row_of<KV>(p.v, k.seq, k.base + key0 + r, kvh) : nullptr; });
+    if constexpr (sizeof(KV) == 1) {
+      const int64_t at = (int64_t)k.seq * sc.blocks * p.hk + kvh;
+      auto byte = [&](const uint8_t* s, int r) { return key0 + r < k.n ? (int)s[at + (int64_t)((key0 + r) >> sc.shift) * p.hk] : 127; };
+      fk.scale(lane, [&](int r) { return byte(sc.k, r); });
+      fv.scale(lane, [&](int r) { return byte(sc.v, r); });
+    }
   };
   float16v O[D / 32];
 #pragma unroll
@@ -471,11 +490,11 @@ __global__ void __launch_bounds__(64 * waves<D>(), 1) k_seq_generic_dkv(SeqParam
   store(p.dv, dV, 1.f);
 }
 
-template <typename T, int D>
-hipError_t fwd(SeqParams p, hipStream_t st) {
+template <typename T, int D, typename KV = T>
+hipError_t fwd(SeqParams p, hipStream_t st, const Cache8Scales& sc = {}) {
   p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, TR);
   if (p.slots == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_seq_generic_fwd<T, D>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(64 * waves<D>()), 0, st, p);
+  hipLaunchKernelGGL((k_seq_generic_fwd<T, D, KV>), dim3((unsigned)p.slots * (unsigned)p.hk), dim3(64 * waves<D>()), 0, st, p, sc);
   return hipGetLastError();
 }
 template <typename T, int D>
@@ -494,6 +513,10 @@ hipError_t bwd(SeqParams p, hipStream_t st) {
 hipError_t launch_seq_generic_fwd(const SeqParams& p, int dtype, hipStream_t st) {
   if (dtype == FREQATTN_BF16) return p.d <= 64 ? fwd<Bf16, 64>(p, st) : fwd<Bf16, 128>(p, st);
   return p.d <= 64 ? fwd<float, 64>(p, st) : fwd<float, 128>(p, st);
+}
+hipError_t launch_cache8_generic(const SeqParams& p, const Cache8Scales& sc, int dtype, hipStream_t st) {
+  if (dtype == FREQATTN_BF16) return p.d <= 64 ? fwd<Bf16, 64, E4m3>(p, st, sc) : fwd<Bf16, 128, E4m3>(p, st, sc);
+  return p.d <= 64 ? fwd<float, 64, E4m3>(p, st, sc) : fwd<float, 128, E4m3>(p, st, sc);
 }
 hipError_t launch_seq_generic_bwd(const SeqParams& p, int dtype, hipStream_t st) {
   if (dtype == FREQATTN_BF16) return p.d <= 64 ? bwd<Bf16, 64>(p, st) : bwd<Bf16, 128>(p, st);

@@ -1,0 +1,187 @@
+"""Layer norm on the GPU, forward and backward, against the plain 64-bit form."""
+import math
+
+import pytest
+import torch
+
+from paper_2604_22808_amd import binding as B
+from tests import tokens_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+def place(t, pad, lead):
+    """The host tensor on the device as a view: `pad` channels between rows, `lead` elements in front."""
+    b, n, c = t.shape
+    x = torch.full((lead + b * n * (c + pad),), U.MARK, dtype=t.dtype, device="cuda")[lead:].view(b, n, c + pad)
+    x[..., :c] = t.cuda()
+    return x[..., :c]
+
+
+def make(seed, dtype, b, n, c, each, mean=0.0, spread=1.0):
+    io, gen = U.TYPES[dtype], torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=gen, dtype=torch.float64)   # noqa: E731
+    x = (mean + spread * r(b, n, c)).to(io)
+    shape = (b, c) if each else (c,)
+    return io, x, (1 + 0.3 * r(*shape)).to(io), (0.5 * r(*shape)).to(io), r(b, n, c).to(io)
+
+
+def expect(x, w, b, eps, io, each, dout=None):
+    """{name: (value, bound)} of the whole call."""
+    n, rows, c = x.shape
+    groups = n if each else 1
+    xs = x.double().reshape(groups, -1, c)
+    do = None if dout is None else dout.double().reshape(groups, -1, c)
+    one, zero = torch.ones(groups, c, dtype=torch.float64), torch.zeros(groups, c, dtype=torch.float64)
+    ws = one if w is None else w.double().reshape(groups, c)
+    bs = zero if b is None else b.double().reshape(groups, c)
+    parts = [U.norm(xs[g], ws[g], bs[g], eps, io, None if do is None else do[g]) for g in range(groups)]
+    res = {}
+    for name in parts[0]:
+        shape = x.shape if name in ("out", "dx") else (n, c) if each else (c,)
+        res[name] = tuple(torch.stack([p[name][i] for p in parts]).reshape(shape) for i in range(2))
+    return res
+
+
+SIZES = [(1, 1, 1), (1, 1, 7), (2, 3, 8), (1, 5, 64), (3, 4, 65), (1, 33, 130), (2, 9, 257), (1, 7, 512), (1, 17, 515), (2, 6, 1000), (1, 300, 999), (1, 9, 1536),
+         (2, 130, 1540), (1, 5, 2048), (1, 6, 2500), (1, 4, 4096), (2, 3, 5001), (1, 3, 8192), (1, 3, 9000), (1, 2, 16384)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("b,n,c", SIZES)
+def test_against_the_plain_form(b, n, c, dtype):
+    for each in ((False, True) if b > 1 else (False,)):
+        io, x, w, bias, dout = make(c + n, dtype, b, n, c, each)
+        for pad, lead in ((0, 0), (8, 0), (3, 1)):
+            dx_, do_, out, dx = place(x, pad, lead), place(dout, pad, lead), place(torch.zeros_like(x), pad, lead), place(torch.zeros_like(x), pad, lead)
+            dw, db = (torch.full(w.shape, U.MARK, device="cuda") for _ in range(2))
+            B.layer_norm(dx_, w.cuda(), bias.cuda(), out, eps=1e-5)
+            B.layer_norm_backward(dx_, w.cuda(), do_, dx, dw, db, eps=1e-5)
+            torch.cuda.synchronize()
+            want = expect(x, w, bias, 1e-5, io, each, dout)
+            for name, got in (("out", out), ("dx", dx), ("dw", dw), ("db", db)):
+                U.check((name, b, n, c, dtype, each, pad), got, *want[name])
+            for t in (out, dx):      # nothing between the rows is written
+                base = t._base if t._base is not None else t
+                if pad:
+                    assert bool((t.as_strided((b, n, pad), t.stride(), t.storage_offset() + c) == U.MARK).all()), (base.shape, pad)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mean,spread", [(1000.0, 1.0), (3.0, 1e-3), (0.0, 1e-12), (0.0, 1e12), (-200.0, 50.0)])
+def test_rows_far_from_zero_and_of_any_size(mean, spread, dtype):
+    io, x, w, bias, dout = make(3, dtype, 1, 40, 640, False, mean, spread)
+    out, dx = torch.empty_like(x, device="cuda"), torch.empty_like(x, device="cuda")
+    B.layer_norm(x.cuda(), w.cuda(), bias.cuda(), out)
+    B.layer_norm_backward(x.cuda(), w.cuda(), dout.cuda(), dx)
+    want = expect(x, w, bias, float(torch.tensor(1e-6)), io, False, dout)
+    U.check("out", out, *want["out"])
+    U.check("dx", dx, *want["dx"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_without_weights_in_place_and_rows_alone(dtype):
+    io, x, w, bias, dout = make(4, dtype, 1, 50, 320, False)
+    want = expect(x, None, None, 1e-6, io, False, dout)
+    at = x[0].cuda()
+    B.layer_norm(at, None, None, at)                       # [rows, channels], over its own input
+    U.check("out", at[None], *want["out"])
+    g, dw = dout.cuda(), torch.empty(320, device="cuda")
+    B.layer_norm_backward(x.cuda(), None, g, g, dw)        # dx over dout, no db
+    U.check("dx", g, *want["dx"])
+    U.check("dw", dw, *want["dw"])
+    xx, db = x.cuda(), torch.empty(320, device="cuda")
+    B.layer_norm_backward(xx, None, dout.cuda(), xx, None, db)
+    U.check("dx", xx, *want["dx"])
+    U.check("db", db, *want["db"])
+
+
+def test_expanded_inputs_and_head_major_batches():
+    io, x, w, bias, dout = make(5, "bf16", 1, 12, 256, False)
+    big = x.cuda().expand(3, 12, 256)                       # a broadcast input: every entry counts in the sums
+    out, dx = torch.empty(3, 12, 256, dtype=io, device="cuda"), torch.empty(3, 12, 256, dtype=io, device="cuda")
+    dw, db = torch.empty(256, device="cuda"), torch.empty(256, device="cuda")
+    do = dout.cuda().expand(3, 12, 256)
+    B.layer_norm(big, w.cuda(), bias.cuda(), out)
+    B.layer_norm_backward(big, w.cuda(), do, dx, dw, db)
+    want = expect(x.expand(3, 12, 256), w, bias, 1e-6, io, False, dout.expand(3, 12, 256))
+    for name, got in (("out", out), ("dx", dx), ("dw", dw), ("db", db)):
+        U.check(name, got, *want[name])
+    t = x[0].reshape(3, 4, 256).cuda().transpose(0, 1)      # batch inside the rows
+    out = torch.empty(4, 3, 256, dtype=io, device="cuda")
+    B.layer_norm(t, w.cuda(), bias.cuda(), out)
+    U.check("out", out, *expect(t.cpu(), w, bias, 1e-6, io, False)["out"])
+
+
+def test_constant_rows_zeros_and_values_that_are_not_finite():
+    x = torch.zeros(6, 200)
+    x[1] = 3.25
+    x[2, 5] = math.inf
+    x[3, 7] = math.nan
+    x[4] = torch.randn(200, generator=torch.Generator().manual_seed(1))
+    w, b = torch.full((200,), 2.0), torch.full((200,), 0.5)
+    out = torch.empty(6, 200, device="cuda")
+    B.layer_norm(x.cuda(), w.cuda(), b.cuda(), out)
+    got = out.cpu()
+    assert bool((got[0] == 0.5).all()) and bool((got[1] == 0.5).all()) and bool((got[5] == 0.5).all())
+    assert bool(torch.isnan(got[2:4]).all()) and bool(torch.isfinite(got[4]).all())     # the other rows do not notice
+    B.layer_norm(x.cuda(), w.cuda(), b.cuda(), out, eps=0.0)
+    assert bool(torch.isnan(out[0]).all())                                              # 0 / 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_against_differences(dtype):
+    """The backward pass against differences of the plain forward pass in 64 bits."""
+    io, x, w, bias, dout = make(6, dtype, 1, 3, 24, False)
+    dx, dw, db = torch.empty_like(x, device="cuda"), torch.empty(24, device="cuda"), torch.empty(24, device="cuda")
+    B.layer_norm_backward(x.cuda(), w.cuda(), dout.cuda(), dx, dw, db, eps=1e-3)
+    f = lambda x, w, b: (U.norm(x[0], w, b, 1e-3, io)["out"][0] * dout[0].double()).sum()   # noqa: E731
+    args = [x.double(), w.double(), bias.double()]
+    bounds = expect(x, w, bias, 1e-3, io, False, dout)
+    for i, (name, got) in enumerate((("dx", dx), ("dw", dw), ("db", db))):
+        diff = torch.zeros_like(args[i])
+        for j in range(diff.numel()):
+            e = torch.zeros_like(args[i]).view(-1)
+            e[j] = 1e-5
+            hi, lo = list(args), list(args)
+            hi[i], lo[i] = args[i] + e.view(args[i].shape), args[i] - e.view(args[i].shape)
+            diff.view(-1)[j] = (f(*hi) - f(*lo)) / 2e-5
+        U.check(name, got, diff, bounds[name][1] + 1e-8)     # differences of 1e-5 in 64 bits: 1e-10 and 1e-11 / 1e-5
+
+
+def test_no_rows_and_sums_that_repeat():
+    w = torch.ones(64, device="cuda")
+    for shape in ((0, 5, 64), (2, 0, 64), (0, 64)):
+        x = torch.empty(shape, device="cuda")
+        dw, db = torch.full((64,), U.MARK, device="cuda"), torch.full((64,), U.MARK, device="cuda")
+        B.layer_norm(x, w, w, torch.empty_like(x))
+        B.layer_norm_backward(x, w, x, torch.empty_like(x), dw, db)
+        assert bool((dw == 0).all()) and bool((db == 0).all())
+    x = torch.empty(3, 0, 64, device="cuda")
+    dw = torch.full((3, 64), U.MARK, device="cuda")
+    B.layer_norm_backward(x, torch.ones(3, 64, device="cuda"), x, torch.empty_like(x), dw)
+    assert bool((dw == 0).all())
+    io, x, w, bias, dout = make(7, "bf16", 2, 3000, 512, True)
+    res = []
+    for fill in (0.0, math.nan, math.inf):                 # what a workspace holds does not matter, and equal calls give equal bits
+        need = B.lib().freqattn_layer_norm_workspace(B.NormShape(2, 3000, 512, B.BF16, 1, 1e-6))
+        ws = torch.full((need // 4 + 64,), fill, device="cuda")
+        dx, dw, db = torch.empty_like(x, device="cuda"), torch.empty(2, 512, device="cuda"), torch.empty(2, 512, device="cuda")
+        B.layer_norm_backward(x.cuda(), w.cuda(), dout.cuda(), dx, dw, db, workspace=ws[:need // 4])
+        assert torch.equal(ws[need // 4:].nan_to_num(1.0), torch.full((64,), fill, device="cuda").nan_to_num(1.0))
+        res.append((dx, dw, db))
+    for r in res[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(r, res[0]))
+
+
+def test_rows_behind_2_31_elements():
+    """Offsets pass 32 bits: the last rows of a strided tensor of 5 GB."""
+    base = torch.zeros(2600, 1 << 20, dtype=torch.bfloat16, device="cuda")
+    x = base[:, :40]
+    row = torch.randn(2600, 40, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16)
+    x.copy_(row.cuda())
+    out = torch.empty(2600, 40, dtype=torch.bfloat16, device="cuda")
+    B.layer_norm(x, None, None, out)
+    U.check("out", out[None], *expect(row[None], None, None, 1e-6, torch.bfloat16, False)["out"])
+    B.layer_norm(x, None, None, x)
+    assert torch.equal(x, out)
