@@ -67,6 +67,7 @@ struct SeqPlan {
   int64_t workspace;    // bytes
   int64_t part_at;      // backward: where the partial sums start in it
 };
+enum { MAX_PIECES = 64, SEQ_FEW_KT = 32, SEQ_MANY_KT = 64 };   // pieces of the keys at most; keys of a tile
 SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu);
 hipError_t launch_seq_fwd(SeqParams p, const SeqPlan& s, hipStream_t st);
 SeqPlan seq_bwd_plan(const SeqParams& p, int num_cu);

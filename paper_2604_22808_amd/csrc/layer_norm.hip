@@ -17,8 +17,13 @@ using namespace rows;
 
 namespace {
 
-// (var + eps)^-1/2 (the instruction is within one step; its argument is a normal number unless both are about zero)
-__device__ __forceinline__ float inv_root(float v) { return v < 1e-30f ? 1.f / sqrtf(v) : __builtin_amdgcn_rsqf(v); }
+// (var + eps)^-1/2: the instruction is within one step, which every channel of a row would have alike, so half of a Newton step goes on top.  (Its argument is a normal
+// number unless both are about zero.)
+__device__ __forceinline__ float inv_root(float v) {
+  if (v < 1e-30f || !(v < 3e38f)) return 1.f / sqrtf(v);
+  const float r = __builtin_amdgcn_rsqf(v);
+  return __builtin_fmaf(0.5f * r, __builtin_fmaf(-v * r, r, 1.f), r);
+}
 
 // Sums of N values over a row's lanes; those of W waves meet in LDS, in the order of the waves.  `turn` alternates between two places, so that one barrier a sum
 // is enough.

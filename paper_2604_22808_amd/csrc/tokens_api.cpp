@@ -253,7 +253,7 @@ freqattn_status cache8_attention_params(const char* who, const freqattn_sequence
 extern "C" int64_t freqattn_cache8_attention_workspace(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows) {
   SeqParams p;
   if (guarded([&] { return seq_params("freqattn_cache8_attention_workspace", s, rows, p); }) != FREQATTN_OK) return 0;
-  return 0;
+  return cache8_plan(p, s->dtype, compute_units()).workspace;
 }
 
 extern "C" freqattn_status freqattn_cache8_attention(const freqattn_sequence_shape* s, const freqattn_sequence_rows* rows, const freqattn_heads* q,
@@ -276,6 +276,10 @@ extern "C" freqattn_status freqattn_cache8_attention(const freqattn_sequence_sha
       p.v = k_ptr(p, &cache->v);
     }
     p.lse = lse;
-    return launched(launch_cache8_generic(p, sc, s->dtype, (hipStream_t)stream), who);
+    const SeqPlan plan = cache8_plan(p, s->dtype, compute_units());
+    if (plan.workspace > 0 && (!workspace || workspace_bytes < plan.workspace)) return fail(FREQATTN_EINVAL, who, "workspace too small");
+    if (plan.workspace > 0 && (uintptr_t)workspace % 16) return fail(FREQATTN_EINVAL, who, "workspace must be 16-byte aligned");
+    p.part = (float*)workspace;
+    return launched(p.vec ? launch_cache8_attention(p, sc, plan, s->dtype, (hipStream_t)stream) : launch_cache8_generic(p, sc, s->dtype, (hipStream_t)stream), who);
   });
 }
