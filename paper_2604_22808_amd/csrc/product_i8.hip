@@ -1,7 +1,7 @@
 // Products of rows of 8-bit codes: out[m][n] = s_a[m] s_w[n] sum_k a[m][k] w[n][k] + bias[n], k adjacent in both.  Sums are whole numbers of 32 bits, exact up to 131,071
 // channels, so neither their order nor their cut shows in the result; scaling and bias are fp32, rounded once to the output's type.
 //
-// Three kernels.  Operands are fed to the matrix cores as 16 bytes a lane, k = 16 g .. 16 g + 15 of a product's channels on lane group g; both sides use the same order, so any
+// Operands are fed to the matrix cores as 16 bytes a lane, k = 16 g .. 16 g + 15 of a product's channels on lane group g; both sides use the same order, so any
 // order of the channels will do.
 #include "rows.h"
 #include "tokens.h"
@@ -182,6 +182,20 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) k_product_few(ProductParams p)
     }
 }
 
+// The tile of a workgroup.  Workgroups are dealt to the 8 XCDs in turn and each XCD has an L2 of its own: XCD x takes the x-th eighth of the tiles, in an order that goes through
+// GROUP rows of tiles column by column, so that the tiles that run at the same time share few rows and columns.
+constexpr int GROUP = 4;
+__device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int& mt, int& nt) {
+  const unsigned all = (unsigned)tiles_m * (unsigned)tiles_n, each = (all + 7) / 8;
+  const unsigned id = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= each || id >= all) return false;
+  const unsigned group = id / (GROUP * (unsigned)tiles_n), in = id - group * GROUP * (unsigned)tiles_n;
+  const unsigned rows_ = min((unsigned)GROUP, (unsigned)tiles_m - group * GROUP);
+  nt = (int)(in / rows_);
+  mt = (int)(group * GROUP + in - (unsigned)nt * rows_);
+  return true;
+}
+
 // ---- tiles: TM x TN results a workgroup of four waves, steps of 128 channels copied straight into LDS, one step ahead -----------------------------------------
 // Rows of a step are 128 bytes in LDS; 16-byte chunk c of row r sits at c ^ ((r >> 1) & 7), through the source address, so that the operand reads of 16 rows
 // fall on 16 different bank groups.
@@ -189,10 +203,9 @@ template <typename T, int TM, int TN>
 __global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles_m, int tiles_n) {
   constexpr int MI = TM / 64, NI = TN / 64;     // 32 x 32 products of a wave: its rows TM / 2, its columns TN / 2
   __shared__ __attribute__((aligned(16))) int8_t As[2][TM * 128], Ws[2][TN * 128];
-  const int xcd = blockIdx.x & 7, seq = blockIdx.x >> 3;
-  const int mt = (seq / tiles_n) * 8 + xcd;
-  if (mt >= tiles_m) return;
-  const int m0 = mt * TM, n0 = (seq % tiles_n) * TN;
+  int mt, nt;
+  if (!tile_of(tiles_m, tiles_n, mt, nt)) return;      // (uniform over the workgroup)
+  const int m0 = mt * TM, n0 = nt * TN;
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6);
   const int wm = wave & 1, wn = wave >> 1;
   const int lr = lane >> 3, lc = lane & 7;
@@ -247,19 +260,145 @@ __global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles
   }
 }
 
-enum { ANY, FEW, TILE };
+// ---- wide tiles: 256 x 256 results a workgroup of eight waves, one workgroup a compute unit ---------------------------------------------------------------
+// The tiles of a step of 128 channels are halves of 128 rows, 16 KB each in LDS, two copies of everything (128 KB).  A wave owns 32 rows of either half of A and 64
+// columns of either half of W, and a step is four phases of 8 products, one per pair of halves, in an order in which every phase changes one half only: A0 W0, A0 W1, A1 W1,
+// A1 W0, then (next step) A0 W1, A0 W0, A1 W0, A1 W1.  So half number j of the sequence A0 W0 W1 A1 | A0 W1 W0 A1 | A0 W0 .. is, in phase
+//   j - 9   copied from memory into the place of half j - 8, which every wave has read in phase j - 10,
+//   j - 2   read into registers by every wave, beside the products of that phase,
+//   j - 1 .. j + 2   multiplied.
+// A copy has seven phases to arrive, six of them are always in flight, and no wait in the loop is for the latest ones.
+constexpr int WM = 256, HALF = 128 * 128;
+
+// TAIL: the channels end inside a step.
+template <typename T, bool TAIL>
+__global__ void __launch_bounds__(512, 2) k_product_wide(ProductParams p, int tiles_m, int tiles_n) {
+  __shared__ __attribute__((aligned(16))) int8_t lds[4][2][HALF];   // [A0, A1, W0, W1][step & 1]
+  int mt, nt;
+  if (!tile_of(tiles_m, tiles_n, mt, nt)) return;
+  const int m0 = mt * WM, n0 = nt * WM;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), nn = lane & 31, g = lane >> 5;
+  const int wm = wave & 3, wn = wave >> 2;              // this wave's 32 rows and 64 columns of every half
+  // 16-byte chunk c of row r sits at c ^ ((r >> 1) & 7); the copies: wave w moves rows 16 w .. 16 w + 15 of a half, 8 per instruction
+  int lr = lane >> 3, chunk = ((lane & 7) ^ ((lane >> 4) & 3)) << 4;   // this lane's row and (even instructions) its chunk
+  const int steps = (p.channels + 127) / 128;
+  int k_i = 0;                                          // the step that is copied next
+  const unsigned copy_at = lds_at(lds[0][0] + 16 * wave * 128);
+  auto copy = [&](int buf, int which) {   // 0, 1: A0, A1; 2, 3: W0, W1
+    const int h = which & 1;
+    const bool w = which >= 2;
+    const char* base = (w ? p.w + (int64_t)n0 * p.w_rs : p.a + (int64_t)m0 * p.a_rs) + k_i;   // wave-uniform
+    const int last = (w ? p.outputs - n0 : p.rows - m0) - 1, first = 128 * h + 16 * wave;     // (rows clamped to what exists)
+    const uint32_t rs = (uint32_t)(w ? p.w_rs : p.a_rs);
+    asm volatile("" : "+v"(lr), "+v"(chunk));   // (addresses formed here: kept for the whole loop they would take the operands' registers)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = chunk ^ (i * 64);
+      const char* at = base + (uint32_t)((uint32_t)min(first + 8 * i + lr, last) * rs + (uint32_t)c);
+      if (TAIL) at = k_i + c < p.channels ? at : (const char*)&zero_piece;
+      copy16(at, copy_at + (which * 2 + buf) * HALF + 8 * i * 128);
+    }
+  };
+  auto advance = [&]() {   // (behind the last step: that step again, into places that nobody reads)
+    if (k_i + 128 < p.channels) k_i += 128;
+  };
+
+  int16v acc[4][2];   // [column tile: half of W, 32 columns][row tile: half of A]
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) acc[ct][rt] = zero16();
+  int4v ra[2][4], rw[2][4][2];   // operands: halves of A and of W
+  const int8_t* const a_at = lds[0][0] + (32 * wm + nn) * 128;
+  const int8_t* const w_at = lds[2][0] + (64 * wn + nn) * 128;
+  auto read = [&](int buf, int which) {
+    const int h = which & 1;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const int pos = ((2 * ks + g) ^ ((nn >> 1) & 7)) << 4;
+      if (which < 2) {
+        ra[h][ks] = *(const int4v*)(a_at + (2 * h + buf) * HALF + pos);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) rw[h][ks][c] = *(const int4v*)(w_at + (2 * h + buf) * HALF + c * 32 * 128 + pos);
+      }
+    }
+  };
+  // One phase: half `a` of A and half `w` of W multiplied; the half `rd` read; the half `cp` copied.
+  auto phase = [&](int a, int w, int rd_buf, int rd, int cp_buf, int cp) {
+    // The half to be read has landed (this wave's part; with the barrier, everybody's), and everybody has the half that was read last.
+    asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    copy(cp_buf, cp);
+    read(rd_buf, rd);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) acc[2 * w + c][a] = __builtin_amdgcn_mfma_i32_32x32x32_i8(rw[w][ks][c], ra[a][ks], acc[2 * w + c][a], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  copy(0, 0); copy(0, 2); copy(0, 3); copy(0, 1); advance();   // halves 0 .. 3
+  copy(1, 0); copy(1, 3); copy(1, 2); copy(1, 1); advance();   // 4 .. 7
+  asm volatile("s_waitcnt vmcnt(12)\n\ts_barrier" ::: "memory");
+  read(0, 0); read(0, 2);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  copy(0, 0);                                                   // 8
+  for (int step = 1; step < steps; step += 2) {
+    phase(0, 0, 0, 3, 0, 2);
+    phase(0, 1, 0, 1, 0, 3);
+    phase(1, 1, 1, 0, 0, 1); advance();
+    phase(1, 0, 1, 3, 1, 0);
+    phase(0, 1, 1, 2, 1, 3);
+    phase(0, 0, 1, 1, 1, 2);
+    phase(1, 0, 0, 0, 1, 1); advance();
+    phase(1, 1, 0, 2, 0, 0);
+  }
+  if (steps & 1) {
+    phase(0, 0, 0, 3, 0, 2);
+    phase(0, 1, 0, 1, 0, 3);
+    phase(1, 1, 1, 0, 0, 1);
+    phase(1, 0, 1, 3, 1, 0);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (copies into this workgroup's LDS)
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt) {
+    const int row = m0 + 128 * rt + 32 * wm + nn;
+    const bool live = row < p.rows;
+    const float sa = live ? p.a_scales[row] : 0.f;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+      store_tile<T>(p, acc[ct][rt], row, n0 + 64 * wn + 128 * (ct >> 1) + 32 * (ct & 1), g, sa, live);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+enum { ANY, FEW, TILE, WIDE };
 
 template <typename T, int TM, int TN>
 hipError_t tile(const ProductParams& p, hipStream_t st) {
   const int tiles_m = (int)(((int64_t)p.rows + TM - 1) / TM), tiles_n = (int)(((int64_t)p.outputs + TN - 1) / TN);
-  const int64_t blocks = ((int64_t)tiles_m + 7) / 8 * 8 * tiles_n;
+  const int64_t blocks = ((int64_t)tiles_m * tiles_n + 7) / 8 * 8;
   if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_product_tile<T, TM, TN>), dim3((unsigned)blocks), dim3(256), 0, st, p, tiles_m, tiles_n);
   return hipGetLastError();
 }
 
 template <typename T>
+hipError_t wide(const ProductParams& p, hipStream_t st) {
+  const int tiles_m = (int)(((int64_t)p.rows + WM - 1) / WM), tiles_n = (int)(((int64_t)p.outputs + WM - 1) / WM);
+  const int64_t blocks = ((int64_t)tiles_m * tiles_n + 7) / 8 * 8;
+  if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
+  if (p.channels % 128) hipLaunchKernelGGL((k_product_wide<T, true>), dim3((unsigned)blocks), dim3(512), 0, st, p, tiles_m, tiles_n);
+  else hipLaunchKernelGGL((k_product_wide<T, false>), dim3((unsigned)blocks), dim3(512), 0, st, p, tiles_m, tiles_n);
+  return hipGetLastError();
+}
+
+template <typename T>
 hipError_t go(const ProductParams& p, const ProductPlan& s, hipStream_t st) {
+  // (the wide kernel's rows lie within 2^31 bytes of their tile's first)
+  const bool near = p.a_rs >= 0 && p.a_rs < (1 << 22) && p.w_rs >= 0 && p.w_rs < (1 << 22);
+  if (s.kind == WIDE && near) return wide<T>(p, st);
   if (s.kind == ANY) {
     const int64_t tiles_n = ((int64_t)p.outputs + AM - 1) / AM, blocks = ((int64_t)p.rows + AM - 1) / AM * tiles_n;
     if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
@@ -274,7 +413,7 @@ hipError_t go(const ProductParams& p, const ProductPlan& s, hipStream_t st) {
     else hipLaunchKernelGGL((k_product_few<T, 4>), grid, block, 0, st, p);
     return hipGetLastError();
   }
-  return s.tile_m == 64 ? tile<T, 64, 64>(p, st) : tile<T, 128, 128>(p, st);
+  return s.kind == TILE && s.tile_m == 64 ? tile<T, 64, 64>(p, st) : tile<T, 128, 128>(p, st);
 }
 
 }  // namespace
@@ -284,6 +423,7 @@ ProductPlan product_plan(const ProductParams& p, int num_cu) {
   s.pieces = 1;
   if (!p.vec) { s.kind = ANY; return s; }
   if (p.rows <= 64) { s.kind = FEW; return s; }
+  if (((int64_t)p.rows + 255) / 256 * (((int64_t)p.outputs + 255) / 256) >= num_cu) { s.kind = WIDE; return s; }
   s.kind = TILE;
   s.tile_m = s.tile_n = ((int64_t)p.rows + 127) / 128 * (((int64_t)p.outputs + 127) / 128) >= 2 * (int64_t)num_cu ? 128 : 64;
   return s;
