@@ -91,7 +91,7 @@ __device__ __forceinline__ void in_order() {
 
 // T: type of queries and results, uint16_t for bf16.  D: channels (64, 128), NW: waves, KT: keys of a tile.
 template <typename T, int D, int NW, int KT, bool HALF>
-__global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 2) k_cache8_attention(SeqParams p, Cache8Scales sc) {
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 2) k_cache8_attention(SeqParams p, Cache8Scales sc, SeqCut cut) {
   constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW, TERMS = sizeof(T) == 4 ? 3 : 1;
   constexpr bool ONE = NW == 1;      // one wave: one tile in LDS, the next one in registers; more: the next one is written while this one is used
   constexpr int NB = ONE ? 1 : 2;
@@ -99,14 +99,32 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
   __shared__ __attribute__((aligned(256))) uint16_t Vs[NB][KT * D];
   const int tid = threadIdx.x, lane = tid & 63, nn = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // key heads fastest, then tiles, the longest first, then pieces of the keys
+  // key heads fastest, then tiles, the longest first, then pieces of the keys; one round of few rows: a sequence's tiles and their pieces behind each other
   unsigned id = blockIdx.x;
   const int kvh = (int)(id % (unsigned)p.hk);
   id /= (unsigned)p.hk;
-  const int split = (int)(id / (unsigned)p.slots), slot = (int)(id % (unsigned)p.slots);
-  int seq_i, tile_i;
-  if (ONE) seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, slot, seq_i, tile_i);
-  else if (!seq_query_tile(p, TILE, lane, slot, seq_i, tile_i)) return;
+  int seq_i, tile_i, split, piece = p.split_tiles;
+  if (cut.resident) {
+    int qt, kt;
+    seq_tiles(p, cut, lane, qt, kt);
+    piece = uniform(seq_piece(p, cut, qt, kt));
+    if (!ONE && (int)(id / (unsigned)p.slots) * piece >= max(lane_max(kt), 1)) return;     // (no sequence has that piece)
+    if (ONE) {
+      const int each = seq_pieces(kt, piece), upto = lane_scan(qt * each);
+      if ((int)id >= __builtin_amdgcn_readlane(upto, 63)) return;
+      seq_i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > (int)id));
+      const int at = (int)id - (seq_i ? __builtin_amdgcn_readlane(upto, seq_i - 1) : 0), n = __builtin_amdgcn_readlane(each, seq_i);
+      tile_i = at / n;
+      split = at - tile_i * n;
+    }
+  }
+  if (!ONE || !cut.resident) {
+    split = (int)(id / (unsigned)p.slots);
+    const int slot = (int)(id % (unsigned)p.slots);
+    if (ONE) seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, slot, seq_i, tile_i);
+    else if (!seq_query_tile(p, TILE, lane, slot, seq_i, tile_i)) return;
+  }
+  split = uniform(split);
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(nullptr, p.k_len, p.k_rows, seq_i));
@@ -123,8 +141,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
   const int my_last = row.live ? row.last : wave_last;         // dead rows of a live wave act as its last one; nothing of them is stored
 
   const int t_all = (wg_last + KT) / KT;                       // tiles the workgroup's rows see (0: none)
-  const int t0 = split * p.split_tiles, t1 = p.nsplit > 1 ? min(t0 + p.split_tiles, t_all) : t_all;
-  if (p.nsplit > 1 && t0 >= t_all && split > 0) return;        // (piece 0 of a row that sees nothing stores that)
+  const bool cuts = p.nsplit > 1 && (!cut.resident || (k.n + KT - 1) / KT > piece);     // (a sequence in one piece needs no join)
+  if (!cuts && split > 0) return;
+  const int t0 = cuts ? split * piece : 0, t1 = cuts ? min(t0 + piece, t_all) : t_all;
+  if (cuts && t0 >= t_all && split > 0) return;                // (piece 0 of a row that sees nothing stores that)
 
   bf16x8 Q[TERMS][DK];
   {
@@ -334,18 +354,18 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
   // ---- normalise and store
   l += other_half(l);
   // (a sum of zero: the row sees nothing, or all its scores are -inf and it has no softmax; of a piece, the join tells)
-  const float inv = l > 0.f || l != l ? 1.f / l : p.nsplit == 1 && row.last >= 0 ? __builtin_nanf("") : 0.f;
+  const float inv = l > 0.f || l != l ? 1.f / l : !cuts && row.last >= 0 ? __builtin_nanf("") : 0.f;
   const int64_t col = (p.q_off ? (int64_t)q.base : (int64_t)seq_i * p.q_rows) + row.token, at = (int64_t)row.head * p.lse_rows + col;
   const float lse2 = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY;
   T* dst = (T*)const_cast<char*>(p.o.p) + (int64_t)q.seq * p.o.bs + (int64_t)(q.base + row.token) * p.o.ts + (int64_t)row.head * p.o.hs;
   float* part = p.part + ((int64_t)split * p.hq * p.lse_rows + at) * p.d;
   if (row.live && g == 0) {
-    if (p.nsplit > 1) p.part[(int64_t)p.nsplit * p.hq * p.lse_rows * p.d + (int64_t)split * p.hq * p.lse_rows + at] = lse2;
+    if (cuts) p.part[(int64_t)p.nsplit * p.hq * p.lse_rows * p.d + (int64_t)split * p.hq * p.lse_rows + at] = lse2;
     else if (p.lse) p.lse[at] = lse2 * LN2;
   }
   each_piece(O, inv, g, [&](int c, const float (&o)[8]) {
     if (!row.live || c >= p.d) return;
-    if (p.nsplit > 1) {
+    if (cuts) {
       *(float4v*)(part + c) = float4v{o[0], o[1], o[2], o[3]};
       *(float4v*)(part + c + 4) = float4v{o[4], o[5], o[6], o[7]};
     } else if constexpr (TERMS == 1) {
@@ -357,11 +377,16 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
   });
 }
 
+// Workgroups of a compute unit that run at the same time, by the registers of their waves.
+constexpr int resident(bool fp32, bool wide, bool few) { return few ? (fp32 ? (wide ? 4 : 8) : wide ? 8 : 12) : fp32 && wide ? 1 : 2; }
+
 template <typename T, int D, int NW, int KT>
-hipError_t go(const SeqParams& p, const Cache8Scales& sc, hipStream_t st) {
-  const dim3 grid((unsigned)p.slots * (unsigned)p.nsplit * (unsigned)p.hk);
-  if (p.d % 16) hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, true>), grid, dim3(64 * NW), 0, st, p, sc);
-  else hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, false>), grid, dim3(64 * NW), 0, st, p, sc);
+hipError_t go(const SeqParams& p, const Cache8Scales& sc, const SeqCut& cut, hipStream_t st) {
+  int64_t blocks = (int64_t)p.slots * p.nsplit * p.hk;
+  if (NW == 1 && cut.resident && blocks > cut.resident) blocks = cut.resident;
+  const dim3 grid((unsigned)blocks);
+  if (p.d % 16) hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, true>), grid, dim3(64 * NW), 0, st, p, sc, cut);
+  else hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, false>), grid, dim3(64 * NW), 0, st, p, sc, cut);
   return hipGetLastError();
 }
 
@@ -371,16 +396,41 @@ hipError_t launch(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, hipStre
   p.split_tiles = s.split_tiles;
   p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, s.few ? 32 : 128);
   if (p.slots == 0) return hipSuccess;
+  const SeqCut cut{s.resident, s.few, s.few ? SEQ_FEW_KT : SEQ_MANY_KT, s.few ? 32 : 128};
   hipError_t e;
-  if (s.few) e = p.d <= 64 ? go<T, 64, 1, SEQ_FEW_KT>(p, sc, st) : go<T, 128, 1, SEQ_FEW_KT>(p, sc, st);
-  else e = p.d <= 64 ? go<T, 64, 4, SEQ_MANY_KT>(p, sc, st) : go<T, 128, 4, SEQ_MANY_KT>(p, sc, st);
+  if (s.few) e = p.d <= 64 ? go<T, 64, 1, SEQ_FEW_KT>(p, sc, cut, st) : go<T, 128, 1, SEQ_FEW_KT>(p, sc, cut, st);
+  else e = p.d <= 64 ? go<T, 64, 4, SEQ_MANY_KT>(p, sc, cut, st) : go<T, 128, 4, SEQ_MANY_KT>(p, sc, cut, st);
   if (e != hipSuccess || s.nsplit == 1) return e;
-  return join_pieces<T>(p, s.split_tiles * (s.few ? SEQ_FEW_KT : SEQ_MANY_KT), st);
+  return join_pieces<T>(p, cut, st);
 }
 
 }  // namespace
 
-SeqPlan cache8_plan(const SeqParams& p, int, int num_cu) { return seq_fwd_plan(p, num_cu); }
+// As for bf16 keys; for 2 to 64 sequences the lengths decide on the device how long pieces are (SeqCut), and the plan says how short they may be.
+SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu) {
+  SeqPlan s = seq_fwd_plan(p, num_cu);
+  if (p.nseq < 2 || p.nseq > 64) return s;
+  const int64_t tiles = ((int64_t)p.k_rows + (s.few ? SEQ_FEW_KT : SEQ_MANY_KT) - 1) / (s.few ? SEQ_FEW_KT : SEQ_MANY_KT);
+  const int64_t groups = seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, s.few ? 32 : 128) * p.hk;
+  const int64_t slots = (int64_t)num_cu * resident(dtype == FREQATTN_F32, p.d > 64, s.few);
+  int64_t n;
+  if (s.few) {
+    if (groups > slots) return s;
+    n = slots / (p.hk > 0 ? p.hk : 1);
+    if (n > MAX_PIECES) n = MAX_PIECES;
+  } else {
+    if (groups > 2 * slots || s.nsplit > 1) return s;
+    n = groups > slots + slots / 2 ? 2 : 4;
+    if (n > tiles / 16) n = tiles / 16;
+  }
+  if (n > tiles) n = tiles;
+  if (n < 2) return s;
+  s.split_tiles = (int)((tiles + n - 1) / n);
+  s.nsplit = (int)((tiles + s.split_tiles - 1) / s.split_tiles);
+  s.workspace = s.nsplit > 1 ? (int64_t)s.nsplit * p.hq * p.lse_rows * (p.d + 1) * 4 : 0;
+  s.resident = s.nsplit > 1 ? (int)slots : 0;
+  return s;
+}
 
 hipError_t launch_cache8_attention(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, int dtype, hipStream_t st) {
   return dtype == FREQATTN_BF16 ? launch<uint16_t>(p, sc, s, st) : launch<float>(p, sc, s, st);

@@ -315,7 +315,7 @@ constexpr int FEW_KT = SEQ_FEW_KT, MANY_KT = SEQ_MANY_KT;
 // beside a prompt of 4096 rows (32 / 8 heads, caches of 4096) take 250 us, alone 123 and 142; packed keys count as one long sequence, so that the pieces of 32
 // tokens against 32 x 4096 packed keys are longer than the sequences: 170 us, as a cache 108.
 SeqPlan seq_fwd_plan(const SeqParams& p, int num_cu) {
-  SeqPlan s;
+  SeqPlan s = {};
   const bool packed = p.q_off != nullptr;
   // By the rows of an average sequence and key head: more than 32 would take several one-wave tiles, each reading all keys.
   const int64_t all = (int64_t)p.q_rows * p.group, mean = packed ? (p.nseq ? all / p.nseq : 0) : all;
@@ -349,7 +349,7 @@ hipError_t launch_seq_fwd(SeqParams p, const SeqPlan& s, hipStream_t st) {
   if (s.few) e = p.d <= 64 ? go<64, 1, FEW_KT>(p, st) : go<128, 1, FEW_KT>(p, st);
   else e = p.d <= 64 ? go<64, 4, MANY_KT>(p, st) : go<128, 4, MANY_KT>(p, st);
   if (e != hipSuccess || s.nsplit == 1) return e;
-  return join_pieces<uint16_t>(p, s.split_tiles * (s.few ? FEW_KT : MANY_KT), st);
+  return join_pieces<uint16_t>(p, SeqCut{0, 0, s.few ? FEW_KT : MANY_KT, s.few ? 32 : 128}, st);
 }
 
 }  // namespace fa
