@@ -101,6 +101,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
 
   // key heads fastest, then tiles, the longest first, then pieces of the keys; one round of few rows: a sequence's tiles and their pieces behind each other
   unsigned id = blockIdx.x;
+  if (ONE) {     // heads that share a line of 128 bytes go to one XCD (workgroups are dealt to the 8 of them in turn), which then fetches it once
+    const unsigned f = (unsigned)sc.heads_of_line;
+    id = (id / (8 * f) * 8 + id % 8) * f + id / 8 % f;
+  }
   const int kvh = (int)(id % (unsigned)p.hk);
   id /= (unsigned)p.hk;
   int seq_i, tile_i, split, piece = p.split_tiles;
@@ -120,6 +124,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
   }
   if (!ONE || !cut.resident) {
     split = (int)(id / (unsigned)p.slots);
+    if (ONE && split >= p.nsplit) return;
     const int slot = (int)(id % (unsigned)p.slots);
     if (ONE) seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, slot, seq_i, tile_i);
     else if (!seq_query_tile(p, TILE, lane, slot, seq_i, tile_i)) return;
@@ -384,6 +389,7 @@ template <typename T, int D, int NW, int KT>
 hipError_t go(const SeqParams& p, const Cache8Scales& sc, const SeqCut& cut, hipStream_t st) {
   int64_t blocks = (int64_t)p.slots * p.nsplit * p.hk;
   if (NW == 1 && cut.resident && blocks > cut.resident) blocks = cut.resident;
+  if (NW == 1) blocks = (blocks + 8 * sc.heads_of_line - 1) / (8 * sc.heads_of_line) * (8 * sc.heads_of_line);
   const dim3 grid((unsigned)blocks);
   if (p.d % 16) hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, true>), grid, dim3(64 * NW), 0, st, p, sc, cut);
   else hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, false>), grid, dim3(64 * NW), 0, st, p, sc, cut);
@@ -391,7 +397,8 @@ hipError_t go(const SeqParams& p, const Cache8Scales& sc, const SeqCut& cut, hip
 }
 
 template <typename T>
-hipError_t launch(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, hipStream_t st) {
+hipError_t launch(SeqParams p, Cache8Scales sc, const SeqPlan& s, hipStream_t st) {
+  sc.heads_of_line = p.k.hs != p.d || p.d > 64 ? 1 : p.d > 32 ? 2 : 4;
   p.nsplit = s.nsplit;
   p.split_tiles = s.split_tiles;
   p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, s.few ? 32 : 128);

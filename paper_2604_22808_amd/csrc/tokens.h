@@ -74,6 +74,7 @@ hipError_t launch_cache8_read(const Cache8Params& p, int dtype, hipStream_t st);
 struct Cache8Scales {
   const uint8_t *k, *v;
   int32_t shift, blocks;
+  int32_t heads_of_line;          // heads whose channels share a line of 128 bytes
 };
 SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu);
 hipError_t launch_cache8_attention(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, int dtype, hipStream_t st);

@@ -262,7 +262,7 @@ extern "C" freqattn_status freqattn_cache8_attention(const freqattn_sequence_sha
   return guarded([&]() -> freqattn_status {
     const char* who = "freqattn_cache8_attention";
     SeqParams p;
-    Cache8Scales sc;
+    Cache8Scales sc = {};
     const freqattn_status fs = cache8_attention_params(who, s, rows, cache, p, sc);
     if (fs != FREQATTN_OK) return fs;
     if (p.lse_rows == 0 || p.nseq == 0) return FREQATTN_OK;
