@@ -66,6 +66,7 @@ struct SeqPlan {
   int nsplit, split_tiles;
   int64_t workspace;    // bytes
   int64_t part_at;      // backward: where the partial sums start in it
+  int tile_rows;        // caches in 8 bits: query rows of a tile
   int resident;         // caches in 8 bits: workgroups that run at the same time, where pieces are cut by lengths (SeqCut); else 0
 };
 enum { MAX_PIECES = 64, SEQ_FEW_KT = 32, SEQ_MANY_KT = 64 };   // pieces of the keys at most; keys of a tile

@@ -10,72 +10,14 @@
 // fp32 queries: K and V have no more than 4 significant bits, so products need fp32 only on the other side.  A query and a probability are three bf16
 // numbers of 8 bits each, exactly, and their products run on the bf16 matrix instructions one after the other: 3 of those instead of fp32 products at a sixteenth of
 // their rate.
+#include "cache8_tile.h"
 #include "seq_join.h"
-#include "seq_mfma.h"
-#include "tokens.h"
 
 namespace fa {
 
 using namespace seq;
 
 namespace {
-
-typedef uint4v uint4byte __attribute__((aligned(1)));
-typedef uint2v uint2byte __attribute__((aligned(1)));
-#define FA_GLOBAL __attribute__((address_space(1)))    // (a choice between two addresses is a load of any address space otherwise)
-
-// A tile of KT rows of codes on its way: NP pieces of 16 codes a thread.
-// HALF: the channels end in half a piece (head_dim % 16 = 8).
-template <int D, int NW, int KT, int USE, bool HALF>
-struct CodeTile {
-  static constexpr int PPR = D / 16, TH = 64 * NW, NP = KT * PPR / TH;
-  static_assert(NP >= 1 && KT * PPR % TH == 0 && 64 / PPR <= 16, "");
-  uint4v x[NP];
-  int e[NP];       // bytes of the scales
-  int64_t off;     // of the thread's first piece in a tile
-  __device__ __forceinline__ void set(int64_t ts, int tid) { off = (int64_t)(tid / PPR) * ts + 16 * (tid % PPR); }
-  // rows key0 .. of a sequence of n > key0 rows at `at` (row 0), d channels; what does not exist is zero
-  __device__ __forceinline__ void load(const char* at, int64_t ts, const uint8_t* scales, int hk, int shift, int key0, int n, int d, int wave, int tid) {
-    const int c = 16 * (tid % PPR);
-    const char* const from = at + (int64_t)key0 * ts;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      e[i] = scales[(int64_t)(min(key0 + (i * TH + wave * 64) / PPR, n - 1) >> shift) * hk];     // (uniform over the wave)
-      const char* p = from + (int64_t)(i * (TH / PPR)) * ts + off;
-      const bool in = key0 + (i * TH + tid) / PPR < n;
-      if constexpr (HALF) {
-        const uint2v lo = *(const FA_GLOBAL uint2byte*)(in && c < d ? p : (const char*)&zero_piece);
-        const uint2v hi = *(const FA_GLOBAL uint2byte*)(in && c + 8 < d ? p + 8 : (const char*)&zero_piece);
-        x[i] = uint4v{lo[0], lo[1], hi[0], hi[1]};
-      } else {
-        x[i] = *(const FA_GLOBAL uint4byte*)(in && c < d ? p : (const char*)&zero_piece);
-      }
-    }
-  }
-  __device__ __forceinline__ void store(uint16_t* tile, int tid) const {
-    asm volatile("" : "+v"(tid));      // (addresses formed here: kept for the whole loop they would take the operands' registers)
-    const int p = tid % PPR;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int r = (i * TH + tid) / PPR;
-      const float s = __uint_as_float((uint32_t)e[i] << 23);      // (255: infinity, with which the conversion gives NaN)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint4v y;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          y[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i][2 * h + j], s, false));
-          y[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i][2 * h + j], s, true));
-        }
-        *(uint4v*)(tile + r * D + (((2 * p + h) ^ swizzle<D, USE>(r)) << 3)) = y;
-      }
-    }
-  }
-};
-
-// The upper 16 bits of a and b as two bf16 numbers.
-__device__ __forceinline__ uint32_t high2(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
-__device__ __forceinline__ float high(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 
 // The order of N operands' products, TERMS each: PF operands up front, then one operand (READS reads) behind the products of one.
 template <int N, int PF, int TERMS, int READS>
@@ -89,47 +31,27 @@ __device__ __forceinline__ void in_order() {
   __builtin_amdgcn_sched_group_barrier(0x008, PF * TERMS, 0);
 }
 
-// T: type of queries and results, uint16_t for bf16.  D: channels (64, 128), NW: waves, KT: keys of a tile.
-template <typename T, int D, int NW, int KT, bool HALF>
-__global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 2) k_cache8_attention(SeqParams p, Cache8Scales sc, SeqCut cut) {
-  constexpr int DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW, TERMS = sizeof(T) == 4 ? 3 : 1;
-  constexpr bool ONE = NW == 1;      // one wave: one tile in LDS, the next one in registers; more: the next one is written while this one is used
-  constexpr int NB = ONE ? 1 : 2;
-  __shared__ __attribute__((aligned(256))) uint16_t Ks[NB][KT * D];
-  __shared__ __attribute__((aligned(256))) uint16_t Vs[NB][KT * D];
+// T: type of queries and results, uint16_t for bf16.  D: channels (64, 128).
+template <typename T, int D, bool HALF>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 2) k_cache8_attention(SeqParams p, Cache8Scales sc, SeqCut cut) {
+  constexpr int NW = 4, KT = SEQ_MANY_KT, DT = D / 32, DK = D / 16, T2 = KT / 32, TILE = 32 * NW, TERMS = sizeof(T) == 4 ? 3 : 1;
+  __shared__ __attribute__((aligned(256))) uint16_t Ks[2][KT * D];
+  __shared__ __attribute__((aligned(256))) uint16_t Vs[2][KT * D];
   const int tid = threadIdx.x, lane = tid & 63, nn = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // key heads fastest, then tiles, the longest first, then pieces of the keys; one round of few rows: a sequence's tiles and their pieces behind each other
+  // key heads fastest, then tiles, the longest first, then pieces of the keys
   unsigned id = blockIdx.x;
-  if (ONE) {     // heads that share a line of 128 bytes go to one XCD (workgroups are dealt to the 8 of them in turn), which then fetches it once
-    const unsigned f = (unsigned)sc.heads_of_line;
-    id = (id / (8 * f) * 8 + id % 8) * f + id / 8 % f;
-  }
   const int kvh = (int)(id % (unsigned)p.hk);
   id /= (unsigned)p.hk;
-  int seq_i, tile_i, split, piece = p.split_tiles;
+  const int split = (int)(id / (unsigned)p.slots);
+  int seq_i, tile_i, piece = p.split_tiles;
   if (cut.resident) {
     int qt, kt;
     seq_tiles(p, cut, lane, qt, kt);
     piece = uniform(seq_piece(p, cut, qt, kt));
-    if (!ONE && (int)(id / (unsigned)p.slots) * piece >= max(lane_max(kt), 1)) return;     // (no sequence has that piece)
-    if (ONE) {
-      const int each = seq_pieces(kt, piece), upto = lane_scan(qt * each);
-      if ((int)id >= __builtin_amdgcn_readlane(upto, 63)) return;
-      seq_i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > (int)id));
-      const int at = (int)id - (seq_i ? __builtin_amdgcn_readlane(upto, seq_i - 1) : 0), n = __builtin_amdgcn_readlane(each, seq_i);
-      tile_i = at / n;
-      split = at - tile_i * n;
-    }
+    if (split * piece >= max(lane_max(kt), 1)) return;     // (no sequence has that piece)
   }
-  if (!ONE || !cut.resident) {
-    split = (int)(id / (unsigned)p.slots);
-    if (ONE && split >= p.nsplit) return;
-    const int slot = (int)(id % (unsigned)p.slots);
-    if (ONE) seq_slot(p.q_off, p.q_rows, p.nseq, p.group, TILE, slot, seq_i, tile_i);
-    else if (!seq_query_tile(p, TILE, lane, slot, seq_i, tile_i)) return;
-  }
-  split = uniform(split);
+  if (!seq_query_tile(p, TILE, lane, (int)(id % (unsigned)p.slots), seq_i, tile_i)) return;
   seq_i = uniform(seq_i);
   tile_i = uniform(tile_i);
   const SeqRange q = uniform(seq_range(p.q_off, p.q_len, p.q_rows, seq_i)), k = uniform(seq_range(nullptr, p.k_len, p.k_rows, seq_i));
@@ -169,19 +91,12 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
           float4v y = {0.f, 0.f, 0.f, 0.f};
           if (in) y = *(const float4v*)(src + c + 4 * h);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[4 * h + j] = y[j] != y[j] ? __builtin_nanf("") : y[j];    // (a NaN that its upper bits show)
+          for (int j = 0; j < 4; ++j) x[4 * h + j] = y[j];
         }
+        bf16x8 t[3];
+        three_terms(x, t);
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-          uint4v w;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            w[j] = high2(x[2 * j], x[2 * j + 1]);
-#pragma unroll
-            for (int i = 2 * j; i < 2 * j + 2; ++i) x[i] = fabsf(x[i]) <= 3.4028235e38f ? x[i] - high(x[i]) : 0.f;
-          }
-          Q[t][s] = __builtin_bit_cast(bf16x8, w);
-        }
+        for (int term = 0; term < TERMS; ++term) Q[term][s] = t[term];
       }
     }
   }
@@ -208,9 +123,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
     kt.store(Ks[buf], tid);
     vt.store(Vs[buf], tid);
   };
-  auto settle = [&] {      // this wave's LDS writes and reads are done; of several waves, everybody's
-    if (ONE) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  auto settle = [&] {      // everybody's LDS writes and reads are done
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
 
   float16v O[DT];
@@ -224,26 +138,19 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
     // (the second pass has other things in its registers than the tile after the next)
     if (t0 < t1) {
       load(t0);
-      if (!ONE) {
-        store(0);
-        if (!careful.value && t0 + 1 < t1) load(t0 + 1);
-        settle();
-      }
+      store(0);
+      if (!careful.value && t0 + 1 < t1) load(t0 + 1);
+      settle();
     }
     for (int t = t0; t < t1; ++t) {
-      const int buf = ONE ? 0 : (t - t0) & 1, key0 = t * KT;
+      const int buf = (t - t0) & 1, key0 = t * KT;
       const unsigned Kt = k_lds + buf * TB, Vt = v_lds + buf * TB;
-      if (ONE) {
-        if (careful.value && t > t0) load(t);
-        store(0);
-        if (!careful.value && t + 1 < t1) load(t + 1);
-        settle();
-      } else if (t + 1 < t1) {
+      if (t + 1 < t1) {
         if (careful.value) load(t + 1);
         store(buf ^ 1);
         if (!careful.value && t + 2 < t1) load(t + 2);
       }
-      if (!careful.value && !ONE && key0 > wave_last) {   // (uniform over the wave) none of its rows sees the tile (set_aside needs every wave: all masked below)
+      if (!careful.value && key0 > wave_last) {   // (uniform over the wave) none of its rows sees the tile (set_aside needs every wave: all masked below)
         settle();
         continue;
       }
@@ -252,7 +159,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
       float16v S[T2];
       __builtin_amdgcn_s_setprio(1);
       {
-        constexpr int NS = T2 * DK, PF = ONE && NS >= 8 ? 8 : 4;
+        constexpr int NS = T2 * DK, PF = 4;
         bf16x8 A[PF];
 #pragma unroll
         for (int i = 0; i < PF; ++i) A[i] = kr.get(Kt, i / DK, i % DK);
@@ -284,26 +191,20 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
         for (int t2 = 0; t2 < T2; ++t2)
 #pragma unroll
           for (int s2 = 0; s2 < 2; ++s2) {
-            uint4v pk[TERMS];
+            float x[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              float a = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j], c2, nref));
-              float b = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + 2 * j + 1], c2, nref));
-              ls[j] += a;
-              ls[j] += b;
-              if constexpr (TERMS == 1) {
-                pk[0][j] = pack2(a, b);
-              } else {
-#pragma unroll
-                for (int term = 0; term < TERMS; ++term) {
-                  pk[term][j] = high2(a, b);
-                  a -= high(a);
-                  b -= high(b);
-                }
-              }
+            for (int j = 0; j < 8; ++j) {
+              x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t2][s2 * 8 + j], c2, nref));
+              ls[j >> 1] += x[j];
             }
+            if constexpr (TERMS == 1) {
+              P[0][t2][s2] = __builtin_bit_cast(bf16x8, pack8(x));
+            } else {
+              bf16x8 t[3];
+              three_parts(x, t);
 #pragma unroll
-            for (int term = 0; term < TERMS; ++term) P[term][t2][s2] = __builtin_bit_cast(bf16x8, pk[term]);
+              for (int term = 0; term < TERMS; ++term) P[term][t2][s2] = t[term];
+            }
           }
         return (ls[0] + ls[1]) + (ls[2] + ls[3]);
       };
@@ -336,7 +237,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
       }
       // ---- O^T += V^T P^T
       {
-        constexpr int NS = 2 * T2 * DT, PF = ONE && NS >= 8 ? 8 : 4;
+        constexpr int NS = 2 * T2 * DT, PF = 4;
         bf16x8 A[PF];
 #pragma unroll
         for (int i = 0; i < PF; ++i) A[i] = vr.get(Vt, i % DT, i / DT);
@@ -382,64 +283,63 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 
   });
 }
 
-// Workgroups of a compute unit that run at the same time, by the registers of their waves.
-constexpr int resident(bool fp32, bool wide, bool few) { return few ? (fp32 ? (wide ? 4 : 8) : wide ? 8 : 12) : fp32 && wide ? 1 : 2; }
-
-template <typename T, int D, int NW, int KT>
+template <typename T, int D>
 hipError_t go(const SeqParams& p, const Cache8Scales& sc, const SeqCut& cut, hipStream_t st) {
-  int64_t blocks = (int64_t)p.slots * p.nsplit * p.hk;
-  if (NW == 1 && cut.resident && blocks > cut.resident) blocks = cut.resident;
-  if (NW == 1) blocks = (blocks + 8 * sc.heads_of_line - 1) / (8 * sc.heads_of_line) * (8 * sc.heads_of_line);
-  const dim3 grid((unsigned)blocks);
-  if (p.d % 16) hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, true>), grid, dim3(64 * NW), 0, st, p, sc, cut);
-  else hipLaunchKernelGGL((k_cache8_attention<T, D, NW, KT, false>), grid, dim3(64 * NW), 0, st, p, sc, cut);
+  const dim3 grid((unsigned)p.slots * (unsigned)p.nsplit * (unsigned)p.hk);
+  if (p.d % 16) hipLaunchKernelGGL((k_cache8_attention<T, D, true>), grid, dim3(256), 0, st, p, sc, cut);
+  else hipLaunchKernelGGL((k_cache8_attention<T, D, false>), grid, dim3(256), 0, st, p, sc, cut);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch(SeqParams p, Cache8Scales sc, const SeqPlan& s, hipStream_t st) {
-  sc.heads_of_line = p.k.hs != p.d || p.d > 64 ? 1 : p.d > 32 ? 2 : 4;
+hipError_t launch(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, hipStream_t st) {
   p.nsplit = s.nsplit;
   p.split_tiles = s.split_tiles;
-  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, s.few ? 32 : 128);
+  p.slots = (int)seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 128);
   if (p.slots == 0) return hipSuccess;
-  const SeqCut cut{s.resident, s.few, s.few ? SEQ_FEW_KT : SEQ_MANY_KT, s.few ? 32 : 128};
-  hipError_t e;
-  if (s.few) e = p.d <= 64 ? go<T, 64, 1, SEQ_FEW_KT>(p, sc, cut, st) : go<T, 128, 1, SEQ_FEW_KT>(p, sc, cut, st);
-  else e = p.d <= 64 ? go<T, 64, 4, SEQ_MANY_KT>(p, sc, cut, st) : go<T, 128, 4, SEQ_MANY_KT>(p, sc, cut, st);
+  const SeqCut cut{s.resident, 0, SEQ_MANY_KT, 128};
+  const hipError_t e = p.d <= 64 ? go<T, 64>(p, sc, cut, st) : go<T, 128>(p, sc, cut, st);
   if (e != hipSuccess || s.nsplit == 1) return e;
   return join_pieces<T>(p, cut, st);
 }
 
 }  // namespace
 
-// As for bf16 keys; for 2 to 64 sequences the lengths decide on the device how long pieces are (SeqCut), and the plan says how short they may be.
+// Few rows of an average sequence and key head, up to 32 (seq_fwd_plan), take tiles of 16 or 32 rows.  For 2 to 64 sequences the lengths decide on the device how long pieces
+// are (SeqCut), and the plan says how short they may be; else it cuts by the tensors' sizes.
 SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu) {
   SeqPlan s = seq_fwd_plan(p, num_cu);
-  if (p.nseq < 2 || p.nseq > 64) return s;
-  const int64_t tiles = ((int64_t)p.k_rows + (s.few ? SEQ_FEW_KT : SEQ_MANY_KT) - 1) / (s.few ? SEQ_FEW_KT : SEQ_MANY_KT);
-  const int64_t groups = seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, s.few ? 32 : 128) * p.hk;
-  const int64_t slots = (int64_t)num_cu * resident(dtype == FREQATTN_F32, p.d > 64, s.few);
-  int64_t n;
+  s.tile_rows = 128;
   if (s.few) {
-    if (groups > slots) return s;
-    n = slots / (p.hk > 0 ? p.hk : 1);
-    if (n > MAX_PIECES) n = MAX_PIECES;
-  } else {
-    if (groups > 2 * slots || s.nsplit > 1) return s;
+    const int64_t all = (int64_t)p.q_rows * p.group, mean = p.q_off ? (p.nseq ? all / p.nseq : 0) : all;
+    s.tile_rows = mean <= 16 ? 16 : 32;
+  }
+  const bool lengths = p.nseq >= 2 && p.nseq <= 64;
+  const int64_t kt = s.few ? 32 * CACHE8_FEW_WAVES : SEQ_MANY_KT, tiles = ((int64_t)p.k_rows + kt - 1) / kt;
+  const int64_t groups = seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, s.tile_rows) * p.hk;
+  const bool fp32 = dtype == FREQATTN_F32, wide = p.d > 64;
+  // workgroups that run at the same time
+  const int64_t slots = (int64_t)num_cu * (s.few ? cache8_few_waves(fp32, wide, s.tile_rows / 16, p.d % 16 != 0) : fp32 && wide ? 1 : 2);
+  int64_t n = 1;
+  if (s.few) {
+    if (groups > 0 && tiles > CACHE8_ONE_PIECE) n = lengths ? (groups <= 2 * slots ? 4 * slots / p.hk : 1) : slots / groups;
+  } else if (!lengths || s.nsplit > 1) {
+    return s;
+  } else if (groups <= 2 * slots) {
     n = groups > slots + slots / 2 ? 2 : 4;
     if (n > tiles / 16) n = tiles / 16;
   }
-  if (n > tiles) n = tiles;
-  if (n < 2) return s;
-  s.split_tiles = (int)((tiles + n - 1) / n);
-  s.nsplit = (int)((tiles + s.split_tiles - 1) / s.split_tiles);
+  n = n > tiles ? tiles : n > MAX_PIECES ? MAX_PIECES : n;
+  if (n < 1) n = 1;
+  s.split_tiles = (int)(tiles > 0 ? (tiles + n - 1) / n : 1);
+  s.nsplit = n > 1 ? (int)((tiles + s.split_tiles - 1) / s.split_tiles) : 1;
   s.workspace = s.nsplit > 1 ? (int64_t)s.nsplit * p.hq * p.lse_rows * (p.d + 1) * 4 : 0;
-  s.resident = s.nsplit > 1 ? (int)slots : 0;
+  s.resident = s.nsplit > 1 && lengths ? (int)slots : 0;
   return s;
 }
 
 hipError_t launch_cache8_attention(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, int dtype, hipStream_t st) {
+  if (s.few) return launch_cache8_few(p, sc, s, dtype, st);
   return dtype == FREQATTN_BF16 ? launch<uint16_t>(p, sc, s, st) : launch<float>(p, sc, s, st);
 }
 

@@ -10,8 +10,10 @@ using namespace seq;
 
 // How the keys of a call are cut.  resident = 0: pieces of SeqParams::split_tiles tiles.  Else, for up to 64 sequences, the length of a piece is found on the device from the
 // sequences' own lengths, by every wave alike: `resident` is how many workgroups run at the same time.
-//   one_round (few query rows): so short, split_tiles at least, that there are no more pieces than that: all run at once and end together.
+//   one_round (few query rows): so short, split_tiles at least, that there are no more pieces than that and all run at once; where such pieces are long, their lengths are uneven and
+//   shorter ones of up to SEQ_ROUNDS rounds end closer together.
 //   else (tiles of many rows): a third of the work that a resident workgroup has on average, where that ends sooner than tiles that are not cut.
+enum { SEQ_ROUNDS = 4, SEQ_LONG_PIECE = 8 };
 struct SeqCut { int resident, one_round, kt, tile_rows; };
 
 // Key tiles of a piece.  qt, kt: the lane's sequence's tiles of queries and of keys (zero from the last sequence on).
@@ -25,8 +27,12 @@ __device__ __forceinline__ int seq_piece(const SeqParams& p, const SeqCut& cut, 
 #pragma unroll
   for (int o = 32; o; o >>= 1) work += __shfl_xor(work, o);
   if (cut.one_round) {     // sum of qt ceil(kt / piece) <= work / piece + tiles
-    const int room = cut.resident / p.hk - tiles;
-    const int piece = room > 0 ? (int)(work / (float)room) + 1 : most;
+    auto rounds = [&](int n) {
+      const int room = n * (cut.resident / p.hk) - tiles;
+      return room > 0 ? (int)(work / (float)room) + 1 : most;
+    };
+    int piece = rounds(1);
+    if (piece > SEQ_LONG_PIECE) piece = max(SEQ_LONG_PIECE, rounds(SEQ_ROUNDS));
     return min(max(piece, p.split_tiles), most);
   }
   const float slots = (float)cut.resident / (float)p.hk, mean = work / slots;

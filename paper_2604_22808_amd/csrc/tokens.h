@@ -74,10 +74,16 @@ hipError_t launch_cache8_read(const Cache8Params& p, int dtype, hipStream_t st);
 struct Cache8Scales {
   const uint8_t *k, *v;
   int32_t shift, blocks;
-  int32_t heads_of_line;          // heads whose channels share a line of 128 bytes
+  int32_t heads_of_row;           // heads of neighbouring channels that are read by one XCD (few rows)
 };
 SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu);
 hipError_t launch_cache8_attention(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, int dtype, hipStream_t st);
+enum { CACHE8_FEW_WAVES = 4, CACHE8_ONE_PIECE = 8 };   // few rows: waves of a workgroup; up to so many steps of all of them are not cut
+// Waves of a SIMD, by their registers: workgroups (of four waves) of a compute unit.
+constexpr int cache8_few_waves(bool fp32, bool wide, int nq, bool half) {
+  return nq == 1 ? (wide ? (fp32 ? 2 : 3) : fp32 ? 4 : 5) : wide ? (fp32 || half ? 1 : 2) : fp32 ? 2 : 3;
+}
+hipError_t launch_cache8_few(const SeqParams& p, const Cache8Scales& sc, const SeqPlan& s, int dtype, hipStream_t st);
 hipError_t launch_cache8_generic(const SeqParams& p, const Cache8Scales& sc, int dtype, hipStream_t st);
 
 }  // namespace fa
