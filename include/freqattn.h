@@ -471,16 +471,13 @@ freqattn_status freqattn_quantize_rows(int32_t dtype, int32_t batch, int32_t row
  * elements, any codes -128..127; sums are exact 32-bit integers, scales and bias are applied in fp32, out is rounded once.  out [rows][outputs] and bias [outputs] (NULL: none) of
  * `dtype`; scales DEVICE fp32.  out must not overlap the inputs.
  * Rows of codes that are not whole 16-byte pieces (addresses, strides, channels) take a slower kernel.
- * workspace DEVICE, freqattn_product_i8_workspace(shape) bytes (may be 0: NULL), 16-byte aligned, content does not matter.
- * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype, a workspace that is too small; EUNSUPPORTED: channels above 131071, more tiles than a launch holds. */
+ * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype; EUNSUPPORTED: channels above 131071, more tiles than a launch holds. */
 typedef struct {
   int32_t rows, channels, outputs;
   int32_t dtype; /* freqattn_dtype of out and bias */
 } freqattn_product_shape;
-int64_t freqattn_product_i8_workspace(const freqattn_product_shape* shape);
 freqattn_status freqattn_product_i8(const freqattn_product_shape* shape, const int8_t* a, int64_t a_stride, const float* a_scales, const int8_t* w,
-                                    int64_t w_stride, const float* w_scales, const void* bias, void* out, int64_t out_stride, void* workspace,
-                                    int64_t workspace_bytes, void* stream);
+                                    int64_t w_stride, const float* w_scales, const void* bias, void* out, int64_t out_stride, void* stream);
 
 /* Caches of keys and values held in 8 bits.  k, v: codes [sequences][k_rows][kv_heads][head_dim], one byte each in e4m3 (OCP: bias 7, largest value 448, NaN
  * 0x7f and 0xff).  k_scales, v_scales: DEVICE bytes [sequences][blocks][kv_heads], blocks = k_rows / block_rows rounded up; the block_rows rows (16, 32, 64, 128 or 256) of a

@@ -70,7 +70,9 @@ class ProductShape(C.Structure):
 
 
 class Cache8(C.Structure):
-    _fields_ = [("k", Heads), ("v", Heads), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("block_rows", C.c_int32)]
+    """freqattn_cache8: codes of keys and values (freqattn_heads, field by field), their scales, rows of a block."""
+    _fields_ = [f for x in "kv" for f in ((x + "_data", C.c_void_p), (x + "_batch_stride", C.c_int64), (x + "_row_stride", C.c_int64), (x + "_head_stride", C.c_int64))] + \
+               [("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("block_rows", C.c_int32)]
 
 
 _H, _P = C.POINTER(Heads), C.c_void_p
@@ -133,8 +135,7 @@ EXPORTS = {
     "freqattn_layer_norm_workspace": (C.c_int64, [_N]),
     "freqattn_layer_norm_backward": (C.c_int, [_N, _R, _P, _R, _R, _P, _P, _P, C.c_int64, _P]),
     "freqattn_quantize_rows": (C.c_int, [C.c_int32] * 4 + [_R, _R, _P, _P]),
-    "freqattn_product_i8_workspace": (C.c_int64, [C.POINTER(ProductShape)]),
-    "freqattn_product_i8": (C.c_int, [C.POINTER(ProductShape), _P, C.c_int64, _P, _P, C.c_int64, _P, _P, _P, C.c_int64, _P, C.c_int64, _P]),
+    "freqattn_product_i8": (C.c_int, [C.POINTER(ProductShape), _P, C.c_int64, _P, _P, C.c_int64, _P, _P, _P, C.c_int64, _P]),
     "freqattn_cache8_append": (C.c_int, _SEQ + [_H, _H, _C8, _P]),
     "freqattn_cache8_read": (C.c_int, _SEQ + [_C8, _H, _H, _P]),
     "freqattn_cache8_attention_workspace": (C.c_int64, _SEQ),
@@ -747,47 +748,52 @@ def _filled(who, name, t, like, dtype, shape):
     return t.data_ptr()
 
 
-def _norm_args(who, x, w, eps, vectors):
-    """The shape and the freqattn_rows of x, and the addresses of `vectors` (name, tensor, type): all [channels] or all [batch, channels]."""
-    hx = _rows(who, "x", x)
+def _weights(who, name, t, x, dtype, b, c):
+    """Address of weights or their gradients, and whether they are [batch, channels] instead of [channels]; None passes as (None, None)."""
+    if t is None:
+        return None, None
+    each = isinstance(t, _Tensor) and t.dim() == 2 and x.dim() == 3
+    return _filled(who, name, t, x, dtype, (b, c) if each else (c,)), each
+
+
+def _one_form(who, *each):
+    """Whether weights are given for every batch entry; they all have to be, or none."""
+    e = [x for x in each if x is not None]
+    if e and any(x != e[0] for x in e):
+        raise ValueError(f"{who}: weights must be all [channels] or all [batch, channels]")
+    return 1 if e and e[0] else 0
+
+
+def _sizes(x):
     sh = x.shape
-    b, n, c = sh if len(sh) == 3 else (1,) + tuple(sh)
-    each, at = None, []
-    for name, t, dtype in vectors:
-        if t is not None:
-            one = getattr(t, "dim", lambda: 0)() == 2 and len(sh) == 3
-            if each is not None and one != each:
-                raise ValueError(f"{who}: weights must be all [channels] or all [batch, channels]")
-            each = one
-            at.append(_filled(who, name, t, x, dtype, (b, c) if one else (c,)))
-        else:
-            at.append(None)
-    return NormShape(b, n, c, _io(x), 1 if each else 0, eps), hx, at
+    return sh if len(sh) == 3 else (1, sh[0], sh[1])
 
 
 def layer_norm(x, w, b, out, eps=1e-6):
     """freqattn_layer_norm: x, out [batch, rows, channels] or [rows, channels]; w, b [channels] or [batch, channels], or None; out may be x."""
     who = "layer_norm"
-    if _Tensor is None:
-        _torch_names()
-    dtype = getattr(x, "dtype", None)
-    shape, hx, at = _norm_args(who, x, w, eps, (("w", w, dtype), ("b", b, dtype)))
+    hx = _rows(who, "x", x)
+    n, r, c = _sizes(x)
+    dtype = x.dtype
+    (aw, ew), (ab, eb) = _weights(who, "w", w, x, dtype, n, c), _weights(who, "b", b, x, dtype, n, c)
+    each = _one_form(who, ew, eb)
     ho = _rows(who, "out", out, x, x.shape, dtype, True)
-    _call(lib().freqattn_layer_norm, x, shape, hx, *at, ho)
+    _call(lib().freqattn_layer_norm, x, NormShape(n, r, c, _io(x), each, eps), hx, aw, ab, ho)
     return out
 
 
 def layer_norm_backward(x, w, dout, dx, dw=None, db=None, eps=1e-6, workspace=None):
     """freqattn_layer_norm_backward: x, w as in layer_norm; dw, db fp32 [channels] or [batch, channels] (as w, where there is one), or None."""
     who = "layer_norm_backward"
-    if _Tensor is None:
-        _torch_names()
-    dtype = getattr(x, "dtype", None)
-    shape, hx, at = _norm_args(who, x, w, eps, (("w", w, dtype), ("dw", dw, _F32), ("db", db, _F32)))
+    hx = _rows(who, "x", x)
+    n, r, c = _sizes(x)
+    dtype = x.dtype
+    (aw, ew), (adw, edw), (adb, edb) = _weights(who, "w", w, x, dtype, n, c), _weights(who, "dw", dw, x, _F32, n, c), _weights(who, "db", db, x, _F32, n, c)
+    shape = NormShape(n, r, c, _io(x), _one_form(who, ew, edw, edb), eps)
     hy, ho = _rows(who, "dout", dout, x, x.shape, dtype), _rows(who, "dx", dx, x, x.shape, dtype, True)
     need = 0 if dw is None and db is None else lib().freqattn_layer_norm_workspace(shape)
     ws, size, keep = _workspace(who, workspace, need, x)
-    _call(lib().freqattn_layer_norm_backward, x, shape, hx, at[0], hy, ho, at[1], at[2], ws, size)
+    _call(lib().freqattn_layer_norm_backward, x, shape, hx, aw, hy, ho, adw, adb, ws, size)
     return dx, dw, db
 
 
@@ -795,13 +801,12 @@ def quantize_rows(x, codes, scales):
     """freqattn_quantize_rows: x [batch, rows, channels] or [rows, channels], codes int8 of its shape, scales fp32 of its shape without the channels."""
     who = "quantize_rows"
     hx = _rows(who, "x", x)
-    hc = _rows(who, "codes", codes, x, x.shape, _INT8, True)
-    at = _filled(who, "scales", scales, x, _F32, x.shape[:-1])
+    sh = x.shape
+    hc = _rows(who, "codes", codes, x, sh, _INT8, True)
+    at = _filled(who, "scales", scales, x, _F32, sh[:-1])
     if at is None:
         raise ValueError(f"{who}: scales must be a tensor")
-    sh = x.shape
-    b, n, c = sh if len(sh) == 3 else (1,) + tuple(sh)
-    _call(lib().freqattn_quantize_rows, x, _io(x), b, n, c, hx, hc, at)
+    _call(lib().freqattn_quantize_rows, x, _io(x), *_sizes(x), hx, hc, at)
     return codes, scales
 
 
@@ -815,28 +820,32 @@ def _flat(who, name, t):
     return sh[0] * sh[1], st[1] if sh[1] > 1 else st[0]
 
 
-def product_i8(a, a_scales, w, w_scales, out, bias=None, workspace=None):
+def product_i8(a, a_scales, w, w_scales, out, bias=None):
     """freqattn_product_i8: a int8 [batch, rows, channels] or [rows, channels], w int8 [outputs, channels], a_scales and w_scales fp32 without the channels, out
     bfloat16 or float32 of a's shape with the outputs in place of the channels, bias [outputs] of out's type or None."""
     who = "product_i8"
     if _Tensor is None:
         _torch_names()
-    _rows(who, "a", a, None, None, _INT8)
-    hw = _rows(who, "w", w, a, None, _INT8)
-    if len(w.shape) != 2 or w.shape[1] != a.shape[-1]:
-        raise ValueError(f"{who}: w must be [outputs, {a.shape[-1]}], got {tuple(w.shape)}")
-    n = w.shape[0]
-    _rows(who, "out", out, a, a.shape[:-1] + (n,), None, True)
-    at = [_filled(who, "a_scales", a_scales, a, _F32, a.shape[:-1]), _filled(who, "w_scales", w_scales, a, _F32, (n,))]
-    if None in at:
+    ha, hw = _rows(who, "a", a, None, None, _INT8), _rows(who, "w", w, a, None, _INT8)
+    ash, wsh = a.shape, w.shape
+    if len(wsh) != 2 or wsh[1] != ash[-1]:
+        raise ValueError(f"{who}: w must be [outputs, {ash[-1]}], got {tuple(wsh)}")
+    n, lead = wsh[0], ash[:-1]
+    ho = _rows(who, "out", out, a, lead + (n,), None, True)
+    sa, sw = _filled(who, "a_scales", a_scales, a, _F32, lead), _filled(who, "w_scales", w_scales, a, _F32, (n,))
+    if sa is None or sw is None:
         raise ValueError(f"{who}: a_scales and w_scales must be tensors")
-    (rows, a_stride), (_, out_stride) = _flat(who, "a", a), _flat(who, "out", out)
-    _count(who, "a", rows)
-    shape = ProductShape(rows, a.shape[-1], n, _io(out))
-    ws, size, keep = _workspace(who, workspace, lib().freqattn_product_i8_workspace(shape), a)
-    _call(lib().freqattn_product_i8, a, shape, a.data_ptr(), a_stride, at[0], w.data_ptr(), hw.row_stride, at[1],
-          _filled(who, "bias", bias, a, out.dtype, (n,)), out.data_ptr(), out_stride, ws, size)
+    if len(ash) == 2:
+        rows, a_stride, out_stride = ash[0], ha.row_stride, ho.row_stride
+    else:
+        (rows, a_stride), (_, out_stride) = _flat(who, "a", a), _flat(who, "out", out)
+        _count(who, "a", rows)
+    _call(lib().freqattn_product_i8, a, ProductShape(rows, ash[-1], n, _io(out)), ha.data, a_stride, sa, hw.data, hw.row_stride, sw,
+          _filled(who, "bias", bias, a, out.dtype, (n,)), ho.data, out_stride)
     return out
+
+
+_BLOCKS = (16, 32, 64, 128, 256)
 
 
 def _cache8(who, cache_k, cache_v, k_scales, v_scales, block):
@@ -849,22 +858,22 @@ def _cache8(who, cache_k, cache_v, k_scales, v_scales, block):
             raise TypeError(f"{who}: {name} must be a torch tensor")
         if not t.is_cuda:
             raise ValueError(f"{who}: {name} must be a device tensor")
-        if t.dtype not in _CODES or t.dim() != 4:
-            raise ValueError(f"{who}: {name} must be a float8_e4m3fn or uint8 tensor [sequences, rows, heads, head_dim], got {t.dtype} {tuple(t.shape)}")
-        if t.shape != cache_k.shape or t.device != cache_k.device:
-            raise ValueError(f"{who}: cache_k and cache_v must have one shape and device")
         st = t.stride()
+        if t.dtype not in _CODES or len(st) != 4:
+            raise ValueError(f"{who}: {name} must be a float8_e4m3fn or uint8 tensor [sequences, rows, heads, head_dim], got {t.dtype} {tuple(t.shape)}")
         if st[3] != 1 and t.shape[3] > 1:
             raise ValueError(f"{who}: the channels of {name} must be adjacent")
-        at.append(Heads(t.data_ptr(), st[0], st[1], st[2]))
-    _count(who, "cache_k", max(cache_k.shape))
-    n, rows, heads, _ = cache_k.shape
-    if block not in (16, 32, 64, 128, 256):
+        at += (t.data_ptr(), st[0], st[1], st[2])
+    sh = cache_k.shape
+    if cache_v.shape != sh or cache_v.device != cache_k.device:
+        raise ValueError(f"{who}: cache_k and cache_v must have one shape and device")
+    _count(who, "cache_k", max(sh))
+    if block not in _BLOCKS:
         raise ValueError(f"{who}: block must be 16, 32, 64, 128 or 256")
-    for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
-        at.append(_filled(who, name, t, cache_k, _BYTE, (n, -(-rows // block), heads)))
-        if at[-1] is None:
-            raise ValueError(f"{who}: {name} must be a tensor")
+    scales = (sh[0], -(-sh[1] // block), sh[2])
+    at += (_filled(who, "k_scales", k_scales, cache_k, _BYTE, scales), _filled(who, "v_scales", v_scales, cache_k, _BYTE, scales))
+    if None in at[8:]:
+        raise ValueError(f"{who}: k_scales and v_scales must be tensors")
     return Cache8(*at, block)
 
 

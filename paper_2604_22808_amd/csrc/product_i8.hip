@@ -196,20 +196,22 @@ __device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int& mt, int& 
   return true;
 }
 
-// ---- tiles: TM x TN results a workgroup of four waves, steps of 128 channels copied straight into LDS, one step ahead -----------------------------------------
+// ---- tiles: TM x TN results a workgroup of four waves, steps of 128 channels copied straight into LDS, S - 1 steps ahead -------------------------------------
 // Rows of a step are 128 bytes in LDS; 16-byte chunk c of row r sits at c ^ ((r >> 1) & 7), through the source address, so that the operand reads of 16 rows
 // fall on 16 different bank groups.
-template <typename T, int TM, int TN>
+template <typename T, int TM, int TN, int S>
 __global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles_m, int tiles_n) {
   constexpr int MI = TM / 64, NI = TN / 64;     // 32 x 32 products of a wave: its rows TM / 2, its columns TN / 2
-  __shared__ __attribute__((aligned(16))) int8_t As[2][TM * 128], Ws[2][TN * 128];
+  constexpr int COPIES = TM / 32 + TN / 32;     // of a wave and step
+  static_assert(S * (TM + TN) * 128 <= 160 * 1024 && (S - 2) * COPIES < 64, "");
+  __shared__ __attribute__((aligned(16))) int8_t As[S][TM * 128], Ws[S][TN * 128];
   int mt, nt;
   if (!tile_of(tiles_m, tiles_n, mt, nt)) return;      // (uniform over the workgroup)
   const int m0 = mt * TM, n0 = nt * TN;
   const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6);
   const int wm = wave & 1, wn = wave >> 1;
   const int lr = lane >> 3, lc = lane & 7;
-  // copy i of a wave: rows (wave * N + i) * 8 .. + 7 of a tile, N = rows / 32
+  // copy i of a wave: rows (wave * N + i) * 8 .. + 7 of a tile, N = rows / 32; channels behind the last one are zeros
   auto stage = [&](int k0, int buf) {
 #pragma unroll
     for (int i = 0; i < TM / 32; ++i) {
@@ -230,12 +232,13 @@ __global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles
 #pragma unroll
     for (int m = 0; m < MI; ++m) acc[n][m] = zero16();
   const int steps = (p.channels + 127) / 128;
-  stage(0, 0);
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) stage(s * 128, s);       // (steps behind the last one are zeros too: the count of copies under way stays the same)
+  int buf = 0;
   for (int s = 0; s < steps; ++s) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (s + 1 < steps) stage((s + 1) * 128, (s + 1) & 1);
-    const int8_t *Ab = As[s & 1] + (wm * (TM / 2) + nn) * 128, *Wb = Ws[s & 1] + (wn * (TN / 2) + nn) * 128;
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * COPIES) : "memory");    // step s is there for everybody, and step s - 1 has been read
+    stage((s + S - 1) * 128, buf == 0 ? S - 1 : buf - 1);
+    const int8_t *Ab = As[buf] + (wm * (TM / 2) + nn) * 128, *Wb = Ws[buf] + (wn * (TN / 2) + nn) * 128;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
       const int pos = ((2 * ks + g) ^ ((nn >> 1) & 7)) << 4;
@@ -249,7 +252,9 @@ __global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles
 #pragma unroll
         for (int m = 0; m < MI; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[n], a[m], acc[n][m], 0, 0, 0);
     }
+    buf = buf == S - 1 ? 0 : buf + 1;
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // (copies into this workgroup's LDS)
 #pragma unroll
   for (int m = 0; m < MI; ++m) {
     const int row = m0 + wm * (TM / 2) + m * 32 + nn;
@@ -373,14 +378,12 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductParams p, int ti
   }
 }
 
-enum { ANY, FEW, TILE, WIDE };
-
-template <typename T, int TM, int TN>
+template <typename T, int TM, int TN, int S>
 hipError_t tile(const ProductParams& p, hipStream_t st) {
   const int tiles_m = (int)(((int64_t)p.rows + TM - 1) / TM), tiles_n = (int)(((int64_t)p.outputs + TN - 1) / TN);
   const int64_t blocks = ((int64_t)tiles_m * tiles_n + 7) / 8 * 8;
   if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((k_product_tile<T, TM, TN>), dim3((unsigned)blocks), dim3(256), 0, st, p, tiles_m, tiles_n);
+  hipLaunchKernelGGL((k_product_tile<T, TM, TN, S>), dim3((unsigned)blocks), dim3(256), 0, st, p, tiles_m, tiles_n);
   return hipGetLastError();
 }
 
@@ -395,42 +398,41 @@ hipError_t wide(const ProductParams& p, hipStream_t st) {
 }
 
 template <typename T>
-hipError_t go(const ProductParams& p, const ProductPlan& s, hipStream_t st) {
+hipError_t any(const ProductParams& p, hipStream_t st) {
+  const int64_t tiles_n = ((int64_t)p.outputs + AM - 1) / AM, blocks = ((int64_t)p.rows + AM - 1) / AM * tiles_n;
+  if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(k_product_any<T>, dim3((unsigned)blocks), dim3(256), 0, st, p, (int)tiles_n);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t few(const ProductParams& p, hipStream_t st) {
+  const int64_t blocks = ((int64_t)p.outputs + 15) / 16;
+  if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)blocks), block(64 * FEW_WAVES);
+  if (p.rows <= 16) hipLaunchKernelGGL((k_product_few<T, 1>), grid, block, 0, st, p);
+  else if (p.rows <= 32) hipLaunchKernelGGL((k_product_few<T, 2>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((k_product_few<T, 4>), grid, block, 0, st, p);
+  return hipGetLastError();
+}
+
+constexpr int S64 = 3, S128 = 2, FEW_ROWS = 32;
+
+template <typename T>
+hipError_t go(const ProductParams& p, int num_cu, hipStream_t st) {
+  if (!p.vec) return any<T>(p, st);
+  if (p.rows <= FEW_ROWS) return few<T>(p, st);
+  auto tiles = [&](int64_t n) { return ((int64_t)p.rows + n - 1) / n * (((int64_t)p.outputs + n - 1) / n); };
   // (the wide kernel's rows lie within 2^31 bytes of their tile's first)
   const bool near = p.a_rs >= 0 && p.a_rs < (1 << 22) && p.w_rs >= 0 && p.w_rs < (1 << 22);
-  if (s.kind == WIDE && near) return wide<T>(p, st);
-  if (s.kind == ANY) {
-    const int64_t tiles_n = ((int64_t)p.outputs + AM - 1) / AM, blocks = ((int64_t)p.rows + AM - 1) / AM * tiles_n;
-    if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(k_product_any<T>, dim3((unsigned)blocks), dim3(256), 0, st, p, (int)tiles_n);
-    return hipGetLastError();
-  }
-  if (s.kind == FEW) {
-    const dim3 grid((unsigned)(((int64_t)p.outputs + 15) / 16)), block(64 * FEW_WAVES);
-    if (((int64_t)p.outputs + 15) / 16 >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
-    if (p.rows <= 16) hipLaunchKernelGGL((k_product_few<T, 1>), grid, block, 0, st, p);
-    else if (p.rows <= 32) hipLaunchKernelGGL((k_product_few<T, 2>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_product_few<T, 4>), grid, block, 0, st, p);
-    return hipGetLastError();
-  }
-  return s.kind == TILE && s.tile_m == 64 ? tile<T, 64, 64>(p, st) : tile<T, 128, 128>(p, st);
+  if (near && tiles(256) >= num_cu) return wide<T>(p, st);
+  return tiles(128) >= 2 * (int64_t)num_cu ? tile<T, 128, 128, S128>(p, st) : tile<T, 64, 64, S64>(p, st);
 }
 
 }  // namespace
 
-ProductPlan product_plan(const ProductParams& p, int num_cu) {
-  ProductPlan s = {};
-  s.pieces = 1;
-  if (!p.vec) { s.kind = ANY; return s; }
-  if (p.rows <= 64) { s.kind = FEW; return s; }
-  if (((int64_t)p.rows + 255) / 256 * (((int64_t)p.outputs + 255) / 256) >= num_cu) { s.kind = WIDE; return s; }
-  s.kind = TILE;
-  s.tile_m = s.tile_n = ((int64_t)p.rows + 127) / 128 * (((int64_t)p.outputs + 127) / 128) >= 2 * (int64_t)num_cu ? 128 : 64;
-  return s;
-}
-
-hipError_t launch_product_i8(ProductParams p, const ProductPlan& s, int dtype, hipStream_t st) {
-  return dtype == FREQATTN_BF16 ? go<Bf16>(p, s, st) : go<float>(p, s, st);
+hipError_t launch_product_i8(const ProductParams& p, int dtype, int num_cu, hipStream_t st) {
+  return dtype == FREQATTN_BF16 ? go<Bf16>(p, num_cu, st) : go<float>(p, num_cu, st);
 }
 
 }  // namespace fa

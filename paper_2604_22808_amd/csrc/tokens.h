@@ -42,19 +42,10 @@ struct ProductParams {
   const float *a_scales, *w_scales;
   const void* bias;               // [outputs] of the output's type or nullptr
   char* out;
-  int32_t* part;                  // pieces of the sum
   int32_t rows, channels, outputs;
   int32_t vec;                    // rows of codes are aligned 16-byte pieces
 };
-// How a product is cut; depends on sizes alone.
-struct ProductPlan {
-  int kind;             // which kernel
-  int tile_m, tile_n;
-  int pieces;           // of the sum over the channels
-  int64_t workspace;    // bytes
-};
-ProductPlan product_plan(const ProductParams& p, int num_cu);
-hipError_t launch_product_i8(ProductParams p, const ProductPlan& s, int dtype, hipStream_t st);
+hipError_t launch_product_i8(const ProductParams& p, int dtype, int num_cu, hipStream_t st);
 enum { PRODUCT_MOST_CHANNELS = 131071 };   // 128 * 128 * 131071 < 2^31
 
 // ---- caches held in 8 bits --------------------------------------------------------------------------------------------

@@ -111,40 +111,22 @@ extern "C" freqattn_status freqattn_quantize_rows(int32_t dtype, int32_t batch, 
   });
 }
 
-namespace {
-
-freqattn_status product_params(const char* who, const freqattn_product_shape* s, ProductParams& p) {
-  if (!s) return fail(FREQATTN_EINVAL, who, "NULL argument");
-  if (!known(s->dtype)) return fail(FREQATTN_EINVAL, who, "unknown dtype");
-  if (s->rows < 0 || s->outputs < 0) return fail(FREQATTN_EINVAL, who, "sizes must not be negative");
-  if (s->channels < 1) return fail(FREQATTN_EINVAL, who, "channels must be positive");
-  if (s->channels > PRODUCT_MOST_CHANNELS) return fail(FREQATTN_EUNSUPPORTED, who, "channels above 131071");
-  p = ProductParams{};
-  p.rows = s->rows;
-  p.channels = s->channels;
-  p.outputs = s->outputs;
-  return FREQATTN_OK;
-}
-
-}  // namespace
-
-extern "C" int64_t freqattn_product_i8_workspace(const freqattn_product_shape* s) {
-  ProductParams p;
-  if (guarded([&] { return product_params("freqattn_product_i8_workspace", s, p); }) != FREQATTN_OK) return 0;
-  p.vec = 1;
-  return product_plan(p, compute_units()).workspace;
-}
-
 extern "C" freqattn_status freqattn_product_i8(const freqattn_product_shape* s, const int8_t* a, int64_t a_stride, const float* a_scales, const int8_t* w,
                                                int64_t w_stride, const float* w_scales, const void* bias, void* out, int64_t out_stride,
-                                               void* workspace, int64_t workspace_bytes, void* stream) {
+                                               void* stream) {
   return guarded([&]() -> freqattn_status {
     const char* who = "freqattn_product_i8";
-    ProductParams p;
-    const freqattn_status fs = product_params(who, s, p);
-    if (fs != FREQATTN_OK) return fs;
+    if (!s) return fail(FREQATTN_EINVAL, who, "NULL argument");
+    if (!known(s->dtype)) return fail(FREQATTN_EINVAL, who, "unknown dtype");
+    if (s->rows < 0 || s->outputs < 0) return fail(FREQATTN_EINVAL, who, "sizes must not be negative");
+    if (s->channels < 1) return fail(FREQATTN_EINVAL, who, "channels must be positive");
+    if (s->channels > PRODUCT_MOST_CHANNELS) return fail(FREQATTN_EUNSUPPORTED, who, "channels above 131071");
     if (s->rows == 0 || s->outputs == 0) return FREQATTN_OK;
     if (!a || !a_scales || !w || !w_scales || !out) return fail(FREQATTN_EINVAL, who, "NULL argument");
+    ProductParams p = {};
+    p.rows = s->rows;
+    p.channels = s->channels;
+    p.outputs = s->outputs;
     p.a = (const char*)a;
     p.w = (const char*)w;
     p.a_rs = s->rows > 1 ? a_stride : 0;
@@ -155,11 +137,7 @@ extern "C" freqattn_status freqattn_product_i8(const freqattn_product_shape* s, 
     p.bias = bias;
     p.out = (char*)out;
     p.vec = p.channels % 16 == 0 && ((uintptr_t)a | (uintptr_t)w | (uintptr_t)p.a_rs | (uintptr_t)p.w_rs) % 16 == 0;
-    const ProductPlan plan = product_plan(p, compute_units());
-    if (plan.workspace > 0 && (!workspace || workspace_bytes < plan.workspace)) return fail(FREQATTN_EINVAL, who, "workspace too small");
-    if (plan.workspace > 0 && (uintptr_t)workspace % 16) return fail(FREQATTN_EINVAL, who, "workspace must be 16-byte aligned");
-    p.part = (int32_t*)workspace;
-    return launched(launch_product_i8(p, plan, s->dtype, (hipStream_t)stream), who);
+    return launched(launch_product_i8(p, s->dtype, compute_units(), (hipStream_t)stream), who);
   });
 }
 

@@ -45,23 +45,21 @@ def test_library_refuses_codes_and_products():
     assert code(c=131072) == B.EUNSUPPORTED and code(b=TOP, n=TOP) == B.EUNSUPPORTED
     assert code(n=0, x=None) == B.OK
     shape = lambda **kw: B.ProductShape(**{**dict(rows=3, channels=32, outputs=5, dtype=1), **kw})   # noqa: E731
-    mul = lambda s, a=16, sa=16, w=16, sw=16, out=16: L.freqattn_product_i8(s, a, 32, sa, w, 32, sw, None, out, 5, None, 0, None)   # noqa: E731
+    mul = lambda s, a=16, sa=16, w=16, sw=16, out=16: L.freqattn_product_i8(s, a, 32, sa, w, 32, sw, None, out, 5, None)   # noqa: E731
     assert mul(None) == B.EINVAL
     for kw in (dict(rows=-1), dict(outputs=-1), dict(channels=0), dict(dtype=-1)):
         assert mul(shape(**kw)) == B.EINVAL, kw
     for kw in (dict(a=None), dict(sa=None), dict(w=None), dict(sw=None), dict(out=None)):
         assert mul(shape(), **kw) == B.EINVAL, kw
     assert mul(shape(channels=131072)) == B.EUNSUPPORTED
-    assert mul(shape(rows=TOP, outputs=TOP)) == B.EUNSUPPORTED or L.freqattn_product_i8_workspace(shape(rows=TOP, outputs=TOP)) > 0
-    assert mul(shape(rows=TOP, outputs=TOP), a=17) == B.EUNSUPPORTED
+    assert mul(shape(rows=TOP, outputs=TOP)) == B.EUNSUPPORTED and mul(shape(rows=TOP, outputs=TOP), a=17) == B.EUNSUPPORTED
     assert mul(shape(rows=0), a=None) == B.OK and mul(shape(outputs=0)) == B.OK
-    assert L.freqattn_product_i8_workspace(None) == 0
 
 
 def test_library_refuses_caches():
     L = B.lib()
     shape = lambda **kw: B.SequenceShape(**{**dict(sequences=2, q_heads=4, kv_heads=2, head_dim=64, q_rows=3, k_rows=100, dtype=1, causal=1), **kw})   # noqa: E731
-    cache = lambda **kw: B.Cache8(**{**dict(k=H, v=H, k_scales=16, v_scales=16, block_rows=64), **kw})   # noqa: E731
+    cache = lambda **kw: B.Cache8(**{**dict(k_data=16, v_data=16, k_row_stride=128, v_row_stride=128, k_scales=16, v_scales=16, block_rows=64), **kw})   # noqa: E731
     app = lambda s, c, rows=None, k=H: L.freqattn_cache8_append(s, rows, k, H, c, None)   # noqa: E731
     read = lambda s, c, rows=None, k=H: L.freqattn_cache8_read(s, rows, c, k, H, None)   # noqa: E731
     att = lambda s, c, rows=None, k=H: L.freqattn_cache8_attention(s, rows, k, c, H, None, None, 0, None)   # noqa: E731
@@ -73,7 +71,7 @@ def test_library_refuses_caches():
         for kw in (dict(sequences=-1), dict(q_rows=-1), dict(k_rows=-1), dict(kv_heads=0), dict(head_dim=0), dict(dtype=7)):
             assert call(shape(**kw), cache()) == B.EINVAL, kw
         assert call(shape(), cache(), rows=off) == B.EINVAL
-        for kw in (dict(k=B.Heads(None, 0, 0, 0)), dict(v=B.Heads(None, 0, 0, 0)), dict(k_scales=None), dict(v_scales=None)):
+        for kw in (dict(k_data=None), dict(v_data=None), dict(k_scales=None), dict(v_scales=None)):
             assert call(shape(), cache(**kw)) == B.EINVAL, kw
         for kw in (dict(head_dim=129), dict(k_rows=1 << 30), dict(sequences=TOP, k_rows=1 << 20, q_rows=1 << 20)):
             assert call(shape(**kw), cache()) == B.EUNSUPPORTED, kw
@@ -140,7 +138,7 @@ def test_binding_refuses_caches():
         refused("block", fn, *args(ck, ck, sc, sc, 24))
         refused("contiguous", fn, *args(ck, ck, c(3, 6, 2), sc, 16))
         refused("contiguous", fn, *args(ck, ck, sc, dev(3, 7, 2), 16))
-        refused("must be a tensor", fn, *args(ck, ck, sc, None, 16))
+        refused("must be tensors", fn, *args(ck, ck, sc, None, 16))
         refused("k_lengths", fn, *args(*cache), k_lengths=dev(4, dtype=I32))
     refused("expanded", B.cache8_append, k, k, c(1, 100, 2, 64).expand(3, 100, 2, 64), ck, sc, sc, 16)
     refused("shape", B.cache8_append, k, dev(3, 4, 2, 65), *cache)
