@@ -39,18 +39,7 @@ __device__ __forceinline__ void values4(uint32_t codes, float (&x)[4]) {
   x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
 }
 
-// Eight channels c .. c + 7 of a row of d.
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int c, int d, float (&x)[8]) {
-  constexpr int N = 8 / PW<T>;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    Piece<T> p;
-    p.load(row, c + i * PW<T>, d);
-#pragma unroll
-    for (int j = 0; j < PW<T>; ++j) x[i * PW<T> + j] = p.get(j);
-  }
-}
+// Eight codes, channels c .. c + 7 of a row of d.
 __device__ __forceinline__ uint2v load_codes(const uint8_t* row, int c, int d) {
   uint2v x = {0u, 0u};
   if (c + 8 <= d) return *(const uint2any*)(row + c);
@@ -85,10 +74,15 @@ __device__ __forceinline__ void touched(const Cache8Params& p, int slot, int& se
 
 constexpr int THREADS = 256;
 
-template <typename T>
-__global__ void __launch_bounds__(THREADS) k_cache8_append(Cache8Params p) {
-  __shared__ uint32_t tops[THREADS / 64];
-  unsigned id = blockIdx.x;
+// W waves append to one block and head, IT pieces of eight channels a lane, which stay in registers between the two passes over them (and are all there are: block rows * pieces of a
+// row <= 64 W IT).
+template <typename T, int W, int IT>
+__global__ void __launch_bounds__(THREADS) k_cache8_append(Cache8Params p, unsigned units) {
+  __shared__ uint32_t tops[W];
+  constexpr int LANES = 64 * W, EACH = THREADS / LANES;
+  const int t = threadIdx.x % LANES;
+  unsigned id = blockIdx.x * EACH + threadIdx.x / LANES;
+  if (id >= units) return;
   const int head = (int)(id % (unsigned)p.heads);
   id /= (unsigned)p.heads;
   const bool is_v = id & 1;
@@ -99,59 +93,72 @@ __global__ void __launch_bounds__(THREADS) k_cache8_append(Cache8Params p) {
   const int length = p.k_len ? seq_clamp(p.k_len[seq], 0, p.k_rows) : p.k_rows;
   const int first = length - q.n, from = first > 0 ? first : 0;      // cache rows from .. length - 1 are new
   const int block = (from >> p.shift) + nth, lo = block << p.shift;
-  if (q.n == 0 || lo >= length) return;
+  if (q.n == 0 || lo >= length) return;                    // (of W waves all, or none)
   const int hi = min(lo + (1 << p.shift), length), start = max(lo, from);
   const HeadsPtr& in = is_v ? p.v : p.k;
   const HeadsPtr& out = is_v ? p.cv : p.ck;
   uint8_t* scale = (is_v ? p.vs : p.ks) + ((int64_t)seq * p.blocks + block) * p.heads + head;
   const int was = *scale, chunks = (p.d + 7) >> 3, items = (hi - start) * chunks;
-  const T* src = (const T*)in.p + (int64_t)q.seq * in.bs + (int64_t)head * in.hs;
+  const T* src = (const T*)in.p + (int64_t)q.seq * in.bs + (int64_t)head * in.hs + (int64_t)(q.base + start - first) * in.ts;
   uint8_t* dst = (uint8_t*)const_cast<char*>(out.p) + (int64_t)seq * out.bs + (int64_t)head * out.hs;
-  auto new_row = [&](int r) { return src + (int64_t)(q.base + start + r - first) * in.ts; };
+  constexpr int N = 8 / PW<T>;
+  Piece<T> x[IT][N];
   uint32_t top = 0;
-  for (int i = threadIdx.x; i < items; i += THREADS) {
-    const int r = i / chunks;
-    float x[8];
-    load8(new_row(r), (i - r * chunks) * 8, p.d, x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t b = __float_as_uint(x[j]) & 0x7fffffffu;
-      top = max(top, b < INF_BITS ? b : 0u);
-    }
+  for (int k = 0; k < IT; ++k) {
+    const int i = t + k * LANES, r = i / chunks, c = (i - r * chunks) * 8;
+    if (k > 0 && k * LANES >= items) break;                // (uniform)
+#pragma unroll
+    for (int h = 0; h < N; ++h) x[k][h].load(src + (int64_t)r * in.ts, c + h * PW<T>, i < items ? p.d : 0);
+  }
+#pragma unroll
+  for (int k = 0; k < IT; ++k) {
+    if (k > 0 && k * LANES >= items) break;
+#pragma unroll
+    for (int h = 0; h < N; ++h)
+#pragma unroll
+      for (int j = 0; j < PW<T>; ++j) {
+        const uint32_t b = __float_as_uint(x[k][h].get(j)) & 0x7fffffffu;
+        top = max(top, b < INF_BITS ? b : 0u);
+      }
   }
   top = __float_as_uint(over_lanes<64>(__uint_as_float(top), [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
-  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-  __syncthreads();
+  if constexpr (W > 1) {
+    static_assert(EACH == 1, "");      // (a barrier for all waves of the workgroup)
+    if ((t & 63) == 0) tops[t >> 6] = top;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) top = max(top, tops[w]);
+    for (int w = 0; w < W; ++w) top = max(top, tops[w]);
+  }
   const int need = least_byte(top), e = start > lo ? max(was, need) : need;
-  for (int i = threadIdx.x; i < items; i += THREADS) {
-    const int r = i / chunks, c = (i - r * chunks) * 8;
-    float x[8];
-    load8(new_row(r), c, p.d, x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = coded(x[j], e);
-    store_codes(dst + (int64_t)(start + r) * out.ts, c, p.d, uint2v{codes4(x[0], x[1], x[2], x[3]), codes4(x[4], x[5], x[6], x[7])});
+  for (int k = 0; k < IT; ++k) {
+    if (k > 0 && k * LANES >= items) break;
+    const int i = t + k * LANES, r = i / chunks, c = (i - r * chunks) * 8;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = coded(x[k][j / PW<T>].get(j % PW<T>), e);
+    if (i < items) store_codes(dst + (int64_t)(start + r) * out.ts, c, p.d, uint2v{codes4(v[0], v[1], v[2], v[3]), codes4(v[4], v[5], v[6], v[7])});
   }
   if (start > lo && e != was) {
-    for (int i = threadIdx.x; i < (start - lo) * chunks; i += THREADS) {
+    for (int i = t; i < (start - lo) * chunks; i += LANES) {
       const int r = i / chunks, c = (i - r * chunks) * 8;
       uint8_t* row = dst + (int64_t)(lo + r) * out.ts;
       const uint2v was_codes = load_codes(row, c, p.d);
       uint2v now;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float x[4];
-        values4(was_codes[h], x);
+        float v[4];
+        values4(was_codes[h], v);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_ldexpf(x[j], was - e);
-        now[h] = codes4(x[0], x[1], x[2], x[3]);
+        for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_ldexpf(v[j], was - e);
+        now[h] = codes4(v[0], v[1], v[2], v[3]);
       }
       store_codes(row, c, p.d, now);
     }
   }
-  __syncthreads();      // (every wave has the byte that it found)
-  if (threadIdx.x == 0) *scale = (uint8_t)e;
+  if (W > 1) __syncthreads();      // (every wave has the byte that it found)
+  if (t == 0) *scale = (uint8_t)e;
 }
 
 template <typename T>
@@ -199,10 +206,21 @@ hipError_t launch_cache8_append(const Cache8Params& p, int dtype, hipStream_t st
   const int64_t slots = p.q_off ? p.q_rows / rows + 2 * (int64_t)p.nseq : (int64_t)p.nseq * ((p.q_rows + rows - 2) / rows + 1);
   if (p.q_rows == 0 || slots == 0) return hipSuccess;
   if (slots >= MOST_BLOCKS || slots * 2 * p.heads >= MOST_BLOCKS) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)(slots * 2 * p.heads));
-  if (dtype == FREQATTN_BF16) hipLaunchKernelGGL(k_cache8_append<Bf16>, grid, dim3(THREADS), 0, st, p);
-  else hipLaunchKernelGGL(k_cache8_append<float>, grid, dim3(THREADS), 0, st, p);
-  return hipGetLastError();
+  // a block and head a wave, four in a workgroup, up to 512 pieces; more are shared by four waves
+  const int64_t units = slots * 2 * p.heads, pieces = rows * ((p.d + 7) / 8);
+  auto go = [&](auto type, auto w, auto it) {
+    constexpr int each = THREADS / (64 * w.value);
+    hipLaunchKernelGGL((k_cache8_append<decltype(type), w.value, it.value>), dim3((unsigned)((units + each - 1) / each)), dim3(THREADS), 0, st, p, (unsigned)units);
+    return hipGetLastError();
+  };
+  auto with = [&](auto type) {
+    using std::integral_constant;
+    if (pieces <= 256) return go(type, integral_constant<int, 1>{}, integral_constant<int, 4>{});
+    if (pieces <= 512) return go(type, integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    if (pieces <= 1024) return go(type, integral_constant<int, 4>{}, integral_constant<int, 4>{});
+    return go(type, integral_constant<int, 4>{}, integral_constant<int, 16>{});
+  };
+  return dtype == FREQATTN_BF16 ? with(Bf16{}) : with(0.f);
 }
 
 hipError_t launch_cache8_read(const Cache8Params& p, int dtype, hipStream_t st) {

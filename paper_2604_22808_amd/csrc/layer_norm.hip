@@ -246,10 +246,18 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_
       }
     } else if (to[which]) {
 #pragma unroll
-      for (int k = 0; k < PT; ++k)
+      for (int k = 0; k < PT; ++k) {
+        const int c = at.channel(k);
+        if (c + PW<T> <= n) {
 #pragma unroll
-        for (int j = 0; j < PW<T>; ++j)
-          if (at.channel(k) + j < n) to[which][at.channel(k) + j] = which ? db[k][j] : dw[k][j];
+          for (int j = 0; j < PW<T>; j += 4)
+            *(float4any*)(to[which] + c + j) = which ? float4v{db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]} : float4v{dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
+        } else {
+#pragma unroll
+          for (int j = 0; j < PW<T>; ++j)
+            if (c + j < n) to[which][c + j] = which ? db[k][j] : dw[k][j];
+        }
+      }
     }
   }
 }
@@ -281,7 +289,10 @@ constexpr int FWD_WAVES = 16, BWD_WAVES = 8;
 int norm_backward_blocks(int64_t n, int64_t groups, int channels, int dtype, int num_cu) {
   auto of = [&](auto l, auto w, auto) {
     using At = Place<float, l.value, w.value, 1>;
-    const int64_t b = blocks_of(n, groups, At::STEP, At::THREADS, BWD_WAVES, num_cu);
+    int64_t b = blocks_of(n, groups, At::STEP, At::THREADS, BWD_WAVES, num_cu);
+    // four rows at least for each row of partial sums, unless that leaves compute units idle
+    const int64_t four = (n + 4 * At::STEP - 1) / (4 * At::STEP), all = (num_cu + groups - 1) / groups;
+    if (b > four && b > all) b = four > all ? four : all;
     return (int)(b < 1 ? 1 : b);
   };
   return dtype == FREQATTN_BF16 ? for_channels<Bf16>(channels, of) : for_channels<float>(channels, of);

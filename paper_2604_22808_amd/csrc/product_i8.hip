@@ -14,8 +14,6 @@ namespace {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int16v __attribute__((ext_vector_type(16)));
-typedef float float4v __attribute__((ext_vector_type(4)));
-typedef float4v float4any __attribute__((aligned(4)));
 
 static __device__ const int4v zero_piece = {0, 0, 0, 0};
 

@@ -2,7 +2,7 @@
 //
 // A row of `channels` lies on LANES = LPR * W lanes (LPR lanes of a wave, or W whole waves), as pieces of 16 bytes: lane l holds pieces l, l + LANES, .. of the
 // row, PT of them at most.  Pieces are loaded whole wherever the row starts (addresses of any element's alignment); channels behind the last whole piece are
-// loaded one by one, and what lies behind the row's end is zero.  Rows are counted in 32 bits.
+// loaded in parts of it, and what lies behind the row's end is zero.  Rows are counted in 32 bits.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -21,7 +21,12 @@ typedef uint4v uint4any __attribute__((aligned(2)));    // at any element's addr
 typedef uint4v uint4byte __attribute__((aligned(1)));
 typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
 typedef uint2v uint2any __attribute__((aligned(1)));
+typedef uint2v uint2two __attribute__((aligned(2)));
 typedef uint32_t u32any __attribute__((aligned(1)));
+typedef uint16_t u16any __attribute__((aligned(1)));
+typedef uint32_t u32two __attribute__((aligned(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float4v float4any __attribute__((aligned(4)));
 
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(Bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
@@ -40,13 +45,24 @@ struct Piece {
     raw = uint4v{0u, 0u, 0u, 0u};
     if (c + PW<T> <= n) {
       raw = *(const uint4any*)(row + c);
-    } else {
+    } else if (c < n) {      // the last channels: four, two, one
+      const int left = n - c;
+      const uint32_t* const at = (const uint32_t*)(row + c);
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int j = 0; j < PW<T> - 1; ++j)
-        if (c + j < n) {
-          if constexpr (sizeof(T) == 4) raw[j] = __float_as_uint(row[c + j]);
-          else raw[j >> 1] |= (uint32_t)row[c + j].u << (16 * (j & 1));
-        }
+        for (int j = 0; j < 3; ++j)
+          if (j < left) raw[j] = *(const u32two*)(at + j);
+      } else {
+        uint32_t two = 0, one = 0;
+        if (left & 4) { const uint2v x = *(const uint2two*)at; raw[0] = x[0]; raw[1] = x[1]; }
+        if (left & 2) two = *(const u32two*)(row + c + (left & 4));
+        if (left & 1) one = row[c + (left & 6)].u;
+        const uint32_t x = (left & 2) ? two : one, y = (left & 2) ? one : 0u;
+        raw[0] = (left & 4) ? raw[0] : x;
+        raw[1] = (left & 4) ? raw[1] : y;
+        raw[2] = (left & 4) ? x : 0u;
+        raw[3] = (left & 4) ? y : 0u;
+      }
     }
   }
   __device__ __forceinline__ float get(int j) const {   // (j a constant)
@@ -64,13 +80,19 @@ struct Piece {
   __device__ __forceinline__ void store(T* row, int c, int n) const {
     if (c + PW<T> <= n) {
       *(uint4any*)(row + c) = raw;
-    } else {
+    } else if (c < n) {
+      const int left = n - c;
+      uint32_t* const at = (uint32_t*)(row + c);
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int j = 0; j < PW<T> - 1; ++j)
-        if (c + j < n) {
-          if constexpr (sizeof(T) == 4) row[c + j] = __uint_as_float(raw[j]);
-          else row[c + j].u = (uint16_t)(raw[j >> 1] >> (16 * (j & 1)));
-        }
+        for (int j = 0; j < 3; ++j)
+          if (j < left) *(u32two*)(at + j) = raw[j];
+      } else {
+        if (left & 4) *(uint2two*)at = uint2v{raw[0], raw[1]};
+        const uint32_t x = (left & 4) ? raw[2] : raw[0], y = (left & 4) ? raw[3] : raw[1];
+        if (left & 2) *(u32two*)(row + c + (left & 4)) = x;
+        if (left & 1) row[c + (left & 6)].u = (uint16_t)((left & 2) ? y : x);
+      }
     }
   }
 };

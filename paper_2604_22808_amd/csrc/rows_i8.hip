@@ -65,10 +65,12 @@ __device__ __forceinline__ void store_codes(int8_t* row, int c, int n, const Pie
   if (c + PW<T> <= n) {
     if constexpr (PW<T> == 8) *(uint2any*)(row + c) = uint2v{w[0], w[1]};
     else *(u32any*)(row + c) = w[0];
-  } else {
-#pragma unroll
-    for (int j = 0; j < PW<T> - 1; ++j)
-      if (c + j < n) row[c + j] = (int8_t)(w[j >> 2] >> (8 * (j & 3)));
+  } else if (c < n) {      // the last codes: four, two, one
+    const int left = n - c;
+    uint32_t x = w[0];
+    if (PW<T> == 8 && (left & 4)) { *(u32any*)(row + c) = x; x = w[PW<T> / 4 - 1]; }
+    if (left & 2) { *(u16any*)(row + c + (left & 4)) = (uint16_t)x; x >>= 16; }
+    if (left & 1) row[c + (left & 6)] = (int8_t)x;
   }
 }
 
