@@ -17,13 +17,14 @@ using namespace rows;
 
 namespace {
 
-// (var + eps)^-1/2: the instruction is within one step, which every channel of a row would have alike, so half of a Newton step goes on top.  (Its argument is a normal
-// number unless both are about zero.)
+// (var + eps)^-1/2: the instruction is within one step, which every channel of a row would have alike, so half of a Newton step goes on top.
 __device__ __forceinline__ float inv_root(float v) {
-  if (v < 1e-30f || !(v < 3e38f)) return 1.f / sqrtf(v);
   const float r = __builtin_amdgcn_rsqf(v);
   return __builtin_fmaf(0.5f * r, __builtin_fmaf(-v * r, r, 1.f), r);
 }
+// Not so: squares that have left fp32, or are about to.  Such a row is taken again, times 2^64 or 2^-64.
+__device__ __forceinline__ bool out_of_range(float v) { return v < 1e-30f || !(v < 3e38f); }
+__device__ __forceinline__ float into_range(float v) { return v < 1e-30f ? 0x1p64f : !(v < 3e38f) ? 0x1p-64f : 1.f; }
 
 // Sums of N values over a row's lanes; those of W waves meet in LDS, in the order of the waves.  `turn` alternates between two places, so that one barrier a sum
 // is enough.
@@ -54,15 +55,15 @@ __device__ __forceinline__ T* row_at(const RowsPtr& v, const NormParams& p, int6
   return p.groups == 1 ? row_of<T>(v, p.rows, i) : (T*)v.p + (int64_t)blockIdx.y * v.bs + i * v.rs;
 }
 
-// Centred values d of a row's pieces (zero where there is no channel).
+// Centred values d of a row's pieces times `times` (zero where there is no channel); mean: of the row times `times`.
 template <typename T, int LPR, int W, int PT>
-__device__ __forceinline__ void centre(const Piece<T> (&x)[PT], float (&d)[PT][PW<T>], const Place<T, LPR, W, PT>& at, int n, float mean) {
+__device__ __forceinline__ void centre(const Piece<T> (&x)[PT], float (&d)[PT][PW<T>], const Place<T, LPR, W, PT>& at, int n, float mean, float times) {
 #pragma unroll
   for (int i = 0; i < PT; ++i) {
     const int c = at.channel(i);
     const float m = c < n ? mean : 0.f;
 #pragma unroll
-    for (int j = 0; j < PW<T>; ++j) d[i][j] = x[i].get(j) - m;
+    for (int j = 0; j < PW<T>; ++j) d[i][j] = __builtin_fmaf(x[i].get(j), times, -m);
     if (c < n && c + PW<T> > n) {
 #pragma unroll
       for (int j = 1; j < PW<T>; ++j) d[i][j] = c + j < n ? d[i][j] : 0.f;
@@ -71,12 +72,12 @@ __device__ __forceinline__ void centre(const Piece<T> (&x)[PT], float (&d)[PT][P
 }
 
 template <typename T, int PT>
-__device__ __forceinline__ float sum_of(const Piece<T> (&x)[PT]) {
+__device__ __forceinline__ float sum_of(const Piece<T> (&x)[PT], float times) {
   float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < PT; ++i)
 #pragma unroll
-    for (int j = 0; j < PW<T>; ++j) s[j & 3] += x[i].get(j);
+    for (int j = 0; j < PW<T>; ++j) s[j & 3] = __builtin_fmaf(x[i].get(j), times, s[j & 3]);
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
@@ -105,6 +106,12 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm(
 #pragma unroll
     for (int k = 0; k < PT; ++k) next[k].load(row, at.channel(k), i < p.n ? n : 0);
   };
+  auto again = [&](Piece<T> (&to)[PT], int64_t i) {
+    asm volatile("" ::: "memory");      // (not the registers that hold it)
+    const T* row = row_at<T>(p.x, p, i < p.n ? i : 0);
+#pragma unroll
+    for (int k = 0; k < PT; ++k) to[k].load(row, at.channel(k), i < p.n ? n : 0);
+  };
   const int64_t step = (int64_t)gridDim.x * At::STEP;
   int64_t i = (int64_t)blockIdx.x * At::STEP;
   if (At::AHEAD) request(i + at.row);
@@ -113,20 +120,30 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm(
 #pragma unroll
     for (int k = 0; k < PT; ++k) x[k] = next[k];
     if (At::AHEAD && i + step < p.n) request(i + step + at.row);
-    float s[1] = {sum_of<T, PT>(x)};
-    row_sums<LPR, W>(s, lds, turn, wave);
-    float d[PT][PW<T>];
-    centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n);
-    float q[2] = {0.f, 0.f};
+    float d[PT][PW<T>], dm, v;
+    auto moments = [&](float times) {
+      float s[1] = {sum_of<T, PT>(x, times)};
+      row_sums<LPR, W>(s, lds, turn, wave);
+      centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n, times);
+      float q[2] = {0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < PT; ++k)
+      for (int k = 0; k < PT; ++k)
 #pragma unroll
-      for (int j = 0; j < PW<T>; ++j) {
-        q[0] += d[k][j];
-        q[1] = __builtin_fmaf(d[k][j], d[k][j], q[1]);
-      }
-    row_sums<LPR, W>(q, lds, turn, wave);
-    const float dm = q[0] * inv_n, r = inv_root(__builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps), k0 = -dm * r;
+        for (int j = 0; j < PW<T>; ++j) {
+          q[0] += d[k][j];
+          q[1] = __builtin_fmaf(d[k][j], d[k][j], q[1]);
+        }
+      row_sums<LPR, W>(q, lds, turn, wave);
+      dm = q[0] * inv_n;
+      v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps * times * times;
+      v = q[1] != q[1] ? q[1] : v;      // (the maximum drops a NaN)
+    };
+    moments(1.f);
+    if (__builtin_amdgcn_ballot_w64(out_of_range(v)) != 0) {      // (all waves of a row find the same; the row is loaded again: kept for this it would take registers)
+      again(x, i + at.row);
+      moments(into_range(v));
+    }
+    const float r = out_of_range(v) ? 1.f / sqrtf(v) : inv_root(v), k0 = -dm * r;
     if (i + at.row < p.n) {
       T* row = row_at<T>(p.y, p, i + at.row);
 #pragma unroll
@@ -171,6 +188,12 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_
       ny[k].load(ry, at.channel(k), i < p.n ? n : 0);
     }
   };
+  auto again = [&](Piece<T> (&to)[PT], int64_t i) {
+    asm volatile("" ::: "memory");      // (not the registers that hold it)
+    const T* row = row_at<T>(p.x, p, i < p.n ? i : 0);
+#pragma unroll
+    for (int k = 0; k < PT; ++k) to[k].load(row, at.channel(k), i < p.n ? n : 0);
+  };
   const int64_t step = (int64_t)gridDim.x * At::STEP;
   int64_t i = (int64_t)blockIdx.x * At::STEP;
   if (At::AHEAD && i < p.n) request(i + at.row);
@@ -179,39 +202,51 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_
 #pragma unroll
     for (int k = 0; k < PT; ++k) { x[k] = nx[k]; dy[k] = ny[k]; }
     if (At::AHEAD && i + step < p.n) request(i + step + at.row);
-    float s[1] = {sum_of<T, PT>(x)};
-    row_sums<LPR, W>(s, lds, turn, wave);
-    float d[PT][PW<T>];
-    centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n);
-    float q[4] = {0.f, 0.f, 0.f, 0.f};     // sums of d, d^2, g, g d
+    float d[PT][PW<T>], q[4], v, times = 1.f;     // q: sums of d, d^2, g, g d
+    auto moments = [&] {
+      float s[1] = {sum_of<T, PT>(x, times)};
+      row_sums<LPR, W>(s, lds, turn, wave);
+      centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n, times);
 #pragma unroll
-    for (int k = 0; k < PT; ++k)
+      for (int k = 0; k < 4; ++k) q[k] = 0.f;
 #pragma unroll
-      for (int j = 0; j < PW<T>; ++j) {
-        const float g = dy[k].get(j) * w[k].get(j);
-        q[0] += d[k][j];
-        q[1] = __builtin_fmaf(d[k][j], d[k][j], q[1]);
-        q[2] += g;
-        q[3] = __builtin_fmaf(g, d[k][j], q[3]);
-      }
-    row_sums<LPR, W>(q, lds, turn, wave);
-    const float dm = q[0] * inv_n, r = inv_root(__builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps), k0 = -dm * r;
+      for (int k = 0; k < PT; ++k)
+#pragma unroll
+        for (int j = 0; j < PW<T>; ++j) {
+          const float g = dy[k].get(j) * w[k].get(j);
+          q[0] += d[k][j];
+          q[1] = __builtin_fmaf(d[k][j], d[k][j], q[1]);
+          q[2] += g;
+          q[3] = __builtin_fmaf(g, d[k][j], q[3]);
+        }
+      row_sums<LPR, W>(q, lds, turn, wave);
+      const float dm = q[0] * inv_n;
+      v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps * times * times;
+      v = q[1] != q[1] ? q[1] : v;
+    };
+    moments();
+    if (__builtin_amdgcn_ballot_w64(out_of_range(v)) != 0) {
+      times = into_range(v);
+      again(x, i + at.row);
+      moments();
+    }
+    const float dm = q[0] * inv_n, r = out_of_range(v) ? 1.f / sqrtf(v) : inv_root(v), k0 = -dm * r, rx = r * times;      // rx: of the row itself
     const float mg = q[2] * inv_n, mgh = r * __builtin_fmaf(-dm, q[2], q[3]) * inv_n;
     if (i + at.row < p.n) {
       T* row = row_at<T>(p.dx, p, i + at.row);
 #pragma unroll
       for (int k = 0; k < PT; ++k) {
         Piece<T> o;
-        float v[PW<T>];
+        float o_[PW<T>];
 #pragma unroll
         for (int j = 0; j < PW<T>; ++j) {
           const float y = dy[k].get(j), g = y * w[k].get(j), h = __builtin_fmaf(d[k][j], r, k0);
           dw[k][j] = __builtin_fmaf(y, h, dw[k][j]);
           db[k][j] += y;
-          v[j] = r * (g - __builtin_fmaf(h, mgh, mg));
+          o_[j] = rx * (g - __builtin_fmaf(h, mgh, mg));
         }
 #pragma unroll
-        for (int j = 0; j < PW<T>; j += 2) o.set(j, v[j], v[j + 1]);
+        for (int j = 0; j < PW<T>; j += 2) o.set(j, o_[j], o_[j + 1]);
         o.store(row, at.channel(k), n);
       }
     }

@@ -25,6 +25,10 @@ __device__ __forceinline__ void copy16(const void* src, unsigned dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory", "m0");
 }
 
+// A sum in the value's units.  (Beyond 2^96 a row's scale times the sum may leave fp32 where the other scale would have brought it back.)
+__device__ __forceinline__ bool far_scale(float sa) { return sa > 0x1p96f; }
+__device__ __forceinline__ float scaled(int sum, float sa, float sw) { return far_scale(sa) ? (float)sum * (sa * sw) : (float)sum * sa * sw; }
+
 // Eight results of a row, columns c .. c + 7.
 template <typename T>
 __device__ __forceinline__ void store8(const ProductParams& p, int64_t row, int c, const int (&acc)[8], float sa) {
@@ -34,6 +38,11 @@ __device__ __forceinline__ void store8(const ProductParams& p, int64_t row, int 
     const float4v s0 = *(const float4any*)(p.w_scales + c), s1 = *(const float4any*)(p.w_scales + c + 4);
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = (float)acc[j] * sa * (j < 4 ? s0[j & 3] : s1[j & 3]);
+    if (far_scale(sa)) {
+      asm volatile("");      // (a branch, not selects for everyone)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = scaled(acc[j], sa, j < 4 ? s0[j & 3] : s1[j & 3]);
+    }
     if (p.bias) {
 #pragma unroll
       for (int i = 0; i < 8 / PW<T>; ++i) {
@@ -54,7 +63,7 @@ __device__ __forceinline__ void store8(const ProductParams& p, int64_t row, int 
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (c + j < p.outputs) {
-        const float x = (float)acc[j] * sa * p.w_scales[c + j];
+        const float x = scaled(acc[j], sa, p.w_scales[c + j]);
         to[c + j] = narrow<T>(p.bias ? x + widen(((const T*)p.bias)[c + j]) : x);
       }
   }
@@ -175,7 +184,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) k_product_few(ProductParams p)
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     if (c + j < p.outputs) {
-      const float x = (float)s[j] * sa * p.w_scales[c + j];
+      const float x = scaled(s[j], sa, p.w_scales[c + j]);
       to[c + j] = narrow<T>(p.bias ? x + widen(((const T*)p.bias)[c + j]) : x);
     }
 }
@@ -423,8 +432,8 @@ hipError_t go(const ProductParams& p, int num_cu, hipStream_t st) {
   auto tiles = [&](int64_t n) { return ((int64_t)p.rows + n - 1) / n * (((int64_t)p.outputs + n - 1) / n); };
   // (the wide kernel's rows lie within 2^31 bytes of their tile's first)
   const bool near = p.a_rs >= 0 && p.a_rs < (1 << 22) && p.w_rs >= 0 && p.w_rs < (1 << 22);
-  if (near && tiles(256) >= num_cu) return wide<T>(p, st);
-  return tiles(128) >= 2 * (int64_t)num_cu ? tile<T, 128, 128, S128>(p, st) : tile<T, 64, 64, S64>(p, st);
+  if (near && p.outputs > 128 && tiles(256) >= num_cu) return wide<T>(p, st);
+  return p.outputs > 64 && tiles(128) >= 2 * (int64_t)num_cu ? tile<T, 128, 128, S128>(p, st) : tile<T, 64, 64, S64>(p, st);
 }
 
 }  // namespace

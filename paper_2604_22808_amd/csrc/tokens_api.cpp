@@ -121,6 +121,7 @@ extern "C" freqattn_status freqattn_product_i8(const freqattn_product_shape* s, 
     if (s->rows < 0 || s->outputs < 0) return fail(FREQATTN_EINVAL, who, "sizes must not be negative");
     if (s->channels < 1) return fail(FREQATTN_EINVAL, who, "channels must be positive");
     if (s->channels > PRODUCT_MOST_CHANNELS) return fail(FREQATTN_EUNSUPPORTED, who, "channels above 131071");
+    if (s->rows > (1 << 30) || s->outputs > (1 << 30)) return fail(FREQATTN_EUNSUPPORTED, who, "too many rows for one call");
     if (s->rows == 0 || s->outputs == 0) return FREQATTN_OK;
     if (!a || !a_scales || !w || !w_scales || !out) return fail(FREQATTN_EINVAL, who, "NULL argument");
     ProductParams p = {};

@@ -278,6 +278,60 @@ def test_long_caches_in_pieces(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_sequences_and_uneven_ones(dtype):
+    """More sequences than lanes of a wave; rows of a few sequences that fill tiles unevenly; caches whose lengths differ by all there is."""
+    lengths = [(37 * i) % 301 for i in range(70)]
+    attend(20, dtype, 70, 2, 1, 64, 16, 300, 1, lengths)
+    attend(21, dtype, 66, 4, 2, 32, 64, 120, 66 * 2, [min(120, 3 + 2 * i) for i in range(66)], q_offsets=[2 * i for i in range(67)])
+    attend(22, dtype, 5, 8, 2, 128, 32, 3000, 23, [3000, 1, 0, 1500, 20], q_offsets=[0, 1, 2, 2, 20, 23])
+    attend(23, dtype, 3, 4, 1, 72, 64, 2500, 8, [2500, 100, 2400])
+    attend(24, dtype, 2, 4, 2, 128, 64, 4200, 330, [4200, 300])
+    attend(25, dtype, 3, 4, 4, 64, 128, 2600, 400, [2600, 900, 0], q_offsets=[0, 300, 390, 400], causal=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_caches_of_no_rows_and_calls_of_none(dtype):
+    io = U.TYPES[dtype]
+    q = torch.randn(2, 3, 4, 64, device="cuda").to(io)
+    out, lse = torch.full_like(q, U.MARK), torch.full((4, 6), U.MARK, device="cuda")
+    none = torch.empty(2, 0, 2, 64, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(2, 0, 2, dtype=torch.uint8, device="cuda")
+    B.cache8_attention(q, none, none, scales, scales, 64, out, lse=lse, causal=True)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    B.cache8_append(q[:, :, :2], q[:, :, :2], none, none, scales, scales, 64)
+    c = Cache(1, 2, 20, 2, 64, 16)
+    B.cache8_append(q[:, :0, :2], q[:, :0, :2], *c.args())
+    B.cache8_attention(q[:, :0], *c.args(), out[:, :0])
+    B.cache8_attention(q[:0], *(t[:0] for t in (*c.dev, *c.dev_scales)), 16, out[:0])
+    B.cache8_read(*(t[:0] for t in (*c.dev, *c.dev_scales)), 16, *(torch.empty(0, 20, 2, 64, dtype=io, device="cuda") for _ in range(2)))
+    torch.cuda.synchronize()
+    same(c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_workspaces_hold_does_not_matter_and_calls_repeat(dtype):
+    """Pieces joined from a workspace of NaN; equal calls give equal bits, also one after the other on one workspace."""
+    io = U.TYPES[dtype]
+    for n, rows, cap, lengths in ((3, 1, 6000, [6000, 100, 2500]), (1, 2, 5000, [4000]), (2, 300, 4000, [4000, 1000])):
+        c = Cache(30, n, cap, 2, 64, 64, clean=True)
+        q = torch.randn(n, rows, 4, 64, generator=torch.Generator().manual_seed(1)).to(io).cuda()
+        need = B.lib().freqattn_cache8_attention_workspace(B.SequenceShape(n, 4, 2, 64, rows, cap, B.BF16 if dtype == "bf16" else B.F32, 1, 0.0), B.SequenceRows(None, None, None, 16))
+        assert need > 0
+        res = []
+        for fill in (math.nan, math.inf, 0.0):
+            ws = torch.full((need // 4 + 64,), fill, device="cuda")
+            for _ in range(2):
+                out, lse = torch.empty_like(q), torch.empty(4, n * rows, device="cuda")
+                B.cache8_attention(q, *c.args(), out, lse=lse, causal=True, k_lengths=ints(lengths), workspace=ws[:need // 4])
+                res.append((out, lse))
+            assert torch.equal(ws[need // 4:].nan_to_num(1.0), torch.full((64,), fill, device="cuda").nan_to_num(1.0))
+        for out, lse in res[1:]:
+            assert torch.equal(out, res[0][0]) and torch.equal(lse, res[0][1])
+        with pytest.raises(B.FreqAttnError):
+            B.cache8_attention(q, *c.args(), out, causal=True, k_lengths=ints(lengths), workspace=ws[:need // 4 - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [1, 20, 150])
 def test_nan_behind_the_diagonal_and_keys_that_are_seen(rows, dtype):
     """NaN codes among the keys of a causal call reach the queries that see them and no others; a scale byte of 255 spoils its block alone."""

@@ -80,6 +80,28 @@ def test_rows_far_from_zero_and_of_any_size(mean, spread, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("c", [40, 200, 700, 1900, 5000, 9000])
+def test_rows_whose_squares_leave_fp32(c, dtype):
+    """Rows of 1e25 and of 1e-25 beside ordinary ones, and rows of zeros: each normalised as if it were alone."""
+    io, x, w, bias, dout = make(c, dtype, 1, 23, c, False)
+    size = torch.ones(23, 1, dtype=torch.float64)
+    size[2], size[3], size[11], size[17] = 1e25, 1e-25, 3e30, 1e-17
+    x = (x.double() * size).to(io)
+    x[0, 11] += 1e32
+    for eps in (0.0, 1e-6):
+        out, dx = torch.empty_like(x, device="cuda"), torch.empty_like(x, device="cuda")
+        dw, db = (torch.empty(c, device="cuda") for _ in range(2))
+        B.layer_norm(x.cuda(), w.cuda(), bias.cuda(), out, eps=eps)
+        B.layer_norm_backward(x.cuda(), w.cuda(), dout.cuda(), dx, dw, db, eps=eps)
+        want = expect(x, w, bias, float(torch.tensor(eps)), io, False, dout)
+        for name, got in (("out", out), ("dx", dx), ("dw", dw), ("db", db)):
+            U.check((name, eps), got, *want[name])
+    x[0, 5] = 0.0
+    B.layer_norm(x.cuda(), w.cuda(), bias.cuda(), out, eps=0.0)
+    assert bool(torch.isnan(out[0, 5]).all()) and int(torch.isnan(out).sum()) == c
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_without_weights_in_place_and_rows_alone(dtype):
     io, x, w, bias, dout = make(4, dtype, 1, 50, 320, False)
     want = expect(x, None, None, 1e-6, io, False, dout)
