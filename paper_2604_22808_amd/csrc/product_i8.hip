@@ -429,11 +429,18 @@ template <typename T>
 hipError_t go(const ProductParams& p, int num_cu, hipStream_t st) {
   if (!p.vec) return any<T>(p, st);
   if (p.rows <= FEW_ROWS) return few<T>(p, st);
-  auto tiles = [&](int64_t n) { return ((int64_t)p.rows + n - 1) / n * (((int64_t)p.outputs + n - 1) / n); };
+  // The kernel whose rounds of the chip take the shortest, us at 2048 channels (others in proportion): a compute unit holds three workgroups of 64 x 64 tiles (one of them alone 9, two
+  // 12, three 13), two of 128 x 128 (16, 28) or one of 256 x 256 (29).  Measured as tiles of 64 / 128 / 256: 1024 x 2048 -> 2048 11.6 / 16.6 / 29.5, 2048 x 2048 -> 2048 21.6 / 18.2 /
+  // 30.5, 4096 x 2048 -> 2048 36 / 27.6 / 33, 2048 x 1536 -> 4608 33.6 / 32.2 / 28.5, 3000 x 4096 -> 4096 91 / 70 / 57, 100,000 x 1024 -> 128 35 / 32 / 39.5.
+  auto cost = [&](int64_t n, int resident, const int (&us)[4]) {
+    const int64_t tiles = ((int64_t)p.rows + n - 1) / n * (((int64_t)p.outputs + n - 1) / n), round = (int64_t)num_cu * resident;
+    return tiles / round * us[resident] + us[(tiles % round + num_cu - 1) / num_cu];
+  };
+  const int64_t c64 = cost(64, 3, {0, 9, 12, 13}), c128 = cost(128, 2, {0, 16, 28, 0}), c256 = cost(256, 1, {0, 29, 0, 0});
   // (the wide kernel's rows lie within 2^31 bytes of their tile's first)
   const bool near = p.a_rs >= 0 && p.a_rs < (1 << 22) && p.w_rs >= 0 && p.w_rs < (1 << 22);
-  if (near && p.outputs > 128 && tiles(256) >= num_cu) return wide<T>(p, st);
-  return p.outputs > 64 && tiles(128) >= 2 * (int64_t)num_cu ? tile<T, 128, 128, S128>(p, st) : tile<T, 64, 64, S64>(p, st);
+  if (near && c256 <= c128 && c256 <= c64) return wide<T>(p, st);
+  return c128 <= c64 ? tile<T, 128, 128, S128>(p, st) : tile<T, 64, 64, S64>(p, st);
 }
 
 }  // namespace
