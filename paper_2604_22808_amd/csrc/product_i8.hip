@@ -117,11 +117,13 @@ __global__ void __launch_bounds__(256) k_product_any(ProductParams p, int tiles_
   const bool a_live = m0 + r < p.rows, w_live = n0 + r < p.outputs;
   const char *a_row = p.a + (a_live ? m0 + r : 0) * p.a_rs, *w_row = p.w + (int64_t)(w_live ? n0 + r : 0) * p.w_rs;
   int16v acc = zero16();
+  int4v a = fetch(a_row, a_live, c0), w = fetch(w_row, w_live, c0);
   for (int k0 = 0; k0 < p.channels; k0 += AK) {
-    const int4v a = fetch(a_row, a_live, k0 + c0), w = fetch(w_row, w_live, k0 + c0);
     __syncthreads();
     *(int4v*)(As + r * AS + c0) = a;
     *(int4v*)(Ws + r * AS + c0) = w;
+    a = fetch(a_row, a_live && k0 + AK < p.channels, k0 + AK + c0);      // (the next step's, while this one is multiplied)
+    w = fetch(w_row, w_live && k0 + AK < p.channels, k0 + AK + c0);
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < AK / 32; ++s) {
