@@ -329,7 +329,8 @@ SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu) {
     n = groups > slots + slots / 2 ? 2 : 4;
     if (n > tiles / 16) n = tiles / 16;
   }
-  n = n > tiles ? tiles : n > MAX_PIECES ? MAX_PIECES : n;
+  if (n > tiles) n = tiles;
+  if (n > MAX_PIECES) n = MAX_PIECES;
   if (n < 1) n = 1;
   s.split_tiles = (int)(tiles > 0 ? (tiles + n - 1) / n : 1);
   s.nsplit = n > 1 ? (int)((tiles + s.split_tiles - 1) / s.split_tiles) : 1;

@@ -278,6 +278,22 @@ def test_long_caches_in_pieces(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,cap,heads,kv_heads,d,lengths", [(1, 20003, 8, 1, 64, [20003]), (1, 24577, 4, 2, 128, None), (2, 20064, 4, 1, 72, [19278, 12312]), (3, 20001, 2, 1, 40, [6085, 20001, 0])])
+def test_caches_of_more_steps_than_pieces(n, cap, heads, kv_heads, d, lengths, dtype):
+    attend(60 + d, dtype, n, heads, kv_heads, d, 64, cap, 1, lengths)
+    attend(61 + d, dtype, n, heads, kv_heads, d, 64, cap, 5, lengths)
+
+
+def test_workspaces_hold_no_more_than_64_pieces():
+    for cap in (8192, 8193, 16640, 20064, 100000):
+        for n in (1, 2, 3, 64, 65):
+            for rows in (1, 30, 1000):
+                shape = B.SequenceShape(n, 8, 1, 64, rows, cap, B.BF16, 1, 0.0)
+                need = B.lib().freqattn_cache8_attention_workspace(shape, B.SequenceRows(None, None, None, 16))
+                assert need <= 64 * 8 * n * rows * 65 * 4, (cap, n, rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_many_sequences_and_uneven_ones(dtype):
     """More sequences than lanes of a wave; rows of a few sequences that fill tiles unevenly; caches whose lengths differ by all there is."""
     lengths = [(37 * i) % 301 for i in range(70)]
