@@ -25,9 +25,10 @@ __device__ __forceinline__ void copy16(const void* src, unsigned dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory", "m0");
 }
 
-// A sum in the value's units.  (Beyond 2^96 a row's scale times the sum may leave fp32 where the other scale would have brought it back.)
+// A sum in the value's units.  Beyond 2^96 a row's scale times the sum may leave fp32 where the other scale would have brought it back: that one comes first then.  (If
+// both are so large, what is not zero has no value in fp32 either way.)
 __device__ __forceinline__ bool far_scale(float sa) { return sa > 0x1p96f; }
-__device__ __forceinline__ float scaled(int sum, float sa, float sw) { return far_scale(sa) ? (float)sum * (sa * sw) : (float)sum * sa * sw; }
+__device__ __forceinline__ float scaled(int sum, float sa, float sw) { return far_scale(sa) ? (float)sum * sw * sa : (float)sum * sa * sw; }
 
 // Eight results of a row, columns c .. c + 7.
 template <typename T>

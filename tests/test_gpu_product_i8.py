@@ -135,6 +135,21 @@ def test_scales_that_are_not_finite_or_far_apart():
         assert torch.equal(torch.isfinite(got[7]), want.abs() <= 3.4028235e38) and bool(torch.isfinite(got[7, 2]))
 
 
+@pytest.mark.parametrize("m,k", [(5, 32), (5, 33), (70, 32), (1500, 32)])
+def test_sums_of_zero_between_scales_whose_product_leaves_fp32(m, k):
+    n = 1500
+    a, w = torch.ones(m, k, dtype=torch.int8), torch.ones(n, k, dtype=torch.int8)
+    a[:, k - 1] = 1 - k      # sums of zero
+    a[1] = 1
+    out = torch.full((m, n), U.MARK, device="cuda")
+    big = 2.0 ** 100
+    B.product_i8(a.cuda(), torch.full((m,), big, device="cuda"), w.cuda(), torch.full((n,), big, device="cuda"), out, torch.ones(n, device="cuda"))
+    got = out.cpu()
+    assert bool((got[1] == math.inf).all())
+    got[1] = 1.0
+    assert bool((got == 1.0).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_linear_layer_in_8_bits(dtype):
     """Rows coded on the device times weights coded by the same call: the product of the coded values, and near the product of the values."""
