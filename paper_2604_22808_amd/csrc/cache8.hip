@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(THREADS) k_cache8_append(Cache8Params p, unsig
   const bool is_v = id & 1;
   int seq, nth;
   touched(p, (int)(id >> 1), seq, nth);
-  if (nth < 0) return;                                     // (offsets that do not ascend)
   const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq);
+  if (nth < 0 || nth > (q.n >> p.shift) + 1) return;       // (offsets that do not ascend; slots that nobody's rows reach: the row numbers below stay within 31 bits)
   const int length = p.k_len ? seq_clamp(p.k_len[seq], 0, p.k_rows) : p.k_rows;
   const int first = length - q.n, from = first > 0 ? first : 0;      // cache rows from .. length - 1 are new
   const int block = (from >> p.shift) + nth, lo = block << p.shift;

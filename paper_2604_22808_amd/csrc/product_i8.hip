@@ -421,8 +421,7 @@ hipError_t few(const ProductParams& p, hipStream_t st) {
   if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(64 * FEW_WAVES);
   if (p.rows <= 16) hipLaunchKernelGGL((k_product_few<T, 1>), grid, block, 0, st, p);
-  else if (p.rows <= 32) hipLaunchKernelGGL((k_product_few<T, 2>), grid, block, 0, st, p);
-  else hipLaunchKernelGGL((k_product_few<T, 4>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((k_product_few<T, 2>), grid, block, 0, st, p);
   return hipGetLastError();
 }
 
