@@ -8,6 +8,8 @@
 // present one is worked on.  The mean as it comes out of fp32 is off by some of its steps, which rows far from zero would feel: the sum of the
 // centred values, taken beside their squares, puts that right.  A wave keeps the weights and, in the backward pass, its share of dw and db in registers over all its rows;
 // a workgroup adds its waves' shares in their order and stores one row of partial sums, k_norm_weights adds those: no atomics, equal calls give equal bits.
+#include <algorithm>
+
 #include "rows.h"
 #include "tokens.h"
 
@@ -317,7 +319,7 @@ __global__ void __launch_bounds__(1024) k_norm_weights(NormParams p) {
   }
 }
 
-constexpr int FWD_WAVES = 16, BWD_WAVES = 8;
+constexpr int FWD_WAVES = 16, FWD_MOST_WAVES = 256, BWD_WAVES = 8;
 
 }  // namespace
 
@@ -337,7 +339,11 @@ template <typename T>
 static hipError_t forward(const NormParams& p, int num_cu, hipStream_t st) {
   return for_channels<T>(p.channels, [&](auto l, auto w, auto pt) {
     using At = Place<T, l.value, w.value, pt.value>;
-    const int64_t blocks = blocks_of(p.n, p.groups, At::STEP, At::THREADS, FWD_WAVES, num_cu);
+    // 16 waves for each compute unit, and more where every workgroup still has four steps: rows that are dealt out as workgroups end keep memory busier than fixed shares of a long
+    // tensor (16 / 4 steps: 131,072 x 2048 bf16 210 / 182 us, 2 x 65,536 x 1536 151 / 142, 20,000 x 4096 60 / 57), while the first row of a workgroup is not requested ahead (one step
+    // each: 65,536 x 1024 45 / 51).  Rows of eight waves stay with 16 (8192 x 8192 45 / 48).
+    int64_t blocks = blocks_of(p.n, p.groups, At::STEP, At::THREADS, FWD_WAVES, num_cu);
+    if (w.value < 8) blocks = std::max(blocks, std::min(p.n / (4 * At::STEP), blocks_of(p.n, p.groups, At::STEP, At::THREADS, FWD_MOST_WAVES, num_cu)));
     hipLaunchKernelGGL((k_layer_norm<T, l.value, w.value, pt.value>), dim3((unsigned)blocks, (unsigned)p.groups), dim3(At::THREADS), 0, st, p);
     return hipGetLastError();
   });

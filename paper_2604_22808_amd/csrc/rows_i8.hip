@@ -143,7 +143,9 @@ __global__ void __launch_bounds__(1024) k_quantize_long(CodeParams p) {
   }
 }
 
-constexpr int WAVES = 32;    // of a compute unit
+// Waves for each compute unit, at most: rows that are dealt out as workgroups end keep memory busier than fixed shares (32 / 256 waves: 131,072 x 2048 bf16 156 / 143 us, 65,536 x 4096
+// 184 / 145, 100,000 x 1024 64 / 58).
+constexpr int WAVES = 256;
 
 template <typename T>
 hipError_t go(const CodeParams& p, int num_cu, hipStream_t st) {
@@ -152,12 +154,17 @@ hipError_t go(const CodeParams& p, int num_cu, hipStream_t st) {
     hipLaunchKernelGGL(k_quantize_long<T>, dim3((unsigned)blocks), dim3(1024), 0, st, p);
     return hipGetLastError();
   }
-  return for_channels<T>(p.channels, [&](auto l, auto w, auto pt) {
+  auto launch = [&](auto l, auto w, auto pt) {
     using At = Place<T, l.value, w.value, pt.value>;
     const int64_t blocks = blocks_of(p.n, 1, At::STEP, At::THREADS, WAVES, num_cu);
     hipLaunchKernelGGL((k_quantize_rows<T, l.value, w.value, pt.value>), dim3((unsigned)blocks), dim3(At::THREADS), 0, st, p);
     return hipGetLastError();
-  });
+  };
+  constexpr int U = 8 / PW<T>;
+  using std::integral_constant;
+  // (one wave with four pieces a lane here too, without a barrier: 131,072 x 2048 bf16 182 us on two waves, 156 on one)
+  if (p.channels > 1536 && p.channels <= 2048) return launch(integral_constant<int, 64>(), integral_constant<int, 1>(), integral_constant<int, 4 * U>());
+  return for_channels<T>(p.channels, launch);
 }
 
 }  // namespace
