@@ -322,7 +322,7 @@ SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu) {
   const int64_t slots = (int64_t)num_cu * (s.few ? cache8_few_waves(fp32, wide, s.tile_rows / 16, p.d % 16 != 0) : fp32 && wide ? 1 : 2);
   int64_t n = 1;
   if (s.few) {
-    if (groups > 0 && tiles > CACHE8_ONE_PIECE) n = lengths ? (groups <= 2 * slots ? 4 * slots / p.hk : 1) : slots / groups;
+    if (groups > 0 && tiles > (wide ? CACHE8_ONE_PIECE_128 : CACHE8_ONE_PIECE_64)) n = lengths ? (groups <= 2 * slots ? 4 * slots / p.hk : 1) : slots / groups;
   } else if (!lengths || s.nsplit > 1) {
     return s;
   } else if (groups <= 2 * slots) {

@@ -11,9 +11,10 @@ using namespace seq;
 // How the keys of a call are cut.  resident = 0: pieces of SeqParams::split_tiles tiles.  Else, for up to 64 sequences, the length of a piece is found on the device from the
 // sequences' own lengths, by every wave alike: `resident` is how many workgroups run at the same time.
 //   one_round (few query rows): so short, split_tiles at least, that there are no more pieces than that and all run at once; where such pieces are long, their lengths are uneven and
-//   shorter ones of up to SEQ_ROUNDS rounds end closer together.
+//   shorter ones of up to SEQ_ROUNDS rounds end closer together (one token of 32 requests, 32 / 8 heads of 128, caches of 200 to 16,384 rows: 159 us in one round, 117 in up to four or
+//   six, fp32 174 / 124 / 126; pieces of four tiles at least 115, 16 at least 129).
 //   else (tiles of many rows): a third of the work that a resident workgroup has on average, where that ends sooner than tiles that are not cut.
-enum { SEQ_ROUNDS = 4, SEQ_LONG_PIECE = 8 };
+enum { SEQ_ROUNDS = 4, SEQ_LONG_PIECE = 4 };
 struct SeqCut { int resident, one_round, kt, tile_rows; };
 
 // Key tiles of a piece.  qt, kt: the lane's sequence's tiles of queries and of keys (zero from the last sequence on).
