@@ -442,7 +442,7 @@ typedef struct {
 
 /* Layer norm, out = (x - mean_c x) (var_c x + eps)^-1/2 * w + b, var the mean of the centred squares.  w, b DEVICE of `dtype`, NULL: ones and zeros;
  * [channels], or, with weights_per_batch != 0, [batch][channels]: scale and shift of their own for every batch entry, as conditioning gives them.  Sums are fp32; the
- * mean's own rounding is taken out again, so rows far from zero keep their precision.  out may be x itself (same pointer and strides), else must not overlap it.
+ * mean's own rounding is taken out again, so rows far from zero keep their precision, and rows whose squares leave fp32 are taken in another scale.  out may be x itself (same pointer and strides), else must not overlap it.
  * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype, eps negative or not finite; EUNSUPPORTED: channels above 16384, 2^31 rows or more, more than 65535
  * batch entries with weights of their own.  Nothing is launched where batch or rows is 0. */
 typedef struct {
@@ -469,7 +469,7 @@ freqattn_status freqattn_quantize_rows(int32_t dtype, int32_t batch, int32_t row
                                        float* scales, void* stream);
 /* out[m][n] = a_scales[m] * w_scales[n] * sum_c a[m][c] w[n][c] + bias[n]: a linear layer on coded rows.  a int8 [rows][channels], w int8 [outputs][channels], row strides in
  * elements, any codes -128..127; sums are exact 32-bit integers, scales and bias are applied in fp32, out is rounded once.  out [rows][outputs] and bias [outputs] (NULL: none) of
- * `dtype`; scales DEVICE fp32.  out must not overlap the inputs.
+ * `dtype`; scales DEVICE fp32.  out must not overlap the inputs.  (A row's scale is applied first, above 2^96 the output's: what leaves fp32 in between is infinite.)
  * Rows of codes that are not whole 16-byte pieces (addresses, strides, channels) take a slower kernel.
  * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype; EUNSUPPORTED: channels above 131071, more tiles than a launch holds. */
 typedef struct {
@@ -481,8 +481,8 @@ freqattn_status freqattn_product_i8(const freqattn_product_shape* shape, const i
 
 /* Caches of keys and values held in 8 bits.  k, v: codes [sequences][k_rows][kv_heads][head_dim], one byte each in e4m3 (OCP: bias 7, largest value 448, NaN
  * 0x7f and 0xff).  k_scales, v_scales: DEVICE bytes [sequences][blocks][kv_heads], blocks = k_rows / block_rows rounded up; the block_rows rows (16, 32, 64, 128 or 256) of a
- * block and head have the scale 2^(byte - 127), byte 255: NaN.  A value is its code times its scale: exact in bf16 and fp32 for the bytes that append writes (10..247;
- * values below 2^-126, which smaller bytes give, may count as zero).
+ * block and head have the scale 2^(byte - 127), byte 255: NaN (a block that holds earlier rows stays so).  A value is its code times its scale: exact in bf16 and fp32
+ * for the bytes that append writes (10..247; values below 2^-126, which smaller bytes give, may count as zero).
  * The calls take the shape and rows of freqattn_sequence_attention: the cache is the batched form of the keys, so k_offsets must be NULL, and k_lengths (NULL: k_rows) says
  * how far each sequence is filled, appended rows included.  Lengths and offsets are held to the tensors' rows on the device. */
 typedef struct {
@@ -493,8 +493,8 @@ typedef struct {
 /* New rows k, v (of dtype, packed by q_offsets or [sequences][q_rows][kv_heads][head_dim], cut by q_lengths) become the last rows of the filled part: sequence i's nq rows
  * go to cache rows k_lengths[i] - nq .. k_lengths[i] - 1 (rows that would lie before row 0 are dropped).  A block's scale is the smallest that brings its largest
  * new value to 448 or less, byte 10 at least; in a block that holds earlier rows it is that or the scale it has, whichever is larger, and where it grows the
- * earlier rows' codes are rounded to it.  Codes are rounded to the nearest, ties to even; NaN and infinities become NaN and do not count for the scale.  Equal calls give
- * equal bytes.  q_heads, causal and softmax_scale of the shape are ignored.  Other rows and blocks stay as they are. */
+ * earlier rows' codes are rounded to it.  Codes are rounded to the nearest, ties to even (a value that rounds to 2^128 reads back infinite); NaN and infinities become NaN
+ * and do not count for the scale.  Equal calls give equal bytes.  q_heads, causal and softmax_scale of the shape are ignored.  Other rows and blocks stay as they are. */
 freqattn_status freqattn_cache8_append(const freqattn_sequence_shape* shape, const freqattn_sequence_rows* rows, const freqattn_heads* k,
                                        const freqattn_heads* v, const freqattn_cache8* cache, void* stream);
 /* Values of the filled rows, k and v [sequences][k_rows][kv_heads][head_dim] of dtype; rows behind a sequence's length stay as they are. */

@@ -4,7 +4,7 @@
 // is x 2^(127 - e) to the nearest e4m3 value, ties to even.  Scales are powers of two so that a value in e4m3 keeps its bits when a block's scale grows:
 // only values that fall among the subnormal codes are rounded again.  With no smaller byte than 10 every value is a normal number in fp32 and exact in bf16.
 //
-// Bound by memory.  A workgroup appends to one block of one head of K or V (nobody else writes there): largest value of the new rows, then codes; rows that the block
+// Bound by memory: 16 x 4096 rows of 8 heads of 128 take 79 us to append (5.1 TB/s; blocks of 16 and 256 rows 80 and 81), 78 to read back (5.2).  A workgroup, or a wave, appends to one block of one head of K or V (nobody else writes there): largest value of the new rows, then codes; rows that the block
 // holds already are rewritten only where its scale has grown.
 #include "rows.h"
 #include "seq_common.h"
@@ -206,7 +206,7 @@ hipError_t launch_cache8_append(const Cache8Params& p, int dtype, hipStream_t st
   const int64_t slots = p.q_off ? p.q_rows / rows + 2 * (int64_t)p.nseq : (int64_t)p.nseq * ((p.q_rows + rows - 2) / rows + 1);
   if (p.q_rows == 0 || slots == 0) return hipSuccess;
   if (slots >= MOST_BLOCKS || slots * 2 * p.heads >= MOST_BLOCKS) return hipErrorInvalidConfiguration;
-  // a block and head a wave, four in a workgroup, up to 512 pieces; more are shared by four waves
+  // a block and head a wave, four in a workgroup, up to 512 pieces; more are shared by four waves (blocks of 16 rows, 8 heads of 128, 16 x 4096 rows: 157 us by four waves each, 92 by one)
   const int64_t units = slots * 2 * p.heads, pieces = rows * ((p.d + 7) / 8);
   auto go = [&](auto type, auto w, auto it) {
     constexpr int each = THREADS / (64 * w.value);

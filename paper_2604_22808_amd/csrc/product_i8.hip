@@ -1,6 +1,10 @@
 // Products of rows of 8-bit codes: out[m][n] = s_a[m] s_w[n] sum_k a[m][k] w[n][k] + bias[n], k adjacent in both.  Sums are whole numbers of 32 bits, exact up to 131,071
 // channels, so neither their order nor their cut shows in the result; scaling and bias are fp32, rounded once to the output's type.
 //
+// Long products are bound by the matrix cores and the clock that power leaves them: 65,536 x 1536 -> 4608 542 us (1.71 POPS; a library's product without scales 557), 131,072 x 2048 -> 2048
+// 605 (1.82; 589), 16,384 x 4096 -> 4096 259 (2.12), 8192 x 4096 -> 4096 131; in a run with counters the second took 692 us, matrix cores busy 42 % at 1.8 GHz.  A few rows are bound by the
+// weights' bytes and latency.
+//
 // Operands are fed to the matrix cores as 16 bytes a lane, k = 16 g .. 16 g + 15 of a product's channels on lane group g; both sides use the same order, so any
 // order of the channels will do.
 #include "rows.h"
@@ -95,7 +99,8 @@ __device__ __forceinline__ int16v zero16() {
   return z;
 }
 
-// ---- any addresses: 64 x 64 tiles, codes fetched byte by byte where a row's piece of 16 is not whole or the rows not aligned --------------------------------
+// ---- any addresses: 64 x 64 tiles, codes through registers into LDS, byte by byte where a row's piece of 16 is not whole -----------------------------------
+// (333 x 1000 -> 1100 8.4 us; 64 x 2049 -> 6144 13, without the next step's codes requested ahead 17.7; 14,599 x 1999 -> 2000 243, 0.48 POPS: a quarter of what aligned rows reach)
 constexpr int AM = 64, AK = 64, AS = AK + 16;    // rows of a tile, channels of a step, bytes of a row in LDS
 
 template <typename T>
@@ -141,6 +146,7 @@ __global__ void __launch_bounds__(256) k_product_any(ProductParams p, int tiles_
 // ---- few rows: 16 columns of the output a workgroup, whose waves share the sum -------------------------------------------------------------------------------
 // The weights' bytes are all that counts: each is loaded once, straight into the registers that the product takes it from (16 x 16 x 64: lane l holds row l % 16), the rows' codes
 // come from the caches.  A step is 128 channels, lane group g taking 32 g .. 32 g + 31, so that a row of a step is a whole line.  The waves' sums meet in LDS.
+// 2048 -> 6144: one row 4.6 us (2.7 TB/s), 16 rows 6.1.
 constexpr int FEW_WAVES = 8;
 
 template <typename T, int MT>
@@ -425,6 +431,8 @@ hipError_t few(const ProductParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Stages of the copies by tile.  Rows for the kernel of few rows: here / on 64 x 64 tiles, 32 rows: 2048 -> 6144 8.2 / 7.9 us, 4096 -> 4096 8.4 / 12.9, 1536 -> 1536 4.7 / 6.5, 8192 -> 1024
+// 13 / 23; 64 rows 2048 -> 6144 12.2 / 8.0.
 constexpr int S64 = 3, S128 = 2, FEW_ROWS = 32;
 
 template <typename T>

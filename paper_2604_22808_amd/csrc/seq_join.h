@@ -13,7 +13,8 @@ using namespace seq;
 //   one_round (few query rows): so short, split_tiles at least, that there are no more pieces than that and all run at once; where such pieces are long, their lengths are uneven and
 //   shorter ones of up to SEQ_ROUNDS rounds end closer together (one token of 32 requests, 32 / 8 heads of 128, caches of 200 to 16,384 rows: 159 us in one round, 117 in up to four or
 //   six, fp32 174 / 124 / 126; pieces of four tiles at least 115, 16 at least 129).
-//   else (tiles of many rows): a third of the work that a resident workgroup has on average, where that ends sooner than tiles that are not cut.
+//   else (tiles of many rows): a third of the work that a resident workgroup has on average, in up to four pieces, where that ends sooner than tiles that are not cut.  (Chunks of 1, 512,
+//   1500 and 2048 rows, 16 / 4 heads of 128: 427 us uncut, 326 so; up to eight pieces of a third 353, of half 338, of a quarter 345.)
 enum { SEQ_ROUNDS = 4, SEQ_LONG_PIECE = 4 };
 struct SeqCut { int resident, one_round, kt, tile_rows; };
 
