@@ -13,7 +13,7 @@
 //
 // Bound by the vector unit beside the matrix cores (widening, exponentials).  4096 rows against 16,384 keys, 16 / 4 heads of 128, causal: 525 us (0.91 PFLOP/s; bf16 keys 461, fp32 queries 1343); 4 x
 // 2048 rows against 8192, heads of 64: 320 (0.75).  In chunks of 1, 512, 1500 and 2048 rows against 777 to 16,000 keys (326 us with the join) compute units were busy 87 % of the time and matrix cores
-// 33 %: the last pieces run on a chip that is no longer full, and the join of 26 us reads 119 MB.
+// 33 %: the last pieces run on a chip that is no longer full, and the join of 24 us reads 119 MB.
 #include "cache8_tile.h"
 #include "seq_join.h"
 
@@ -53,6 +53,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 2) k
     int qt, kt;
     seq_tiles(p, cut, lane, qt, kt);
     piece = uniform(seq_piece(p, cut, qt, kt));
+    seq_tell(p, piece, kt);
     if (split * piece >= max(lane_max(kt), 1)) return;     // (no sequence has that piece)
   }
   if (!seq_query_tile(p, TILE, lane, (int)(id % (unsigned)p.slots), seq_i, tile_i)) return;
@@ -326,7 +327,7 @@ SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu) {
   const int64_t slots = (int64_t)num_cu * (s.few ? cache8_few_waves(fp32, wide, s.tile_rows / 16, p.d % 16 != 0) : fp32 && wide ? 1 : 2);
   int64_t n = 1;
   if (s.few) {
-    if (groups > 0 && tiles > (wide ? CACHE8_ONE_PIECE_128 : CACHE8_ONE_PIECE_64)) n = lengths ? (groups <= 2 * slots ? 4 * slots / p.hk : 1) : slots / groups;
+    if (groups > 0 && tiles > CACHE8_ONE_PIECE) n = lengths ? (groups <= 2 * slots ? 4 * slots / p.hk : 1) : slots / groups;
   } else if (!lengths || s.nsplit > 1) {
     return s;
   } else if (groups <= 2 * slots) {
@@ -340,6 +341,7 @@ SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu) {
   s.nsplit = n > 1 ? (int)((tiles + s.split_tiles - 1) / s.split_tiles) : 1;
   s.workspace = s.nsplit > 1 ? (int64_t)s.nsplit * p.hq * p.lse_rows * (p.d + 1) * 4 : 0;
   s.resident = s.nsplit > 1 && lengths ? (int)slots : 0;
+  if (s.resident) s.workspace += 16;      // (seq_piece_at)
   return s;
 }
 

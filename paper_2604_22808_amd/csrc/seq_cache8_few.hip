@@ -57,6 +57,7 @@ __global__ void __launch_bounds__(64 * NW, cache8_few_waves(sizeof(T) == 4, D > 
     int qt, kt;
     seq_tiles(p, cut, lane, qt, kt);
     piece = uniform(seq_piece(p, cut, qt, kt));
+    seq_tell(p, piece, kt);
     const int each = seq_pieces(kt, piece), upto = lane_scan(qt * each);
     if ((int)id >= __builtin_amdgcn_readlane(upto, 63)) return;
     seq_i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > (int)id));

@@ -14,7 +14,7 @@ using namespace seq;
 //   shorter ones of up to SEQ_ROUNDS rounds end closer together (one token of 32 requests, 32 / 8 heads of 128, caches of 200 to 16,384 rows: 159 us in one round, 117 in up to four or
 //   six, fp32 174 / 124 / 126; pieces of four tiles at least 115, 16 at least 129).
 //   else (tiles of many rows): a third of the work that a resident workgroup has on average, in up to four pieces, where that ends sooner than tiles that are not cut.  (Chunks of 1, 512,
-//   1500 and 2048 rows, 16 / 4 heads of 128: 427 us uncut, 326 so; up to eight pieces of a third 353, of half 338, of a quarter 345.)
+//   1500 and 2048 rows, 16 / 4 heads of 128: 392 us uncut, 325 so; up to eight pieces of a third 353, of half 338, of a quarter 345.)
 enum { SEQ_ROUNDS = 4, SEQ_LONG_PIECE = 4 };
 struct SeqCut { int resident, one_round, kt, tile_rows; };
 
@@ -41,6 +41,12 @@ __device__ __forceinline__ int seq_piece(const SeqParams& p, const SeqCut& cut, 
   const int piece = max(p.split_tiles, (int)(mean * (1.f / 3.f)));
   return mean + (float)piece < 0.9f * ceilf((float)tiles / slots) * (float)most ? piece : most;
 }
+// For the join, behind the partial results: the piece in tiles, or 0 where it is longer than every sequence, so that nothing is to be joined.
+__device__ __forceinline__ int* seq_piece_at(const SeqParams& p) { return (int*)(p.part + (int64_t)p.nsplit * p.hq * p.lse_rows * (p.d + 1)); }
+__device__ __forceinline__ void seq_tell(const SeqParams& p, int piece, int kt) {
+  const int most = lane_max(kt);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *seq_piece_at(p) = most <= piece ? 0 : piece;
+}
 // The lane's sequence, for seq_piece.
 __device__ __forceinline__ void seq_tiles(const SeqParams& p, const SeqCut& cut, int lane, int& qt, int& kt) {
   qt = kt = 0;
@@ -57,19 +63,15 @@ template <typename T, int RPW>
 __global__ void __launch_bounds__(256) k_seq_join(SeqParams p, SeqCut cut) {
   __shared__ float weights[4][MAX_PIECES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int piece = cut.resident ? *seq_piece_at(p) : p.split_tiles;
+  if (piece == 0) return;
   const int kvh = (int)(blockIdx.x % (unsigned)p.hk);
   int seq_i, tile_i;
   seq_slot(p.q_off, p.q_rows, p.nseq, p.group, 4 * RPW, (int)(blockIdx.x / (unsigned)p.hk), seq_i, tile_i);
   const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq_i), k = seq_range(p.k_off, p.k_len, p.k_rows, seq_i);
   const int first = (tile_i * 4 + wave) * RPW;
   if ((int64_t)tile_i * 4 * RPW + wave * RPW >= (int64_t)q.n * p.group) return;      // (the whole wave; nothing here waits for another wave)
-  int piece = p.split_tiles;
-  if (cut.resident) {
-    int qt, kt;
-    seq_tiles(p, cut, lane, qt, kt);
-    piece = seq_piece(p, cut, qt, kt);
-    if ((k.n + cut.kt - 1) / cut.kt <= piece) return;      // (not cut: stored where it was computed)
-  }
+  if (cut.resident && (k.n + cut.kt - 1) / cut.kt <= piece) return;      // (not cut: stored where it was computed)
   const int piece_keys = piece * cut.kt;
   const int64_t all = (int64_t)p.hq * p.lse_rows;
   const float* lse = p.part + p.nsplit * all * p.d;
@@ -119,10 +121,10 @@ __global__ void __launch_bounds__(256) k_seq_join(SeqParams p, SeqCut cut) {
 // T: float, or uint16_t for bf16.
 template <typename T>
 hipError_t join_pieces(const SeqParams& p, const SeqCut& cut, hipStream_t st) {
-  // (where pieces are found on the device every wave does so, also where there is nothing to join: eight rows share that)
-  const int rpw = cut.resident && !cut.one_round ? 8 : 1;
+  // (many rows: four a wave; 1 / 4 / 8 of them, chunks of prompts with the pieces 332 / 325 / 325 us, 1000, 300 and 1700 rows of 12 / 4 heads without a mask 135 / 133 / 139)
+  const int rpw = cut.resident && !cut.one_round ? 4 : 1;
   const dim3 grid((unsigned)(seq_slots(p.q_off != nullptr, p.q_rows, p.nseq, p.group, 4 * rpw) * p.hk));
-  if (rpw == 8) hipLaunchKernelGGL((k_seq_join<T, 8>), grid, dim3(256), 0, st, p, cut);
+  if (rpw == 4) hipLaunchKernelGGL((k_seq_join<T, 4>), grid, dim3(256), 0, st, p, cut);
   else hipLaunchKernelGGL((k_seq_join<T, 1>), grid, dim3(256), 0, st, p, cut);
   return hipGetLastError();
 }

@@ -69,9 +69,10 @@ struct Cache8Scales {
 };
 SeqPlan cache8_plan(const SeqParams& p, int dtype, int num_cu);
 hipError_t launch_cache8_attention(SeqParams p, const Cache8Scales& sc, const SeqPlan& s, int dtype, hipStream_t st);
-// Few rows: waves of a workgroup; up to so many steps of all of them (128 keys each; by channels up to 64 or 128) are not cut, which saves the join: us in one piece / cut, one token,
-// 32 / 8 heads of 128: 500 keys 8.8 / 9.4, 1000 keys 12.9 / 9.2; 16 / 2 heads of 64: 777 keys 8.1 / 9.1, 1000 keys 8.9 / 8.2, 1500 keys 11.3 / 9.0.
-enum { CACHE8_FEW_WAVES = 4, CACHE8_ONE_PIECE_64 = 7, CACHE8_ONE_PIECE_128 = 5 };
+// Few rows: waves of a workgroup; up to so many steps of all of them (128 keys each) are not cut, which saves the join: us of the device in one piece / cut, one token, 32 / 8 heads of 128: 500
+// keys 8.8 / 9.4, 1000 keys 12.9 / 9.2, 2000 keys 20.9 / 9.5; 16 / 2 heads of 64: 777 keys 8.1 / 9.1, 1000 keys 8.9 / 8.2, 1500 keys 11.3 / 9.0; called one by one the second launch and its
+// workspace take the host another 4.6 (capacity 1000, 16 / 2 heads of 64: 11.5 / 16.1).
+enum { CACHE8_FEW_WAVES = 4, CACHE8_ONE_PIECE = 8 };
 // Waves of a SIMD, by their registers: workgroups (of four waves) of a compute unit.
 constexpr int cache8_few_waves(bool fp32, bool wide, int nq, bool half) {
   return nq == 1 ? (wide ? (fp32 ? 2 : 3) : fp32 ? 4 : 5) : wide ? (fp32 || half ? 1 : 2) : fp32 ? 2 : 3;

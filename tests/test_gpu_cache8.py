@@ -290,7 +290,7 @@ def test_workspaces_hold_no_more_than_64_pieces():
             for rows in (1, 30, 1000):
                 shape = B.SequenceShape(n, 8, 1, 64, rows, cap, B.BF16, 1, 0.0)
                 need = B.lib().freqattn_cache8_attention_workspace(shape, B.SequenceRows(None, None, None, 16))
-                assert need <= 64 * 8 * n * rows * 65 * 4, (cap, n, rows)
+                assert need <= 64 * 8 * n * rows * 65 * 4 + 16, (cap, n, rows)      # 64 results and log sums a row and head; 16 bytes for the length of a piece
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
