@@ -4,8 +4,8 @@
 // is x 2^(127 - e) to the nearest e4m3 value, ties to even.  Scales are powers of two so that a value in e4m3 keeps its bits when a block's scale grows:
 // only values that fall among the subnormal codes are rounded again.  With no smaller byte than 10 every value is a normal number in fp32 and exact in bf16.
 //
-// Bound by memory: 16 x 4096 rows of 8 heads of 128 take 79 us to append (5.1 TB/s; blocks of 16 and 256 rows 80 and 81), 78 to read back (5.2).  A workgroup, or a wave, appends to one block of one head of K or V (nobody else writes there): largest value of the new rows, then codes; rows that the block
-// holds already are rewritten only where its scale has grown.
+// Bound by memory: 16 x 4096 packed rows of 8 heads of 128 take 83 us to append (4.8 TB/s; blocks of 16 rows 81), 80 to read back (5.0).  A workgroup, or a wave, appends to one block
+// of one head of K or V (nobody else writes there): largest value of the new rows, then codes; rows that the block holds already are rewritten only where its scale has grown.
 #include "rows.h"
 #include "seq_common.h"
 #include "tokens.h"
@@ -56,20 +56,33 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int c, int d, uint2v x
 }
 
 // Blocks that n new rows touch start at slot floor(offset / rows of a block) + 2 i of a launch: they are floor(n / rows) + 2 at most.
-__device__ __forceinline__ void touched(const Cache8Params& p, int slot, int& seq, int& nth) {
+__device__ __forceinline__ void touched(const Cache8Params& p, int slot, int& seq, int& nth, SeqRange& q, int& length) {
+  if (p.q_off && p.nseq <= 64) {      // a sequence a lane: everything about them in one load each, not in a chain of loads (16 x 4096 rows of 8 x 128 92 / 83 us)
+    const int lane = threadIdx.x & 63, mine = min(lane, p.nseq - 1);
+    const SeqRange r = seq_range(p.q_off, p.q_len, p.q_rows, mine);
+    const int filled = p.k_len ? seq_clamp(p.k_len[mine], 0, p.k_rows) : p.k_rows, at = (r.base >> p.shift) + 2 * mine;
+    const uint64_t before = __builtin_amdgcn_ballot_w64(lane < p.nseq && at <= slot);
+    seq = before ? 63 - __builtin_clzll(before) : 0;
+    nth = slot - __builtin_amdgcn_readlane(at, seq);
+    q = SeqRange{0, __builtin_amdgcn_readlane(r.base, seq), __builtin_amdgcn_readlane(r.n, seq)};
+    length = __builtin_amdgcn_readlane(filled, seq);
+    return;
+  }
   if (!p.q_off) {
     const int per = ((p.q_rows + (1 << p.shift) - 2) >> p.shift) + 1;
     seq = slot / per;
     nth = slot - seq * per;
-    return;
+  } else {
+    int lo = 0, hi = p.nseq - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((seq_clamp(p.q_off[mid], 0, p.q_rows) >> p.shift) + 2 * mid <= slot) lo = mid; else hi = mid - 1;
+    }
+    seq = lo;
+    nth = slot - ((seq_clamp(p.q_off[lo], 0, p.q_rows) >> p.shift) + 2 * lo);
   }
-  int lo = 0, hi = p.nseq - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if ((seq_clamp(p.q_off[mid], 0, p.q_rows) >> p.shift) + 2 * mid <= slot) lo = mid; else hi = mid - 1;
-  }
-  seq = lo;
-  nth = slot - ((seq_clamp(p.q_off[lo], 0, p.q_rows) >> p.shift) + 2 * lo);
+  q = seq_range(p.q_off, p.q_len, p.q_rows, seq);
+  length = p.k_len ? seq_clamp(p.k_len[seq], 0, p.k_rows) : p.k_rows;
 }
 
 constexpr int THREADS = 256;
@@ -86,11 +99,10 @@ __global__ void __launch_bounds__(THREADS) k_cache8_append(Cache8Params p, unsig
   const int head = (int)(id % (unsigned)p.heads);
   id /= (unsigned)p.heads;
   const bool is_v = id & 1;
-  int seq, nth;
-  touched(p, (int)(id >> 1), seq, nth);
-  const SeqRange q = seq_range(p.q_off, p.q_len, p.q_rows, seq);
+  int seq, nth, length;
+  SeqRange q;
+  touched(p, (int)(id >> 1), seq, nth, q, length);
   if (nth < 0 || nth > (q.n >> p.shift) + 1) return;       // (offsets that do not ascend; slots that nobody's rows reach: the row numbers below stay within 31 bits)
-  const int length = p.k_len ? seq_clamp(p.k_len[seq], 0, p.k_rows) : p.k_rows;
   const int first = length - q.n, from = first > 0 ? first : 0;      // cache rows from .. length - 1 are new
   const int block = (from >> p.shift) + nth, lo = block << p.shift;
   if (q.n == 0 || lo >= length) return;                    // (of W waves all, or none)

@@ -98,6 +98,12 @@ def test_appended_rows(block, heads, d, cap, new, lengths, dtype):
                 assert bool((at == 0x55).all())
 
 
+@pytest.mark.parametrize("n", [63, 64, 65, 90])
+def test_rows_of_about_as_many_sequences_as_lanes(n):
+    new = [(5 * i) % 19 for i in range(n)]
+    test_appended_rows(16, 2, 24, 40, new, [x + i % 21 for i, x in enumerate(new)], "bf16")
+
+
 def test_a_row_at_a_time_is_what_growing_scales_make_it():
     """Fifty single rows of growing and shrinking sizes, each after the other, and the same rows in pieces."""
     n, heads, d, block, cap = 2, 2, 16, 16, 60
