@@ -215,18 +215,22 @@ __device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int& mt, int& 
 // ---- tiles: TM x TN results a workgroup of four waves, steps of 128 channels copied straight into LDS, S - 1 steps ahead -------------------------------------
 // Rows of a step are 128 bytes in LDS; 16-byte chunk c of row r sits at c ^ ((r >> 1) & 7), through the source address, so that the operand reads of 16 rows
 // fall on 16 different bank groups.
-template <typename T, int TM, int TN, int S>
-__global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles_m, int tiles_n) {
+// G groups of four waves take every G-th step, with tiles of their own in LDS, and add their sums up there.
+template <typename T, int TM, int TN, int S, int G>
+__global__ void __launch_bounds__(256 * G) k_product_tile(ProductParams p, int tiles_m, int tiles_n) {
   constexpr int MI = TM / 64, NI = TN / 64;     // 32 x 32 products of a wave: its rows TM / 2, its columns TN / 2
   constexpr int COPIES = TM / 32 + TN / 32;     // of a wave and step
-  static_assert(S * (TM + TN) * 128 <= 160 * 1024 && (S - 2) * COPIES < 64, "");
-  __shared__ __attribute__((aligned(16))) int8_t As[S][TM * 128], Ws[S][TN * 128];
+  static_assert(G * S * (TM + TN) * 128 <= 160 * 1024 && (S - 2) * COPIES < 64, "");
+  static_assert(G == 1 || (MI * NI == 1 && (G - 1) * 4 * 64 * 64 <= G * S * TM * 128), "");
+  __shared__ __attribute__((aligned(16))) int8_t all_a[G][S][TM * 128], all_w[G][S][TN * 128];
   int mt, nt;
   if (!tile_of(tiles_m, tiles_n, mt, nt)) return;      // (uniform over the workgroup)
   const int m0 = mt * TM, n0 = nt * TN;
-  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = uniform(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, group = G == 1 ? 0 : uniform(threadIdx.x >> 8), wave = uniform(threadIdx.x >> 6) & 3;
   const int wm = wave & 1, wn = wave >> 1;
   const int lr = lane >> 3, lc = lane & 7;
+  int8_t(*const As)[TM * 128] = all_a[group];
+  int8_t(*const Ws)[TN * 128] = all_w[group];
   // copy i of a wave: rows (wave * N + i) * 8 .. + 7 of a tile, N = rows / 32; channels behind the last one are zeros
   auto stage = [&](int k0, int buf) {
 #pragma unroll
@@ -247,13 +251,13 @@ __global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles
   for (int n = 0; n < NI; ++n)
 #pragma unroll
     for (int m = 0; m < MI; ++m) acc[n][m] = zero16();
-  const int steps = (p.channels + 127) / 128;
+  const int steps = (p.channels + 128 * G - 1) / (128 * G);      // of a group
 #pragma unroll
-  for (int s = 0; s < S - 1; ++s) stage(s * 128, s);       // (steps behind the last one are zeros too: the count of copies under way stays the same)
+  for (int s = 0; s < S - 1; ++s) stage((s * G + group) * 128, s);       // (steps behind the last one are zeros too: the count of copies under way stays the same)
   int buf = 0;
   for (int s = 0; s < steps; ++s) {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * COPIES) : "memory");    // step s is there for everybody, and step s - 1 has been read
-    stage((s + S - 1) * 128, buf == 0 ? S - 1 : buf - 1);
+    stage(((s + S - 1) * G + group) * 128, buf == 0 ? S - 1 : buf - 1);
     const int8_t *Ab = As[buf] + (wm * (TM / 2) + nn) * 128, *Wb = Ws[buf] + (wn * (TN / 2) + nn) * 128;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
@@ -271,6 +275,24 @@ __global__ void __launch_bounds__(256) k_product_tile(ProductParams p, int tiles
     buf = buf == S - 1 ? 0 : buf + 1;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // (copies into this workgroup's LDS)
+  if constexpr (G > 1) {
+    __syncthreads();
+    int4v* const sums = (int4v*)all_a;
+    if (group > 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums[(((group - 1) * 4 + j) * 4 + wave) * 64 + lane] = int4v{acc[0][0][4 * j], acc[0][0][4 * j + 1], acc[0][0][4 * j + 2], acc[0][0][4 * j + 3]};
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int o = 0; o < G - 1; ++o)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int4v x = sums[((o * 4 + j) * 4 + wave) * 64 + lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[0][0][4 * j + k] += x[k];
+      }
+  }
 #pragma unroll
   for (int m = 0; m < MI; ++m) {
     const int row = m0 + wm * (TM / 2) + m * 32 + nn;
@@ -394,12 +416,12 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductParams p, int ti
   }
 }
 
-template <typename T, int TM, int TN, int S>
+template <typename T, int TM, int TN, int S, int G>
 hipError_t tile(const ProductParams& p, hipStream_t st) {
   const int tiles_m = (int)(((int64_t)p.rows + TM - 1) / TM), tiles_n = (int)(((int64_t)p.outputs + TN - 1) / TN);
   const int64_t blocks = ((int64_t)tiles_m * tiles_n + 7) / 8 * 8;
   if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((k_product_tile<T, TM, TN, S>), dim3((unsigned)blocks), dim3(256), 0, st, p, tiles_m, tiles_n);
+  hipLaunchKernelGGL((k_product_tile<T, TM, TN, S, G>), dim3((unsigned)blocks), dim3(256 * G), 0, st, p, tiles_m, tiles_n);
   return hipGetLastError();
 }
 
@@ -431,26 +453,30 @@ hipError_t few(const ProductParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Stages of the copies by tile.  Rows for the kernel of few rows: here / on 64 x 64 tiles, 32 rows: 2048 -> 6144 8.2 / 7.9 us, 4096 -> 4096 8.4 / 12.9, 1536 -> 1536 4.7 / 6.5, 8192 -> 1024
-// 13 / 23; 64 rows 2048 -> 6144 12.2 / 8.0.
+// Stages of the copies by tile.  Rows for the kernel of few rows: here / on 64 x 64 tiles, 32 rows: 2048 -> 6144 8.2 / 6.3 us, 4096 -> 4096 8.4 / 9.2, 8192 -> 1024 13 / 15; 64
+// rows: 2048 -> 6144 12.1 / 6.4, 4096 -> 4096 12.6 / 9.2, 8192 -> 1024 20.5 / 15.2.
+// On 64 x 64 tiles of a single round two groups share the steps: one / two / four of them, 64 rows 2048 -> 6144 7.7 / 6.4 / 6.5 us, 8192 -> 1024 21.3 / 15.2 / 13.7, 512 rows 8192 -> 1024
+// 22.2 / 16.6 / 16.7, 6250 rows 8000 -> 96 22.5 / 18.8 / 22.6; in more rounds 2048 x 1536 -> 1536 11.6 / 15.3 / 16.1.
 constexpr int S64 = 3, S128 = 2, FEW_ROWS = 32;
 
 template <typename T>
 hipError_t go(const ProductParams& p, int num_cu, hipStream_t st) {
   if (!p.vec) return any<T>(p, st);
   if (p.rows <= FEW_ROWS) return few<T>(p, st);
-  // The kernel whose rounds of the chip take the shortest, us at 2048 channels (others in proportion): a compute unit holds three workgroups of 64 x 64 tiles (one of them alone 9, two
-  // 12, three 13), two of 128 x 128 (16, 28) or one of 256 x 256 (29).  Measured as tiles of 64 / 128 / 256: 1024 x 2048 -> 2048 11.6 / 16.6 / 29.5, 2048 x 2048 -> 2048 21.6 / 18.2 /
+  // The kernel whose rounds of the chip take the shortest, us at 2048 channels (others in proportion): a compute unit holds three workgroups of 64 x 64 tiles (one of them alone 9, or 7 in
+  // two groups, two 12, three 13), two of 128 x 128 (16, 28) or one of 256 x 256 (29).  Measured as tiles of 64 / 128 / 256: 1024 x 2048 -> 2048 11.6 / 16.6 / 29.5, 2048 x 2048 -> 2048 21.6 / 18.2 /
   // 30.5, 4096 x 2048 -> 2048 36 / 27.6 / 33, 2048 x 1536 -> 4608 33.6 / 32.2 / 28.5, 3000 x 4096 -> 4096 91 / 70 / 57, 100,000 x 1024 -> 128 35 / 32 / 39.5.
   auto cost = [&](int64_t n, int resident, const int (&us)[4]) {
     const int64_t tiles = ((int64_t)p.rows + n - 1) / n * (((int64_t)p.outputs + n - 1) / n), round = (int64_t)num_cu * resident;
     return tiles / round * us[resident] + us[(tiles % round + num_cu - 1) / num_cu];
   };
-  const int64_t c64 = cost(64, 3, {0, 9, 12, 13}), c128 = cost(128, 2, {0, 16, 28, 0}), c256 = cost(256, 1, {0, 29, 0, 0});
+  const bool one = ((int64_t)p.rows + 63) / 64 * (((int64_t)p.outputs + 63) / 64) <= num_cu;
+  const int64_t c64 = one ? 7 : cost(64, 3, {0, 9, 12, 13}), c128 = cost(128, 2, {0, 16, 28, 0}), c256 = cost(256, 1, {0, 29, 0, 0});
   // (the wide kernel's rows lie within 2^31 bytes of their tile's first)
   const bool near = p.a_rs >= 0 && p.a_rs < (1 << 22) && p.w_rs >= 0 && p.w_rs < (1 << 22);
   if (near && c256 <= c128 && c256 <= c64) return wide<T>(p, st);
-  return c128 <= c64 ? tile<T, 128, 128, S128>(p, st) : tile<T, 64, 64, S64>(p, st);
+  if (c128 <= c64) return tile<T, 128, 128, S128, 1>(p, st);
+  return one ? tile<T, 64, 64, S64, 2>(p, st) : tile<T, 64, 64, S64, 1>(p, st);
 }
 
 }  // namespace

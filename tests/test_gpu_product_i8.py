@@ -80,7 +80,8 @@ def expect(a, w, sa, sw, bias, io):
 
 
 SIZES = [(1, 1, 1), (1, 16, 16), (2, 15, 3), (1, 2048, 48), (16, 2048, 6144), (5, 1040, 250), (17, 512, 100), (33, 4096, 40), (64, 144, 1000), (65, 128, 64), (100, 96, 130),
-         (333, 1000, 1100), (200, 1008, 129), (257, 2048, 512), (128, 256, 128), (1000, 384, 700), (513, 1536, 4608), (2100, 160, 2304), (70000, 64, 48), (70001, 48, 100), (66000, 80, 200), (32, 304, 4000), (3, 8192, 1024), (70, 131056, 65)]
+         (333, 1000, 1100), (200, 1008, 129), (257, 2048, 512), (128, 256, 128), (1000, 384, 700), (513, 1536, 4608), (2100, 160, 2304), (70000, 64, 48), (70001, 48, 100), (66000, 80, 200), (32, 304, 4000), (3, 8192, 1024), (70, 131056, 65),
+         (1000, 2064, 2048), (300, 4112, 608), (64, 656, 1000), (40, 128, 64)]
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
