@@ -7,6 +7,8 @@
 //
 // Operands are fed to the matrix cores as 16 bytes a lane, k = 16 g .. 16 g + 15 of a product's channels on lane group g; both sides use the same order, so any
 // order of the channels will do.
+#include <algorithm>
+
 #include "rows.h"
 #include "tokens.h"
 
@@ -99,48 +101,125 @@ __device__ __forceinline__ int16v zero16() {
   return z;
 }
 
-// ---- any addresses: 64 x 64 tiles, codes through registers into LDS, byte by byte where a row's piece of 16 is not whole -----------------------------------
-// (333 x 1000 -> 1100 8.4 us; 64 x 2049 -> 6144 13, without the next step's codes requested ahead 17.7; 14,599 x 1999 -> 2000 243, 0.48 POPS: a quarter of what aligned rows reach)
-constexpr int AM = 64, AK = 64, AS = AK + 16;    // rows of a tile, channels of a step, bytes of a row in LDS
+// The tile of a workgroup.  Workgroups are dealt to the 8 XCDs in turn and each XCD has an L2 of its own: XCD x takes the x-th eighth of the tiles, in an order that goes through
+// GROUP rows of tiles column by column, so that the tiles that run at the same time share few rows and columns.
+constexpr int GROUP = 4;
+__device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int& mt, int& nt) {
+  const unsigned all = (unsigned)tiles_m * (unsigned)tiles_n, each = (all + 7) / 8;
+  const unsigned id = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= each || id >= all) return false;
+  const unsigned group = id / (GROUP * (unsigned)tiles_n), in = id - group * GROUP * (unsigned)tiles_n;
+  const unsigned rows_ = min((unsigned)GROUP, (unsigned)tiles_m - group * GROUP);
+  nt = (int)(in / rows_);
+  mt = (int)(group * GROUP + in - (unsigned)nt * rows_);
+  return true;
+}
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_product_any(ProductParams p, int tiles_n) {
-  __shared__ __attribute__((aligned(16))) int8_t As[AM * AS], Ws[AM * AS];
-  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6;
-  const int64_t m0 = (int64_t)(blockIdx.x / (unsigned)tiles_n) * AM;
-  const int n0 = (int)(blockIdx.x % (unsigned)tiles_n) * AM;
-  const int r = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 16;     // the piece of 16 codes that this thread fetches of either tile
-  auto fetch = [&](const char* row, bool live, int k) {
-    int4v x = {0, 0, 0, 0};
-    if (live && k + 16 <= p.channels) x = __builtin_bit_cast(int4v, *(const uint4byte*)(row + k));
-    else if (live) {
+// ---- any addresses: TM x TM tiles, codes through registers into LDS, two steps ahead of the products ---------------------------------------------------------
+// (333 x 1000 -> 1100 7.1 us; 64 x 2049 -> 6144 12.5, with nothing requested ahead 17.7; 14,599 x 1999 -> 2000 137, 0.85 POPS)
+constexpr int AK = 64, AS = AK + 16;    // channels of a step, bytes of a row in LDS
+
+// Codes k .. k + 15 of a row of n, zeros from n on.
+__device__ __forceinline__ int4v row_piece(const char* row, int k, int n) {
+  if (k >= n) return int4v{0, 0, 0, 0};
+  if (k + 16 <= n) return __builtin_bit_cast(int4v, *(const uint4byte*)(row + k));
+  if (n >= 16) {      // the row's last 16, shifted down
+    typedef uint64_t long2 __attribute__((ext_vector_type(2)));
+    const long2 x = __builtin_bit_cast(long2, *(const uint4byte*)(row + n - 16));
+    const int down = 8 * (k + 16 - n);      // 8 .. 120
+    const long2 y = down >= 64 ? long2{x[1] >> (down - 64), 0} : long2{x[0] >> down | x[1] << (64 - down), x[1] >> down};
+    return __builtin_bit_cast(int4v, y);
+  }
+  int4v x = {0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < 15; ++j)
-        if (k + j < p.channels) x[j >> 2] |= (int)((uint32_t)(uint8_t)row[k + j] << (8 * (j & 3)));
+  for (int j = 0; j < 15; ++j)
+    if (k + j < n) x[j >> 2] |= (int)((uint32_t)(uint8_t)row[k + j] << (8 * (j & 3)));
+  return x;
+}
+
+template <typename T, int TM>
+__global__ void __launch_bounds__(256) k_product_any(ProductParams p, int tiles_m, int tiles_n) {
+  constexpr int MI = TM / 64;      // 32 x 32 products of a wave each way; pieces of 16 codes of a thread and operand
+  __shared__ __attribute__((aligned(16))) int8_t As[2][TM * AS], Ws[2][TM * AS];
+  int mt, nt;
+  if (!tile_of(tiles_m, tiles_n, mt, nt)) return;
+  const int64_t m0 = (int64_t)mt * TM;
+  const int n0 = nt * TM;
+  const int lane = threadIdx.x & 63, nn = lane & 31, g = lane >> 5, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
+  const int r = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 16;
+  const char *a_row[MI], *w_row[MI];      // (rows that do not exist: the last one, and nobody stores what comes of it)
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    a_row[i] = p.a + min(m0 + r + 64 * i, (int64_t)p.rows - 1) * p.a_rs + c0;
+    w_row[i] = p.w + (int64_t)min(n0 + r + 64 * i, p.outputs - 1) * p.w_rs + c0;
+  }
+  int16v acc[MI][MI];
+#pragma unroll
+  for (int n = 0; n < MI; ++n)
+#pragma unroll
+    for (int m = 0; m < MI; ++m) acc[n][m] = zero16();
+  struct Step { int4v a[MI], w[MI]; };
+  auto fetch = [&](Step& x, int k0) {
+    if (k0 + AK <= p.channels) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        x.a[i] = __builtin_bit_cast(int4v, *(const uint4byte*)(a_row[i] + k0));
+        x.w[i] = __builtin_bit_cast(int4v, *(const uint4byte*)(w_row[i] + k0));
+      }
+    } else if (k0 < p.channels) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        x.a[i] = row_piece(a_row[i] - c0, k0 + c0, p.channels);
+        x.w[i] = row_piece(w_row[i] - c0, k0 + c0, p.channels);
+      }
     }
-    return x;
   };
-  const bool a_live = m0 + r < p.rows, w_live = n0 + r < p.outputs;
-  const char *a_row = p.a + (a_live ? m0 + r : 0) * p.a_rs, *w_row = p.w + (int64_t)(w_live ? n0 + r : 0) * p.w_rs;
-  int16v acc = zero16();
-  int4v a = fetch(a_row, a_live, c0), w = fetch(w_row, w_live, c0);
-  for (int k0 = 0; k0 < p.channels; k0 += AK) {
-    __syncthreads();
-    *(int4v*)(As + r * AS + c0) = a;
-    *(int4v*)(Ws + r * AS + c0) = w;
-    a = fetch(a_row, a_live && k0 + AK < p.channels, k0 + AK + c0);      // (the next step's, while this one is multiplied)
-    w = fetch(w_row, w_live && k0 + AK < p.channels, k0 + AK + c0);
-    __syncthreads();
+  auto store = [&](const Step& x, int buf) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      *(int4v*)(As[buf] + (r + 64 * i) * AS + c0) = x.a[i];
+      *(int4v*)(Ws[buf] + (r + 64 * i) * AS + c0) = x.w[i];
+    }
+  };
+  auto multiply = [&](int buf) {
 #pragma unroll
     for (int s = 0; s < AK / 32; ++s) {
-      const int4v rows_ = *(const int4v*)(As + ((wave & 1) * 32 + nn) * AS + s * 32 + g * 16);
-      const int4v cols = *(const int4v*)(Ws + ((wave >> 1) * 32 + nn) * AS + s * 32 + g * 16);
-      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(cols, rows_, acc, 0, 0, 0);
+      int4v rows_[MI], cols[MI];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        rows_[i] = *(const int4v*)(As[buf] + (wm * (TM / 2) + i * 32 + nn) * AS + s * 32 + g * 16);
+        cols[i] = *(const int4v*)(Ws[buf] + (wn * (TM / 2) + i * 32 + nn) * AS + s * 32 + g * 16);
+      }
+#pragma unroll
+      for (int n = 0; n < MI; ++n)
+#pragma unroll
+        for (int m = 0; m < MI; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(cols[n], rows_[m], acc[n][m], 0, 0, 0);
+    }
+  };
+  // two steps under way in registers, one in LDS
+  Step even, odd;
+  fetch(even, 0);
+  fetch(odd, AK);
+  for (int k0 = 0; k0 < p.channels; k0 += 2 * AK) {
+    store(even, 0);
+    fetch(even, k0 + 2 * AK);
+    __syncthreads();
+    multiply(0);
+    if (k0 + AK < p.channels) {
+      store(odd, 1);
+      fetch(odd, k0 + 3 * AK);
+      __syncthreads();
+      multiply(1);
     }
   }
-  const int64_t row = m0 + (wave & 1) * 32 + nn;
-  const bool live = row < p.rows;
-  store_tile<T>(p, acc, row, n0 + (wave >> 1) * 32, g, live ? p.a_scales[row] : 0.f, live);
+#pragma unroll
+  for (int m = 0; m < MI; ++m) {
+    const int64_t row = m0 + wm * (TM / 2) + m * 32 + nn;
+    const bool live = row < p.rows;
+    const float sa = live ? p.a_scales[row] : 0.f;
+#pragma unroll
+    for (int n = 0; n < MI; ++n) store_tile<T>(p, acc[n][m], row, n0 + wn * (TM / 2) + n * 32, g, sa, live);
+  }
 }
 
 // ---- few rows: 16 columns of the output a workgroup, whose waves share the sum -------------------------------------------------------------------------------
@@ -196,20 +275,6 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) k_product_few(ProductParams p)
       const float x = scaled(s[j], sa, p.w_scales[c + j]);
       to[c + j] = narrow<T>(p.bias ? x + widen(((const T*)p.bias)[c + j]) : x);
     }
-}
-
-// The tile of a workgroup.  Workgroups are dealt to the 8 XCDs in turn and each XCD has an L2 of its own: XCD x takes the x-th eighth of the tiles, in an order that goes through
-// GROUP rows of tiles column by column, so that the tiles that run at the same time share few rows and columns.
-constexpr int GROUP = 4;
-__device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int& mt, int& nt) {
-  const unsigned all = (unsigned)tiles_m * (unsigned)tiles_n, each = (all + 7) / 8;
-  const unsigned id = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= each || id >= all) return false;
-  const unsigned group = id / (GROUP * (unsigned)tiles_n), in = id - group * GROUP * (unsigned)tiles_n;
-  const unsigned rows_ = min((unsigned)GROUP, (unsigned)tiles_m - group * GROUP);
-  nt = (int)(in / rows_);
-  mt = (int)(group * GROUP + in - (unsigned)nt * rows_);
-  return true;
 }
 
 // ---- tiles: TM x TN results a workgroup of four waves, steps of 128 channels copied straight into LDS, S - 1 steps ahead -------------------------------------
@@ -435,11 +500,12 @@ hipError_t wide(const ProductParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, int TM>
 hipError_t any(const ProductParams& p, hipStream_t st) {
-  const int64_t tiles_n = ((int64_t)p.outputs + AM - 1) / AM, blocks = ((int64_t)p.rows + AM - 1) / AM * tiles_n;
+  const int tiles_m = (int)(((int64_t)p.rows + TM - 1) / TM), tiles_n = (int)(((int64_t)p.outputs + TM - 1) / TM);
+  const int64_t blocks = ((int64_t)tiles_m * tiles_n + 7) / 8 * 8;
   if (blocks >= ((int64_t)1 << 23)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(k_product_any<T>, dim3((unsigned)blocks), dim3(256), 0, st, p, (int)tiles_n);
+  hipLaunchKernelGGL((k_product_any<T, TM>), dim3((unsigned)blocks), dim3(256), 0, st, p, tiles_m, tiles_n);
   return hipGetLastError();
 }
 
@@ -461,7 +527,14 @@ constexpr int S64 = 3, S128 = 2, FEW_ROWS = 32;
 
 template <typename T>
 hipError_t go(const ProductParams& p, int num_cu, hipStream_t st) {
-  if (!p.vec) return any<T>(p, st);
+  if (!p.vec) {
+    // by the time of the launch, us at 2048 channels: tiles of 64 take 7.2 on a full compute unit and 13 alone, of 128 19 and 25 (14,599 x 1999 -> 2000 206 / 137, 2000 x 3001 -> 1000
+    // 23 / 34, 333 x 1000 -> 1100 7.1 / 13.5)
+    auto time = [&](int64_t n, float each, float alone) {
+      return std::max(alone, each * (float)(((int64_t)p.rows + n - 1) / n * (((int64_t)p.outputs + n - 1) / n)) / (float)num_cu);
+    };
+    return time(128, 19.f, 25.f) < time(64, 7.2f, 13.f) ? any<T, 128>(p, st) : any<T, 64>(p, st);
+  }
   if (p.rows <= FEW_ROWS) return few<T>(p, st);
   // The kernel whose rounds of the chip take the shortest, us at 2048 channels (others in proportion): a compute unit holds three workgroups of 64 x 64 tiles (one of them alone 9, or 7 in
   // two groups, two 12, three 13), two of 128 x 128 (16, 28) or one of 256 x 256 (29).  Measured as tiles of 64 / 128 / 256: 1024 x 2048 -> 2048 11.6 / 16.6 / 29.5, 2048 x 2048 -> 2048 21.6 / 18.2 /
