@@ -1,8 +1,8 @@
 // Products of rows of 8-bit codes: out[m][n] = s_a[m] s_w[n] sum_k a[m][k] w[n][k] + bias[n], k adjacent in both.  Sums are whole numbers of 32 bits, exact up to 131,071
 // channels, so neither their order nor their cut shows in the result; scaling and bias are fp32, rounded once to the output's type.
 //
-// Long products are bound by the matrix cores and the clock that power leaves them: 65,536 x 1536 -> 4608 542 us (1.71 POPS; a library's product without scales 557), 131,072 x 2048 -> 2048
-// 605 (1.82; 589), 16,384 x 4096 -> 4096 259 (2.12), 8192 x 4096 -> 4096 131; in a run with counters the second took 692 us, matrix cores busy 42 % at 1.8 GHz.  A few rows are bound by the
+// Long products are bound by the matrix cores and the clock that power leaves them: 65,536 x 1536 -> 4608 536 us (1.73 POPS; a library's product without scales 557), 131,072 x 2048 -> 2048
+// 605-619 (1.8; 589), 16,384 x 4096 -> 4096 256 (2.15), 8192 x 4096 -> 4096 130; in a run with counters the second took 692 us, matrix cores busy 42 % at 1.8 GHz.  A few rows are bound by the
 // weights' bytes and latency.
 //
 // Operands are fed to the matrix cores as 16 bytes a lane, k = 16 g .. 16 g + 15 of a product's channels on lane group g; both sides use the same order, so any
@@ -36,11 +36,10 @@ __device__ __forceinline__ void copy16(const void* src, unsigned dst) {
 __device__ __forceinline__ bool far_scale(float sa) { return sa > 0x1p96f; }
 __device__ __forceinline__ float scaled(int sum, float sa, float sw) { return far_scale(sa) ? (float)sum * sw * sa : (float)sum * sa * sw; }
 
-// Eight results of a row, columns c .. c + 7.
+// Eight results of a row, columns c .. c + 7 (zeros where there is no column), as pieces of the output.
 template <typename T>
-__device__ __forceinline__ void store8(const ProductParams& p, int64_t row, int c, const int (&acc)[8], float sa) {
+__device__ __forceinline__ void finish8(const ProductParams& p, int c, const int (&acc)[8], float sa, Piece<T> (&x)[8 / PW<T>]) {
   float o[8];
-  T* to = (T*)p.out + row * p.out_rs;
   if (c + 8 <= p.outputs) {
     const float4v s0 = *(const float4any*)(p.w_scales + c), s1 = *(const float4any*)(p.w_scales + c + 4);
 #pragma unroll
@@ -59,38 +58,72 @@ __device__ __forceinline__ void store8(const ProductParams& p, int64_t row, int 
         for (int j = 0; j < PW<T>; ++j) o[i * PW<T> + j] += b.get(j);
       }
     }
-#pragma unroll
-    for (int i = 0; i < 8 / PW<T>; ++i) {
-      Piece<T> x;
-#pragma unroll
-      for (int j = 0; j < PW<T>; j += 2) x.set(j, o[i * PW<T> + j], o[i * PW<T> + j + 1]);
-      *(uint4any*)(to + c + i * PW<T>) = x.raw;
-    }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < 8; ++j) {
+      o[j] = 0.f;
       if (c + j < p.outputs) {
-        const float x = scaled(acc[j], sa, p.w_scales[c + j]);
-        to[c + j] = narrow<T>(p.bias ? x + widen(((const T*)p.bias)[c + j]) : x);
+        o[j] = scaled(acc[j], sa, p.w_scales[c + j]);
+        if (p.bias) o[j] += widen(((const T*)p.bias)[c + j]);
       }
+    }
   }
+#pragma unroll
+  for (int i = 0; i < 8 / PW<T>; ++i)
+#pragma unroll
+    for (int j = 0; j < PW<T>; j += 2) x[i].set(j, o[i * PW<T> + j], o[i * PW<T> + j + 1]);
 }
 
 // The accumulators of a 32 x 32 product hold one row a lane and the columns 8 (r / 4) + 4 g + r % 4: after a swap of registers with lane ^ 32 (the same row) a lane has
 // 8 neighbouring columns.
+__device__ __forceinline__ void neighbours(const int16v& acc, int j, int (&o)[8]) {
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const auto sw = __builtin_amdgcn_permlane32_swap((unsigned)acc[8 * j + b], (unsigned)acc[8 * j + 4 + b], false, false);
+    o[b] = (int)sw[0];
+    o[4 + b] = (int)sw[1];
+  }
+}
 template <typename T>
 __device__ __forceinline__ void store_tile(const ProductParams& p, const int16v& acc, int64_t row, int col, int g, float sa, bool live) {
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     int o[8];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const auto sw = __builtin_amdgcn_permlane32_swap((unsigned)acc[8 * j + b], (unsigned)acc[8 * j + 4 + b], false, false);
-      o[b] = (int)sw[0];
-      o[4 + b] = (int)sw[1];
-    }
+    neighbours(acc, j, o);
     const int c = col + j * 16 + g * 8;
-    if (live && c < p.outputs) store8<T>(p, row, c, o, sa);
+    if (live && c < p.outputs) {
+      Piece<T> x[8 / PW<T>];
+      finish8<T>(p, c, o, sa, x);
+#pragma unroll
+      for (int i = 0; i < 8 / PW<T>; ++i) x[i].store((T*)p.out + row * p.out_rs, c + i * PW<T>, p.outputs);
+    }
+  }
+}
+
+// 32 rows x 64 columns, two products side by side, through a wave's 8 KB (fp32; bf16: 4) of LDS, so that a store covers whole lines of a few rows instead of 32 bytes of each
+// (100,000 x 96 -> 4096 338 / 282 us, 65,536 x 256 -> 4096 270 / 235, 65,536 x 1536 -> 4608 543 / 536).
+template <typename T>
+__device__ __forceinline__ void store_wide(const ProductParams& p, const int16v& left, const int16v& right, int first, int col, int lane, uint4v* mine) {
+  constexpr int CH = 64 / PW<T>, STORES = 32 * CH / 64;      // pieces of such a row; stores of a lane
+  const int nn = lane & 31, g = lane >> 5;
+  const float sa = p.a_scales[min(first + nn, p.rows - 1)];
+#pragma unroll
+  for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      int o[8];
+      neighbours(c2 ? right : left, j, o);
+      Piece<T> x[8 / PW<T>];
+      finish8<T>(p, col + 32 * c2 + 16 * j + 8 * g, o, sa, x);
+#pragma unroll
+      for (int i = 0; i < 8 / PW<T>; ++i) mine[nn * CH + (((4 * c2 + 2 * j + g) * (8 / PW<T>) + i) ^ (nn & 7))] = x[i].raw;
+    }
+#pragma unroll
+  for (int i = 0; i < STORES; ++i) {
+    const int r = i * (64 / CH) + lane / CH, ch = lane % CH;
+    Piece<T> x;
+    x.raw = mine[r * CH + (ch ^ (r & 7))];
+    if (first + r < p.rows) x.store((T*)p.out + (int64_t)(first + r) * p.out_rs, col + ch * PW<T>, p.outputs);
   }
 }
 
@@ -140,7 +173,8 @@ __device__ __forceinline__ int4v row_piece(const char* row, int k, int n) {
 template <typename T, int TM>
 __global__ void __launch_bounds__(256) k_product_any(ProductParams p, int tiles_m, int tiles_n) {
   constexpr int MI = TM / 64;      // 32 x 32 products of a wave each way; pieces of 16 codes of a thread and operand
-  __shared__ __attribute__((aligned(16))) int8_t As[2][TM * AS], Ws[2][TM * AS];
+  __shared__ __attribute__((aligned(16))) int8_t both[4][TM * AS];
+  int8_t(*const As)[TM * AS] = both, (*const Ws)[TM * AS] = both + 2;
   int mt, nt;
   if (!tile_of(tiles_m, tiles_n, mt, nt)) return;
   const int64_t m0 = (int64_t)mt * TM;
@@ -212,13 +246,15 @@ __global__ void __launch_bounds__(256) k_product_any(ProductParams p, int tiles_
       multiply(1);
     }
   }
+  if constexpr (MI == 2) {
+    static_assert(MI == 1 || 4 * TM * AS >= 4 * 8192, "");
+    __syncthreads();
 #pragma unroll
-  for (int m = 0; m < MI; ++m) {
-    const int64_t row = m0 + wm * (TM / 2) + m * 32 + nn;
+    for (int m = 0; m < MI; ++m) store_wide<T>(p, acc[0][m], acc[1][m], (int)m0 + wm * (TM / 2) + m * 32, n0 + wn * (TM / 2), lane, (uint4v*)(both[0] + wave * 8192));
+  } else {
+    const int64_t row = m0 + wm * (TM / 2) + nn;
     const bool live = row < p.rows;
-    const float sa = live ? p.a_scales[row] : 0.f;
-#pragma unroll
-    for (int n = 0; n < MI; ++n) store_tile<T>(p, acc[n][m], row, n0 + wn * (TM / 2) + n * 32, g, sa, live);
+    store_tile<T>(p, acc[0][0], row, n0 + wn * (TM / 2), g, live ? p.a_scales[row] : 0.f, live);
   }
 }
 
@@ -286,6 +322,7 @@ __global__ void __launch_bounds__(256 * G) k_product_tile(ProductParams p, int t
   constexpr int MI = TM / 64, NI = TN / 64;     // 32 x 32 products of a wave: its rows TM / 2, its columns TN / 2
   constexpr int COPIES = TM / 32 + TN / 32;     // of a wave and step
   static_assert(G * S * (TM + TN) * 128 <= 160 * 1024 && (S - 2) * COPIES < 64, "");
+  static_assert(NI == 1 ? MI == 1 : NI == 2 && G * S * TM * 128 >= 4 * 8192, "");
   static_assert(G == 1 || (MI * NI == 1 && (G - 1) * 4 * 64 * 64 <= G * S * TM * 128), "");
   __shared__ __attribute__((aligned(16))) int8_t all_a[G][S][TM * 128], all_w[G][S][TN * 128];
   int mt, nt;
@@ -358,13 +395,14 @@ __global__ void __launch_bounds__(256 * G) k_product_tile(ProductParams p, int t
         for (int k = 0; k < 4; ++k) acc[0][0][4 * j + k] += x[k];
       }
   }
+  if constexpr (NI == 2) {
+    __syncthreads();
 #pragma unroll
-  for (int m = 0; m < MI; ++m) {
-    const int row = m0 + wm * (TM / 2) + m * 32 + nn;
+    for (int m = 0; m < MI; ++m) store_wide<T>(p, acc[0][m], acc[1][m], m0 + wm * (TM / 2) + m * 32, n0 + wn * (TN / 2), lane, (uint4v*)(all_a[0][0] + wave * 8192));
+  } else {
+    const int row = m0 + wm * (TM / 2) + nn;
     const bool live = row < p.rows;
-    const float sa = live ? p.a_scales[row] : 0.f;
-#pragma unroll
-    for (int n = 0; n < NI; ++n) store_tile<T>(p, acc[n][m], row, n0 + wn * (TN / 2) + n * 32, g, sa, live);
+    store_tile<T>(p, acc[0][0], row, n0 + wn * (TN / 2), g, live ? p.a_scales[row] : 0.f, live);
   }
 }
 
@@ -468,17 +506,14 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductParams p, int ti
     phase(1, 0, 1, 3, 1, 0);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (copies into this workgroup's LDS)
+  __syncthreads();
 #pragma unroll
-  for (int rt = 0; rt < 2; ++rt) {
-    const int row = m0 + 128 * rt + 32 * wm + nn;
-    const bool live = row < p.rows;
-    const float sa = live ? p.a_scales[row] : 0.f;
+  for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct) {
-      store_tile<T>(p, acc[ct][rt], row, n0 + 64 * wn + 128 * (ct >> 1) + 32 * (ct & 1), g, sa, live);
+    for (int h = 0; h < 2; ++h) {
+      store_wide<T>(p, acc[2 * h][rt], acc[2 * h + 1][rt], m0 + 128 * rt + 32 * wm, n0 + 64 * wn + 128 * h, lane, (uint4v*)(lds[0][0] + wave * HALF));
       __builtin_amdgcn_sched_barrier(0);
     }
-  }
 }
 
 template <typename T, int TM, int TN, int S, int G>
