@@ -10,7 +10,7 @@
 // a workgroup adds its waves' shares in their order and stores one row of partial sums, k_norm_weights adds those: no atomics, equal calls give equal bits.
 //
 // Measured (us, bf16 unless said): 131,072 x 2048 forward 182 (5.9 TB/s), backward 325 (4.95); 2 x 65,536 x 1536 with weights each 142 and 235; 10,007 x 999 fp32 16 and 29, of which adding up
-// dw and db 4 (rows of odd length start at any element); 60,000 x 173 18 and 42, bound by the loads' number, not their bytes; a single row 3 and 4.
+// dw and db 4 (rows of odd length start at any element); 60,000 x 173 15 and 33, bound by vector work and the loads' number, not their bytes; a single row 3 and 4.
 #include <algorithm>
 
 #include "rows.h"
@@ -322,27 +322,27 @@ __global__ void __launch_bounds__(1024) k_norm_weights(NormParams p) {
   }
 }
 
-// Waves for each compute unit.  Backward: every workgroup leaves a row of partial sums (8 / 16 waves: 131,072 x 2048 bf16 325 / 368 us, 65,536 x 1024 80 / 94, 10,007 x 999 fp32 29 / 37; rows of
-// 173 channels alone gain by more, 42 / 31).
-constexpr int FWD_WAVES = 16, FWD_MOST_WAVES = 256, BWD_WAVES = 8;
+// Waves for each compute unit.  Backward: every workgroup leaves a row of partial sums (8 / 16 waves: 131,072 x 2048 bf16 325 / 368 us, 65,536 x 1024 80 / 94, 10,007 x 999 fp32 29 / 37; up to
+// 512 channels, whose registers are few: 60,000 x 173 43 / 33, 30,000 x 336 34 / 27, 100,000 x 250 fp32 78 / 58, 200,000 x 64 23 / 22, 500,000 x 128 fp32 137 / 149).
+constexpr int FWD_WAVES = 16, FWD_MOST_WAVES = 256, BWD_WAVES = 8, BWD_WAVES_NARROW = 16;
 
 }  // namespace
 
 int norm_backward_blocks(int64_t n, int64_t groups, int channels, int dtype, int num_cu) {
   auto of = [&](auto l, auto w, auto) {
     using At = Place<float, l.value, w.value, 1>;
-    int64_t b = blocks_of(n, groups, At::STEP, At::THREADS, BWD_WAVES, num_cu);
+    int64_t b = blocks_of(n, groups, At::STEP, At::THREADS, channels <= 512 ? BWD_WAVES_NARROW : BWD_WAVES, num_cu);
     // four rows at least for each row of partial sums, unless that leaves compute units idle
     const int64_t four = (n + 4 * At::STEP - 1) / (4 * At::STEP), all = (num_cu + groups - 1) / groups;
     if (b > four && b > all) b = four > all ? four : all;
     return (int)(b < 1 ? 1 : b);
   };
-  return dtype == FREQATTN_BF16 ? for_channels<Bf16>(channels, of) : for_channels<float>(channels, of);
+  return dtype == FREQATTN_BF16 ? for_channels<Bf16, false>(channels, of) : for_channels<float, false>(channels, of);
 }
 
 template <typename T>
 static hipError_t forward(const NormParams& p, int num_cu, hipStream_t st) {
-  return for_channels<T>(p.channels, [&](auto l, auto w, auto pt) {
+  return for_channels<T, sizeof(T) == 2>(p.channels, [&](auto l, auto w, auto pt) {
     using At = Place<T, l.value, w.value, pt.value>;
     // 16 waves for each compute unit, and more where every workgroup still has four steps: rows that are dealt out as workgroups end keep memory busier than fixed shares of a long
     // tensor (16 / 4 steps: 131,072 x 2048 bf16 210 / 182 us, 2 x 65,536 x 1536 151 / 142, 20,000 x 4096 60 / 57), while the first row of a workgroup is not requested ahead (one step
@@ -355,7 +355,7 @@ static hipError_t forward(const NormParams& p, int num_cu, hipStream_t st) {
 }
 template <typename T>
 static hipError_t backward(const NormParams& p, hipStream_t st) {
-  return for_channels<T>(p.channels, [&](auto l, auto w, auto pt) {
+  return for_channels<T, false>(p.channels, [&](auto l, auto w, auto pt) {
     using At = Place<T, l.value, w.value, pt.value>;
     hipLaunchKernelGGL((k_layer_norm_backward<T, l.value, w.value, pt.value>), dim3((unsigned)p.blocks, (unsigned)p.groups), dim3(At::THREADS), 0, st, p);
     return hipGetLastError();

@@ -140,13 +140,18 @@ __device__ __forceinline__ T* row_of(const RowsPtr& v, int rows, int64_t i) {
   return (T*)v.p + b * v.bs + (i - b * rows) * v.rs;
 }
 
-// The variant whose lanes hold a row: go(LPR, W, PT).
-template <typename T, typename F>
+// The variant whose lanes hold a row: go(LPR, W, PT).  TWO: rows of up to 512 channels lie on half as many lanes, two pieces of eight channels each, so that a wave's sums over lanes are of
+// twice as many rows.  That gains where vector work bounds such rows (one piece / two: norm of 60,000 x 173 bf16 19.2 / 14.8 us, 300,000 x 128 27.1 / 25.5; codes of the same 18.1 / 12.7,
+// 34 / 23.5, of 200,000 x 99 fp32 22.4 / 21.0) and loses elsewhere (norm of 200,000 x 99 fp32 28 / 31; backward of 60,000 x 173 bf16 33 / 37, 100,000 x 250 fp32 58 / 80).
+template <typename T, bool TWO, typename F>
 auto for_channels(int channels, F&& go) {
   constexpr int U = 8 / PW<T>;      // pieces of eight channels
   const int eights = (channels + 7) / 8;
 #define FA_ROWS(L_, W_, P_) if (eights <= (L_) * (W_) * (P_)) return go(std::integral_constant<int, L_>(), std::integral_constant<int, W_>(), std::integral_constant<int, (P_) * U>());
-  FA_ROWS(8, 1, 1) FA_ROWS(16, 1, 1) FA_ROWS(32, 1, 1) FA_ROWS(64, 1, 1) FA_ROWS(64, 1, 2) FA_ROWS(64, 1, 3)
+  FA_ROWS(8, 1, 1)
+  if constexpr (TWO) { FA_ROWS(8, 1, 2) FA_ROWS(16, 1, 2) FA_ROWS(32, 1, 2) }
+  else { FA_ROWS(16, 1, 1) FA_ROWS(32, 1, 1) FA_ROWS(64, 1, 1) }
+  FA_ROWS(64, 1, 2) FA_ROWS(64, 1, 3)
   FA_ROWS(64, 2, 2) FA_ROWS(64, 4, 2) FA_ROWS(64, 8, 2)
 #undef FA_ROWS
   return go(std::integral_constant<int, 64>(), std::integral_constant<int, 8>(), std::integral_constant<int, 4 * U>());
