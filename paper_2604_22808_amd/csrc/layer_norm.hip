@@ -10,7 +10,7 @@
 // a workgroup adds its waves' shares in their order and stores one row of partial sums, k_norm_weights adds those: no atomics, equal calls give equal bits.
 //
 // Measured (us, bf16 unless said): 131,072 x 2048 forward 182 (5.9 TB/s), backward 325 (4.95); 2 x 65,536 x 1536 with weights each 142 and 235; 10,007 x 999 fp32 16 and 29, of which adding up
-// dw and db 4 (rows of odd length start at any element); 60,000 x 173 15 and 33, bound by vector work and the loads' number, not their bytes; a single row 3 and 4.
+// dw and db 4 (rows of odd length start at any element); 60,000 x 173 13 and 33, bound by vector work and the loads' number, not their bytes; a single row 3 and 4.
 #include <algorithm>
 
 #include "rows.h"
@@ -337,12 +337,12 @@ int norm_backward_blocks(int64_t n, int64_t groups, int channels, int dtype, int
     if (b > four && b > all) b = four > all ? four : all;
     return (int)(b < 1 ? 1 : b);
   };
-  return dtype == FREQATTN_BF16 ? for_channels<Bf16, false>(channels, of) : for_channels<float, false>(channels, of);
+  return dtype == FREQATTN_BF16 ? for_channels<Bf16, HALF_PACKED>(channels, of) : for_channels<float, HALF_PACKED>(channels, of);
 }
 
 template <typename T>
 static hipError_t forward(const NormParams& p, int num_cu, hipStream_t st) {
-  return for_channels<T, sizeof(T) == 2>(p.channels, [&](auto l, auto w, auto pt) {
+  return for_channels<T, sizeof(T) == 2 ? PACKED : SPREAD>(p.channels, [&](auto l, auto w, auto pt) {
     using At = Place<T, l.value, w.value, pt.value>;
     // 16 waves for each compute unit, and more where every workgroup still has four steps: rows that are dealt out as workgroups end keep memory busier than fixed shares of a long
     // tensor (16 / 4 steps: 131,072 x 2048 bf16 210 / 182 us, 2 x 65,536 x 1536 151 / 142, 20,000 x 4096 60 / 57), while the first row of a workgroup is not requested ahead (one step
@@ -355,7 +355,7 @@ static hipError_t forward(const NormParams& p, int num_cu, hipStream_t st) {
 }
 template <typename T>
 static hipError_t backward(const NormParams& p, hipStream_t st) {
-  return for_channels<T, false>(p.channels, [&](auto l, auto w, auto pt) {
+  return for_channels<T, HALF_PACKED>(p.channels, [&](auto l, auto w, auto pt) {
     using At = Place<T, l.value, w.value, pt.value>;
     hipLaunchKernelGGL((k_layer_norm_backward<T, l.value, w.value, pt.value>), dim3((unsigned)p.blocks, (unsigned)p.groups), dim3(At::THREADS), 0, st, p);
     return hipGetLastError();

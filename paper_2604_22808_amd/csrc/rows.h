@@ -140,17 +140,21 @@ __device__ __forceinline__ T* row_of(const RowsPtr& v, int rows, int64_t i) {
   return (T*)v.p + b * v.bs + (i - b * rows) * v.rs;
 }
 
-// The variant whose lanes hold a row: go(LPR, W, PT).  TWO: rows of up to 512 channels lie on half as many lanes, two pieces of eight channels each, so that a wave's sums over lanes are of
-// twice as many rows.  That gains where vector work bounds such rows (one piece / two: norm of 60,000 x 173 bf16 19.2 / 14.8 us, 300,000 x 128 27.1 / 25.5; codes of the same 18.1 / 12.7,
-// 34 / 23.5, of 200,000 x 99 fp32 22.4 / 21.0) and loses elsewhere (norm of 200,000 x 99 fp32 28 / 31; backward of 60,000 x 173 bf16 33 / 37, 100,000 x 250 fp32 58 / 80).
-template <typename T, bool TWO, typename F>
+// How rows of up to 768 channels lie.  SPREAD: on as many lanes as there are pieces of eight channels.  PACKED: on half as many or fewer, two or three such pieces each, so that a wave's sums
+// over lanes are of more rows: that gains where vector work bounds them (spread / packed: norm of 60,000 x 173 bf16 19.2 / 13.4 us, 60,000 x 768 36 / 31, 300,000 x 128 27.1 / 25.5; codes of
+// the same 18.1 / 11.5, 33 / 26, 34 / 23.5, of 200,000 x 99 fp32 22.4 / 21.0), and loses elsewhere (norm of 200,000 x 99 fp32 28 / 31, 30,000 x 700 30.5 / 33.3).  HALF_PACKED: the
+// backward pass, whose registers are more (spread / packed: 60,000 x 173 bf16 33 / 37, 100,000 x 250 fp32 58 / 80, but 60,000 x 768 bf16 87 / 52, 40,000 x 640 53 / 41, 30,000 x 600 fp32 50 / 46).
+enum Lay { SPREAD, PACKED, HALF_PACKED };
+// The variant whose lanes hold a row: go(LPR, W, PT).
+template <typename T, Lay LAY, typename F>
 auto for_channels(int channels, F&& go) {
   constexpr int U = 8 / PW<T>;      // pieces of eight channels
   const int eights = (channels + 7) / 8;
 #define FA_ROWS(L_, W_, P_) if (eights <= (L_) * (W_) * (P_)) return go(std::integral_constant<int, L_>(), std::integral_constant<int, W_>(), std::integral_constant<int, (P_) * U>());
   FA_ROWS(8, 1, 1)
-  if constexpr (TWO) { FA_ROWS(8, 1, 2) FA_ROWS(16, 1, 2) FA_ROWS(32, 1, 2) }
+  if constexpr (LAY == PACKED) { FA_ROWS(8, 1, 2) FA_ROWS(8, 1, 3) FA_ROWS(16, 1, 2) FA_ROWS(16, 1, 3) FA_ROWS(32, 1, 2) }
   else { FA_ROWS(16, 1, 1) FA_ROWS(32, 1, 1) FA_ROWS(64, 1, 1) }
+  if constexpr (LAY != SPREAD) { FA_ROWS(32, 1, 3) }
   FA_ROWS(64, 1, 2) FA_ROWS(64, 1, 3)
   FA_ROWS(64, 2, 2) FA_ROWS(64, 4, 2) FA_ROWS(64, 8, 2)
 #undef FA_ROWS

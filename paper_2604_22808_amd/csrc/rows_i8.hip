@@ -165,7 +165,7 @@ hipError_t go(const CodeParams& p, int num_cu, hipStream_t st) {
   using std::integral_constant;
   // (one wave with four pieces a lane here too, without a barrier: 131,072 x 2048 bf16 182 us on two waves, 156 on one)
   if (p.channels > 1536 && p.channels <= 2048) return launch(integral_constant<int, 64>(), integral_constant<int, 1>(), integral_constant<int, 4 * U>());
-  return for_channels<T, true>(p.channels, launch);
+  return for_channels<T, PACKED>(p.channels, launch);
 }
 
 }  // namespace
