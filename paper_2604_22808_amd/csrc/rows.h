@@ -140,10 +140,12 @@ __device__ __forceinline__ T* row_of(const RowsPtr& v, int rows, int64_t i) {
   return (T*)v.p + b * v.bs + (i - b * rows) * v.rs;
 }
 
-// How rows of up to 768 channels lie.  SPREAD: on as many lanes as there are pieces of eight channels.  PACKED: on half as many or fewer, two or three such pieces each, so that a wave's sums
+// How rows lie.  SPREAD: up to 512 channels on as many lanes as there are pieces of eight.  PACKED: up to 768 on half as many or fewer, two or three such pieces each, so that a wave's sums
 // over lanes are of more rows: that gains where vector work bounds them (spread / packed: norm of 60,000 x 173 bf16 19.2 / 13.4 us, 60,000 x 768 36 / 31, 300,000 x 128 27.1 / 25.5; codes of
 // the same 18.1 / 11.5, 33 / 26, 34 / 23.5, of 200,000 x 99 fp32 22.4 / 21.0), and loses elsewhere (norm of 200,000 x 99 fp32 28 / 31, 30,000 x 700 30.5 / 33.3).  HALF_PACKED: the
 // backward pass, whose registers are more (spread / packed: 60,000 x 173 bf16 33 / 37, 100,000 x 250 fp32 58 / 80, but 60,000 x 768 bf16 87 / 52, 40,000 x 640 53 / 41, 30,000 x 600 fp32 50 / 46).
+// Rows of two and four waves likewise: both take three pieces a lane for more than 2048 and 4096 channels, as far as that reaches (20,000 x 2500 bf16 forward 47 / 41, backward 146 / 99, codes 38 / 32; 8000 x 6000
+// fp32 forward 74 / 84, backward 143 / 129, codes 40 / 35).
 enum Lay { SPREAD, PACKED, HALF_PACKED };
 // The variant whose lanes hold a row: go(LPR, W, PT).
 template <typename T, Lay LAY, typename F>
@@ -156,7 +158,11 @@ auto for_channels(int channels, F&& go) {
   else { FA_ROWS(16, 1, 1) FA_ROWS(32, 1, 1) FA_ROWS(64, 1, 1) }
   if constexpr (LAY != SPREAD) { FA_ROWS(32, 1, 3) }
   FA_ROWS(64, 1, 2) FA_ROWS(64, 1, 3)
-  FA_ROWS(64, 2, 2) FA_ROWS(64, 4, 2) FA_ROWS(64, 8, 2)
+  FA_ROWS(64, 2, 2)
+  if constexpr (LAY != SPREAD) { FA_ROWS(64, 2, 3) }
+  FA_ROWS(64, 4, 2)
+  if constexpr (LAY != SPREAD) { FA_ROWS(64, 4, 3) }
+  FA_ROWS(64, 8, 2)
 #undef FA_ROWS
   return go(std::integral_constant<int, 64>(), std::integral_constant<int, 8>(), std::integral_constant<int, 4 * U>());
 }

@@ -45,7 +45,7 @@ def expect(x, w, b, eps, io, each, dout=None):
 
 SIZES = [(1, 1, 1), (1, 1, 7), (2, 3, 8), (1, 5, 64), (3, 4, 65), (1, 33, 130), (2, 9, 257), (1, 7, 512), (1, 17, 515), (2, 6, 1000), (1, 300, 999), (1, 9, 1536),
          (2, 130, 1540), (1, 5, 2048), (1, 6, 2500), (1, 4, 4096), (2, 3, 5001), (1, 3, 8192), (1, 3, 9000), (1, 2, 16384),
-         (1, 41, 150), (1, 35, 350), (2, 30, 500), (1, 70, 601), (1, 50, 760)]
+         (1, 41, 150), (1, 35, 350), (2, 30, 500), (1, 70, 601), (1, 50, 760), (1, 7, 3333), (1, 4, 6001)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

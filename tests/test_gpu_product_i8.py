@@ -17,7 +17,7 @@ def codes_of(x):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n,c", [(1, 1), (3, 7), (70, 16), (33, 65), (5, 250), (21, 150), (11, 350), (9, 601), (64, 512), (9, 1000), (40, 1536), (6, 2048), (5, 4096), (4, 5001), (3, 16384), (2, 20001), (2, 131071)])
+@pytest.mark.parametrize("n,c", [(1, 1), (3, 7), (70, 16), (33, 65), (5, 250), (21, 150), (11, 350), (9, 601), (64, 512), (9, 1000), (40, 1536), (6, 2048), (4, 2500), (3, 3333), (5, 4096), (4, 5001), (3, 7001), (3, 16384), (2, 20001), (2, 131071)])
 def test_codes_are_exact(n, c, dtype):
     io, gen = U.TYPES[dtype], torch.Generator().manual_seed(n * c)
     x = torch.randn(n, c, generator=gen, dtype=torch.float64).to(io)
