@@ -2,7 +2,7 @@
 // channels, so neither their order nor their cut shows in the result; scaling and bias are fp32, rounded once to the output's type.
 //
 // Long products are bound by the matrix cores and the clock that power leaves them: 65,536 x 1536 -> 4608 536 us (1.73 POPS; a library's product without scales 557), 131,072 x 2048 -> 2048
-// 605-619 (1.8; 589), 16,384 x 4096 -> 4096 256 (2.15), 8192 x 4096 -> 4096 130; in a run with counters the second took 692 us, matrix cores busy 42 % at 1.8 GHz.  A few rows are bound by the
+// 605-619 (1.8; 589), 16,384 x 4096 -> 4096 256 (2.15), 8192 x 4096 -> 4096 130; in a run with counters the second took 675 us, matrix cores busy 45 % at 1.8 GHz.  A few rows are bound by the
 // weights' bytes and latency.
 //
 // Operands are fed to the matrix cores as 16 bytes a lane, k = 16 g .. 16 g + 15 of a product's channels on lane group g; both sides use the same order, so any
