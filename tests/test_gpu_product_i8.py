@@ -81,7 +81,8 @@ def expect(a, w, sa, sw, bias, io):
 
 SIZES = [(1, 1, 1), (1, 16, 16), (2, 15, 3), (1, 2048, 48), (16, 2048, 6144), (5, 1040, 250), (17, 512, 100), (33, 4096, 40), (64, 144, 1000), (65, 128, 64), (100, 96, 130),
          (333, 1000, 1100), (200, 1008, 129), (257, 2048, 512), (128, 256, 128), (1000, 384, 700), (513, 1536, 4608), (2100, 160, 2304), (70000, 64, 48), (70001, 48, 100), (66000, 80, 200), (32, 304, 4000), (3, 8192, 1024), (70, 131056, 65),
-         (1000, 2064, 2048), (300, 4112, 608), (64, 656, 1000), (40, 128, 64)]
+         (1000, 2064, 2048), (300, 4112, 608), (64, 656, 1000), (40, 128, 64),
+         (2000, 400, 4600), (2001, 640, 4603), (1990, 128, 4604), (2048, 16, 4608), (2047, 1280, 4601), (2100, 161, 2304), (1900, 33, 2301), (2050, 129, 2400)]
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
@@ -136,9 +137,9 @@ def test_scales_that_are_not_finite_or_far_apart():
         assert torch.equal(torch.isfinite(got[7]), want.abs() <= 3.4028235e38) and bool(torch.isfinite(got[7, 2]))
 
 
-@pytest.mark.parametrize("m,k", [(5, 32), (5, 33), (70, 32), (1500, 32)])
+@pytest.mark.parametrize("m,k", [(5, 32), (5, 33), (70, 32), (1500, 32), (2000, 32)])
 def test_sums_of_zero_between_scales_whose_product_leaves_fp32(m, k):
-    n = 1500
+    n = 4600 if m == 2000 else 1500
     a, w = torch.ones(m, k, dtype=torch.int8), torch.ones(n, k, dtype=torch.int8)
     a[:, k - 1] = 1 - k      # sums of zero
     a[1] = 1
