@@ -97,9 +97,9 @@ def test_products(m, k, n, io):
         assert bool((out[:, n:] == U.MARK).all())
 
 
-@pytest.mark.parametrize("m", [5, 60, 200, 900])
+@pytest.mark.parametrize("m", [5, 60, 200, 900, 2000])
 def test_rows_of_any_stride_and_address(m):
-    k, n = 272, 96
+    k, n = 272, 4700 if m == 2000 else 96
     a, w, sa, sw, _ = case(m, m, k, n)
     want = expect(a, w, sa, sw, None, torch.float32)
     for pad, lead in ((16, 0), (16, 16), (1, 0), (0, 1), (7, 3)):
@@ -107,9 +107,11 @@ def test_rows_of_any_stride_and_address(m):
             at = torch.full((lead + x.shape[0] * (k + pad),), 77, dtype=torch.int8, device="cuda")[lead:].view(-1, k + pad)[:, :k]
             at.copy_(x)
             return at
-        out = torch.empty(m, n, device="cuda")
+        rows = torch.full((m, n + pad), U.MARK, device="cuda")
+        out = rows[:, :n]
         B.product_i8(place(a), sa.cuda(), place(w), sw.cuda(), out)
         U.check((m, pad, lead), out, *want)
+        assert bool((rows[:, n:] == U.MARK).all())
 
 
 def test_sums_that_need_all_32_bits():
