@@ -141,7 +141,7 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm(
       row_sums<LPR, W>(q, lds, turn, wave);
       dm = q[0] * inv_n;
       v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps * times * times;
-      v = q[1] != q[1] ? q[1] : v;      // (the maximum drops a NaN)
+      v = q[1] < INFINITY ? v : q[1];      // (the maximum drops a NaN, which a mean beyond fp32 leaves too)
     };
     moments(1.f);
     if (__builtin_amdgcn_ballot_w64(out_of_range(v)) != 0) {      // (all waves of a row find the same; the row is loaded again: kept for this it would take registers)
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_
       row_sums<LPR, W>(q, lds, turn, wave);
       const float dm = q[0] * inv_n;
       v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps * times * times;
-      v = q[1] != q[1] ? q[1] : v;
+      v = q[1] < INFINITY ? v : q[1];
     };
     moments();
     if (__builtin_amdgcn_ballot_w64(out_of_range(v)) != 0) {
