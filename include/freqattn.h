@@ -442,7 +442,7 @@ typedef struct {
 
 /* Layer norm, out = (x - mean_c x) (var_c x + eps)^-1/2 * w + b, var the mean of the centred squares.  w, b DEVICE of `dtype`, NULL: ones and zeros;
  * [channels], or, with weights_per_batch != 0, [batch][channels]: scale and shift of their own for every batch entry, as conditioning gives them.  Sums are fp32; the
- * mean's own rounding is taken out again, so rows far from zero keep their precision, and rows whose squares leave fp32 are taken in another scale.  out may be x itself (same pointer and strides), else must not overlap it.
+ * mean's own rounding is taken out again, so rows far from zero keep their precision, and rows whose sum or squares leave fp32 are taken in a scale of their own, whatever eps is.  out may be x itself (same pointer and strides), else must not overlap it.
  * EINVAL: NULL, sizes < 0, channels < 1, unknown dtype, eps negative or not finite; EUNSUPPORTED: channels above 16384, 2^31 rows or more, more than 65535
  * batch entries with weights of their own.  Nothing is launched where batch or rows is 0. */
 typedef struct {

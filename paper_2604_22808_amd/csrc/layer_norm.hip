@@ -27,9 +27,8 @@ __device__ __forceinline__ float inv_root(float v) {
   const float r = __builtin_amdgcn_rsqf(v);
   return __builtin_fmaf(0.5f * r, __builtin_fmaf(-v * r, r, 1.f), r);
 }
-// Not so: squares that have left fp32, or are about to.  Such a row is taken again, times 2^64 or 2^-64.
+// Not so: squares that have left fp32, or are about to.  Such a row is taken again in a scale of its own (own_scale).
 __device__ __forceinline__ bool out_of_range(float v) { return v < 1e-30f || !(v < 3e38f); }
-__device__ __forceinline__ float into_range(float v) { return v < 1e-30f ? 0x1p64f : !(v < 3e38f) ? 0x1p-64f : 1.f; }
 
 // Sums of N values over a row's lanes; those of W waves meet in LDS, in the order of the waves.  `turn` alternates between two places, so that one barrier a sum
 // is enough.
@@ -77,13 +76,70 @@ __device__ __forceinline__ void centre(const Piece<T> (&x)[PT], float (&d)[PT][P
 }
 
 template <typename T, int PT>
-__device__ __forceinline__ float sum_of(const Piece<T> (&x)[PT], float times) {
+__device__ __forceinline__ float sum_of(const Piece<T> (&x)[PT]) {
   float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < PT; ++i)
 #pragma unroll
-    for (int j = 0; j < PW<T>; ++j) s[j & 3] = __builtin_fmaf(x[i].get(j), times, s[j & 3]);
+    for (int j = 0; j < PW<T>; ++j) s[j & 3] += x[i].get(j);
   return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// The largest magnitude of a row, by its bits (a NaN counts as the largest).
+template <int LPR, int W>
+__device__ __forceinline__ uint32_t row_top(float x, float (*lds)[W][4], int& turn, int wave) {
+  auto larger = [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); };
+  x = over_lanes<LPR>(__uint_as_float(__float_as_uint(x) & 0x7fffffffu), larger);
+  if constexpr (W > 1) {
+    float (*at)[4] = lds[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) at[wave][0] = x;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) x = larger(x, at[w][0]);
+  }
+  return __float_as_uint(x);
+}
+
+// How the centred values d = x times - mean of a row are taken.  eps: in their units.  back: the power of two that they are times the row's own.
+struct Scale { float times, mean, eps, back; };
+
+// A row whose variance v is out_of_range gets a scale of its own: the power of two by which its largest centred value, or eps^1/2 where that is larger, lies in 2^16 .. 2^17, so that neither
+// sums nor squares leave fp32 and eps counts for what it is.  (A large row comes down first, since its sum has to stay.)  The mean is found twice, by division: what the first leaves of a
+// row of equal values are a few steps of them, whose sum and mean have no rounding, so that such a row becomes zero exactly.  The row is read again piece by piece, which takes no
+// registers; `count`: its channels, 0 of a row that does not exist.  Other rows of the wave stay as they are.
+template <typename T, int LPR, int W, int PT>
+__device__ __forceinline__ void own_scale(const T* row, const Place<T, LPR, W, PT>& at, int count, int n, float v, float (*lds)[W][4], int& turn, int wave, Scale& sc) {
+  const float down = v < 3e38f ? 1.f : 0x1p-20f;
+  float mean = 0.f;
+  uint32_t top = 0;
+  int pieces = PT;
+  if constexpr (PT == 1) asm volatile("" : "+s"(pieces));      // (a loop all the same: nothing of it is moved up)
+#pragma nounroll
+  for (int pass = 0; pass < 3; ++pass) {      // sum, what is left of it, largest centred value
+    float s[1] = {0.f};
+    top = 0;
+#pragma nounroll
+    for (int k = 0; k < pieces; ++k) {
+      asm volatile("" ::: "memory");
+      Piece<T> x;
+      const int c = at.channel(k);
+      x.load(row, c, count);
+#pragma unroll
+      for (int j = 0; j < PW<T>; ++j) {
+        const float y = c + j < count ? __builtin_fmaf(x.get(j), down, -mean) : 0.f;
+        s[0] += y;
+        top = max(top, __float_as_uint(y) & 0x7fffffffu);
+      }
+    }
+    row_sums<LPR, W>(s, lds, turn, wave);
+    top = row_top<LPR, W>(__uint_as_float(top), lds, turn, wave);
+    if (pass < 2) mean += s[0] / (float)n;
+  }
+  const int e = (int)(max(top, __float_as_uint(sqrtf(sc.eps) * down)) >> 23);
+  const float up = __uint_as_float((uint32_t)min(270 - e, 247) << 23), all = down * up;      // 2^120 at most: the smallest numbers are 2^-29 then
+  // (equal values are zeros in any scale, also where their mean would leave fp32 in the scale of eps)
+  if (out_of_range(v)) sc = Scale{top ? all : 0.f, top ? mean * up : 0.f, sc.eps * all * all, all};
 }
 
 template <typename T, int LPR, int W, int PT>
@@ -126,10 +182,11 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm(
     for (int k = 0; k < PT; ++k) x[k] = next[k];
     if (At::AHEAD && i + step < p.n) request(i + step + at.row);
     float d[PT][PW<T>], dm, v;
-    auto moments = [&](float times) {
-      float s[1] = {sum_of<T, PT>(x, times)};
-      row_sums<LPR, W>(s, lds, turn, wave);
-      centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n, times);
+    float s[1] = {sum_of<T, PT>(x)};
+    row_sums<LPR, W>(s, lds, turn, wave);
+    Scale sc = {1.f, s[0] * inv_n, p.eps, 1.f};
+    auto spread = [&](float times, float mean, float eps) {
+      centre<T, LPR, W, PT>(x, d, at, n, mean, times);
       float q[2] = {0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < PT; ++k)
@@ -140,15 +197,17 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm(
         }
       row_sums<LPR, W>(q, lds, turn, wave);
       dm = q[0] * inv_n;
-      v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps * times * times;
+      v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + eps;
       v = q[1] < INFINITY ? v : q[1];      // (the maximum drops a NaN, which a mean beyond fp32 leaves too)
     };
-    moments(1.f);
-    if (__builtin_amdgcn_ballot_w64(out_of_range(v)) != 0) {      // (all waves of a row find the same; the row is loaded again: kept for this it would take registers)
-      again(x, i + at.row);
-      moments(into_range(v));
+    spread(1.f, sc.mean, p.eps);
+    if (__builtin_amdgcn_ballot_w64(out_of_range(v)) != 0) {      // (all waves of a row find the same)
+      const bool in = i + at.row < p.n;
+      own_scale<T, LPR, W, PT>(row_at<T>(p.x, p, in ? i + at.row : 0), at, in ? n : 0, n, v, lds, turn, wave, sc);
+      again(x, i + at.row);      // (kept for this it would take registers)
+      spread(sc.times, sc.mean, sc.eps);
     }
-    const float r = out_of_range(v) ? 1.f / sqrtf(v) : inv_root(v), k0 = -dm * r;
+    const float r = out_of_range(v) ? 1.f / sqrtf(v) : inv_root(v), k0 = -dm * r;      // (out of range still: zero or NaN)
     if (i + at.row < p.n) {
       T* row = row_at<T>(p.y, p, i + at.row);
 #pragma unroll
@@ -207,11 +266,12 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_
 #pragma unroll
     for (int k = 0; k < PT; ++k) { x[k] = nx[k]; dy[k] = ny[k]; }
     if (At::AHEAD && i + step < p.n) request(i + step + at.row);
-    float d[PT][PW<T>], q[4], v, times = 1.f;     // q: sums of d, d^2, g, g d
-    auto moments = [&] {
-      float s[1] = {sum_of<T, PT>(x, times)};
-      row_sums<LPR, W>(s, lds, turn, wave);
-      centre<T, LPR, W, PT>(x, d, at, n, s[0] * inv_n, times);
+    float d[PT][PW<T>], q[4], v;     // q: sums of d, d^2, g, g d
+    float s[1] = {sum_of<T, PT>(x)};
+    row_sums<LPR, W>(s, lds, turn, wave);
+    Scale sc = {1.f, s[0] * inv_n, p.eps, 1.f};
+    auto spread = [&](float times, float mean, float eps) {
+      centre<T, LPR, W, PT>(x, d, at, n, mean, times);
 #pragma unroll
       for (int k = 0; k < 4; ++k) q[k] = 0.f;
 #pragma unroll
@@ -226,16 +286,18 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_
         }
       row_sums<LPR, W>(q, lds, turn, wave);
       const float dm = q[0] * inv_n;
-      v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + p.eps * times * times;
+      v = __builtin_fmaxf(__builtin_fmaf(-dm, dm, q[1] * inv_n), 0.f) + eps;
       v = q[1] < INFINITY ? v : q[1];
     };
-    moments();
-    if (__builtin_amdgcn_ballot_w64(out_of_range(v)) != 0) {
-      times = into_range(v);
+    spread(1.f, sc.mean, p.eps);
+    const bool scaled = __builtin_amdgcn_ballot_w64(out_of_range(v)) != 0;
+    if (scaled) {
+      const bool in = i + at.row < p.n;
+      own_scale<T, LPR, W, PT>(row_at<T>(p.x, p, in ? i + at.row : 0), at, in ? n : 0, n, v, lds, turn, wave, sc);
       again(x, i + at.row);
-      moments();
+      spread(sc.times, sc.mean, sc.eps);
     }
-    const float dm = q[0] * inv_n, r = out_of_range(v) ? 1.f / sqrtf(v) : inv_root(v), k0 = -dm * r, rx = r * times;      // rx: of the row itself
+    const float dm = q[0] * inv_n, r = out_of_range(v) ? 1.f / sqrtf(v) : inv_root(v), k0 = -dm * r;
     const float mg = q[2] * inv_n, mgh = r * __builtin_fmaf(-dm, q[2], q[3]) * inv_n;
     if (i + at.row < p.n) {
       T* row = row_at<T>(p.dx, p, i + at.row);
@@ -248,7 +310,11 @@ __global__ void __launch_bounds__((Place<T, LPR, W, PT>::THREADS)) k_layer_norm_
           const float y = dy[k].get(j), g = y * w[k].get(j), h = __builtin_fmaf(d[k][j], r, k0);
           dw[k][j] = __builtin_fmaf(y, h, dw[k][j]);
           db[k][j] += y;
-          o_[j] = rx * (g - __builtin_fmaf(h, mgh, mg));
+          o_[j] = r * (g - __builtin_fmaf(h, mgh, mg));
+        }
+        if (scaled) {      // (r is of the scaled row; its product with the scale may leave fp32)
+#pragma unroll
+          for (int j = 0; j < PW<T>; ++j) o_[j] *= sc.back;
         }
 #pragma unroll
         for (int j = 0; j < PW<T>; j += 2) o.set(j, o_[j], o_[j + 1]);

@@ -40,3 +40,53 @@ def test_norm_of_rows_whose_sum_leaves_fp32(c, size, dtype):
             got, want = both_passes(x, w, bias, do, eps), expect(x, w, bias, in_fp32(eps), io, False, do)
             for name in got:
                 U.check((name, eps), got[name], *want[name])
+
+
+SIZES_FAR = [1.5e-45, 3e-44, 1e-42, 1e-40, 1e-38, 1e-30, 1.0, 1e18, 1e30, 3e36, 3e38]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("c", [8, 64, 150, 700, 1900, 5000, 16384])
+def test_norm_of_rows_of_any_size_fp32_holds(c, dtype):
+    """Rows from the smallest numbers to the largest, each normalised as if it were alone, and beside them the same rows around a large mean of their own."""
+    io, x, w, bias, dout = make(c, dtype, 1, 2 * len(SIZES_FAR) + 1, c, False)
+    x = x.double().clamp(-4, 4) / 4.1
+    for i, s in enumerate(SIZES_FAR):
+        x[0, i] *= s
+        x[0, len(SIZES_FAR) + i] = 0.75 * s + 0.25 * s * x[0, len(SIZES_FAR) + i]
+    x = x.to(io)
+    x[0, -1] = torch.where(torch.arange(c) % 3 == 0, -1.0, 1.0) * 3.3e38       # centred values beyond fp32
+    assert bool(torch.isfinite(x.float()).all())
+    near, far = dout.double(), dout.double()
+    for i, s in enumerate(SIZES_FAR + SIZES_FAR + [3e38]):
+        far[0, i] = far[0, i] * (1e-25 if s < 1e-20 else 1e20 if s > 1e20 else 1.0)    # dx of 1e-19 to 1e20: neither hidden by the bound's 1e-30 nor infinite
+    flat = (x[0].double().var(1, correction=0) == 0)          # (what the type rounds to one value: 0 / 0 with eps 0)
+    far, near = far.to(io), near.to(io)
+    keep = ~flat
+    for eps in (0.0, 1e-6, 1e-31, 1e38):
+        rows = keep if eps == 0.0 else torch.ones_like(keep)
+        xs, ds = x[:, rows], (near[:, rows], far[:, rows])
+        for do, names in zip(ds, (("out", "dw", "db"), ("out", "dx"))):
+            got, want = both_passes(xs, w, bias, do, eps), expect(xs, w, bias, in_fp32(eps), io, False, do)
+            for name in names:
+                U.check((name, eps), got[name], *want[name])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("c", [64, 100, 700, 1999, 5000, 9001])
+def test_norm_of_constant_rows_of_any_size(c, dtype):
+    """A row of one value gives b, and a gradient of eps^-1/2 (g - mean g), however large the value and however small eps."""
+    io, x, w, bias, dout = make(c, dtype, 1, 7, c, False)
+    x[0, 0], x[0, 2], x[0, 3], x[0, 5] = 2.0 ** 66, -1e37, 3e38, 2.0 ** 70
+    g = dout.double() * w.double()
+    for eps in (1e-31, 1e-6):
+        got = both_passes(x, w, bias, dout, eps)
+        r = 1 / math.sqrt(in_fp32(eps))
+        dx = r * (g - g.mean(2, keepdim=True))
+        for i in (0, 2, 3, 5) if c == 64 else (2, 3):     # (powers of two: where 1 / channels is none either, their mean is off by a rounding)
+            assert torch.equal(got["out"][0, i].cpu(), bias), (eps, i)
+            # the mean of g, the root, its product, the store
+            bound = r * (U.CHAIN + 4) * U.F32 * (g[0, i].abs().mean() + g[0, i].abs()) + (8 * U.F32 + U.STEP[io] * (1 + 2.0 ** -6)) * dx[0, i].abs()
+            U.check(("dx", eps, i), got["dx"][0, i], dx[0, i], bound)
+        assert bool(torch.isfinite(got["dw"]).all()), eps
+        U.check(("db", eps), got["db"], *expect(x, w, bias, in_fp32(eps), io, False, dout)["db"])
