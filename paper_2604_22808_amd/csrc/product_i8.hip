@@ -107,6 +107,8 @@ __device__ __forceinline__ void store_wide(const ProductParams& p, const int16v&
   constexpr int CH = 64 / PW<T>, STORES = 32 * CH / 64;      // pieces of such a row; stores of a lane
   const int nn = lane & 31, g = lane >> 5;
   const float sa = p.a_scales[min(first + nn, p.rows - 1)];
+  // (lanes read what others wrote: a wave's accesses to LDS stay in order, and the waits keep the compiler from moving one past another whose address it can tell apart within a lane)
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
   for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
@@ -118,6 +120,7 @@ __device__ __forceinline__ void store_wide(const ProductParams& p, const int16v&
 #pragma unroll
       for (int i = 0; i < 8 / PW<T>; ++i) mine[nn * CH + (((4 * c2 + 2 * j + g) * (8 / PW<T>) + i) ^ (nn & 7))] = x[i].raw;
     }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
   for (int i = 0; i < STORES; ++i) {
     const int r = i * (64 / CH) + lane / CH, ch = lane % CH;

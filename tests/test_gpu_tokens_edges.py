@@ -90,3 +90,17 @@ def test_norm_of_constant_rows_of_any_size(c, dtype):
             U.check(("dx", eps, i), got["dx"][0, i], dx[0, i], bound)
         assert bool(torch.isfinite(got["dw"]).all()), eps
         U.check(("db", eps), got["db"], *expect(x, w, bias, in_fp32(eps), io, False, dout)["db"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", [(2048, 16, 4608), (1990, 130, 4604), (1000, 2064, 2048), (1001, 400, 1999), (2100, 161, 2304), (1900, 33, 2301)])
+def test_results_that_pass_through_lds_land_in_their_places(m, k, n, dtype):
+    """256 x 256 and 128 x 128 tiles, copied and of any alignment: a wave's lanes store what others computed, one 32-row strip after another.  Sums below 2^24 are exact in
+    fp32, and in bf16 rounded once."""
+    gen = torch.Generator().manual_seed(m + n)
+    a, w = (torch.randint(-40, 41, (r, k), generator=gen).to(torch.int8) for r in (m, n))
+    out = torch.full((m, n), U.MARK, dtype=U.TYPES[dtype], device="cuda")
+    one = torch.ones(max(m, n), device="cuda")
+    for _ in range(3):
+        B.product_i8(a.cuda(), one[:m], w.cuda(), one[:n], out)
+        assert torch.equal(out.cpu(), (a.double() @ w.double().T).to(U.TYPES[dtype]))
