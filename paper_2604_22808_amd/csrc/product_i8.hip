@@ -557,11 +557,20 @@ hipError_t few(const ProductParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Stages of the copies by tile.  Rows for the kernel of few rows: here / on 64 x 64 tiles, 32 rows: 2048 -> 6144 8.2 / 6.3 us, 4096 -> 4096 8.4 / 9.2, 8192 -> 1024 13 / 15; 64
-// rows: 2048 -> 6144 12.1 / 6.4, 4096 -> 4096 12.6 / 9.2, 8192 -> 1024 20.5 / 15.2.
+// Stages of the copies by tile.
+//
+// The kernel of few rows takes up to 32 of them where its workgroups run side by side, one a compute unit for 17 to 32 rows and two for up to 16 (or few channels): each reads all rows' codes,
+// which more workgroups wait for one after the other, while 64 x 64 tiles read them once for 64 outputs.  Here / on tiles, 32 rows: 2048 -> 4096 5.5 / 6.2 us, 4112 7.9 / 6.2, 6144 8.2 / 6.2,
+// 4096 -> 4096 8.5 / 9.1, 6144 13.7 / 9.2, 8192 -> 1024 13.1 / 15.3, 8192 24.6 / 15.8, 1024 -> 1024 4.1 / 4.6; 17 rows: 2048 -> 4096 4.8 / 6.1, 6144 6.8 / 6.1, 8192 -> 8192 19.6 / 15.7.  16
+// rows: 2048 -> 8192 6.2 / 6.2, 16,384 10.4 / 6.9, 4096 -> 6144 10.0 / 9.1, 12,288 13.9 / 10.7, 8192 -> 1024 9.4 / 15.2; one row: 2048 -> 8192 4.7 / 6.2, 16,384 7.5 / 7.0, 4096 -> 12,288 10.3 /
+// 10.4, 512 -> 12,288 3.4 / 3.9 (16 rows 4.2 / 4.0).  64 rows: 2048 -> 6144 12.1 / 6.4, 8192 -> 1024 20.5 / 15.2.
 // On 64 x 64 tiles of a single round two groups share the steps: one / two / four of them, 64 rows 2048 -> 6144 7.7 / 6.4 / 6.5 us, 8192 -> 1024 21.3 / 15.2 / 13.7, 512 rows 8192 -> 1024
 // 22.2 / 16.6 / 16.7, 6250 rows 8000 -> 96 22.5 / 18.8 / 22.6; in more rounds 2048 x 1536 -> 1536 11.6 / 15.3 / 16.1.
-constexpr int S64 = 3, S128 = 2, FEW_ROWS = 32;
+constexpr int S64 = 3, S128 = 2, FEW_ROWS = 32, FEW_CHANNELS = 512;
+bool few_rows(const ProductParams& p, int num_cu) {
+  const int64_t blocks = ((int64_t)p.outputs + 15) / 16;
+  return p.rows <= 16 ? blocks <= 2 * (int64_t)num_cu || p.channels <= FEW_CHANNELS : p.rows <= FEW_ROWS && blocks <= num_cu;
+}
 
 template <typename T>
 hipError_t go(const ProductParams& p, int num_cu, hipStream_t st) {
@@ -573,7 +582,7 @@ hipError_t go(const ProductParams& p, int num_cu, hipStream_t st) {
     };
     return time(128, 19.f, 25.f) < time(64, 7.2f, 13.f) ? any<T, 128>(p, st) : any<T, 64>(p, st);
   }
-  if (p.rows <= FEW_ROWS) return few<T>(p, st);
+  if (few_rows(p, num_cu)) return few<T>(p, st);
   // The kernel whose rounds of the chip take the shortest, us at 2048 channels (others in proportion): a compute unit holds three workgroups of 64 x 64 tiles (one of them alone 9, or 7 in
   // two groups, two 12, three 13), two of 128 x 128 (16, 28) or one of 256 x 256 (29).  Measured as tiles of 64 / 128 / 256: 1024 x 2048 -> 2048 11.6 / 16.6 / 29.5, 2048 x 2048 -> 2048 21.6 / 18.2 /
   // 30.5, 4096 x 2048 -> 2048 36 / 27.6 / 33, 2048 x 1536 -> 4608 33.6 / 32.2 / 28.5, 3000 x 4096 -> 4096 91 / 70 / 57, 100,000 x 1024 -> 128 35 / 32 / 39.5.

@@ -104,3 +104,18 @@ def test_results_that_pass_through_lds_land_in_their_places(m, k, n, dtype):
     for _ in range(3):
         B.product_i8(a.cuda(), one[:m], w.cuda(), one[:n], out)
         assert torch.equal(out.cpu(), (a.double() @ w.double().T).to(U.TYPES[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", [(1, 1024, 8192), (1, 1040, 8208), (16, 528, 8193), (16, 512, 16400), (17, 2048, 4096), (17, 512, 4097), (32, 1040, 4112), (2, 528, 70000), (13, 528, 140001),
+                                   (1, 544, 262144)])
+def test_few_rows_on_either_side_of_the_choice_of_their_kernel(m, k, n, dtype):
+    t, gen = U.TYPES[dtype], torch.Generator().manual_seed(m + n)
+    a, w = (torch.randint(-127, 128, (r, k), generator=gen).to(torch.int8) for r in (m, n))
+    sa, sw, bias = torch.rand(m, generator=gen) + 0.01, torch.rand(n, generator=gen) * 0.02 + 1e-4, torch.randn(n, generator=gen).to(t)
+    rows = torch.full((m, n + 3), U.MARK, dtype=t, device="cuda")
+    B.product_i8(a.cuda(), sa.cuda(), w.cuda(), sw.cuda(), rows[:, :n], bias=bias.cuda())
+    y = (a.double() @ w.double().T) * sa.double()[:, None] * sw.double()[None]
+    want = y + bias.double()
+    U.check((m, k, n), rows[:, :n], want, 4 * U.F32 * y.abs() + (U.F32 + U.STEP[t] * (1 + 2.0 ** -6)) * want.abs() + 1e-37)
+    assert bool((rows[:, n:] == U.MARK).all())
