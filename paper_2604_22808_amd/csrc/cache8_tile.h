@@ -100,6 +100,16 @@ __device__ __forceinline__ void three_terms(const float (&v)[8], bf16x8 (&t)[3])
   }
 }
 
+// Eight values with zeros in place of those that are not finite: what the terms behind the first are multiplied by where a result was not finite.  Those may be zero where the number
+// itself is not, and an infinite value counts once.
+__device__ __forceinline__ bf16x8 finite8(const bf16x8& v) {
+  uint4v w = __builtin_bit_cast(uint4v, v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w[j] = ((w[j] & 0x7f80u) == 0x7f80u ? 0u : (w[j] & 0xffffu)) | ((w[j] & 0x7f800000u) == 0x7f800000u ? 0u : (w[j] & 0xffff0000u));
+  return __builtin_bit_cast(bf16x8, w);
+}
+
 }  // namespace seq
 
 }  // namespace fa

@@ -172,8 +172,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 2) k
         for (int i = 0; i < NS; ++i) {
           const bf16x8 a = A[i % PF];
           if (i + PF < NS) A[i % PF] = kr.get(Kt, (i + PF) / DK, (i + PF) % DK);
+          bf16x8 lower = a;
+          if constexpr (careful.value && TERMS > 1) lower = finite8(a);
 #pragma unroll
-          for (int term = TERMS - 1; term >= 0; --term) S[i / DK] = mfma(a, Q[term][i % DK], i % DK == 0 && term == TERMS - 1 ? zero16() : S[i / DK]);
+          for (int term = TERMS - 1; term >= 0; --term) S[i / DK] = mfma(term ? lower : a, Q[term][i % DK], i % DK == 0 && term == TERMS - 1 ? zero16() : S[i / DK]);
         }
         in_order<NS, PF, TERMS, 1>();
       }
@@ -233,7 +235,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? (D == 64 ? 2 : 1) : 2) k
         psum = probabilities();
       }
       l += psum;
-      if (careful.value && key0 + KT - 1 > wg_first) {
+      if (careful.value && (TERMS > 1 || key0 + KT - 1 > wg_first)) {      // (fp32: an infinite value must not meet a zero among a probability's terms)
 #pragma unroll
         for (int t2 = 0; t2 < T2; ++t2) {
           const uint32_t none = row_bits(g, [&](int r) { return !(P[0][t2][r >> 3][r & 7] != (__bf16)0.f); });

@@ -11,8 +11,8 @@
 // Bound by memory once the caches are long: one token of 32 requests against 16,384 rows, 32 / 8 heads of 128: 211 us, 5.1 TB/s (bf16 cache 380; fp32 queries 220); 128 against 1024: 48, 5.6; heads of 64,
 // 8 / 8: 114, 4.7; caches of 200 to 16,384 rows 115, of which the join 7.  Short ones by latency: one token of one request against 777 rows 8.1, against 16,384 in two launches 15.5.
 //
-// A value that is not finite and that not every row of the tile sees must not reach the others as 0 x NaN: where a wave's result is not finite, it runs again, with the tiles
-// that have masked pairs multiplied pair by pair.
+// A value that is not finite and that not every row of the tile sees must not reach the others as 0 x NaN, nor an infinite one meet a zero among the three terms of an fp32 number: where a
+// wave's result is not finite, it runs again, with the tiles that have masked pairs (fp32: or such values) multiplied pair by pair, and such keys by the first term alone.
 #include "cache8_tile.h"
 #include "seq_join.h"
 
@@ -183,11 +183,13 @@ __global__ void __launch_bounds__(64 * NW, cache8_few_waves(sizeof(T) == 4, D > 
 #pragma unroll
         for (int st = 0; st < ST; ++st) {
           const bf16x8 a = __builtin_bit_cast(bf16x8, widen8(kx[h][st >> 1][2 * (st & 1)], kx[h][st >> 1][2 * (st & 1) + 1], ke[h]));
+          bf16x8 lower = a;
+          if constexpr (careful.value && TERMS > 1) lower = finite8(a);
 #pragma unroll
           for (int i = 0; i < NQ; ++i)
 #pragma unroll
             for (int term = TERMS - 1; term >= 0; --term)
-              S[i][h] = mfma16(a, Q[i][term][st], st == 0 && term == TERMS - 1 ? float4v{0.f, 0.f, 0.f, 0.f} : S[i][h]);
+              S[i][h] = mfma16(term ? lower : a, Q[i][term][st], st == 0 && term == TERMS - 1 ? float4v{0.f, 0.f, 0.f, 0.f} : S[i][h]);
         }
       }
       vt.store(tile, lane);
@@ -243,7 +245,16 @@ __global__ void __launch_bounds__(64 * NW, cache8_few_waves(sizeof(T) == 4, D > 
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (careful.value && mask) {
+      bool by_pairs = careful.value && mask;
+      if constexpr (careful.value && TERMS > 1) {      // (also where a value is not finite: a term of a probability may be zero)
+        bool odd = false;
+        for (int c = lane; c < 32 * D / 2; c += 64) {
+          const uint32_t x = ((const uint32_t*)tile)[c];
+          odd = odd || (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+        }
+        by_pairs = by_pairs || __builtin_amdgcn_ballot_w64(odd) != 0;
+      }
+      if (by_pairs) {
         // pair by pair: key 16 h + 4 gg + r's probability is on lane group gg
 #pragma nounroll
         for (int gg = 0; gg < 4; ++gg)

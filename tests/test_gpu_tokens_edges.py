@@ -119,3 +119,48 @@ def test_few_rows_on_either_side_of_the_choice_of_their_kernel(m, k, n, dtype):
     want = y + bias.double()
     U.check((m, k, n), rows[:, :n], want, 4 * U.F32 * y.abs() + (U.F32 + U.STEP[t] * (1 + 2.0 ** -6)) * want.abs() + 1e-37)
     assert bool((rows[:, n:] == U.MARK).all())
+
+
+def definition(q, k, v, causal, scale):
+    """Attention of one sequence and head in 64 bits, q [rows, d], keys and values that may be infinite; masked pairs do not count."""
+    nq, nk = q.shape[0], k.shape[0]
+    seen = torch.arange(nk)[None] <= torch.arange(nq)[:, None] + nk - nq if causal else torch.ones(nq, nk, dtype=torch.bool)
+    s = ((q[:, None] * k[None]).sum(2) * scale).masked_fill(~seen, -math.inf)
+    p = torch.exp(s - s.amax(1, keepdim=True))
+    p = p / p.sum(1, keepdim=True)
+    return torch.where(seen[:, :, None], p[:, :, None] * v[None], 0.0).sum(1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bits", [8, 16, 24])
+@pytest.mark.parametrize("rows,cap,d,q_pad", [(1, 200, 64, 0), (20, 200, 128, 0), (150, 300, 64, 0), (150, 300, 72, 0), (3, 5000, 128, 0), (40, 200, 64, 3)])
+def test_values_that_read_back_infinite(rows, cap, d, q_pad, bits, dtype):
+    """Code 256 at the largest byte that append writes is 2^128: attention takes it as an infinite value, and as an infinite key, whatever bits the queries have."""
+    io, heads, block, at = U.TYPES[dtype], 3, 16, 100
+    gen = torch.Generator().manual_seed(rows + d)
+    codes = [torch.randint(0, 0x7f, (1, cap, heads, d), generator=gen).to(torch.uint8) for _ in range(2)]
+    scales = [torch.full((1, -(-cap // block), heads), 117, dtype=torch.uint8) for _ in range(2)]
+    hot = at // block
+    lo, hi = hot * block, hot * block + block
+    # head 0: an infinite value and a negative one; head 1: an infinite key; head 2: neither
+    codes[1][0, lo:hi, 0], codes[0][0, lo:hi, 1] = 0, 0
+    scales[1][0, hot, 0], scales[0][0, hot, 1] = 247, 247
+    codes[1][0, at, 0, 3], codes[1][0, at + 1, 0, 9], codes[0][0, at, 1, 5] = 0x78, 0xf8, 0x78
+    q = torch.randn(1, rows, heads, d, generator=gen)
+    q = (q.view(torch.int32) & -(1 << (24 - bits))).view(torch.float32).to(io)      # `bits` significant bits
+    q[0, :, 1, 5] = torch.where(torch.arange(rows) % 2 == 0, -q[0, :, 1, 5].abs(), q[0, :, 1, 5].abs())
+    kv = [U.cache_values(codes[w], scales[w], block).float() for w in range(2)]
+    assert bool(torch.isinf(kv[1][0, at, 0, 3])) and bool(torch.isinf(kv[0][0, at, 1, 5]))
+    for causal in (False, True):
+        for last in (cap, at + 3):      # the row of the infinities in the middle, and among the keys that not every query sees
+            dev = torch.empty(1, rows, heads, d + q_pad, dtype=io, device="cuda")[..., q_pad:]
+            dev.copy_(q)
+            out = torch.empty(1, rows, heads, d + q_pad, dtype=io, device="cuda")[..., q_pad:]
+            B.cache8_attention(dev, *(c.cuda() for c in codes), *(s.cuda() for s in scales), block, out, causal=causal, k_lengths=torch.tensor([last], dtype=torch.int32).cuda())
+            for h in range(heads):
+                first = max(0, rows - last) if causal else 0       # (queries before the first key see nothing)
+                want = definition(q[0, :, h].double(), kv[0][0, :last, h].double(), kv[1][0, :last, h].double(), causal, 1 / math.sqrt(d))[first:]
+                # scores of up to 8 d^1/2: fp32 sums of three terms a product and probabilities (bf16: one more rounding), as tests of finite caches count them
+                size = kv[1][0, :last, h][torch.isfinite(kv[1][0, :last, h])].abs().max().double()
+                step = 3 * (2 * U.F32 * (d + 8) * 16 * math.sqrt(d) + 2 * (last + 16) * U.F32) + (2 * U.STEP[io] if io is torch.bfloat16 else 0.0)
+                U.check((h, causal, last), out[0, first:, h], want, step * size + U.STEP[io] * want.abs().nan_to_num(0.0, 0.0, 0.0))
