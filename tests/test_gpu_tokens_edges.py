@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2604_22808_amd import binding as B
+from paper_2604_22808_amd import workloads as WL
 from tests import tokens_util as U
 from tests.test_gpu_layer_norm import expect, make
 
@@ -164,3 +165,64 @@ def test_values_that_read_back_infinite(rows, cap, d, q_pad, bits, dtype):
                 size = kv[1][0, :last, h][torch.isfinite(kv[1][0, :last, h])].abs().max().double()
                 step = 3 * (2 * U.F32 * (d + 8) * 16 * math.sqrt(d) + 2 * (last + 16) * U.F32) + (2 * U.STEP[io] if io is torch.bfloat16 else 0.0)
                 U.check((h, causal, last), out[0, first:, h], want, step * size + U.STEP[io] * want.abs().nan_to_num(0.0, 0.0, 0.0))
+
+
+@pytest.mark.parametrize("name,heads", [("tiny_f32", 2), ("16k", 8)])
+def test_projections_in_8_bits_into_the_frequency_domain_forward(name, heads):
+    """Norm, codes and the fused product into a part of wider rows, which forward_tokens takes as they lie: the bits of the same call on copies of their own, eager and captured,
+    and every stage before it against its plain form."""
+    wl = WL.WORKLOADS[name]
+    io, d, n, model = U.TYPES["bf16" if wl.dtype == "bf16" else "f32"], wl.head_dim, wl.n_tokens, 192
+    ctx = B.Context(1, heads, d, wl.grid, B.BF16 if wl.dtype == "bf16" else B.F32, B.make_cfg(**wl.band))
+    alloc = [1, 4] if heads == 2 else [1, 1, 2, 2, 2, 4, 4, 7]
+    gen = torch.Generator().manual_seed(5)
+    outs = 3 * heads * d
+    w, b = (1 + 0.2 * torch.randn(model, generator=gen)).to(io), (0.2 * torch.randn(model, generator=gen)).to(io)
+    wqk = [(1 + 0.2 * torch.randn(d, generator=gen)).to(io).cuda() for _ in range(2)]
+    wt = (torch.randn(outs, model, generator=gen) / 14).cuda()
+    wc, ws = B.quantize_rows(wt, torch.empty(outs, model, dtype=torch.int8, device="cuda"), torch.empty(outs, device="cuda"))
+    rot = B.Rotary(d, [16, 24, 24], layout=B.ROTARY_INTERLEAVED, grid=wl.grid)
+    e = lambda *s, dtype=io: torch.empty(s, dtype=dtype, device="cuda")   # noqa: E731
+    x, h, hc, hs, out = e(1, n, model), e(1, n, model), e(1, n, model, dtype=torch.int8), e(1, n, dtype=torch.float32), e(1, heads, n, d)
+    rows = torch.full((1, n, outs + 24), U.MARK, dtype=io, device="cuda")
+    qkv = rows[..., 8:8 + outs]
+
+    def step():
+        B.layer_norm(x, w_, b_, h)
+        B.quantize_rows(h, hc, hs)
+        B.product_i8(hc, hs, wc, ws, qkv)
+        q, k, v = (t.unflatten(2, (heads, d)) for t in qkv.split(heads * d, 2))
+        return ctx.forward_tokens(q, k, v, alloc, out, *wqk, rotary=rot)
+
+    w_, b_ = w.cuda(), b.cuda()
+    fill = lambda: x.copy_(torch.randn(1, n, model, generator=gen).to(io))   # noqa: E731
+    fill()
+    step()
+    torch.cuda.synchronize()
+    some = torch.arange(0, n, 37)
+    U.check("norm", h[0, some], *U.norm(x[0, some].cpu().double(), w.double(), b.double(), 1e-6, io)["out"])
+    codes, scales = U.code_rows(h[0, some].cpu())
+    assert torch.equal(hc[0, some].cpu(), codes) and torch.equal(hs[0, some].cpu(), scales)
+    y = (codes.double() @ wc.cpu().double().T) * scales.double()[:, None] * ws.cpu().double()
+    U.check("product", qkv[0, some], y, (4 * U.F32 + U.STEP[io] * (1 + 2.0 ** -6)) * y.abs() + 1e-37)
+    assert bool((rows[..., :8] == U.MARK).all()) and bool((rows[..., 8 + outs:] == U.MARK).all())
+
+    def copies():
+        q, k, v = (t.unflatten(2, (heads, d)).contiguous() for t in qkv.split(heads * d, 2))
+        return ctx.forward_tokens(q, k, v, alloc, torch.empty_like(out), *wqk, rotary=rot)
+
+    got = out.clone()
+    assert torch.equal(got, copies()) and bool(torch.isfinite(got.float()).all())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        fill()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(got, copies()), i
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out), i
+    ctx.destroy()
