@@ -9,7 +9,7 @@
 // centred values, taken beside their squares, puts that right.  A wave keeps the weights and, in the backward pass, its share of dw and db in registers over all its rows;
 // a workgroup adds its waves' shares in their order and stores one row of partial sums, k_norm_weights adds those: no atomics, equal calls give equal bits.
 //
-// Measured (us, bf16 unless said): 131,072 x 2048 forward 182 (5.9 TB/s), backward 325 (4.95); 2 x 65,536 x 1536 with weights each 142 and 235; 10,007 x 999 fp32 16 and 29, of which adding up
+// Measured (us, bf16 unless said): 131,072 x 2048 forward 182 (5.9 TB/s), backward 326 (4.95); 2 x 65,536 x 1536 with weights each 142 and 235; 10,007 x 999 fp32 16 and 30, of which adding up
 // dw and db 4 (rows of odd length start at any element); 60,000 x 173 13 and 33, bound by vector work and the loads' number, not their bytes; a single row 3 and 4.
 #include <algorithm>
 
@@ -388,8 +388,10 @@ __global__ void __launch_bounds__(1024) k_norm_weights(NormParams p) {
   }
 }
 
-// Waves for each compute unit.  Backward: every workgroup leaves a row of partial sums (8 / 16 waves: 131,072 x 2048 bf16 325 / 368 us, 65,536 x 1024 80 / 94, 10,007 x 999 fp32 29 / 37; up to
-// 512 channels, whose registers are few: 60,000 x 173 43 / 33, 30,000 x 336 34 / 27, 100,000 x 250 fp32 78 / 58, 200,000 x 64 23 / 22, 500,000 x 128 fp32 137 / 149).
+// Waves for each compute unit.  Backward: every workgroup leaves a row of partial sums, and above 512 channels the registers (up to 256) leave place for two or three waves a SIMD: more only
+// wait for it (8 / 16 waves: 131,072 x 2048 bf16 325 / 368 us, 65,536 x 1024 80 / 94, 10,007 x 999 fp32, 173 registers, 29 / 37; up to 512 channels, whose registers are fewer: 60,000 x 173
+// 43 / 33, 30,000 x 336 34 / 27, 100,000 x 250 fp32 78 / 58, 200,000 x 64 23 / 22, 500,000 x 128 fp32 137 / 149).  The masks of row ends, found once, take more scalars than there are: up to
+// 77 forward and 102 backward lie in lanes of vector registers.
 constexpr int FWD_WAVES = 16, FWD_MOST_WAVES = 256, BWD_WAVES = 8, BWD_WAVES_NARROW = 16;
 
 }  // namespace

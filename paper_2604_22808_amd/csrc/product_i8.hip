@@ -1,9 +1,10 @@
 // Products of rows of 8-bit codes: out[m][n] = s_a[m] s_w[n] sum_k a[m][k] w[n][k] + bias[n], k adjacent in both.  Sums are whole numbers of 32 bits, exact up to 131,071
 // channels, so neither their order nor their cut shows in the result; scaling and bias are fp32, rounded once to the output's type.
 //
-// Long products are bound by the matrix cores and the clock that power leaves them: 65,536 x 1536 -> 4608 536 us (1.73 POPS; a library's product without scales 557), 131,072 x 2048 -> 2048
-// 605-619 (1.8; 589), 16,384 x 4096 -> 4096 256 (2.15), 8192 x 4096 -> 4096 130; in a run with counters the second took 675 us, matrix cores busy 45 % at 1.8 GHz.  A few rows are bound by the
-// weights' bytes and latency.
+// Long products run on 256 x 256 tiles, whose round of the chip takes about 11 us whatever the channels and 13 ns more for each of them (65,536 rows, 4096 outputs: 128 channels 12.2 us a
+// round, 1024 24.6, 2048 37.8, 8192 117, which is 2.3 POPS): during the first copies of a tile, and while its results go out, the compute unit's only workgroup multiplies nothing.
+// 65,536 x 1536 -> 4608 533 us (1.74 POPS; a library's product without scales 557; fp32 results 585), 131,072 x 2048 -> 2048 605-619 (1.8; 589; 675), 16,384 x 4096 -> 4096 252 (2.18; fp32
+// results 270), 8192 x 4096 -> 4096 130; in a run with counters the second took 660 us, matrix cores busy 45 % of the cycles.  A few rows are bound by the weights' bytes and latency.
 //
 // Operands are fed to the matrix cores as 16 bytes a lane, k = 16 g .. 16 g + 15 of a product's channels on lane group g; both sides use the same order, so any
 // order of the channels will do.

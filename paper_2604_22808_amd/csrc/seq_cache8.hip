@@ -11,6 +11,9 @@
 // numbers of 8 bits each, exactly, and their products run on the bf16 matrix instructions one after the other: 3 of those instead of fp32 products at a sixteenth of
 // their rate.
 //
+// bf16 queries: a probability is rounded to bf16 as an operand, as the kernel of bf16 keys rounds it: the results' relative error is 2.2-2.3e-3 then, of which their own rounding to bf16 makes
+// 1.7e-3; a second term would take the products with V once more.  The sum of the probabilities is of the unrounded ones.
+//
 // Bound by the vector unit beside the matrix cores (widening, exponentials).  4096 rows against 16,384 keys, 16 / 4 heads of 128, causal: 525 us (0.91 PFLOP/s; bf16 keys 461, fp32 queries 1343); 4 x
 // 2048 rows against 8192, heads of 64: 320 (0.75).  In chunks of 1, 512, 1500 and 2048 rows against 777 to 16,000 keys (326 us with the join) compute units were busy 87 % of the time and matrix cores
 // 33 %: the last pieces run on a chip that is no longer full, and the join of 24 us reads 119 MB.

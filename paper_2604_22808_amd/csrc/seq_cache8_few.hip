@@ -6,6 +6,7 @@
 //   S^T = K Q^T    a lane holds the codes of one key: they are widened in registers and multiplied as they stand.  The channels of a step are those that the lane's 16-byte
 //                  pieces hold (64 (s / 2) + 16 g + 8 (s % 2) for lane group g), which the queries follow
 //   O^T += V^T P^T a lane of S^T holds keys 4 g + r and 16 + 4 g + r of one query, which is the order in which V's rows come from transposing LDS reads
+// With bf16 queries a probability is rounded to bf16 as an operand (see there).
 // Few registers (O takes D / 4 a lane and 16 rows) let many waves run at once, each with its next 32 keys under way.
 //
 // Bound by memory once the caches are long: one token of 32 requests against 16,384 rows, 32 / 8 heads of 128: 211 us, 5.1 TB/s (bf16 cache 380; fp32 queries 220); 128 against 1024: 48, 5.6; heads of 64,
